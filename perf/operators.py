@@ -1,0 +1,429 @@
+"""Serving from a mapped cache: pages for the new tokens, rows kept in 8 bits, and
+the target model's queries reading them.
+
+A case is a dict of plain values.  ``op`` names the entry point:
+  plan    kvx.plan_pages      block tables, slots and positions from request lengths
+  store   kvx.store_cache8    rows into the 8-bit pool, a scale per page, head and K|V
+  attend  kvx.attend_cache8   causal attention of the new tokens over the 8-bit pool
+``B`` requests hold old_lo .. old_hi tokens each (drawn over their logarithm from
+``pick``, the same for every seed) and bring new_lo .. new_hi new ones; pages hold
+``P`` tokens.  ``L`` layers, ``H`` KV heads, ``G`` query heads for each of them, head
+dimension ``d``; ``ended`` requests of a plan give their pages back.
+"""
+
+import math
+import random
+
+import torch
+
+own = False
+
+_E4M3_MAX = 448.0
+_DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _case(op, B, H=8, G=1, L=1, d=128, P=16, old=(0, 0), new=(1, 1), dtype="bf16", ended=0,
+          pick=1, name=None):
+    c = dict(op=op, B=B, H=H, G=G, L=L, d=d, P=P, old_lo=old[0], old_hi=old[1], new_lo=new[0],
+             new_hi=new[1], dtype=dtype, ended=ended, pick=pick)
+    if name is not None:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # a decoding step of a small batch: a token for each request, a page now and then
+        _case("plan", 16, old=(1, 8192), name="plan_step"),
+        # new turns of many running conversations, some of which have ended
+        _case("plan", 160, old=(1, 8192), new=(1, 16384), ended=23, pick=2, name="plan_turns"),
+        # a decoding step's rows of one layer, as the projection leaves them ([T, H, d])
+        _case("store", 64, old=(1, 8192), pick=3, name="store_step"),
+        # one short new turn of a running conversation, all layers of the mapped cache
+        _case("store", 1, L=40, old=(5000, 5000), new=(333, 333), name="store_turn"),
+        # a long mapped prompt, all layers
+        _case("store", 1, L=64, P=64, new=(8192, 8192), name="store_prompt"),
+        # the toy models in fp32: several short ragged turns
+        _case("store", 5, H=2, L=6, d=64, P=32, old=(1, 256), new=(1, 256), dtype="f32", pick=4,
+              name="store_f32"),
+        # the next token of one conversation: latency
+        _case("attend", 1, G=5, old=(5332, 5332), name="attend_one"),
+        # a decoding step of a full batch with ragged lengths
+        _case("attend", 64, G=8, old=(15, 8191), pick=5, name="attend_step"),
+        # a few long contexts beside a short one
+        _case("attend", 4, G=8, P=64, old=(9, 131070), pick=8, name="attend_long"),
+        # five drafted tokens each, checked in fp32 by the toy model
+        _case("attend", 3, H=2, G=2, d=64, P=32, old=(0, 251), new=(5, 5), dtype="f32", pick=6,
+              name="attend_f32"),
+        # a chunk of a prompt after a mapped prefix
+        _case("attend", 1, G=8, P=64, old=(8192, 8192), new=(2048, 2048), name="attend_chunk"),
+        # chunks and single tokens in one batch, head dimension 64
+        _case("attend", 8, G=4, d=64, P=32, old=(1, 4096), new=(1, 1024), pick=7, name="attend_mixed"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    if lo >= hi:
+        return lo
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(max(lo, 0.5)), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(["plan", "store", "store", "attend", "attend", "attend", "attend"])
+    P, d = rng.choice([16, 16, 32, 64, 128]), rng.choice([64, 128, 128])
+    H, dtype = rng.choice([1, 2, 3, 4, 8, 8]), rng.choice(["bf16", "bf16", "bf16", "f32"])
+    pick = rng.randrange(1 << 20)
+    if op == "plan":
+        B = _log_int(rng, 1, 1000)
+        new = (1, rng.choice([1, 1, _log_int(rng, 2, min(16384, 2500000 // B))]))
+        return _case(op, B, P=P, old=(rng.choice([0, 1]), _log_int(rng, 1, 8192)), new=new,
+                     ended=rng.choice([0, 0, rng.randint(0, B - 1)]), pick=pick)
+    if op == "store":
+        L = rng.choice([1, 1, rng.randint(2, 80)])
+        B = _log_int(rng, 1, 128)
+        most = max(1, 4 * 2 ** 20 // (L * H * B * (2 if dtype == "f32" else 1)))
+        return _case(op, B, H=H, L=L, d=d, P=P, old=(0, _log_int(rng, 1, 2048)),
+                     new=(1, _log_int(rng, 1, min(8192, most))), dtype=dtype, pick=pick)
+    G, B = rng.choice([1, 2, 3, 4, 5, 7, 8, 8, 16]), _log_int(rng, 1, 128)
+    kind = rng.choice(["step", "step", "draft", "chunk"])
+    new_hi = {"step": 1, "draft": rng.randint(2, 8), "chunk": _log_int(rng, 16, 2048)}[kind]
+    # padded pairs of (query row, key) and padded keys stay under the largest listed cases'
+    most = min(131072, 4 * 131072 // B, (2 ** 30 if dtype == "bf16" else 2 ** 27) // (B * H * G * new_hi))
+    while most < 2 * new_hi and B > 1:
+        B = B // 2
+        most = min(131072, 4 * 131072 // B, (2 ** 30 if dtype == "bf16" else 2 ** 27) // (B * H * G * new_hi))
+    old_hi = _log_int(rng, 1, max(1, most - new_hi))
+    return _case(op, B, H=H, G=G, d=d, P=P, old=(0, old_hi), new=(rng.choice([1, new_hi]), new_hi),
+                 dtype=dtype, pick=pick)
+
+
+def _lengths(case):
+    """Tokens held and new tokens of each request (a case's own, whatever the seed)."""
+    rng = random.Random(case["pick"])
+    old = [_log_int(rng, case["old_lo"], case["old_hi"]) for _ in range(case["B"])]
+    new = [_log_int(rng, case["new_lo"], case["new_hi"]) for _ in range(case["B"])]
+    if case["B"] > 1:   # the longest one is always there
+        old[-1] = case["old_hi"]
+    for b in rng.sample(range(case["B"]), case["ended"]):
+        new[b] = -1
+    return old, new
+
+
+def _pages(n, P):
+    return -(-n // P)
+
+
+def _layout(case, seed, dev):
+    """Lengths on the device, and block tables over a pool whose pages are handed out in
+    an order of the seed's."""
+    old, new = _lengths(case)
+    P = case["P"]
+    after = [o + max(n, 0) for o, n in zip(old, new)]
+    used = sum(_pages(a, P) for a in after)
+    num_pages = used + used // 8 + 4
+    max_pages = max(_pages(a, P) for a in after) + 2
+    g = torch.Generator().manual_seed(seed)
+    perm = torch.randperm(num_pages, generator=g).to(torch.int32)
+    counts = torch.tensor([_pages(a, P) for a in after])
+    starts = torch.cumsum(counts, 0) - counts
+    col = torch.arange(max_pages)
+    tables = torch.where(col < counts[:, None],
+                         perm[(starts[:, None] + col).clamp(max=num_pages - 1)], -1)
+    cu = torch.zeros(case["B"] + 1, dtype=torch.int32)
+    cu[1:] = torch.cumsum(torch.tensor(new).clamp(min=0), 0)
+    return dict(old=torch.tensor(old, dtype=torch.int32).to(dev),
+                new=torch.tensor(new, dtype=torch.int32).to(dev),
+                lens=torch.tensor(after, dtype=torch.int32).to(dev), cu=cu.to(dev),
+                tables=tables.to(torch.int32).to(dev), perm=perm.to(dev), used=used,
+                num_pages=num_pages, max_pages=max_pages, T=sum(max(n, 0) for n in new),
+                longest=max(after), most_new=max(max(new), 1))
+
+
+def _rows(shape, g, dev, dtype):
+    """Cached rows: a few large key channels for each head, as trained models have them."""
+    x = torch.randn(shape, generator=g, device=dev)
+    big = torch.rand(shape[:-2] + (1, shape[-1]), generator=g, device=dev) < 4 / shape[-1]
+    return torch.where(big, 10 * x, x).to(dtype)
+
+
+def _pow2_scale(amax):
+    """The smallest power of two s with amax / s <= 448, at least 2^-118."""
+    m, e = torch.frexp(amax)                    # amax = m * 2^e, 0.5 <= m < 1
+    e = torch.where(m > 0.875, e - 8, e - 9)    # 448 = 0.875 * 2^9
+    e = torch.where(amax > 0, e, -118).clamp(min=-118)
+    return ((e + 127) << 23).view(torch.float32)
+
+
+def prepare(case, seed):
+    dev = torch.device("cuda:0")
+    s = _layout(case, seed, dev)
+    s["case"] = case
+    B, H, L, d, P, dt = case["B"], case["H"], case["L"], case["d"], case["P"], _DTYPES[case["dtype"]]
+    g = torch.Generator(device=dev).manual_seed(seed)
+    N = s["num_pages"]
+    if case["op"] == "plan":
+        # the pages of the tokens held are in the tables, the others in the ring of free pages
+        held = -(-s["old"].long() // P)
+        col = torch.arange(s["max_pages"], device=dev)
+        mine = torch.where(col < held[:, None], s["tables"], -1)
+        owned = torch.zeros(N, dtype=torch.bool, device=dev)
+        owned[mine[mine >= 0].long()] = True
+        free = s["perm"][~owned[s["perm"].long()]]
+        head = seed % N
+        ring = torch.full((N,), -1, dtype=torch.int32, device=dev)
+        ring[(head + torch.arange(len(free), device=dev)) % N] = free
+        s.update(tables=mine.to(torch.int32), ring=ring,
+                 free=torch.tensor([head, len(free), 0, 0], dtype=torch.int32, device=dev),
+                 rows=_pages(s["T"], 64) * 64)     # a step's buffers are padded
+        return s
+    at = torch.arange(s["T"], device=dev)
+    b = torch.searchsorted(s["cu"][1:].long(), at, right=True)
+    pos = s["old"].long()[b] + at - s["cu"].long()[b]
+    s["slots"] = (s["tables"][b, pos // P].long() * P + pos % P).to(torch.int32)
+    if case["op"] == "store":
+        if L == 1:       # a layer's projections: token by token
+            k, v = (_rows((H, s["T"], d), g, dev, dt).transpose(0, 1).contiguous().transpose(0, 1)[None]
+                    for _ in range(2))
+        else:            # a mapped cache
+            kv = torch.stack([_rows((2, H, s["T"], d), g, dev, dt) for _ in range(L)])
+            k, v = kv[:, 0], kv[:, 1]
+        s.update(k=k, v=v)
+    planes = L * 2 * H
+    pool = torch.empty((planes, N, P, d), dtype=torch.uint8, device=dev)
+    scales = torch.empty((planes, N), dtype=torch.float32, device=dev)
+    for n in range(planes):
+        x = _rows((N, P, d), g, dev, torch.float32) * (0.7 if case["op"] == "store" else 1.0)
+        scales[n] = _pow2_scale(x.abs().amax((1, 2)))
+        pool[n] = (x / scales[n][:, None, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    s["pool"] = pool.view(L, 2, H, N * P, d).view(torch.float8_e4m3fn)
+    s["scales"] = scales.view(L, 2, H, N)
+    if case["op"] == "attend":
+        s["pool"], s["scales"] = s["pool"][0], s["scales"][0]
+        s["q"] = torch.randn((s["T"], H * case["G"], d), generator=g, device=dev).to(dt)
+    return s
+
+
+# ---- plain forms ----
+
+def _plan_plain(s):
+    P, N, T = s["case"]["P"], s["num_pages"], s["rows"]
+    lens, add, tables, ring = s["old"].long(), s["new"].long(), s["tables"].long(), s["ring"].long()
+    head, count = s["free"][0].long(), s["free"][1].long()
+    M = tables.shape[1]
+    grow, ends = add.clamp(min=0), add < 0
+    end = torch.cumsum(grow, 0)
+    start = end - grow
+    have, need = (lens + P - 1) // P, (lens + grow + P - 1) // P
+    fits = (need <= M) & (end <= T)
+    ask = torch.where(fits, need - have, 0)
+    pstart = torch.cumsum(ask, 0) - ask
+    ok = fits & ((ask == 0) | (pstart + ask <= count))
+    col = torch.arange(M, device=lens.device)
+    fresh = ok[:, None] & (col >= have[:, None]) & (col < need[:, None])
+    tables_out = torch.where(fresh, ring[(head + pstart[:, None] + col - have[:, None]) % N], tables)
+    back = torch.where(ends, have, 0)
+    rend = torch.cumsum(back, 0)
+    r = (torch.arange(N, device=lens.device) - head - count) % N
+    rb = torch.searchsorted(rend, r, right=True).clamp(max=len(lens) - 1)
+    given = tables[rb, (r - rend[rb] + back[rb]).clamp(0, M - 1)]
+    ring_out = torch.where(r < rend[-1], given, ring)
+    t = torch.arange(T, device=lens.device)
+    b = torch.searchsorted(end, t, right=True).clamp(max=len(lens) - 1)
+    live = t < end[-1]
+    pos = torch.where(live, lens[b] + t - start[b], 0)
+    page = tables_out[b, (pos // P).clamp(max=M - 1)]
+    slots = torch.where(live & ok[b], page * P + pos % P, -1)
+    taken = torch.where(ok, ask, 0).sum()
+    free = torch.stack([(head + taken) % N, count - taken + rend[-1], (~ok).sum(),
+                        end[-1].clamp(max=T)])
+    cu = torch.cat([torch.zeros_like(end[:1]), end.clamp(max=T)])
+    lens_out = torch.where(ends, 0, torch.where(ok, lens + grow, lens))
+    i32 = torch.int32
+    return dict(lens=lens_out.to(i32), cu=cu.to(i32), positions=pos.to(i32), slots=slots.to(i32),
+                free=free.to(i32), tables=tables_out.to(i32), ring=ring_out.to(i32))
+
+
+def _store_plain(s):
+    c = s["case"]
+    L, H, d, P, N, T = c["L"], c["H"], c["d"], c["P"], s["num_pages"], s["T"]
+    x = torch.stack([s["k"], s["v"]], 1).float().reshape(L * 2 * H, T, d)
+    slots = s["slots"].long()
+    page, off = slots // P, slots % P
+    codes = s["pool"].view(torch.uint8).view(L * 2 * H, N, P, d)
+    old = s["scales"].view(L * 2 * H, N)
+    amax = torch.zeros_like(old).scatter_reduce_(
+        1, page.expand(L * 2 * H, T), x.abs().amax(2), "amax")
+    first = torch.full((N,), P, device=x.device).scatter_reduce_(0, page, off, "amin")
+    new = _pow2_scale(amax)
+    scale = torch.where(first == P, old, torch.where(first == 0, new, torch.maximum(old, new)))
+    # what a request's first page holds already is coded again where its scale has grown
+    begun = page[s["cu"][:-1].long()]
+    held = codes[:, begun].view(torch.float8_e4m3fn).float()
+    held = held * (old[:, begun] / scale[:, begun])[:, :, None, None]
+    live = torch.arange(P, device=x.device) < first[begun][:, None]
+    codes[:, begun] = torch.where(live[None, :, :, None],
+                                  held.to(torch.float8_e4m3fn).view(torch.uint8), codes[:, begun])
+    rows = (x / scale[:, page][:, :, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    codes.view(L * 2 * H, N * P, d)[:, slots] = rows
+    old.copy_(scale)
+    return dict(pool=s["pool"], scales=s["scales"])
+
+
+def _attend_plain(s):
+    c = s["case"]
+    B, H, G, d, P, T = c["B"], c["H"], c["G"], c["d"], c["P"], s["T"]
+    dev = s["q"].device
+    n, m = s["longest"], s["most_new"]
+    lens, cu = s["lens"].long(), s["cu"].long()
+    key = torch.arange(n, device=dev)
+    page = torch.where(key < lens[:, None], s["tables"][:, key // P].long(), 0)
+    slot = page * P + key % P                                           # [B, n]
+    kv = s["pool"].view(torch.uint8)[:, :, slot].view(torch.float8_e4m3fn).float()
+    kv = kv * s["scales"][:, :, page][..., None]                        # [2, H, B, n, d]
+    i = torch.arange(m, device=dev)
+    row = (cu[:-1, None] + i).clamp(max=T - 1)                          # [B, m]
+    q = s["q"].float().view(T, H, G, d)[row].permute(2, 0, 3, 1, 4).reshape(H, B, G * m, d)
+    score = torch.matmul(q, kv[0].transpose(2, 3)).view(H, B, G, m, n) * (1 / math.sqrt(d))
+    last = lens[:, None] - (cu[1:] - cu[:-1])[:, None] + i              # a row's own position
+    seen = (key <= last[:, :, None]) & (key < lens[:, None, None])      # [B, m, n]
+    score = torch.where(seen[None, :, None], score, -math.inf)
+    top = score.amax(4, keepdim=True)
+    top = torch.where(top == -math.inf, 0, top)
+    p = torch.exp(score - top)
+    total = p.sum(4, keepdim=True)
+    p = p / torch.where(total > 0, total, 1)
+    o = torch.matmul(p.view(H, B, G * m, n), kv[1]).view(H, B, G, m, d)
+    lse = (top + torch.log(total))[..., 0]
+    t = torch.arange(T, device=dev)
+    b = torch.searchsorted(cu[1:].contiguous(), t, right=True)
+    i = t - cu[b]
+    return dict(out=o[:, b, :, i].reshape(T, H * G, d).to(s["q"].dtype),
+                lse=lse[:, b, :, i].reshape(T, H * G))
+
+
+def run(s):
+    op = s["case"]["op"]
+    if not own:
+        return {"plan": _plan_plain, "store": _store_plain, "attend": _attend_plain}[op](s)
+    from paper_2608_03893_amd import kvx
+    if op == "plan":
+        p = kvx.plan_pages(s["old"], s["new"], s["tables"], s["ring"], s["free"], s["rows"], s["case"]["P"])
+        return dict(lens=p.lens, cu=p.cu, positions=p.positions, slots=p.slots, free=p.free,
+                    tables=s["tables"], ring=s["ring"])
+    if op == "store":
+        kvx.store_cache8(s["k"], s["v"], s["slots"], s["pool"], s["scales"])
+        return dict(pool=s["pool"], scales=s["scales"])
+    if "workspace" not in s:      # kept from step to step
+        s["workspace"] = kvx.attend_workspace(s["q"], s["pool"], s["tables"])
+    out, lse = kvx.attend_cache8(s["q"], s["pool"], s["scales"], s["tables"], s["lens"], s["cu"],
+                                 with_lse=True, workspace=s["workspace"])
+    return dict(out=out, lse=lse)
+
+
+def work(case):
+    old, new = _lengths(case)
+    H, G, L, d, P, B = case["H"], case["G"], case["L"], case["d"], case["P"], case["B"]
+    e = 2 if case["dtype"] == "bf16" else 4
+    T = sum(max(n, 0) for n in new)
+    if case["op"] == "plan":
+        pages = sum(_pages(o + n, P) - _pages(o, P) if n >= 0 else _pages(o, P) for o, n in zip(old, new))
+        # lengths in and out, row starts; a position and a slot per row; a page id moved
+        return dict(bytes=16 * B + 8 * _pages(T, 64) * 64 + 8 * pages, flops=0)
+    if case["op"] == "store":
+        pages = sum(_pages(o + n, P) - o // P for o, n in zip(old, new))
+        return dict(bytes=2 * L * H * (T * d * (e + 1) + pages * 4) + 4 * T, flops=2 * L * H * T * d * 2)
+    keys = sum(o + n for o, n in zip(old, new))
+    pairs = sum(n * o + n * (n + 1) // 2 for o, n in zip(old, new))
+    pages = sum(_pages(o + n, P) for o, n in zip(old, new))
+    return dict(bytes=2 * H * (keys * d + pages * 4) + 4 * pages + T * H * G * (2 * d * e + 4),
+                flops=4 * d * H * G * pairs)
+
+
+# ---- the operators' definitions in 64 bits, a request at a time ----
+
+def _power(e):
+    """2^e in float64, exactly, for whole e."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _log2_down(x):
+    """The largest whole e with 2^e <= x, for positive float64 x."""
+    e = torch.floor(torch.log2(x))
+    e = torch.where(_power(e + 1) <= x, e + 1, e)
+    return torch.where(_power(e) > x, e - 1, e)
+
+
+def _e4m3(x):
+    """x (float64, at most 448 in size) rounded to the nearest e4m3 value, ties to even:
+    three bits after the leading one, steps of 2^-9 below 2^-6."""
+    step = _power(_log2_down(x.abs().clamp(min=2.0 ** -6)) - 3)
+    return torch.round(x / step) * step
+
+
+def _exact_store(s):
+    c = s["case"]
+    P, N = c["P"], s["num_pages"]
+    pool, scales = s["pool"].float().double(), s["scales"].double()
+    pool = pool.view(pool.shape[:3] + (N, P, c["d"]))
+    rows = (s["k"], s["v"])
+    tables, cu = s["tables"].tolist(), s["cu"].tolist()
+    old = s["old"].tolist()
+    for b in range(c["B"]):
+        n = cu[b + 1] - cu[b]
+        at = 0
+        while at < n:
+            page, off = tables[b][(old[b] + at) // P], (old[b] + at) % P
+            m = min(P - off, n - at)
+            for kv in range(2):
+                x = rows[kv][:, :, cu[b] + at:cu[b] + at + m].double()
+                amax = x.abs().amax((2, 3))
+                best = _power(_log2_down(amax.clamp(min=2.0 ** -110)) - 9)
+                for _ in range(2):      # from a quarter of it or half of it
+                    best = torch.where(best * _E4M3_MAX < amax, best * 2, best)
+                best = torch.where(amax < 2.0 ** -110, 2.0 ** -118, best)
+                was = scales[:, kv, :, page]
+                now = best if off == 0 else torch.maximum(was, best)
+                if off:
+                    pool[:, kv, :, page, :off] = _e4m3(pool[:, kv, :, page, :off] * (was / now)[..., None, None])
+                pool[:, kv, :, page, off:off + m] = _e4m3(x / now[..., None, None])
+                scales[:, kv, :, page] = now
+            at += m
+    return dict(pool=pool.float().view(s["pool"].shape).to(torch.float8_e4m3fn), scales=scales.float())
+
+
+def _exact_attend(s):
+    c = s["case"]
+    H, G, d, P, T = c["H"], c["G"], c["d"], c["P"], s["T"]
+    dev = s["q"].device
+    out = torch.zeros((T, H * G, d), dtype=torch.float64, device=dev)
+    lse = torch.full((T, H * G), -math.inf, dtype=torch.float64, device=dev)
+    cu, lens = s["cu"].tolist(), s["lens"].tolist()
+    for b in range(c["B"]):
+        n, a, z = lens[b], cu[b], cu[b + 1]
+        if a == z:
+            continue
+        pages = s["tables"][b, :_pages(n, P)].long()
+        for h in range(H):
+            k, v = ((s["pool"][i, h].view(torch.uint8).view(-1, P, d)[pages].view(torch.float8_e4m3fn)
+                     .float().double() * s["scales"][i, h, pages].double()[:, None, None]
+                     ).view(-1, d)[:n] for i in range(2))
+            last = n - (z - a) + torch.arange(z - a, device=dev)
+            hidden = torch.arange(n, device=dev) > last[:, None]
+            for q in range(h * G, (h + 1) * G):
+                x = (s["q"][a:z, q].double() @ k.t()) / math.sqrt(d)
+                x.masked_fill_(hidden, -math.inf)
+                lse[a:z, q] = torch.logsumexp(x, 1)
+                out[a:z, q] = torch.softmax(x, 1) @ v
+    return dict(out=out, lse=lse)
+
+
+def exact(case, seed):
+    if case["op"] == "plan":
+        return None      # whole numbers
+    s = prepare(case, seed)
+    if case["op"] == "attend":
+        return _exact_attend(s)
+    # a request's page at a time: too many of them take too long
+    if case["B"] * (2 + case["new_hi"] // case["P"]) > 4000:
+        return None
+    return _exact_store(s)
