@@ -214,7 +214,7 @@ def _plan_plain(s):
     end = torch.cumsum(grow, 0)
     start = end - grow
     have, need = (lens + P - 1) // P, (lens + grow + P - 1) // P
-    fits = (need <= M) & (end <= T)
+    fits = (grow == 0) | ((need <= M) & (end <= T))
     ask = torch.where(fits, need - have, 0)
     pstart = torch.cumsum(ask, 0) - ask
     ok = fits & ((ask == 0) | (pstart + ask <= count))
