@@ -446,6 +446,123 @@ kvx_status kvx_map_cache_noalloc(const kvx_dims* dims, kvx_dtype dtype,
                                  const int32_t* positions, void* tgt_kv,
                                  uint32_t flags, void* stream);
 
+/* ---- Serving from the mapped cache, in 8 bits --------------------------
+ *
+ * The multi-turn handoff of Sec. 4.6 leaves rows in a slot-addressed pool.  The
+ * entry points below build the slots (kvx_plan_pages), keep rows in a pool of
+ * 8-bit codes (kvx_store_cache8) and let the target model's queries read that
+ * pool (kvx_attend_cache8).  A slot is page * page_size + the token's offset in
+ * its page, as in slot_mapping of kvx_map_cache_slots, and the 8-bit pool has
+ * that pool's layout: codes [L, 2, H, num_pages * page_size, d] in OCP e4m3, and
+ * scales [L, 2, H, num_pages] in fp32; a row's values are codes * scale of its
+ * page.  num_pages * page_size must stay below 2^31.  Lengths, tables and slots
+ * are device memory that the host does not read: entries out of range are
+ * skipped as each entry point states, never followed. */
+typedef struct kvx_pool {
+  int32_t num_pages;   /* pages of every (layer, K|V, head) plane            */
+  int32_t page_size;   /* tokens of a page: 16, 32, 64 or 128                */
+  int32_t max_pages;   /* entries of one row of block_tables                 */
+} kvx_pool;
+
+/* Most requests of a kvx_plan_pages or kvx_attend_cache8 call. */
+#define KVX_MAX_REQUESTS 4096
+
+/* Pages, slots and positions of a step's new tokens, from request lengths.
+ * Request b (0 <= b < B; B == 0 is a valid empty call) holds lens[b] tokens and
+ * brings add[b] new ones; add[b] == 0 leaves it as it is, add[b] < 0 says that it
+ * has ended and gives its pages back.  The new tokens of all requests are packed
+ * in order of b: request b's are rows cu_out[b] .. cu_out[b + 1] - 1 of the step's
+ * T rows.  Free pages wait in a ring (first in, first out) of num_pages entries;
+ * request b takes as many as its new tokens need beyond the pages it has.
+ * A request with new tokens is refused, whole, when its pages would pass
+ * max_pages, its rows would pass T, or the free pages run out (requests are served
+ * in order, and behind one that finds too few none gets any; the pages of
+ * requests that end in this call are free from the next call on): its length
+ * stays, its rows' slots are -1, and it takes no page.
+ *   lens, add      int32 [B]
+ *   block_tables   int32 [B, max_pages], updated: page ids of each request, in
+ *                  order of position; only entries of newly taken pages are
+ *                  written
+ *   free_ring      int32 [num_pages], updated: pages given back are appended
+ *   free_in        int32 [2]: index of the ring's first free page, their count
+ *   lens_out       int32 [B]: lens + add; lens where refused; 0 where ended
+ *   cu_out         int32 [B + 1]: row starts, at most T
+ *   positions      int32 [T]: position of each row's token; 0 beyond the last row
+ *   slot_mapping   int32 [T]: its slot; -1 beyond the last row and where refused
+ *   free_out       int32 [4]: the ring's index and count after the call, the
+ *                  number of refused requests, the number of rows (at most T)
+ * lens_out and free_out are the next call's lens and free_in.  Outputs must not
+ * overlap inputs or one another.  A negative length counts as 0. */
+kvx_status kvx_plan_pages(const kvx_pool* pool, int32_t B, int32_t T, const int32_t* lens,
+                          const int32_t* add, int32_t* block_tables, int32_t* free_ring,
+                          const int32_t* free_in, int32_t* lens_out, int32_t* cu_out,
+                          int32_t* positions, int32_t* slot_mapping, int32_t* free_out,
+                          void* stream);
+
+/* Keep T packed rows in the 8-bit pool: row t of layer l, head h goes to slot
+ * slot_mapping[t] of that plane (rows with a slot outside the pool are skipped).
+ *   k, v         bf16 or fp32 rows; element (l, h, t, c) is at
+ *                l * strides[0] + h * strides[1] + t * strides[2] + c, strides
+ *                (HOST int64 [3], in elements) not negative and multiples of 16
+ *                bytes: a mapped cache [L, 2, H, T, d] and a projection's
+ *                [T, H, d] are both taken as they are
+ *   codes        e4m3 [L, 2, H, num_pages * page_size, d], updated
+ *   scales       fp32 [L, 2, H, num_pages], updated
+ * The scale of a page is the smallest power of two s >= 2^-118 with |x| <= 448 s
+ * for all its finite rows; codes are x / s rounded to nearest even (448 is e4m3's
+ * largest value, so nothing saturates).  A power of two makes the division exact,
+ * and a floating-point code is no finer for a closer scale.  NaN and infinities
+ * become e4m3's NaN and do not count for the scale.
+ * The rows of one page must be adjacent in the call, in order of position, as
+ * kvx_plan_pages packs them; a page's earlier rows are those below the offset of
+ * the call's first one in it.  They keep their scale where it suffices; else their
+ * codes are coded again for the larger scale (exact, but for codes that fall
+ * below e4m3's least normal value).  A page whose offset 0 is written starts
+ * anew, whatever it held. */
+kvx_status kvx_store_cache8(const kvx_pool* pool, kvx_dtype dtype, int32_t L, int32_t H, int32_t T,
+                            int32_t d, const void* k, const int64_t* k_strides, const void* v,
+                            const int64_t* v_strides, const int32_t* slot_mapping, uint8_t* codes,
+                            float* scales, void* stream);
+
+/* Sizes of an attention call: B requests, H KV heads with G query heads each
+ * (query head h * G + g reads KV head h), T packed query rows, head dimension d
+ * (64 or 128). */
+typedef struct kvx_attend_dims {
+  int32_t B, H, G, T, d;
+} kvx_attend_dims;
+
+/* Bytes of workspace kvx_attend_cache8 needs (0 for B == 0, T == 0 or invalid
+ * arguments). */
+size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
+
+/* Causal attention of each request's newest tokens over its keys and values in
+ * one layer of the 8-bit pool.  Request b has lens[b] tokens in the pool, its
+ * query rows cu[b] .. cu[b + 1] - 1 belong to the last of them: row i of the n rows
+ * sees the keys at positions 0 .. lens[b] - n + i.  For row t, query head a = h*G + g:
+ *   s_j = scale * q[t, a] . K_j,  out[t, a] = sum_j exp(s_j - lse) V_j,
+ *   lse[t, a] = ln sum_j exp(s_j).
+ * A row that sees no key gives out = 0 and lse = -inf.  Keys behind a table entry
+ * outside [0, num_pages) count as unseen; lens is taken as at most
+ * max_pages * page_size, cu as rising and at most T; rows outside every request
+ * are not written.
+ *   q              bf16 or fp32; (t, a, c) at t * q_strides[0] + a * q_strides[1] + c
+ *                  (HOST int64 [2], in elements, not negative, multiples of 16 bytes)
+ *   codes, scales  one layer: [2, H, num_pages * page_size, d], [2, H, num_pages]
+ *   block_tables   int32 [B, max_pages];  lens int32 [B];  cu int32 [B + 1]
+ *   scale          factor of the scores (1 / sqrt(d) in most models), finite
+ *   out            [T, H * G, d] in q's type
+ *   lse            fp32 [T, H * G] or NULL
+ *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned
+ * Scores, softmax statistics and sums are held in fp32.  For bf16 queries the
+ * probabilities (times the page's value scale) are rounded to bf16 before their
+ * product with the values; for fp32 queries both products carry the operands'
+ * 24 bits.  Codes enter exactly. */
+kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype,
+                             const void* q, const int64_t* q_strides, const uint8_t* codes,
+                             const float* scales, const int32_t* block_tables,
+                             const int32_t* lens, const int32_t* cu, float scale, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for the last non-OK status returned on the calling thread ("" if
  * none).  The pointer stays valid until the next kvx call on that thread. */
 const char* kvx_last_error(void);

@@ -1,0 +1,200 @@
+// Page plan: block tables, slots and positions of a step's new tokens from request
+// lengths, and the ring of free pages.
+//
+// With grow_b = max(add_b, 0), pages p(n) = ceil(n / P) and prefix sums over b,
+//   end_b  = sum grow          rows of requests 0 .. b
+//   pend_b = sum ask           ask_b = p(len_b + grow_b) - p(len_b), 0 where the
+//                              request passes the table or the step's rows
+//   rend_b = sum p(len_b) of ended requests
+// row t belongs to the first b with end_b > t, the j-th page taken to the first b
+// with pend_b > j, the j-th page given back to the first b with rend_b > j.
+#include "kvx_serve.h"
+
+namespace kvx {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Inclusive sum over the workgroup's threads; every thread calls it.  `part`: one
+// entry per wave.
+__device__ int64_t block_scan(int64_t v, int64_t* part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int n = 1; n < 64; n <<= 1) {
+    const int64_t u = __shfl_up(v, n, 64);
+    if (lane >= n) v += u;
+  }
+  __syncthreads();
+  if (lane == 63) part[wave] = v;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) v += part[w];
+  return v;
+}
+
+// First b with end[b] > x, at most B (end rises).
+__device__ __forceinline__ int find(const int32_t* end, int B, int32_t x) {
+  int lo = 0, n = B;
+  while (n > 0) {
+    const int half = n >> 1;
+    if (end[lo + half] > x) n = half;
+    else { lo += half + 1; n -= half + 1; }
+  }
+  return lo;
+}
+
+// What a request asks for, its rows' end known.
+struct Request {
+  int32_t len, grow, have, ask, back;
+  bool fits;
+};
+__device__ __forceinline__ Request request(const PlanArgs& a, int b, int64_t end) {
+  Request r;
+  r.len = a.lens[b] > 0 ? a.lens[b] : 0;
+  const int32_t add = a.add[b];
+  r.grow = add > 0 ? add : 0;
+  const int64_t up = (1 << a.log2p) - 1;
+  const int64_t have = (r.len + up) >> a.log2p, need = (r.len + (int64_t)r.grow + up) >> a.log2p;
+  r.have = (int32_t)have;
+  r.fits = r.grow == 0 || (need <= a.M && end <= a.T);
+  r.ask = r.fits ? (int32_t)(need - have) : 0;
+  r.back = add < 0 ? (int32_t)(have < a.M ? have : a.M) : 0;
+  return r;
+}
+
+__device__ __forceinline__ int32_t least(int64_t x, int64_t most) {
+  return (int32_t)(x < most ? x : most);
+}
+
+// Every workgroup sums over all requests (a few loads a thread) and keeps the three
+// prefix sums in LDS, so one launch does it all; then the workgroups share the rows,
+// the pages and the requests.  Sums are taken in 64 bits and kept up to the first
+// value that no request may reach.
+__global__ void __launch_bounds__(kThreads) plan_pages_kernel(PlanArgs a) {
+  extern __shared__ int32_t lds[];
+  int32_t* end = lds;
+  int32_t* pend = lds + a.B;
+  int32_t* rend = lds + 2 * a.B;
+  __shared__ int64_t part[kThreads / 64];
+  __shared__ int32_t refused;
+  const int tid = threadIdx.x, B = a.B, T = a.T, N = a.N;
+  const int chunk = (B + kThreads - 1) / kThreads;
+  const int b0 = tid * chunk < B ? tid * chunk : B, b1 = b0 + chunk < B ? b0 + chunk : B;
+  int32_t count = a.free_in[1];
+  count = count < 0 ? 0 : count > N ? N : count;
+  const int32_t head = (int32_t)((uint32_t)a.free_in[0] % (uint32_t)N);
+
+  int64_t rows = 0;
+  for (int b = b0; b < b1; ++b) rows += a.add[b] > 0 ? a.add[b] : 0;
+  int64_t at = block_scan(rows, part) - rows;
+  int64_t asks = 0, backs = 0;
+  for (int b = b0; b < b1; ++b) {
+    at += a.add[b] > 0 ? a.add[b] : 0;
+    end[b] = least(at, (int64_t)T + 1);
+    const Request r = request(a, b, at);
+    asks += r.ask;
+    backs += r.back;
+  }
+  int64_t pat = block_scan(asks, part) - asks;
+  int64_t rat = block_scan(backs, part) - backs;
+  at = block_scan(rows, part) - rows;
+  int32_t bad = 0;
+  if (tid == 0) refused = 0;
+  __syncthreads();
+  for (int b = b0; b < b1; ++b) {
+    at += a.add[b] > 0 ? a.add[b] : 0;
+    const Request r = request(a, b, at);
+    pat += r.ask;
+    rat += r.back;
+    pend[b] = least(pat, (int64_t)N + 1);
+    rend[b] = least(rat, (int64_t)N + 1);
+    bad += !r.fits || (r.ask > 0 && pat > count);
+  }
+  if (bad) atomicAdd(&refused, bad);
+  __syncthreads();
+
+  // The requests that get pages are those whose sum fits the free ones.
+  const int n_ok = find(pend, B, count);
+  const int32_t taken = n_ok > 0 ? pend[n_ok - 1] : 0;
+  const int32_t total = B > 0 ? least(end[B - 1], T) : 0;
+  const int32_t back = B > 0 ? least(rend[B - 1], N - count) : 0;
+
+  const int first = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
+  for (int b = first; b < B; b += step) {
+    // rows past T: any end past it refuses
+    const Request r = request(a, b, end[b]);
+    const bool granted = r.fits && (r.ask == 0 || pend[b] <= count);
+    a.lens_out[b] = a.add[b] < 0 ? 0 : granted ? r.len + r.grow : a.lens[b];
+    a.cu[b + 1] = least(end[b], T);
+  }
+  if (first == 0) {
+    a.cu[0] = 0;
+    a.free_out[0] = (int32_t)(((int64_t)head + taken) % N);
+    a.free_out[1] = count - taken + back;
+    a.free_out[2] = refused;
+    a.free_out[3] = total;
+  }
+  for (int j = first; j < taken; j += step) {
+    const int b = find(pend, B, j);
+    const Request r = request(a, b, end[b]);
+    const int32_t j0 = b > 0 ? pend[b - 1] : 0;
+    a.tables[(int64_t)b * a.M + r.have + (j - j0)] = a.ring[((int64_t)head + j) % N];
+  }
+  for (int j = first; j < back; j += step) {
+    const int b = find(rend, B, j);
+    const int32_t j0 = b > 0 ? rend[b - 1] : 0;
+    a.ring[((int64_t)head + count + j) % N] = a.tables[(int64_t)b * a.M + (j - j0)];
+  }
+  // Four rows a thread and step, written together.
+  for (int g = first; g < (T + 3) / 4; g += step) {
+    int32_t pos[4], slot[4];
+    int b = find(end, B, 4 * g);
+    Request r;
+    bool granted = false;
+    int32_t start = 0, pstart = 0, stop = -1;   // of request b; stop: its last row's successor
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 4 * g + i;
+      pos[i] = 0;
+      slot[i] = -1;
+      if (t >= total) continue;
+      if (t >= stop) {
+        while (end[b] <= t) ++b;
+        r = request(a, b, end[b]);
+        granted = r.fits && (r.ask == 0 || pend[b] <= count);
+        start = b > 0 ? end[b - 1] : 0;
+        pstart = b > 0 ? pend[b - 1] : 0;
+        stop = end[b];
+      }
+      const int64_t p = (int64_t)r.len + (t - start);
+      pos[i] = (int32_t)p;
+      if (!granted) continue;
+      const int32_t n = (int32_t)(p >> a.log2p);
+      const int32_t page = n < r.have ? a.tables[(int64_t)b * a.M + n]
+                                      : a.ring[((int64_t)head + pstart + (n - r.have)) % N];
+      if (page >= 0 && page < N) slot[i] = (page << a.log2p) + (int32_t)(p & ((1 << a.log2p) - 1));
+    }
+    if (4 * g + 3 < T) {
+      *reinterpret_cast<int4*>(a.positions + 4 * g) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(a.slots + 4 * g) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * g + i < T) {
+          a.positions[4 * g + i] = pos[i];
+          a.slots[4 * g + i] = slot[i];
+        }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_plan(const PlanArgs& a, hipStream_t stream) {
+  // a thread for four rows, or for eight pages of the ring (most steps move few)
+  int64_t wg = ((int64_t)(a.T / 4 > a.N / 8 ? a.T / 4 : a.N / 8) + kThreads) / kThreads;
+  if (wg > 512) wg = 512;
+  hipLaunchKernelGGL(plan_pages_kernel, dim3((unsigned)wg), dim3(kThreads), (size_t)a.B * 12, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace kvx

@@ -7,13 +7,15 @@ non-OK status into ``KvxError``.  There is no fallback: if the library is not
 built, ``load()`` raises.
 
 Entry points mirror include/kvx.h: ``workspace_bytes``, ``rope_prepare``,
-``map_cache``, ``map_layer``, ``map_cache_slots``.
+``map_cache``, ``map_layer``, ``map_cache_slots``; and for serving from the
+mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``.
 """
 
 from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -25,7 +27,9 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "xhead_workspace_bytes", "map_cache_xhead", "map_layer_xhead",
            "map_cache_slots_xhead", "map_cache_noalloc", "SCRATCH_MAX_BYTES",
            "fit_workspace_bytes", "fit_cache", "probe_workspace_bytes", "probe_r2",
-           "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer"]
+           "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
+           "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
+           "attend_workspace_bytes", "attend_workspace", "attend_cache8"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -69,6 +73,18 @@ class Mlp(ctypes.Structure):
     """Device pointers of one set of MLP mapper weights (kvx_mlp)."""
     _fields_ = [("W1", ctypes.c_void_p), ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p),
                 ("b2", ctypes.c_void_p), ("W3", ctypes.c_void_p), ("b3", ctypes.c_void_p)]
+
+
+class Pool(ctypes.Structure):
+    """kvx_pool: pages of a slot-addressed pool and of a block table's row."""
+    _fields_ = [("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class AttendDims(ctypes.Structure):
+    """kvx_attend_dims: sizes of an attention call over the 8-bit pool."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("G", ctypes.c_int32),
+                ("T", ctypes.c_int32), ("d", ctypes.c_int32)]
 
 
 class Rope(ctypes.Structure):
@@ -149,6 +165,15 @@ def load():
     L.kvx_mlp_map_cache.restype = I32
     L.kvx_mlp_map_layer.argtypes = [DP, I32, I32, I32, P, P, MP, MP, RP, RP, P, P, P, SZ, U32, P]
     L.kvx_mlp_map_layer.restype = I32
+    PP, AP, F32 = ctypes.POINTER(Pool), ctypes.POINTER(AttendDims), ctypes.c_float
+    L.kvx_plan_pages.argtypes = [PP, I32, I32, P, P, P, P, P, P, P, P, P, P, P]
+    L.kvx_plan_pages.restype = I32
+    L.kvx_store_cache8.argtypes = [PP, I32, I32, I32, I32, I32, P, P, P, P, P, P, P, P]
+    L.kvx_store_cache8.restype = I32
+    L.kvx_attend_workspace_bytes.argtypes = [AP, I32]
+    L.kvx_attend_workspace_bytes.restype = SZ
+    L.kvx_attend_cache8.argtypes = [AP, PP, I32, P, P, P, P, P, P, P, F32, P, P, P, SZ, P]
+    L.kvx_attend_cache8.restype = I32
     L.kvx_last_error.argtypes = []
     L.kvx_last_error.restype = ctypes.c_char_p
     L.kvx_version.argtypes = []
@@ -575,3 +600,149 @@ def mlp_map_layer(l_t, src, idx, mlp_K, mlp_V, rope_src, rope_tgt, positions, ou
         ctypes.byref(rs), ctypes.byref(rt), _ptr(positions), _ptr(out), _ptr(workspace),
         workspace.numel(), flags, _stream(stream, src.device)))
     return out
+
+
+# ------------------------------------------------- serving from the mapped cache
+
+class PagePlan(NamedTuple):
+    """What plan_pages computes (device int32 tensors)."""
+    lens: torch.Tensor        # [B] tokens of each request after the step
+    cu: torch.Tensor          # [B + 1] row starts of the step's new tokens
+    positions: torch.Tensor   # [T]
+    slots: torch.Tensor       # [T], -1: no slot
+    free: torch.Tensor        # [4] first free page's place in the ring, free pages,
+                              # refused requests, rows
+
+
+def _int32(name, t, shape):
+    if t.dtype != torch.int32 or t.shape != shape:
+        raise ValueError(f"{name} must be int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None, stream=None):
+    """Pages, slots and positions of a step's new tokens; returns a PagePlan
+    (enqueued on the stream).
+
+    lens, add [B] int32 (add < 0: the request has ended), block_tables
+    [B, max_pages] and free_ring [num_pages] int32, updated in place; free: int32,
+    the ring's first place and count (the last plan's ``free``); T rows."""
+    B, T = lens.shape[0], int(T)
+    if block_tables.dim() != 2 or free_ring.dim() != 1:
+        raise ValueError("block_tables must be [B, max_pages], free_ring [num_pages]")
+    if free.dtype != torch.int32 or free.dim() != 1 or free.shape[0] < 2:
+        raise ValueError("free must be int32 with the ring's first place and count")
+    pool = Pool(num_pages=free_ring.shape[0], page_size=int(page_size),
+                max_pages=block_tables.shape[1])
+    args = [_int32("lens", lens, (B,)), _int32("add", add, (B,)),
+            _int32("block_tables", block_tables, (B, pool.max_pages)),
+            _int32("free_ring", free_ring, (pool.num_pages,)), _ptr(free)]
+    if out is None:
+        with torch.cuda.stream(_torch_stream(stream, lens.device)):
+            out = PagePlan(*[torch.empty(n, dtype=torch.int32, device=lens.device)
+                             for n in (B, B + 1, T, T, 4)])
+    _check(load().kvx_plan_pages(
+        ctypes.byref(pool), B, T, *args,
+        *[_int32(name, t, (n,)) for name, t, n in zip(PagePlan._fields, out, (B, B + 1, T, T, 4))],
+        _stream(stream, lens.device)))
+    return out
+
+
+def _rows_ptr(name, t):
+    """Pointer of a tensor whose last dimension is dense, whatever the other strides."""
+    if not t.is_cuda:
+        raise ValueError("tensor arguments must live on the GPU")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    return ctypes.c_void_p(t.data_ptr()) if t.numel() else None
+
+
+def _strides(t):
+    n = t.dim() - 1
+    return (ctypes.c_int64 * n)(*t.stride()[:n])
+
+
+def _pool8(pool, scales, lead):
+    """kvx_pool of an 8-bit pool [*lead, num_slots, d] and its scales [*lead, num_pages]."""
+    n = len(lead)
+    if (pool.dtype != torch.float8_e4m3fn or pool.dim() != n + 2 or tuple(pool.shape[:n]) != lead):
+        raise ValueError(f"pool must be float8_e4m3fn {lead} + [num_slots, d]")
+    if scales.dtype != torch.float32 or scales.dim() != n + 1 or tuple(scales.shape[:n]) != lead:
+        raise ValueError(f"scales must be float32 {lead} + [num_pages]")
+    slots, pages = pool.shape[n], scales.shape[n]
+    if pages < 1 or slots % pages:
+        raise ValueError(f"{slots} slots do not divide into {pages} pages")
+    return Pool(num_pages=pages, page_size=slots // pages, max_pages=1)
+
+
+def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
+    """Keep rows in the 8-bit pool (enqueued on the stream).
+
+    k, v [L, H, T, d] bf16 or fp32, any strides of 16 bytes with d dense (a mapped
+    cache's out[:, 0] and out[:, 1], or a projection's [T, H, d] transposed);
+    slot_mapping int32 [T]; pool [L, 2, H, num_slots, d] float8_e4m3fn and scales
+    [L, 2, H, num_pages] float32, updated in place."""
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must be [L, H, T, d] of one dtype")
+    L, H, T, d = k.shape
+    p = _pool8(pool, scales, (L, 2, H))
+    if pool.shape[4] != d:
+        raise ValueError(f"pool rows have {pool.shape[4]} channels, k and v {d}")
+    _check(load().kvx_store_cache8(
+        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_ptr("k", k), _strides(k),
+        _rows_ptr("v", v), _strides(v), _int32("slot_mapping", slot_mapping, (T,)), _ptr(pool),
+        _ptr(scales), _stream(stream, k.device)))
+    return pool
+
+
+def _attend_dims(q, pool, block_tables):
+    if q.dim() != 3 or pool.dim() != 4 or block_tables.dim() != 2:
+        raise ValueError("q must be [T, H*G, d], pool [2, H, num_slots, d], block_tables [B, max_pages]")
+    T, heads, d = q.shape
+    H = pool.shape[1]
+    if heads % H or pool.shape[3] != d:
+        raise ValueError(f"{heads} query heads of {d} channels on a pool of {H} heads of {pool.shape[3]}")
+    return AttendDims(B=block_tables.shape[0], H=H, G=heads // H, T=T, d=d)
+
+
+def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
+    return int(load().kvx_attend_workspace_bytes(ctypes.byref(dims), 0 if dtype == "bf16" else 1))
+
+
+def attend_workspace(q, pool, block_tables):
+    """A workspace for attend_cache8 calls of these shapes, to be kept between them."""
+    dims = _attend_dims(q, pool, block_tables)
+    need = attend_workspace_bytes(dims, "bf16" if q.dtype == torch.bfloat16 else "f32")
+    return torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+
+
+def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None, with_lse=False,
+                  workspace=None, stream=None):
+    """Causal attention of the newest tokens over one layer of the 8-bit pool
+    (enqueued on the stream); returns out [T, H*G, d], with_lse also lse [T, H*G].
+
+    q [T, H*G, d] bf16 or fp32 (d dense); pool [2, H, num_slots, d], scales
+    [2, H, num_pages]; block_tables [B, max_pages], lens [B] (tokens in the pool,
+    the new ones included), cu [B + 1] (their rows in q) int32; scale: factor of
+    the scores, 1 / sqrt(d) by default."""
+    dims = _attend_dims(q, pool, block_tables)
+    p = _pool8(pool, scales, (2, dims.H))
+    p.max_pages = block_tables.shape[1]
+    B, code = dims.B, _dtype_code(q)
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
+        raise ValueError("out must have q's shape and dtype")
+    args = [_rows_ptr("q", q), _strides(q), _ptr(pool), _ptr(scales),
+            _int32("block_tables", block_tables, (B, p.max_pages)), _int32("lens", lens, (B,)),
+            _int32("cu", cu, (B + 1,))]
+    with torch.cuda.stream(_torch_stream(stream, q.device)):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+    if workspace is None:
+        with torch.cuda.stream(_torch_stream(stream, q.device)):
+            workspace = attend_workspace(q, pool, block_tables)
+    _check(load().kvx_attend_cache8(
+        ctypes.byref(dims), ctypes.byref(p), code, *args,
+        dims.d ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(lse), _ptr(workspace),
+        workspace.numel(), _stream(stream, q.device)))
+    return (out, lse) if with_lse else out
