@@ -552,7 +552,9 @@ size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
  *   scale          factor of the scores (1 / sqrt(d) in most models), finite
  *   out            [T, H * G, d] in q's type
  *   lse            fp32 [T, H * G] or NULL
- *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned
+ *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned; filled with
+ *                  zeros before its first use (it holds counters, which every call
+ *                  leaves at zero); calls of any sizes may follow one another in it
  * Scores, softmax statistics and sums are held in fp32.  For bf16 queries the
  * probabilities (times the page's value scale) are rounded to bf16 before their
  * product with the values; for fp32 queries both products carry the operands'

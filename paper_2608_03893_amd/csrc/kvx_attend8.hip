@@ -1,106 +1,531 @@
-// Attention over the 8-bit pool.
+// Attention over the 8-bit pool, split over the keys: few query rows a request
+// (decoding steps, drafted tokens).
+//
+// For a block of 16 query rows (tokens times the G heads of a KV head) and a tile of
+// 16 keys the scores are S^T = K Q^T on the matrix cores: a lane then holds one query
+// row's scores for 4 keys, so the softmax needs no exchange but the maximum over four
+// lanes, and P^T has the layout that O^T = V^T P^T takes as its second operand.  e4m3
+// codes are bf16 numbers, so K and V enter exactly; a page's scales multiply the scores
+// and the probabilities.  fp32 queries and probabilities enter as three bf16 terms, which
+// hold all 24 bits.
+//
+// Bound by the bytes of K and V, which go from memory straight to registers, each once:
+// a lane reads 16 bytes of one key's row, or 8 bytes of 8 value rows whose bytes it then
+// pairs up for V^T.
+//
+// The grid is fixed and every workgroup takes an equal share of all (request, row block,
+// head, 128 keys) quanta, whatever the lengths: it finds its share from a prefix sum over
+// the requests.  A block of rows whose keys span workgroups is joined by the workgroup
+// that comes last, from partial sums in order of the keys, so results do not depend on
+// timing.
 #include "kvx_e4m3.h"
 #include "kvx_serve.h"
 
 namespace kvx {
 namespace {
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int n = 32; n; n >>= 1) v = fmaxf(v, __shfl_xor(v, n, 64));
-  return v;
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kStep = 32;                  // keys of a wave's step
+constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
+constexpr int kRows = 16;                  // query rows of a block
+constexpr int kGrid = 512;                 // workgroups: two per CU
+constexpr int kJoin = 16;                  // partial sums joined at a time
+constexpr float kLazy = 8.0f;              // growth of a row's maximum (log2) that is let pass
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+// Largest / sum of a value over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float quad_max(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int n = 32; n; n >>= 1) v += __shfl_xor(v, n, 64);
-  return v;
+__device__ __forceinline__ float quad_sum(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-// A wave for each (row, query head): 64 keys at a time, a lane each for the scores, then
-// the lanes' channels for the sum of values.
-template <int DT, int D>
-__global__ void __launch_bounds__(64) attend8_kernel(AttendArgs a) {
-  __shared__ float qs[D];
-  const int lane = threadIdx.x, head = blockIdx.y, h = head / a.G, Hq = a.H * a.G;
-  const int t = blockIdx.x;
-  // the request of row t: the first one whose rows end behind it
-  int b = 0, n = a.B;
-  while (n > 0) {
-    const int half = n >> 1;
-    if (a.cu[b + half + 1] > t) n = half;
-    else { b += half + 1; n -= half + 1; }
+// Codes 2 HALF and 2 HALF + 1 of a word as bf16, exactly.
+template <bool HALF>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HALF));
+}
+__device__ __forceinline__ bf16x8_t bf16_octet(uint32_t lo, uint32_t hi) {
+  const u32x4_t r = {bf16_pair<false>(lo), bf16_pair<true>(lo), bf16_pair<false>(hi), bf16_pair<true>(hi)};
+  return __builtin_bit_cast(bf16x8_t, r);
+}
+
+__device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// x as DT == 0: one bf16 term (x is a bf16 number, or is rounded to one); 1: three terms
+// whose sum is x to 24 bits.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float* x, bf16x8_t* out) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    u32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[i] = pack2(rest[2 * i], rest[2 * i + 1]);
+      rest[2 * i] -= lo_bf16(r[i]);
+      rest[2 * i + 1] -= hi_bf16(r[i]);
+    }
+    out[t] = __builtin_bit_cast(bf16x8_t, r);
   }
-  if (b == a.B || a.cu[b] > t) return;
-  const int end = a.cu[b + 1] < a.T ? a.cu[b + 1] : a.T;
+}
+
+// Quanta of request b's blocks of rows.
+struct Request {
+  int32_t rows, len, row0;        // query rows (tokens * G), keys, first token row
+  int32_t tokens, blocks, quanta; // new tokens; blocks of rows; quanta of one block and head
+};
+__device__ __forceinline__ Request request(const AttendArgs& a, int b) {
+  Request r;
+  int c0 = a.cu[b], c1 = a.cu[b + 1];
+  c0 = c0 < 0 ? 0 : c0;
+  c1 = c1 > a.T ? a.T : c1;
+  r.row0 = c0;
+  r.tokens = c1 > c0 ? c1 - c0 : 0;
   const int64_t cap = (int64_t)a.M << a.log2p;
-  const int len = a.lens[b] < cap ? a.lens[b] : (int)cap;
-  const int seen = len - (end - t) + 1;   // keys 0 .. seen - 1
-  for (int c = lane; c < D; c += 64) {
-    const int64_t at = t * a.q_stride[0] + head * a.q_stride[1] + c;
-    qs[c] = DT == 0 ? lo_bf16(static_cast<const uint16_t*>(a.q)[at]) : static_cast<const float*>(a.q)[at];
+  r.len = a.lens[b] < 0 ? 0 : a.lens[b] < cap ? a.lens[b] : (int)cap;
+  r.rows = r.tokens * a.G;
+  r.blocks = (r.rows + kRows - 1) / kRows;
+  // rows without any key still have an output
+  r.quanta = r.len > kQuant ? (int)(((int64_t)r.len + kQuant - 1) / kQuant) : 1;
+  return r;
+}
+
+// A step's keys and values, as loaded.
+template <int D>
+struct Stage {
+  static constexpr int U = D / 64, V = D / 64;
+  uint4 k[2][U];            // tile t: row lane & 15, bytes 64 u + 16 (lane >> 4) ..
+  uint32_t v[8][V];         // key (lane >> 4) * 4 + (j & 3) of tile j >> 2, bytes (lane & 15) * 4 V ..
+};
+
+template <int DT, int D>
+__global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+  constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
+  constexpr int RS = D + 4;                                        // row stride in LDS
+  constexpr int SLOT = kRows * (D + 2);                            // floats of a partial sum
+  extern __shared__ int64_t pre[];                                 // [B] quanta of requests 0 .. b
+  __shared__ int64_t part[kWaves];
+  __shared__ __attribute__((aligned(16))) float jo[kWaves][kRows * RS];
+  __shared__ float jm[kWaves][kRows], jl[kWaves][kRows];
+  __shared__ int last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g4 = lane >> 4;
+
+  {  // prefix sum of the requests' quanta
+    const int chunk = (a.B + kThreads - 1) / kThreads;
+    const int b0 = tid * chunk < a.B ? tid * chunk : a.B, b1 = b0 + chunk < a.B ? b0 + chunk : a.B;
+    int64_t sum = 0;
+    for (int b = b0; b < b1; ++b) {
+      const Request r = request(a, b);
+      sum += (int64_t)r.blocks * r.quanta * a.H;
+    }
+    int64_t v = sum;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int64_t u = __shfl_up(v, s, 64);
+      if (lane >= s) v += u;
+    }
+    if (lane == 63) part[wave] = v;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += part[w];
+    v -= sum;
+    for (int b = b0; b < b1; ++b) {
+      const Request r = request(a, b);
+      v += (int64_t)r.blocks * r.quanta * a.H;
+      pre[b] = v;
+    }
+    __syncthreads();
   }
-  __syncthreads();
+  const int64_t total = pre[a.B - 1];
+  const int64_t per = (total + kGrid - 1) / kGrid;
+  int64_t at = (int64_t)blockIdx.x * per;
+  const int64_t end = at + per < total ? at + per : total;
+  if (at >= end) return;
+  int b = 0;
+  for (int left = a.B; left > 0;) {   // first request whose quanta end behind `at`
+    const int half = left >> 1;
+    if (pre[b + half] > at) left = half;
+    else { b += half + 1; left -= half + 1; }
+  }
+
   const int64_t plane = ((int64_t)a.N << a.log2p) * D;
-  const uint8_t* kc = a.codes + h * plane;
-  const uint8_t* vc = a.codes + (a.H + h) * plane;
-  const float* ks = a.scales + (int64_t)h * a.N;
-  const float* vs = a.scales + (int64_t)(a.H + h) * a.N;
-  float top = -INFINITY, total = 0.0f, o[D / 64] = {};
-  for (int j0 = 0; j0 < seen; j0 += 64) {
-    const int j = j0 + lane;
-    float s = -INFINITY, sv = 0.0f;
-    int64_t row = 0;
-    if (j < seen) {
-      const int page = a.tables[(int64_t)b * a.M + (j >> a.log2p)];
-      if (page >= 0 && page < a.N) {
-        row = (((int64_t)page << a.log2p) + (j & ((1 << a.log2p) - 1))) * D;
-        float dot = 0.0f;
-        for (int c = 0; c < D; c += 4) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(kc + row + c);
-          dot = fmaf(qs[c], from_e4m3<0>(w), dot);
-          dot = fmaf(qs[c + 1], from_e4m3<1>(w), dot);
-          dot = fmaf(qs[c + 2], from_e4m3<2>(w), dot);
-          dot = fmaf(qs[c + 3], from_e4m3<3>(w), dot);
+  const int P1 = (1 << a.log2p) - 1;
+  while (at < end) {
+    while (pre[b] <= at) ++b;
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int64_t base = b > 0 ? pre[b - 1] : 0;
+    const Request r = request(a, b);
+    const int64_t unit = (at - base) / r.quanta;
+    const int blk = (int)(unit / a.H), h = (int)(unit % a.H);
+    const int64_t unit0 = base + unit * r.quanta;              // its first quantum
+    const int q0 = __builtin_amdgcn_readfirstlane((int)(at - unit0));
+    const int q1 = __builtin_amdgcn_readfirstlane(
+        (int)(end - unit0 < r.quanta ? end - unit0 : r.quanta));
+
+    // this lane's query row: limit of its keys, its channels
+    const int row = blk * kRows + n;
+    const bool mine = row < r.rows;
+    const int token = mine ? row / a.G : 0, head = h * a.G + (mine ? row % a.G : 0);
+    const int lim = mine ? r.len - r.tokens + token : -1;      // last key it sees
+    const int first_tok = blk * kRows / a.G;
+    const int last_row = (blk + 1) * kRows < r.rows ? (blk + 1) * kRows - 1 : r.rows - 1;
+    const bool full = (blk + 1) * kRows <= r.rows;
+    const int lim_lo = full ? r.len - r.tokens + first_tok : -1;          // least and largest
+    const int lim_hi = r.len - r.tokens + last_row / a.G;                 // of the block
+    bf16x8_t qf[2 * U][TERMS];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int64_t off = (int64_t)(r.row0 + token) * a.q_stride[0] + (int64_t)head * a.q_stride[1] +
+                            64 * u + 16 * g4 + 8 * w;
+        if (DT == 0) {
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (mine) x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + off);
+          qf[2 * u + w][0] = as_bf16x8(x);
+        } else {
+          float x[8];
+          float4 lo = make_float4(0, 0, 0, 0), hi = lo;
+          if (mine) {
+            lo = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
+            hi = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off + 4);
+          }
+          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
+          x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+          split_terms<TERMS>(x, qf[2 * u + w]);
         }
-        s = dot * (ks[page] * a.scale_log2);
-        sv = vs[page];
+      }
+
+    const uint8_t* kc = a.codes + h * plane;
+    const uint8_t* vc = a.codes + (a.H + h) * plane;
+    const uint32_t k_lane = (uint32_t)n * D + 16 * g4, v_lane = (uint32_t)g4 * 4 * D + n * (D / 16);
+    float m = -INFINITY, l = 0.0f;
+    f32x4_t o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = (f32x4_t){0, 0, 0, 0};
+
+    // pages of this wave's next 32 steps: lane 2 s + t has tile t of step s
+    for (int qa = q0; qa < q1; qa += 32) {
+      const int qb = qa + 32 < q1 ? qa + 32 : q1;
+      int page = -1;
+      {
+        const int64_t key = (int64_t)(qa + (lane >> 1)) * kQuant + wave * kStep + (lane & 1) * 16;
+        if (key < r.len) page = a.tables[(int64_t)b * a.M + (key >> a.log2p)];
+        if (page >= a.N) page = -1;
+      }
+      float ksc = 0.0f, vsc = 0.0f;
+      if (page >= 0) {
+        ksc = a.scales[(int64_t)h * a.N + page] * a.scale_log2;
+        vsc = a.scales[(int64_t)(a.H + h) * a.N + page];
+      }
+      auto load = [&](Stage<D>& s, int q) {
+        const int key = q * kQuant + wave * kStep;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          int p = __builtin_amdgcn_readlane(page, 2 * (q - qa) + t);
+          p = p < 0 ? 0 : p;
+          const int64_t off = (((int64_t)p << a.log2p) + ((key + 16 * t) & P1)) * D;
+          const uint8_t* kp = kc + off;
+          const uint8_t* vp = vc + off;
+#pragma unroll
+          for (int u = 0; u < U; ++u) s.k[t][u] = *reinterpret_cast<const uint4*>(kp + k_lane + 64 * u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (D == 128) {
+              const uint2 x = *reinterpret_cast<const uint2*>(vp + v_lane + j * D);
+              s.v[4 * t + j][0] = x.x;
+              s.v[4 * t + j][U - 1] = x.y;
+            } else {
+              s.v[4 * t + j][0] = *reinterpret_cast<const uint32_t*>(vp + v_lane + j * D);
+            }
+          }
+        }
+      };
+      auto compute = [&](Stage<D>& s, int q) {
+        const int key = q * kQuant + wave * kStep;
+        float x[8];
+        bool nan_v = false;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          f32x4_t acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const bf16x8_t k0 = bf16_octet(s.k[t][u].x, s.k[t][u].y), k1 = bf16_octet(s.k[t][u].z, s.k[t][u].w);
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) {
+              acc = mfma(k0, qf[2 * u][e], acc);
+              acc = mfma(k1, qf[2 * u + 1][e], acc);
+            }
+          }
+          const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), 2 * (q - qa) + t));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[4 * t + i] = acc[i] * sc;
+        }
+        const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa));
+        const int p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
+        const float v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa)));
+        const float v1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa) + 1));
+        const bool masked = p0 < 0 || p1 < 0 || key + kStep - 1 > lim_lo;
+        if (masked) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int kk = key + 16 * (j >> 2) + 4 * g4 + (j & 3);
+            const bool real = (j < 4 ? p0 : p1) >= 0 && kk < r.len;
+            if (!(real && kk <= lim)) x[j] = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < U; ++w) {
+              if (!real) s.v[j][w] = 0;     // nobody's codes, NaN perhaps
+              nan_v |= (((s.v[j][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+          }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+        top = quad_max(top);
+        // The reference of the exponentials follows the maximum only when that has
+        // grown by 2^8: the sums hold that, and O is seldom rescaled.
+        if (__any(top > m + kLazy)) {
+          const float now = fmaxf(m, top);
+          const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+          m = now;
+          l *= keep;
+#pragma unroll
+          for (int c = 0; c < C; ++c) o[c] *= keep;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = __builtin_amdgcn_exp2f(x[j] - ref);
+          l += p[j];
+        }
+        bf16x8_t seen = {};
+        const bool any_nan = masked && __any(nan_v);
+        if (any_nan) {     // which keys each row sees
+          u32x4_t w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = (x[2 * j] == -INFINITY ? 0u : 0x3f80u) | (x[2 * j + 1] == -INFINITY ? 0u : 0x3f800000u);
+          seen = __builtin_bit_cast(bf16x8_t, w);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float y = p[j] * (j < 4 ? v0 : v1);
+          p[j] = masked && x[j] == -INFINITY ? 0.0f : y;
+        }
+        bf16x8_t pf[TERMS];
+        split_terms<TERMS>(p, pf);
+#pragma unroll
+        for (int w = 0; w < U; ++w) {
+          uint32_t y[4][2];   // pairs of keys: bytes (c, c), (c + 1, c + 1) | the next two channels
+          if (any_nan) {
+            // NaN values count only in rows that see their key
+            uint32_t z[4][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t nan = ((((s.v[j][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+              s.v[j][w] &= ~nan;
+              const uint32_t one = nan & 0x38383838u;     // e4m3's 1.0
+              if (j & 1) {
+                z[j >> 1][1] = __builtin_amdgcn_perm(one, z[j >> 1][0], 0x07030602u);
+                z[j >> 1][0] = __builtin_amdgcn_perm(one, z[j >> 1][0], 0x05010400u);
+              } else {
+                z[j >> 1][0] = one;
+              }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              u32x4_t f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                f[j] = c & 1 ? bf16_pair<true>(z[j][c >> 1]) : bf16_pair<false>(z[j][c >> 1]);
+              const f32x4_t hit = mfma(__builtin_bit_cast(bf16x8_t, f), seen, (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (hit[i] != 0.0f) o[4 * w + c][i] = __builtin_nanf("");
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            y[j][0] = __builtin_amdgcn_perm(s.v[2 * j + 1][w], s.v[2 * j][w], 0x05010400u);
+            y[j][1] = __builtin_amdgcn_perm(s.v[2 * j + 1][w], s.v[2 * j][w], 0x07030602u);
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            u32x4_t f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              f[j] = c & 1 ? bf16_pair<true>(y[j][c >> 1]) : bf16_pair<false>(y[j][c >> 1]);
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e)
+              o[4 * w + c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[e], o[4 * w + c]);
+          }
+        }
+      };
+      // this wave's steps with a key that some row sees
+      const int64_t room = (int64_t)lim_hi - wave * kStep;
+      int qe = room < 0 ? qa : (int)(room / kQuant) + 1;
+      qe = qe < qb ? qe : qb;
+      Stage<D> s0, s1;
+      if (qa < qe) load(s0, qa);
+      for (int q = qa; q < qe; q += 2) {
+        if (q + 1 < qe) load(s1, q + 1);
+        compute(s0, q);
+        if (q + 1 < qe) {
+          if (q + 2 < qe) load(s0, q + 2);
+          compute(s1, q + 1);
+        }
       }
     }
-    const float now = fmaxf(top, wave_max(s));
-    const float ref = now == -INFINITY ? 0.0f : now;
-    const float keep = exp2f(top - ref);
-    const float p = s == -INFINITY ? 0.0f : exp2f(s - ref);   // NaN stays
-    total = total * keep + wave_sum(p);
-    top = now;
-    for (int i = 0; i < D / 64; ++i) o[i] *= keep;
-    const float pv = p * sv;
-    for (int i = 0; i < 64; ++i) {
-      if (__shfl(s, i, 64) == -INFINITY) continue;
-      const float w = __shfl(pv, i, 64);
-      const uint8_t* v = vc + __shfl((long long)row, i, 64);
-      for (int c = 0; c < D / 64; ++c) o[c] = fmaf(w, from_e4m3<0>(v[lane + 64 * c]), o[c]);
+
+    // the four waves' sums: lane (n, g4) has of row n the channels (4 g4 + i) C + c
+    l = quad_sum(l);
+    if (g4 == 0) {
+      jm[wave][n] = m;
+      jl[wave][n] = l;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < C; c += 4)
+        *reinterpret_cast<f32x4_t*>(&jo[wave][n * RS + (4 * g4 + i) * C + c]) =
+            (f32x4_t){o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+    __syncthreads();
+    // thread (row, C channels) from here on
+    const int jr = tid >> 4, jc = (tid & 15) * C;
+    const int out_row = blk * kRows + jr;
+    float sum[C] = {}, top = -INFINITY, den = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, jm[w][jr]);
+    {
+      const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2f(jm[w][jr] - ref);    // 0 for a wave that saw nothing; NaN sums stay
+        den += f * jl[w][jr];
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum[c] += f * jo[w][jr * RS + jc + c];
+      }
+    }
+    // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`
+    const int64_t g0 = unit0 / per, g1 = (unit0 + r.quanta - 1) / per;
+    bool done = g0 == g1;
+    if (!done) {
+      const int parts = (int)(g1 - g0) + 1, mine_at = (int)(blockIdx.x - g0);
+      auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
+      auto put = [&](int i) {
+        float* to = partial + (int64_t)slot(i) * SLOT;
+        if (out_row < r.rows) {
+#pragma unroll
+          for (int c = 0; c < C; c += 4)
+            *reinterpret_cast<f32x4_t*>(to + jr * D + jc + c) = (f32x4_t){sum[c], sum[c + 1], sum[c + 2], sum[c + 3]};
+          if ((tid & 15) == 0) {
+            to[kRows * D + jr] = top;
+            to[kRows * D + kRows + jr] = den;
+          }
+        }
+      };
+      // joins `count` partial sums first, first + stride, ..
+      auto join = [&](int first, int stride, int count) {
+        top = -INFINITY;
+        den = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum[c] = 0.0f;
+        if (out_row >= r.rows) return;
+        for (int i = 0; i < count; ++i)
+          top = fmaxf(top, partial[(int64_t)slot(first + i * stride) * SLOT + kRows * D + jr]);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        for (int i = 0; i < count; ++i) {
+          const float* from = partial + (int64_t)slot(first + i * stride) * SLOT;
+          const float f = exp2f(from[kRows * D + jr] - ref);
+          den += f * from[kRows * D + kRows + jr];
+#pragma unroll
+          for (int c = 0; c < C; ++c) sum[c] += f * from[jr * D + jc + c];
+        }
+      };
+      // true in the workgroup that comes last of `count`; the counter is zero again then
+      auto arrive = [&](int* counter, int count) {
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+          last = atomicAdd(counter, 1) == count - 1;
+          if (last) *counter = 0;
+        }
+        __syncthreads();
+        const bool is_last = last != 0;
+        if (is_last) __threadfence();
+        return is_last;
+      };
+      put(mine_at);
+      const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
+      const int in_group = parts - group * kJoin < kJoin ? parts - group * kJoin : kJoin;
+      if (arrive(counters + 2 * slot(group * kJoin), in_group)) {
+        join(group * kJoin, 1, in_group);
+        done = groups == 1;
+        if (!done) {
+          __syncthreads();       // all have read the partial sums that put overwrites
+          put(group * kJoin);
+          if (arrive(counters + 2 * slot(0) + 1, groups)) {
+            join(0, kJoin, groups);
+            done = true;
+          }
+        }
+      }
+    }
+    if (done && out_row < r.rows) {
+      const int64_t to = (int64_t)(r.row0 + out_row / a.G) * a.H * a.G + h * a.G + out_row % a.G;
+      const float f = den == 0.0f ? 0.0f : 1.0f / den;    // no key: 0
+      if (DT == 0) {
+        uint32_t* y = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + to * D + jc);
+#pragma unroll
+        for (int c = 0; c < C / 2; ++c) y[c] = pack2(sum[2 * c] * f, sum[2 * c + 1] * f);
+      } else {
+        float* y = static_cast<float*>(a.out) + to * D + jc;
+#pragma unroll
+        for (int c = 0; c < C; ++c) y[c] = sum[c] * f;
+      }
+      if (a.lse != nullptr && (tid & 15) == 0)
+        a.lse[to] = den == 0.0f ? -INFINITY : (top + log2f(den)) * 0.69314718055994530942f;
+    }
+    __syncthreads();    // the LDS arrays are free again
+    at = unit0 + q1;
   }
-  const float r = total == 0.0f ? 0.0f : 1.0f / total;   // NaN stays
-  const int64_t at = (int64_t)t * Hq + head;
-  for (int c = 0; c < D / 64; ++c) {
-    if (DT == 0) static_cast<uint16_t*>(a.out)[at * D + lane + 64 * c] = (uint16_t)pack2(o[c] * r, 0.0f);
-    else static_cast<float*>(a.out)[at * D + lane + 64 * c] = o[c] * r;
-  }
-  if (a.lse != nullptr && lane == 0)
-    a.lse[at] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.69314718055994530942f;
 }
 
 }  // namespace
 
-size_t attend_ws_bytes(int, int, int, int, int, int) { return 0; }
+// Two counters and two partial sums for each workgroup's first and last unit.
+size_t attend_ws_bytes(int, int, int, int, int d, int) {
+  return (size_t)kGrid * 4 * sizeof(int) + (size_t)kGrid * 2 * kRows * (d + 2) * sizeof(float);
+}
 
-hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void*, hipStream_t stream) {
-  const dim3 grid(a.T, a.H * a.G);
-  if (dtype == 0 && d == 64) hipLaunchKernelGGL((attend8_kernel<0, 64>), grid, dim3(64), 0, stream, a);
-  else if (dtype == 0) hipLaunchKernelGGL((attend8_kernel<0, 128>), grid, dim3(64), 0, stream, a);
-  else if (d == 64) hipLaunchKernelGGL((attend8_kernel<1, 64>), grid, dim3(64), 0, stream, a);
-  else hipLaunchKernelGGL((attend8_kernel<1, 128>), grid, dim3(64), 0, stream, a);
+hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
+  int* counters = static_cast<int*>(ws);
+  float* partial = reinterpret_cast<float*>(counters + kGrid * 4);
+  const size_t lds = (size_t)a.B * sizeof(int64_t);
+  const dim3 grid(kGrid), block(kThreads);
+  if (dtype == 0 && d == 64)
+    hipLaunchKernelGGL((attend8_split_kernel<0, 64>), grid, block, lds, stream, a, partial, counters);
+  else if (dtype == 0)
+    hipLaunchKernelGGL((attend8_split_kernel<0, 128>), grid, block, lds, stream, a, partial, counters);
+  else if (d == 64)
+    hipLaunchKernelGGL((attend8_split_kernel<1, 64>), grid, block, lds, stream, a, partial, counters);
+  else
+    hipLaunchKernelGGL((attend8_split_kernel<1, 128>), grid, block, lds, stream, a, partial, counters);
   return hipGetLastError();
 }
 

@@ -713,7 +713,7 @@ def attend_workspace(q, pool, block_tables):
     """A workspace for attend_cache8 calls of these shapes, to be kept between them."""
     dims = _attend_dims(q, pool, block_tables)
     need = attend_workspace_bytes(dims, "bf16" if q.dtype == torch.bfloat16 else "f32")
-    return torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    return torch.zeros(max(need, 1), dtype=torch.uint8, device=q.device)
 
 
 def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None, with_lse=False,
