@@ -103,6 +103,17 @@ __device__ __forceinline__ Request request(const AttendArgs& a, int b) {
   return r;
 }
 
+// Two floats written through to memory / read from there, past this XCD's L2.
+__device__ __forceinline__ void put2(float* to, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* from) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
 // A step's keys and values, as loaded.
 template <int D>
 struct Stage {
@@ -427,48 +438,67 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
     if (!done) {
       const int parts = (int)(g1 - g0) + 1, mine_at = (int)(blockIdx.x - g0);
       auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
+      // Partial sums pass between workgroups on different XCDs, each with its own L2: they
+      // are written through and read past it (agent scope), which spares the write-back
+      // of the whole L2 that a fence at that scope costs.
       auto put = [&](int i) {
         float* to = partial + (int64_t)slot(i) * SLOT;
         if (out_row < r.rows) {
 #pragma unroll
-          for (int c = 0; c < C; c += 4)
-            *reinterpret_cast<f32x4_t*>(to + jr * D + jc + c) = (f32x4_t){sum[c], sum[c + 1], sum[c + 2], sum[c + 3]};
-          if ((tid & 15) == 0) {
-            to[kRows * D + jr] = top;
-            to[kRows * D + kRows + jr] = den;
-          }
+          for (int c = 0; c < C; c += 2) put2(to + jr * D + jc + c, sum[c], sum[c + 1]);
+          if ((tid & 15) == 0) put2(to + kRows * D + 2 * jr, top, den);
         }
       };
-      // joins `count` partial sums first, first + stride, ..
+      // joins `count` partial sums first, first + stride, .., four in flight
       auto join = [&](int first, int stride, int count) {
         top = -INFINITY;
         den = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) sum[c] = 0.0f;
         if (out_row >= r.rows) return;
-        for (int i = 0; i < count; ++i)
-          top = fmaxf(top, partial[(int64_t)slot(first + i * stride) * SLOT + kRows * D + jr]);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        for (int i = 0; i < count; ++i) {
-          const float* from = partial + (int64_t)slot(first + i * stride) * SLOT;
-          const float f = exp2f(from[kRows * D + jr] - ref);
-          den += f * from[kRows * D + kRows + jr];
+        for (int i0 = 0; i0 < count; i0 += 4) {
+          float2 md[4], x[4][C / 2];
 #pragma unroll
-          for (int c = 0; c < C; ++c) sum[c] += f * from[jr * D + jc + c];
+          for (int i = 0; i < 4; ++i) {
+            const int at_i = i0 + i < count ? i0 + i : count - 1;
+            const float* from = partial + (int64_t)slot(first + at_i * stride) * SLOT;
+            md[i] = get2(from + kRows * D + 2 * jr);
+#pragma unroll
+            for (int c = 0; c < C / 2; ++c) x[i][c] = get2(from + jr * D + jc + 2 * c);
+          }
+          float now = top;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) now = fmaxf(now, md[i].x);
+          const float ref = now == -INFINITY ? 0.0f : now;
+          const float keep = exp2f(top - ref);
+          top = now;
+          den *= keep;
+#pragma unroll
+          for (int c = 0; c < C; ++c) sum[c] *= keep;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (i0 + i >= count) break;
+            const float f = exp2f(md[i].x - ref);
+            den += f * md[i].y;
+#pragma unroll
+            for (int c = 0; c < C / 2; ++c) {
+              sum[2 * c] += f * x[i][c].x;
+              sum[2 * c + 1] += f * x[i][c].y;
+            }
+          }
         }
       };
       // true in the workgroup that comes last of `count`; the counter is zero again then
       auto arrive = [&](int* counter, int count) {
-        __threadfence();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's partial sums are out
         __syncthreads();
         if (tid == 0) {
-          last = atomicAdd(counter, 1) == count - 1;
-          if (last) *counter = 0;
+          const int n = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          last = n == count - 1;
+          if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         __syncthreads();
-        const bool is_last = last != 0;
-        if (is_last) __threadfence();
-        return is_last;
+        return last != 0;
       };
       put(mine_at);
       const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
