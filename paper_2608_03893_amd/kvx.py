@@ -603,6 +603,9 @@ def mlp_map_layer(l_t, src, idx, mlp_K, mlp_V, rope_src, rope_tgt, positions, ou
 
 
 # ------------------------------------------------- serving from the mapped cache
+#
+# These calls take a few microseconds on the GPU, so the binding keeps its own work small:
+# plain integers for pointers, the raw stream handle, no stream context for the default.
 
 class PagePlan(NamedTuple):
     """What plan_pages computes (device int32 tensors)."""
@@ -614,10 +617,30 @@ class PagePlan(NamedTuple):
                               # refused requests, rows
 
 
+def _raw_stream(stream, device):
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _new(shape, dtype, device, stream):
+    """An output allocated on the launch stream (see _scratch)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _addr(name, t):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
 def _int32(name, t, shape):
     if t.dtype != torch.int32 or t.shape != shape:
         raise ValueError(f"{name} must be int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    return _addr(name, t)
 
 
 def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None, stream=None):
@@ -627,52 +650,48 @@ def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None,
     lens, add [B] int32 (add < 0: the request has ended), block_tables
     [B, max_pages] and free_ring [num_pages] int32, updated in place; free: int32,
     the ring's first place and count (the last plan's ``free``); T rows."""
-    B, T = lens.shape[0], int(T)
     if block_tables.dim() != 2 or free_ring.dim() != 1:
         raise ValueError("block_tables must be [B, max_pages], free_ring [num_pages]")
     if free.dtype != torch.int32 or free.dim() != 1 or free.shape[0] < 2:
         raise ValueError("free must be int32 with the ring's first place and count")
-    pool = Pool(num_pages=free_ring.shape[0], page_size=int(page_size),
-                max_pages=block_tables.shape[1])
-    args = [_int32("lens", lens, (B,)), _int32("add", add, (B,)),
-            _int32("block_tables", block_tables, (B, pool.max_pages)),
-            _int32("free_ring", free_ring, (pool.num_pages,)), _ptr(free)]
+    B, M = block_tables.shape
+    N, T, dev = free_ring.shape[0], int(T), lens.device
+    args = (_int32("lens", lens, (B,)), _int32("add", add, (B,)),
+            _int32("block_tables", block_tables, (B, M)), _int32("free_ring", free_ring, (N,)),
+            _addr("free", free))
     if out is None:
-        with torch.cuda.stream(_torch_stream(stream, lens.device)):
-            out = PagePlan(*[torch.empty(n, dtype=torch.int32, device=lens.device)
-                             for n in (B, B + 1, T, T, 4)])
-    _check(load().kvx_plan_pages(
-        ctypes.byref(pool), B, T, *args,
-        *[_int32(name, t, (n,)) for name, t, n in zip(PagePlan._fields, out, (B, B + 1, T, T, 4))],
-        _stream(stream, lens.device)))
+        out = PagePlan(*[_new(n, torch.int32, dev, stream) for n in (B, B + 1, T, T, 4)])
+        outs = [t.data_ptr() for t in out]
+    else:
+        outs = [_int32(name, t, (n,)) for name, t, n in zip(PagePlan._fields, out, (B, B + 1, T, T, 4))]
+    _check(load().kvx_plan_pages(ctypes.byref(Pool(N, int(page_size), M)), B, T, *args, *outs,
+                                 _raw_stream(stream, dev)))
     return out
 
 
-def _rows_ptr(name, t):
-    """Pointer of a tensor whose last dimension is dense, whatever the other strides."""
+def _rows_addr(name, t):
+    """Address of a tensor whose last dimension is dense, whatever the other strides."""
     if not t.is_cuda:
-        raise ValueError("tensor arguments must live on the GPU")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be dense in its last dimension")
-    return ctypes.c_void_p(t.data_ptr()) if t.numel() else None
+    return t.data_ptr()
 
 
-def _strides(t):
-    n = t.dim() - 1
-    return (ctypes.c_int64 * n)(*t.stride()[:n])
+_Strides2, _Strides3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
 
-def _pool8(pool, scales, lead):
+def _pool8(pool, scales, lead, max_pages):
     """kvx_pool of an 8-bit pool [*lead, num_slots, d] and its scales [*lead, num_pages]."""
-    n = len(lead)
-    if (pool.dtype != torch.float8_e4m3fn or pool.dim() != n + 2 or tuple(pool.shape[:n]) != lead):
-        raise ValueError(f"pool must be float8_e4m3fn {lead} + [num_slots, d]")
-    if scales.dtype != torch.float32 or scales.dim() != n + 1 or tuple(scales.shape[:n]) != lead:
-        raise ValueError(f"scales must be float32 {lead} + [num_pages]")
-    slots, pages = pool.shape[n], scales.shape[n]
+    shape, spages = pool.shape, scales.shape
+    if pool.dtype != torch.float8_e4m3fn or len(shape) != len(lead) + 2 or shape[:-2] != lead:
+        raise ValueError(f"pool must be float8_e4m3fn {tuple(lead)} + [num_slots, d]")
+    if scales.dtype != torch.float32 or len(spages) != len(lead) + 1 or spages[:-1] != lead:
+        raise ValueError(f"scales must be float32 {tuple(lead)} + [num_pages]")
+    slots, pages = shape[-2], spages[-1]
     if pages < 1 or slots % pages:
         raise ValueError(f"{slots} slots do not divide into {pages} pages")
-    return Pool(num_pages=pages, page_size=slots // pages, max_pages=1)
+    return Pool(pages, slots // pages, max_pages)
 
 
 def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
@@ -685,13 +704,13 @@ def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
     if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("k and v must be [L, H, T, d] of one dtype")
     L, H, T, d = k.shape
-    p = _pool8(pool, scales, (L, 2, H))
+    p = _pool8(pool, scales, (L, 2, H), 1)
     if pool.shape[4] != d:
         raise ValueError(f"pool rows have {pool.shape[4]} channels, k and v {d}")
     _check(load().kvx_store_cache8(
-        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_ptr("k", k), _strides(k),
-        _rows_ptr("v", v), _strides(v), _int32("slot_mapping", slot_mapping, (T,)), _ptr(pool),
-        _ptr(scales), _stream(stream, k.device)))
+        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_addr("k", k), _Strides3(*k.stride()[:3]),
+        _rows_addr("v", v), _Strides3(*v.stride()[:3]), _int32("slot_mapping", slot_mapping, (T,)),
+        _addr("pool", pool), _addr("scales", scales), _raw_stream(stream, k.device)))
     return pool
 
 
@@ -702,18 +721,22 @@ def _attend_dims(q, pool, block_tables):
     H = pool.shape[1]
     if heads % H or pool.shape[3] != d:
         raise ValueError(f"{heads} query heads of {d} channels on a pool of {H} heads of {pool.shape[3]}")
-    return AttendDims(B=block_tables.shape[0], H=H, G=heads // H, T=T, d=d)
+    return AttendDims(block_tables.shape[0], H, heads // H, T, d)
 
 
 def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
+    if dtype not in ("bf16", "f32"):
+        raise ValueError("dtype must be 'bf16' or 'f32'")
     return int(load().kvx_attend_workspace_bytes(ctypes.byref(dims), 0 if dtype == "bf16" else 1))
 
 
-def attend_workspace(q, pool, block_tables):
-    """A workspace for attend_cache8 calls of these shapes, to be kept between them."""
-    dims = _attend_dims(q, pool, block_tables)
-    need = attend_workspace_bytes(dims, "bf16" if q.dtype == torch.bfloat16 else "f32")
-    return torch.zeros(max(need, 1), dtype=torch.uint8, device=q.device)
+def attend_workspace(q, pool, block_tables, stream=None):
+    """A workspace for attend_cache8 calls of these shapes, to be kept between them
+    (zeros, as its first use needs)."""
+    need = int(load().kvx_attend_workspace_bytes(
+        ctypes.byref(_attend_dims(q, pool, block_tables)), _dtype_code(q)))
+    with torch.cuda.stream(_torch_stream(stream, q.device)):
+        return torch.zeros(max(need, 1), dtype=torch.uint8, device=q.device)
 
 
 def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None, with_lse=False,
@@ -726,23 +749,22 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     the new ones included), cu [B + 1] (their rows in q) int32; scale: factor of
     the scores, 1 / sqrt(d) by default."""
     dims = _attend_dims(q, pool, block_tables)
-    p = _pool8(pool, scales, (2, dims.H))
-    p.max_pages = block_tables.shape[1]
-    B, code = dims.B, _dtype_code(q)
-    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
+    B, M = block_tables.shape
+    p = _pool8(pool, scales, (2, dims.H), M)
+    code, dev, shape = _dtype_code(q), q.device, q.shape
+    args = (_rows_addr("q", q), _Strides2(*q.stride()[:2]), _addr("pool", pool), _addr("scales", scales),
+            _int32("block_tables", block_tables, (B, M)), _int32("lens", lens, (B,)),
+            _int32("cu", cu, (B + 1,)))
+    if out is None:
+        out = _new(shape, q.dtype, dev, stream)
+    elif out.shape != shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and dtype")
-    args = [_rows_ptr("q", q), _strides(q), _ptr(pool), _ptr(scales),
-            _int32("block_tables", block_tables, (B, p.max_pages)), _int32("lens", lens, (B,)),
-            _int32("cu", cu, (B + 1,))]
-    with torch.cuda.stream(_torch_stream(stream, q.device)):
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+    lse = _new(shape[:2], torch.float32, dev, stream) if with_lse else None
     if workspace is None:
-        with torch.cuda.stream(_torch_stream(stream, q.device)):
-            workspace = attend_workspace(q, pool, block_tables)
+        workspace = attend_workspace(q, pool, block_tables, stream)
     _check(load().kvx_attend_cache8(
         ctypes.byref(dims), ctypes.byref(p), code, *args,
-        dims.d ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(lse), _ptr(workspace),
-        workspace.numel(), _stream(stream, q.device)))
+        dims.d ** -0.5 if scale is None else float(scale), _addr("out", out),
+        None if lse is None else lse.data_ptr(), _addr("workspace", workspace),
+        workspace.numel(), _raw_stream(stream, dev)))
     return (out, lse) if with_lse else out
