@@ -1,0 +1,147 @@
+// Shared by the attention kernels over the 8-bit pool (device code only): codes as matrix
+// operands, reductions over the lanes that share a query row, requests, partial sums that
+// pass between workgroups.
+#pragma once
+
+#include "kvx_e4m3.h"
+#include "kvx_serve.h"
+
+namespace kvx {
+namespace {
+
+constexpr float kLazy = 8.0f;    // growth of a row's maximum (log2) that is let pass
+constexpr int kJoin = 16;        // partial sums joined at a time
+// Arrival counters, first in the workspace (four for each workgroup of the larger grid):
+// all kernels keep them there and leave them at zero, and partial sums behind.
+constexpr int kCounters = 4 * 512;
+
+// Largest / sum of a value over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float quad_max(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// Codes 2 HALF and 2 HALF + 1 of a word as bf16, exactly.
+template <bool HALF>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HALF));
+}
+__device__ __forceinline__ bf16x8_t bf16_octet(uint32_t lo, uint32_t hi) {
+  const u32x4_t r = {bf16_pair<false>(lo), bf16_pair<true>(lo), bf16_pair<false>(hi), bf16_pair<true>(hi)};
+  return __builtin_bit_cast(bf16x8_t, r);
+}
+
+__device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// x as DT == 0: one bf16 term (x is a bf16 number, or is rounded to one); 1: three terms
+// whose sum is x to 24 bits.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float* x, bf16x8_t* out) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    u32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[i] = pack2(rest[2 * i], rest[2 * i + 1]);
+      rest[2 * i] -= lo_bf16(r[i]);
+      rest[2 * i + 1] -= hi_bf16(r[i]);
+    }
+    out[t] = __builtin_bit_cast(bf16x8_t, r);
+  }
+}
+
+// A request's rows and keys, clamped to what the arrays hold.
+struct Request {
+  int32_t row0, tokens, rows;   // first query row, new tokens, rows of a KV head (tokens * G)
+  int32_t len;                  // keys
+};
+__device__ __forceinline__ Request request(const AttendArgs& a, int b) {
+  Request r;
+  int c0 = a.cu[b], c1 = a.cu[b + 1];
+  c0 = c0 < 0 ? 0 : c0;
+  c1 = c1 > a.T ? a.T : c1;
+  r.row0 = c0;
+  r.tokens = c1 > c0 ? c1 - c0 : 0;
+  const int64_t cap = (int64_t)a.M << a.log2p;
+  r.len = a.lens[b] < 0 ? 0 : a.lens[b] < cap ? a.lens[b] : (int)cap;
+  r.rows = r.tokens * a.G;
+  return r;
+}
+
+// Two floats written through to memory / read from there, past this XCD's L2.
+__device__ __forceinline__ void put2(float* to, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* from) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// pre[b] = sum of weight(request 0 .. b), by a workgroup of THREADS; part: an entry per wave.
+template <int THREADS, typename W>
+__device__ __forceinline__ void prefix_requests(const AttendArgs& a, int64_t* pre, int64_t* part, W weight) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int chunk = (a.B + THREADS - 1) / THREADS;
+  const int b0 = tid * chunk < a.B ? tid * chunk : a.B, b1 = b0 + chunk < a.B ? b0 + chunk : a.B;
+  int64_t sum = 0;
+  for (int b = b0; b < b1; ++b) sum += weight(request(a, b));
+  int64_t v = sum;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t u = __shfl_up(v, s, 64);
+    if (lane >= s) v += u;
+  }
+  if (lane == 63) part[tid >> 6] = v;
+  __syncthreads();
+  for (int w = 0; w < tid >> 6; ++w) v += part[w];
+  v -= sum;
+  for (int b = b0; b < b1; ++b) {
+    v += weight(request(a, b));
+    pre[b] = v;
+  }
+  __syncthreads();
+}
+
+// First b with pre[b] > x.
+__device__ __forceinline__ int find_request(const int64_t* pre, int B, int64_t x) {
+  int b = 0;
+  for (int left = B; left > 0;) {
+    const int half = left >> 1;
+    if (pre[b + half] > x) left = half;
+    else { b += half + 1; left -= half + 1; }
+  }
+  return b;
+}
+
+// True in the workgroup that comes last of `count` at a counter, which is zero again then.
+// What its threads wrote with put2 before is out; `last` is a word of LDS.  Relaxed
+// operations at agent scope: the stores went past this XCD's L2 and have been waited for.
+__device__ __forceinline__ bool arrive(int* counter, int count, int* last) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int n = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *last = n == count - 1;
+    if (*last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return *last != 0;
+}
+
+}  // namespace
+}  // namespace kvx

@@ -18,8 +18,7 @@
 // the requests.  A block of rows whose keys span workgroups is joined by the workgroup
 // that comes last, from partial sums in order of the keys, so results do not depend on
 // timing.
-#include "kvx_e4m3.h"
-#include "kvx_serve.h"
+#include "kvx_attend8.h"
 
 namespace kvx {
 namespace {
@@ -29,89 +28,12 @@ constexpr int kStep = 32;                  // keys of a wave's step
 constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
 constexpr int kRows = 16;                  // query rows of a block
 constexpr int kGrid = 512;                 // workgroups: two per CU
-constexpr int kJoin = 16;                  // partial sums joined at a time
-constexpr float kLazy = 8.0f;              // growth of a row's maximum (log2) that is let pass
 
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-
-// Largest / sum of a value over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float quad_max(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// Codes 2 HALF and 2 HALF + 1 of a word as bf16, exactly.
-template <bool HALF>
-__device__ __forceinline__ uint32_t bf16_pair(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HALF));
-}
-__device__ __forceinline__ bf16x8_t bf16_octet(uint32_t lo, uint32_t hi) {
-  const u32x4_t r = {bf16_pair<false>(lo), bf16_pair<true>(lo), bf16_pair<false>(hi), bf16_pair<true>(hi)};
-  return __builtin_bit_cast(bf16x8_t, r);
-}
-
-__device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-// x as DT == 0: one bf16 term (x is a bf16 number, or is rounded to one); 1: three terms
-// whose sum is x to 24 bits.
-template <int TERMS>
-__device__ __forceinline__ void split_terms(const float* x, bf16x8_t* out) {
-  float rest[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) rest[i] = x[i];
-#pragma unroll
-  for (int t = 0; t < TERMS; ++t) {
-    u32x4_t r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r[i] = pack2(rest[2 * i], rest[2 * i + 1]);
-      rest[2 * i] -= lo_bf16(r[i]);
-      rest[2 * i + 1] -= hi_bf16(r[i]);
-    }
-    out[t] = __builtin_bit_cast(bf16x8_t, r);
-  }
-}
-
-// Quanta of request b's blocks of rows.
-struct Request {
-  int32_t rows, len, row0;        // query rows (tokens * G), keys, first token row
-  int32_t tokens, blocks, quanta; // new tokens; blocks of rows; quanta of one block and head
-};
-__device__ __forceinline__ Request request(const AttendArgs& a, int b) {
-  Request r;
-  int c0 = a.cu[b], c1 = a.cu[b + 1];
-  c0 = c0 < 0 ? 0 : c0;
-  c1 = c1 > a.T ? a.T : c1;
-  r.row0 = c0;
-  r.tokens = c1 > c0 ? c1 - c0 : 0;
-  const int64_t cap = (int64_t)a.M << a.log2p;
-  r.len = a.lens[b] < 0 ? 0 : a.lens[b] < cap ? a.lens[b] : (int)cap;
-  r.rows = r.tokens * a.G;
-  r.blocks = (r.rows + kRows - 1) / kRows;
-  // rows without any key still have an output
-  r.quanta = r.len > kQuant ? (int)(((int64_t)r.len + kQuant - 1) / kQuant) : 1;
-  return r;
-}
-
-// Two floats written through to memory / read from there, past this XCD's L2.
-__device__ __forceinline__ void put2(float* to, float x, float y) {
-  const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get2(const float* from) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+// Blocks of rows, and quanta of one block and head (rows without any key still have an
+// output).
+__device__ __forceinline__ int blocks_of(const Request& r) { return (r.rows + kRows - 1) / kRows; }
+__device__ __forceinline__ int quanta_of(const Request& r) {
+  return r.len > kQuant ? (int)(((int64_t)r.len + kQuant - 1) / kQuant) : 1;
 }
 
 // A step's keys and values, as loaded.
@@ -135,42 +57,15 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g4 = lane >> 4;
 
-  {  // prefix sum of the requests' quanta
-    const int chunk = (a.B + kThreads - 1) / kThreads;
-    const int b0 = tid * chunk < a.B ? tid * chunk : a.B, b1 = b0 + chunk < a.B ? b0 + chunk : a.B;
-    int64_t sum = 0;
-    for (int b = b0; b < b1; ++b) {
-      const Request r = request(a, b);
-      sum += (int64_t)r.blocks * r.quanta * a.H;
-    }
-    int64_t v = sum;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int64_t u = __shfl_up(v, s, 64);
-      if (lane >= s) v += u;
-    }
-    if (lane == 63) part[wave] = v;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) v += part[w];
-    v -= sum;
-    for (int b = b0; b < b1; ++b) {
-      const Request r = request(a, b);
-      v += (int64_t)r.blocks * r.quanta * a.H;
-      pre[b] = v;
-    }
-    __syncthreads();
-  }
+  prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
+    return (int64_t)blocks_of(r) * quanta_of(r) * a.H;
+  });
   const int64_t total = pre[a.B - 1];
   const int64_t per = (total + kGrid - 1) / kGrid;
   int64_t at = (int64_t)blockIdx.x * per;
   const int64_t end = at + per < total ? at + per : total;
   if (at >= end) return;
-  int b = 0;
-  for (int left = a.B; left > 0;) {   // first request whose quanta end behind `at`
-    const int half = left >> 1;
-    if (pre[b + half] > at) left = half;
-    else { b += half + 1; left -= half + 1; }
-  }
+  int b = find_request(pre, a.B, at);
 
   const int64_t plane = ((int64_t)a.N << a.log2p) * D;
   const int P1 = (1 << a.log2p) - 1;
@@ -179,12 +74,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
     b = __builtin_amdgcn_readfirstlane(b);
     const int64_t base = b > 0 ? pre[b - 1] : 0;
     const Request r = request(a, b);
-    const int64_t unit = (at - base) / r.quanta;
+    const int quanta = quanta_of(r);
+    const int64_t unit = (at - base) / quanta;
     const int blk = (int)(unit / a.H), h = (int)(unit % a.H);
-    const int64_t unit0 = base + unit * r.quanta;              // its first quantum
+    const int64_t unit0 = base + unit * quanta;              // its first quantum
     const int q0 = __builtin_amdgcn_readfirstlane((int)(at - unit0));
     const int q1 = __builtin_amdgcn_readfirstlane(
-        (int)(end - unit0 < r.quanta ? end - unit0 : r.quanta));
+        (int)(end - unit0 < quanta ? end - unit0 : quanta));
 
     // this lane's query row: limit of its keys, its channels
     const int row = blk * kRows + n;
@@ -303,14 +199,14 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
             }
           }
         }
+        // The reference of the exponentials follows the maximum only when that has
+        // grown by 2^8: the sums hold that, no lane has to ask the others in most
+        // steps, and O is seldom rescaled.
         float top = x[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-        top = quad_max(top);
-        // The reference of the exponentials follows the maximum only when that has
-        // grown by 2^8: the sums hold that, and O is seldom rescaled.
         if (__any(top > m + kLazy)) {
-          const float now = fmaxf(m, top);
+          const float now = fmaxf(m, quad_max(top));
           const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
           m = now;
           l *= keep;
@@ -433,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
       }
     }
     // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`
-    const int64_t g0 = unit0 / per, g1 = (unit0 + r.quanta - 1) / per;
+    const int64_t g0 = unit0 / per, g1 = (unit0 + quanta - 1) / per;
     bool done = g0 == g1;
     if (!done) {
       const int parts = (int)(g1 - g0) + 1, mine_at = (int)(blockIdx.x - g0);
@@ -488,28 +384,16 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
           }
         }
       };
-      // true in the workgroup that comes last of `count`; the counter is zero again then
-      auto arrive = [&](int* counter, int count) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's partial sums are out
-        __syncthreads();
-        if (tid == 0) {
-          const int n = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          last = n == count - 1;
-          if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        return last != 0;
-      };
       put(mine_at);
       const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
       const int in_group = parts - group * kJoin < kJoin ? parts - group * kJoin : kJoin;
-      if (arrive(counters + 2 * slot(group * kJoin), in_group)) {
+      if (arrive(counters + 2 * slot(group * kJoin), in_group, &last)) {
         join(group * kJoin, 1, in_group);
         done = groups == 1;
         if (!done) {
           __syncthreads();       // all have read the partial sums that put overwrites
           put(group * kJoin);
-          if (arrive(counters + 2 * slot(0) + 1, groups)) {
+          if (arrive(counters + 2 * slot(0) + 1, groups, &last)) {
             join(0, kJoin, groups);
             done = true;
           }
@@ -536,16 +420,21 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
   }
 }
 
+// Which kernel: many rows a request share the widened codes over eight waves.
+bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G > (int64_t)B * 32; }
+
 }  // namespace
 
-// Two counters and two partial sums for each workgroup's first and last unit.
-size_t attend_ws_bytes(int, int, int, int, int d, int) {
-  return (size_t)kGrid * 4 * sizeof(int) + (size_t)kGrid * 2 * kRows * (d + 2) * sizeof(float);
+// Counters and two partial sums for each workgroup's first and last unit.
+size_t attend_ws_bytes(int B, int, int G, int T, int d, int dtype) {
+  if (by_rows(B, G, T, dtype)) return attend_rows_ws_bytes(d);
+  return kCounters * sizeof(int) + (size_t)kGrid * 2 * kRows * (d + 2) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
+  if (by_rows(a.B, a.G, a.T, dtype)) return launch_attend_rows(a, d, ws, stream);
   int* counters = static_cast<int*>(ws);
-  float* partial = reinterpret_cast<float*>(counters + kGrid * 4);
+  float* partial = reinterpret_cast<float*>(counters + kCounters);
   const size_t lds = (size_t)a.B * sizeof(int64_t);
   const dim3 grid(kGrid), block(kThreads);
   if (dtype == 0 && d == 64)

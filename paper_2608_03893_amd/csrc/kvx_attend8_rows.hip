@@ -1,0 +1,494 @@
+// Attention over the 8-bit pool, split over the query rows: chunks of new tokens, bf16.
+//
+// A workgroup of 8 waves takes 8 * 16 NB query rows of a KV head (tokens times the G heads)
+// through 128 keys at a time; a wave has 16 NB rows.  The codes become bf16 matrix
+// operands once: each wave takes half of 32 keys (K or V) from memory to registers,
+// widens them to the layout of the matrix instruction's first operand and leaves them in
+// LDS, whole operands one after another, so that reads and writes of LDS are 16 bytes a
+// lane without conflicts.  Two such buffers: while the waves compute on one, the loads of
+// the next are in flight.  The products are those of the split kernel (kvx_attend8.hip).
+// A value's scale is applied as the code is widened (a power of two is exact there).
+//
+// Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them.
+//
+// One workgroup a CU; each takes an equal share of the weight of all (request, head, block
+// of rows), a block's weight being the keys that its last row sees.  Neighbouring
+// shares lie on the same XCD, whose L2 then holds a head's codes for all of its blocks.
+#include "kvx_attend8.h"
+
+namespace kvx {
+namespace {
+
+constexpr int kThreads = 512, kWaves = 8;
+constexpr int kSteps = 4, kStep = 32, kQuant = kSteps * kStep;
+constexpr int kGrid = 256;                 // workgroups: one per CU
+constexpr int kXcds = 8;
+
+// Codes 2 HALF and 2 HALF + 1 of a word times a power of two, as bf16.
+template <bool HALF>
+__device__ __forceinline__ uint32_t bf16_pair_by(uint32_t w, float by) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, by, HALF));
+}
+
+template <int NB>
+struct Weights {
+  static constexpr int kRows = kWaves * 16 * NB, kSlope = kRows / kQuant;
+  // Weight of block k (0-based) of a request and head, in quanta times G: the keys before the
+  // new tokens, and those up to its last row.
+  __device__ static int64_t before(const Request& r, int G) {
+    return (int64_t)G * ((r.len > r.tokens ? r.len - r.tokens : 0) / kQuant + 1);
+  }
+  __device__ static int blocks(const Request& r) { return (r.rows + kRows - 1) / kRows; }
+  // of blocks 0 .. n - 1
+  __device__ static int64_t sum(int64_t before, int64_t n) { return n * before + kSlope * (n * (n + 1) / 2); }
+};
+
+template <int D, int NB>
+__global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a, float* partial, int* counters) {
+  using WT = Weights<NB>;
+  constexpr int U = D / 64, C = D / 16, KF = 4 * U, F = KF + C;   // operands of a step: keys, all
+  constexpr int ROWS = WT::kRows;
+  constexpr int SLOT = kWaves * NB * (4 * C + 2) * 64;            // floats of a partial sum
+  __shared__ __attribute__((aligned(16))) u32x4_t kv[2][kSteps][F][64];
+  __shared__ float ksc[2][kSteps][2];       // scale of the scores of a 16-key tile
+  __shared__ int kbad[2][kSteps];           // bit t: tile t has no page
+  __shared__ int vnan[2][kSteps];           // some value is NaN (where rows differ in what they see)
+  __shared__ int64_t part[kWaves];
+  __shared__ int last;
+  static_assert(sizeof(kv) >= KVX_MAX_REQUESTS * sizeof(int64_t), "the prefix sums fit");
+  int64_t* pre = reinterpret_cast<int64_t*>(kv);   // until the first unit
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g4 = lane >> 4;
+  const int step_of = wave & 3;             // the step whose keys (waves 0-3) or values this wave widens
+
+  prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
+    return a.H * WT::sum(WT::before(r, a.G), WT::blocks(r));
+  });
+  const int64_t total = pre[a.B - 1];
+  const int64_t per = (total + kGrid - 1) / kGrid;
+  const int me = (blockIdx.x % kXcds) * (kGrid / kXcds) + blockIdx.x / kXcds;   // share `me`
+  int64_t at = me * per;
+  const int64_t end = at + per < total ? at + per : total;
+  if (at >= end) return;
+  int b = __builtin_amdgcn_readfirstlane(find_request(pre, a.B, at));
+  int64_t base = b > 0 ? pre[b - 1] : 0;
+  __syncthreads();
+
+  const int64_t plane = ((int64_t)a.N << a.log2p) * D;
+  const int P1 = (1 << a.log2p) - 1;
+  while (at < end) {
+    // the unit (request, head, block) at `at`
+    const Request r = request(a, b);
+    const int64_t before = WT::before(r, a.G);
+    const int blocks = WT::blocks(r);
+    const int64_t head_w = WT::sum(before, blocks);
+    if (at >= base + a.H * head_w) {
+      base += a.H * head_w;
+      ++b;
+      continue;
+    }
+    const int h = __builtin_amdgcn_readfirstlane((int)((at - base) / head_w));
+    const int64_t z = at - base - h * head_w;
+    int blk = 0;
+    for (int left = blocks; left > 0;) {   // last block whose first weight is at most z
+      const int half = left >> 1;
+      if (WT::sum(before, blk + half + 1) <= z) { blk += half + 1; left -= half + 1; }
+      else left = half;
+    }
+    blk = __builtin_amdgcn_readfirstlane(blk);
+    const int64_t unit0 = base + h * head_w + WT::sum(before, blk);
+    const int64_t weight = WT::sum(before, blk + 1) - WT::sum(before, blk);
+    const int last_row = (blk + 1) * ROWS < r.rows ? (blk + 1) * ROWS - 1 : r.rows - 1;
+    const int lim_block = r.len - r.tokens + last_row / a.G;     // last key of the block
+    const int quanta = lim_block < 0 ? 1 : lim_block / kQuant + 1;
+    const int q0 = __builtin_amdgcn_readfirstlane((int)((at - unit0) * quanta / weight));
+    const int q1 = __builtin_amdgcn_readfirstlane(
+        end - unit0 >= weight ? quanta : (int)((end - unit0) * quanta / weight));
+
+    int lim[NB];
+    bool mine[NB];
+    bf16x8_t qf[2 * U][NB];
+    const int row0 = blk * ROWS + wave * 16 * NB;
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+      const int row = row0 + 16 * x + n;
+      mine[x] = row < r.rows;
+      const int token = mine[x] ? row / a.G : 0, head = h * a.G + (mine[x] ? row % a.G : 0);
+      lim[x] = mine[x] ? r.len - r.tokens + token : -1;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          u32x4_t v = {0, 0, 0, 0};
+          if (mine[x])
+            v = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) +
+                                                  (int64_t)(r.row0 + token) * a.q_stride[0] +
+                                                  (int64_t)head * a.q_stride[1] + 64 * u + 16 * g4 + 8 * w);
+          qf[2 * u + w][x] = __builtin_bit_cast(bf16x8_t, v);
+        }
+    }
+    // least and largest of the wave's limits, and the least of the block's
+    const bool wave_full = row0 + 16 * NB <= r.rows, block_full = (blk + 1) * ROWS <= r.rows;
+    const int wave_last = row0 + 16 * NB - 1 < r.rows ? row0 + 16 * NB - 1 : r.rows - 1;
+    const int lim_lo = wave_full ? r.len - r.tokens + row0 / a.G : -1;
+    const int lim_hi = row0 < r.rows ? r.len - r.tokens + wave_last / a.G : -1;
+    const int block_lo = block_full ? r.len - r.tokens + blk * ROWS / a.G : -1;
+
+    f32x4_t o[NB][C];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+      m[x] = -INFINITY;
+      l[x] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[x][c] = (f32x4_t){0, 0, 0, 0};
+    }
+
+    const uint8_t* codes = a.codes + (wave < 4 ? h : a.H + h) * plane;
+    const float* scales = a.scales + (int64_t)(wave < 4 ? h : a.H + h) * a.N;
+    const uint32_t lane_off = wave < 4 ? (uint32_t)n * D + 16 * g4 : (uint32_t)g4 * 4 * D + n * (D / 16);
+    int page = -1, qa = 0;        // lane 2 s + t: page of tile t of this wave's step in quantum qa + s
+    float scale = 0.0f;
+    uint32_t st[8 * U];
+    auto pages = [&](int q) {
+      qa = q;
+      page = -1;
+      scale = 1.0f;
+      const int64_t key = (int64_t)(q + (lane >> 1)) * kQuant + step_of * kStep + (lane & 1) * 16;
+      if (key < r.len) page = a.tables[(int64_t)b * a.M + (key >> a.log2p)];
+      if (page >= a.N) page = -1;
+      if (page >= 0) scale = scales[page];
+    };
+    auto load = [&](int q) {
+      const int key = q * kQuant + step_of * kStep;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        int p = __builtin_amdgcn_readlane(page, 2 * (q - qa) + t);
+        p = p < 0 ? 0 : p;
+        const uint8_t* from = codes + (((int64_t)p << a.log2p) + ((key + 16 * t) & P1)) * D + lane_off;
+        if (wave < 4) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(from + 64 * u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[4 * (t * U + u) + i] = v[i];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (D == 128) {
+              const uint2 v = *reinterpret_cast<const uint2*>(from + j * D);
+              st[(4 * t + j) * U] = v.x;
+              st[(4 * t + j) * U + U - 1] = v.y;
+            } else {
+              st[4 * t + j] = *reinterpret_cast<const uint32_t*>(from + j * D);
+            }
+          }
+        }
+      }
+    };
+    auto widen = [&](int q, int buf) {
+      const int key = q * kQuant + step_of * kStep;
+      const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa)), p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
+      const float s0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa)));
+      const float s1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa) + 1));
+      if (wave < 4) {
+#pragma unroll
+        for (int i = 0; i < 2 * U; ++i) {
+          kv[buf][step_of][2 * i][lane] = __builtin_bit_cast(u32x4_t, bf16_octet(st[4 * i], st[4 * i + 1]));
+          kv[buf][step_of][2 * i + 1][lane] = __builtin_bit_cast(u32x4_t, bf16_octet(st[4 * i + 2], st[4 * i + 3]));
+        }
+        if (lane == 0) {
+          ksc[buf][step_of][0] = s0 * a.scale_log2;
+          ksc[buf][step_of][1] = s1 * a.scale_log2;
+          kbad[buf][step_of] = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
+        }
+      } else {
+        bool nan = false;
+        if (p0 < 0 || p1 < 0 || key + kStep - 1 > block_lo) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int kk = key + 16 * (j >> 2) + 4 * g4 + (j & 3);
+            const bool real = (j < 4 ? p0 : p1) >= 0 && kk < r.len;
+#pragma unroll
+            for (int w = 0; w < U; ++w) {
+              if (!real) st[j * U + w] = 0;
+              nan |= (((st[j * U + w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+          }
+        }
+        nan = __any(nan);
+        if (lane == 0) vnan[buf][step_of] = nan;
+        // powers of two, normal and positive
+        const bool exact = ((__float_as_uint(s0) | __float_as_uint(s1)) & 0x807fffffu) == 0 &&
+                           fminf(s0, s1) >= 0x1p-126f;
+#pragma unroll
+        for (int w = 0; w < U; ++w) {
+          uint32_t y[4][2];   // keys 2 j, 2 j + 1 of channels (c, c + 1 | c + 2, c + 3)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            y[j][0] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x05010400u);
+            y[j][1] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x07030602u);
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            u32x4_t f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float by = exact ? (j < 2 ? s0 : s1) : 1.0f;
+              f[j] = c & 1 ? bf16_pair_by<true>(y[j][c >> 1], by) : bf16_pair_by<false>(y[j][c >> 1], by);
+              if (!exact)   // a caller's own scale: rounded to bf16 once more
+                f[j] = pack2(lo_bf16(f[j]) * (j < 2 ? s0 : s1), hi_bf16(f[j]) * (j < 2 ? s0 : s1));
+            }
+            kv[buf][step_of][KF + 4 * w + c][lane] = f;
+          }
+        }
+      }
+    };
+
+    auto compute = [&](int q, int buf) {
+#pragma unroll 1
+      for (int s = 0; s < kSteps; ++s) {
+        const int key = q * kQuant + s * kStep;
+        if (key > lim_hi) break;
+        f32x4_t x[2][NB];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) x[t][i] = (f32x4_t){0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < 2 * U; ++k) {
+            const bf16x8_t f = __builtin_bit_cast(bf16x8_t, kv[buf][s][t * 2 * U + k][lane]);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[t][i] = mfma(f, qf[k][i], x[t][i]);
+          }
+        }
+        const float sc0 = ksc[buf][s][0], sc1 = ksc[buf][s][1];
+        const int bad = __builtin_amdgcn_readfirstlane(kbad[buf][s]);
+        const bool masked = bad != 0 || key + kStep - 1 > lim_lo;
+        bool grown = false;
+        float top[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const float ref = m[i] == -INFINITY ? 0.0f : m[i];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float y = __builtin_fmaf(x[t][i][e], t ? sc1 : sc0, -ref);
+              if (masked) {
+                const int kk = key + 16 * t + 4 * g4 + e;
+                if ((bad >> t & 1) || kk > lim[i]) y = -INFINITY;
+              }
+              x[t][i][e] = y;
+            }
+          top[i] = fmaxf(fmaxf(fmaxf(x[0][i][0], x[0][i][1]), fmaxf(x[0][i][2], x[0][i][3])),
+                         fmaxf(fmaxf(x[1][i][0], x[1][i][1]), fmaxf(x[1][i][2], x[1][i][3])));
+          grown |= top[i] > (m[i] == -INFINITY ? -INFINITY : kLazy);
+        }
+        // The reference of the exponentials follows the maximum only when that has grown
+        // by 2^8: no exchange between lanes, no rescaling in most steps.
+        if (__any(grown)) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            const float ref = m[i] == -INFINITY ? 0.0f : m[i];
+            const float now = fmaxf(m[i], quad_max(top[i]) + ref);
+            const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[i] - now);
+            const float shift = now == -INFINITY ? 0.0f : ref - now;
+            m[i] = now;
+            l[i] *= keep;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[i][c] *= keep;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) x[t][i] += shift;
+          }
+        }
+        bf16x8_t pf[NB];
+        const bool any_nan = masked && __builtin_amdgcn_readfirstlane(vnan[buf][s]) != 0;
+        bf16x8_t seen[NB];
+        if (any_nan) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            u32x4_t w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = (x[j >> 1][i][2 * (j & 1)] == -INFINITY ? 0u : 0x3f80u) |
+                     (x[j >> 1][i][2 * (j & 1) + 1] == -INFINITY ? 0u : 0x3f800000u);
+            seen[i] = __builtin_bit_cast(bf16x8_t, w);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          u32x4_t w;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[t][i][e] = __builtin_amdgcn_exp2f(x[t][i][e]);
+            l[i] += (x[t][i][0] + x[t][i][1]) + (x[t][i][2] + x[t][i][3]);
+            w[2 * t] = pack2(x[t][i][0], x[t][i][1]);
+            w[2 * t + 1] = pack2(x[t][i][2], x[t][i][3]);
+          }
+          pf[i] = __builtin_bit_cast(bf16x8_t, w);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          u32x4_t f = kv[buf][s][KF + c][lane];
+          if (any_nan) {     // NaN values count only in rows that see their key
+            u32x4_t hit;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const bool lo = (f[j] & 0x7fffu) > 0x7f80u, hi = (f[j] & 0x7fff0000u) > 0x7f800000u;
+              hit[j] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
+              f[j] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+            }
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), seen[i], (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (count[e] != 0.0f) o[i][c][e] = __builtin_nanf("");
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NB; ++i) o[i][c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[i], o[i][c]);
+        }
+      }
+    };
+
+    if (q0 < q1) {
+      pages(q0);
+      load(q0);
+      widen(q0, 0);
+      __syncthreads();
+      for (int q = q0; q < q1; ++q) {
+        const int buf = (q - q0) & 1;
+        const bool more = q + 1 < q1;
+        if (more) {
+          if (q + 1 - qa == 32) pages(q + 1);
+          load(q + 1);
+        }
+        compute(q, buf);
+        if (more) widen(q + 1, buf ^ 1);
+        __syncthreads();
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < NB; ++x) l[x] = quad_sum(l[x]);
+
+    // shares that hold a part of this unit: g0 .. g1, each gives a partial sum (of no key
+    // where its share of the weight holds no whole quantum)
+    const int64_t g0 = unit0 / per, g1 = (unit0 + weight - 1) / per;
+    bool done = g0 == g1;
+    if (!done) {
+      const int parts = (int)(g1 - g0) + 1, mine_at = (int)(me - g0);
+      auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
+      auto put = [&](int i) {
+        float* to = partial + (int64_t)slot(i) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * lane;
+        if (row0 >= r.rows) return;
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            put2(to + (x * (2 * C + 1) + 2 * c) * 128, o[x][c][0], o[x][c][1]);
+            put2(to + (x * (2 * C + 1) + 2 * c + 1) * 128, o[x][c][2], o[x][c][3]);
+          }
+          put2(to + (x * (2 * C + 1) + 2 * C) * 128, m[x], l[x]);
+        }
+      };
+      auto join = [&](int first, int stride, int count) {
+        if (row0 >= r.rows) return;
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+          m[x] = -INFINITY;
+          l[x] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < C; ++c) o[x][c] = (f32x4_t){0, 0, 0, 0};
+        }
+        for (int i = 0; i < count; ++i) {
+          const float* from = partial + (int64_t)slot(first + i * stride) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * lane;
+#pragma unroll
+          for (int x = 0; x < NB; ++x) {
+            float2 v[2 * C];
+#pragma unroll
+            for (int c = 0; c < 2 * C; ++c) v[c] = get2(from + (x * (2 * C + 1) + c) * 128);
+            const float2 ml = get2(from + (x * (2 * C + 1) + 2 * C) * 128);
+            const float now = fmaxf(m[x], ml.x), ref = now == -INFINITY ? 0.0f : now;
+            const float keep = exp2f(m[x] - ref), f = exp2f(ml.x - ref);
+            m[x] = now;
+            l[x] = l[x] * keep + ml.y * f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              o[x][c][0] = o[x][c][0] * keep + v[2 * c].x * f;
+              o[x][c][1] = o[x][c][1] * keep + v[2 * c].y * f;
+              o[x][c][2] = o[x][c][2] * keep + v[2 * c + 1].x * f;
+              o[x][c][3] = o[x][c][3] * keep + v[2 * c + 1].y * f;
+            }
+          }
+        }
+      };
+      put(mine_at);
+      const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
+      const int in_group = parts - group * kJoin < kJoin ? parts - group * kJoin : kJoin;
+      if (arrive(counters + 2 * slot(group * kJoin), in_group, &last)) {
+        join(group * kJoin, 1, in_group);
+        done = groups == 1;
+        if (!done) {
+          put(group * kJoin);    // each wave overwrites what only it has read
+          if (arrive(counters + 2 * slot(0) + 1, groups, &last)) {
+            join(0, kJoin, groups);
+            done = true;
+          }
+        }
+      }
+    }
+    if (done) {
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        if (!mine[x]) continue;
+        const int row = row0 + 16 * x + n;
+        const int64_t to = (int64_t)(r.row0 + row / a.G) * a.H * a.G + h * a.G + row % a.G;
+        const float f = l[x] == 0.0f ? 0.0f : 1.0f / l[x];    // no key: 0
+        u32x4_t* y = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) + to * D + 4 * C * g4);
+        // channel (4 g4 + i) C + c
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (C == 8) {
+            u32x4_t w;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[c] = pack2(o[x][(2 * c) % C][i] * f, o[x][(2 * c + 1) % C][i] * f);
+            y[i] = w;
+          } else if (i % 2 == 0) {
+            y[i / 2] = (u32x4_t){pack2(o[x][0][i] * f, o[x][1][i] * f), pack2(o[x][2][i] * f, o[x][3][i] * f),
+                                 pack2(o[x][0][i + 1] * f, o[x][1][i + 1] * f),
+                                 pack2(o[x][2][i + 1] * f, o[x][3][i + 1] * f)};
+          }
+        }
+        if (a.lse != nullptr && g4 == 0)
+          a.lse[to] = l[x] == 0.0f ? -INFINITY : (m[x] + log2f(l[x])) * 0.69314718055994530942f;
+      }
+    }
+    __syncthreads();     // `last` and the buffers are free again
+    at = unit0 + weight;
+  }
+}
+
+constexpr int kNb = 2;
+
+}  // namespace
+
+// A counter pair and two partial sums for each share's first and last unit.
+size_t attend_rows_ws_bytes(int d) {
+  return kCounters * sizeof(int) + (size_t)kGrid * 2 * kWaves * kNb * (d / 4 + 2) * 64 * sizeof(float);
+}
+
+hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream) {
+  int* counters = static_cast<int*>(ws);
+  float* partial = reinterpret_cast<float*>(counters + kCounters);
+  if (d == 64)
+    hipLaunchKernelGGL((attend8_rows_kernel<64, kNb>), dim3(kGrid), dim3(kThreads), 0, stream, a, partial, counters);
+  else
+    hipLaunchKernelGGL((attend8_rows_kernel<128, kNb>), dim3(kGrid), dim3(kThreads), 0, stream, a, partial, counters);
+  return hipGetLastError();
+}
+
+}  // namespace kvx
