@@ -92,6 +92,12 @@ __device__ __forceinline__ float2 get2(const float* from) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
+// A value that all lanes share, in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(uint32_t)v) | (uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32);
+}
+
 // pre[b] = sum of weight(request 0 .. b), by a workgroup of THREADS; part: an entry per wave.
 template <int THREADS, typename W>
 __device__ __forceinline__ void prefix_requests(const AttendArgs& a, int64_t* pre, int64_t* part, W weight) {

@@ -27,7 +27,14 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kStep = 32;                  // keys of a wave's step
 constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
 constexpr int kRows = 16;                  // query rows of a block
-constexpr int kGrid = 512;                 // workgroups: two per CU
+#ifndef KLS
+#define KLS 1
+#endif
+#ifndef KG
+#define KG 512
+#endif
+constexpr int kLeast = KLS;
+constexpr int kGrid = KG;                 // workgroups: two per CU
 
 // Blocks of rows, and quanta of one block and head (rows without any key still have an
 // output).
@@ -61,7 +68,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
     return (int64_t)blocks_of(r) * quanta_of(r) * a.H;
   });
   const int64_t total = pre[a.B - 1];
-  const int64_t per = (total + kGrid - 1) / kGrid;
+  int64_t per = (total + kGrid - 1) / kGrid;
+  per = per > kLeast ? per : kLeast;
   int64_t at = (int64_t)blockIdx.x * per;
   const int64_t end = at + per < total ? at + per : total;
   if (at >= end) return;
@@ -322,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
       const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2f(jm[w][jr] - ref);    // 0 for a wave that saw nothing; NaN sums stay
+        const float f = __builtin_amdgcn_exp2f(jm[w][jr] - ref);    // 0 for a wave that saw nothing; NaN sums stay
         den += f * jl[w][jr];
 #pragma unroll
         for (int c = 0; c < C; ++c) sum[c] += f * jo[w][jr * RS + jc + c];
@@ -366,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
 #pragma unroll
           for (int i = 0; i < 4; ++i) now = fmaxf(now, md[i].x);
           const float ref = now == -INFINITY ? 0.0f : now;
-          const float keep = exp2f(top - ref);
+          const float keep = __builtin_amdgcn_exp2f(top - ref);
           top = now;
           den *= keep;
 #pragma unroll
@@ -374,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             if (i0 + i >= count) break;
-            const float f = exp2f(md[i].x - ref);
+            const float f = __builtin_amdgcn_exp2f(md[i].x - ref);
             den += f * md[i].y;
 #pragma unroll
             for (int c = 0; c < C / 2; ++c) {
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
         for (int c = 0; c < C; ++c) y[c] = sum[c] * f;
       }
       if (a.lse != nullptr && (tid & 15) == 0)
-        a.lse[to] = den == 0.0f ? -INFINITY : (top + log2f(den)) * 0.69314718055994530942f;
+        a.lse[to] = den == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
     }
     __syncthreads();    // the LDS arrays are free again
     at = unit0 + q1;
@@ -421,7 +429,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
 }
 
 // Which kernel: many rows a request share the widened codes over eight waves.
-bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G > (int64_t)B * 32; }
+#ifndef BR
+#define BR 32
+#endif
+bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G > (int64_t)B * BR; }
 
 }  // namespace
 

@@ -23,6 +23,14 @@ constexpr int kThreads = 512, kWaves = 8;
 constexpr int kSteps = 4, kStep = 32, kQuant = kSteps * kStep;
 constexpr int kGrid = 256;                 // workgroups: one per CU
 constexpr int kXcds = 8;
+#ifndef RING
+#define RING 4
+#endif
+constexpr int kRing = RING;                   // operands on their way from LDS
+#ifndef KL
+#define KL 1
+#endif
+constexpr int kLeast = KL;
 
 // Codes 2 HALF and 2 HALF + 1 of a word times a power of two, as bf16.
 template <bool HALF>
@@ -53,31 +61,37 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   __shared__ float ksc[2][kSteps][2];       // scale of the scores of a 16-key tile
   __shared__ int kbad[2][kSteps];           // bit t: tile t has no page
   __shared__ int vnan[2][kSteps];           // some value is NaN (where rows differ in what they see)
+  __shared__ uint32_t nans[2][kSteps][U][64];   // which
   __shared__ int64_t part[kWaves];
   __shared__ int last;
   static_assert(sizeof(kv) >= KVX_MAX_REQUESTS * sizeof(int64_t), "the prefix sums fit");
   int64_t* pre = reinterpret_cast<int64_t*>(kv);   // until the first unit
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 15, g4 = lane >> 4;
   const int step_of = wave & 3;             // the step whose keys (waves 0-3) or values this wave widens
 
   prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
     return a.H * WT::sum(WT::before(r, a.G), WT::blocks(r));
   });
-  const int64_t total = pre[a.B - 1];
-  const int64_t per = (total + kGrid - 1) / kGrid;
+  const int64_t total = uniform(pre[a.B - 1]);
+  int64_t per = uniform((total + kGrid - 1) / kGrid);
+  const int64_t least = (int64_t)a.G * kLeast;
+  per = per > least ? per : least;
   const int me = (blockIdx.x % kXcds) * (kGrid / kXcds) + blockIdx.x / kXcds;   // share `me`
-  int64_t at = me * per;
-  const int64_t end = at + per < total ? at + per : total;
+  int64_t at = uniform(me * per);
+  const int64_t end = uniform(at + per < total ? at + per : total);
   if (at >= end) return;
-  int b = __builtin_amdgcn_readfirstlane(find_request(pre, a.B, at));
-  int64_t base = b > 0 ? pre[b - 1] : 0;
+  int b = uniform(find_request(pre, a.B, at));
+  int64_t base = uniform(b > 0 ? pre[b - 1] : (int64_t)0);
   __syncthreads();
 
   const int64_t plane = ((int64_t)a.N << a.log2p) * D;
   const int P1 = (1 << a.log2p) - 1;
   while (at < end) {
-    // the unit (request, head, block) at `at`
+    // the unit (request, head, block) at `at`; a lane's offsets are formed anew, which
+    // costs less than keeping them over the main loop
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int n = ln & 15, g4 = ln >> 4;
     const Request r = request(a, b);
     const int64_t before = WT::before(r, a.G);
     const int blocks = WT::blocks(r);
@@ -96,10 +110,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
       else left = half;
     }
     blk = __builtin_amdgcn_readfirstlane(blk);
-    const int64_t unit0 = base + h * head_w + WT::sum(before, blk);
-    const int64_t weight = WT::sum(before, blk + 1) - WT::sum(before, blk);
+    const int64_t unit0 = uniform(base + h * head_w + WT::sum(before, blk));
+    const int64_t weight = uniform(WT::sum(before, blk + 1) - WT::sum(before, blk));
     const int last_row = (blk + 1) * ROWS < r.rows ? (blk + 1) * ROWS - 1 : r.rows - 1;
-    const int lim_block = r.len - r.tokens + last_row / a.G;     // last key of the block
+    const int lim_block = __builtin_amdgcn_readfirstlane(r.len - r.tokens + last_row / a.G);     // last key of the block
     const int quanta = lim_block < 0 ? 1 : lim_block / kQuant + 1;
     const int q0 = __builtin_amdgcn_readfirstlane((int)((at - unit0) * quanta / weight));
     const int q1 = __builtin_amdgcn_readfirstlane(
@@ -130,9 +144,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
     // least and largest of the wave's limits, and the least of the block's
     const bool wave_full = row0 + 16 * NB <= r.rows, block_full = (blk + 1) * ROWS <= r.rows;
     const int wave_last = row0 + 16 * NB - 1 < r.rows ? row0 + 16 * NB - 1 : r.rows - 1;
-    const int lim_lo = wave_full ? r.len - r.tokens + row0 / a.G : -1;
-    const int lim_hi = row0 < r.rows ? r.len - r.tokens + wave_last / a.G : -1;
-    const int block_lo = block_full ? r.len - r.tokens + blk * ROWS / a.G : -1;
+    const int lim_lo = __builtin_amdgcn_readfirstlane(wave_full ? r.len - r.tokens + row0 / a.G : -1);
+    const int lim_hi = __builtin_amdgcn_readfirstlane(row0 < r.rows ? r.len - r.tokens + wave_last / a.G : -1);
+    const int block_lo = __builtin_amdgcn_readfirstlane(block_full ? r.len - r.tokens + blk * ROWS / a.G : -1);
 
     f32x4_t o[NB][C];
     float m[NB], l[NB];
@@ -208,63 +222,90 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
         if (p0 < 0 || p1 < 0 || key + kStep - 1 > block_lo) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int kk = key + 16 * (j >> 2) + 4 * g4 + (j & 3);
-            const bool real = (j < 4 ? p0 : p1) >= 0 && kk < r.len;
+            const bool real = (j < 4 ? p0 : p1) >= 0 && key + 16 * (j >> 2) + 4 * g4 + (j & 3) < r.len;
 #pragma unroll
             for (int w = 0; w < U; ++w) {
               if (!real) st[j * U + w] = 0;
-              nan |= (((st[j * U + w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+              nan |= e4m3_nan(st[j * U + w]) != 0;
             }
           }
         }
         nan = __any(nan);
         if (lane == 0) vnan[buf][step_of] = nan;
-        // powers of two, normal and positive
+        if (nan) {      // kept apart where rows differ in what they see: bit 4 j + i is key j, byte i
+#pragma unroll
+          for (int w = 0; w < U; ++w) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t h = e4m3_nan(st[j * U + w]);
+              bits |= ((h >> 7 & 1) | (h >> 14 & 2) | (h >> 21 & 4) | (h >> 28 & 8)) << (4 * j);
+              st[j * U + w] &= ~((h >> 7) * 0xffu);
+            }
+            nans[buf][step_of][w][lane] = bits;
+          }
+        }
+        // powers of two, normal and positive, are applied with the conversion
         const bool exact = ((__float_as_uint(s0) | __float_as_uint(s1)) & 0x807fffffu) == 0 &&
                            fminf(s0, s1) >= 0x1p-126f;
+        auto operands = [&](auto by) {
 #pragma unroll
-        for (int w = 0; w < U; ++w) {
-          uint32_t y[4][2];   // keys 2 j, 2 j + 1 of channels (c, c + 1 | c + 2, c + 3)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            y[j][0] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x05010400u);
-            y[j][1] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x07030602u);
-          }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            u32x4_t f;
+          for (int w = 0; w < U; ++w) {
+            uint32_t y[4][2];   // keys 2 j, 2 j + 1 of channels (c, c + 1 | c + 2, c + 3)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float by = exact ? (j < 2 ? s0 : s1) : 1.0f;
-              f[j] = c & 1 ? bf16_pair_by<true>(y[j][c >> 1], by) : bf16_pair_by<false>(y[j][c >> 1], by);
-              if (!exact)   // a caller's own scale: rounded to bf16 once more
-                f[j] = pack2(lo_bf16(f[j]) * (j < 2 ? s0 : s1), hi_bf16(f[j]) * (j < 2 ? s0 : s1));
+              y[j][0] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x05010400u);
+              y[j][1] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x07030602u);
             }
-            kv[buf][step_of][KF + 4 * w + c][lane] = f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              u32x4_t f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) f[j] = by(y[j][c >> 1], c & 1, j < 2 ? s0 : s1);
+              kv[buf][step_of][KF + 4 * w + c][lane] = f;
+            }
           }
+        };
+        if (exact) {
+          operands([](uint32_t w, bool half, float s) { return half ? bf16_pair_by<true>(w, s) : bf16_pair_by<false>(w, s); });
+        } else {   // a caller's own scale: rounded to bf16 once more
+          operands([](uint32_t w, bool half, float s) {
+            const uint32_t f = half ? bf16_pair<true>(w) : bf16_pair<false>(w);
+            return pack2(lo_bf16(f) * s, hi_bf16(f) * s);
+          });
         }
       }
     };
 
+    // A step takes its operands from LDS in order, the keys' and then the values', kRing of
+    // them on the way at any time; the scheduling barriers keep that order.
     auto compute = [&](int q, int buf) {
+      int key = q * kQuant;
+      if (key > lim_hi) return;
+      const u32x4_t* from = &kv[buf][0][0][lane];
+      u32x4_t f[kRing];
+#pragma unroll
+      for (int i = 0; i < kRing; ++i) f[i] = from[i * 64];
 #pragma unroll 1
-      for (int s = 0; s < kSteps; ++s) {
-        const int key = q * kQuant + s * kStep;
-        if (key > lim_hi) break;
+      for (int s = 0; s < kSteps && key <= lim_hi; ++s, key += kStep) {
+        const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};
+        const int bad = __builtin_amdgcn_readfirstlane(kbad[buf][s]);
+        const u32x4_t* next = s + 1 < kSteps ? from + F * 64 : from;   // the last step's are not used
         f32x4_t x[2][NB];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < NB; ++i) x[t][i] = (f32x4_t){0, 0, 0, 0};
 #pragma unroll
-          for (int k = 0; k < 2 * U; ++k) {
-            const bf16x8_t f = __builtin_bit_cast(bf16x8_t, kv[buf][s][t * 2 * U + k][lane]);
+        for (int k = 0; k < KF; ++k) {
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < NB; ++i) x[t][i] = mfma(f, qf[k][i], x[t][i]);
-          }
+          for (int i = 0; i < NB; ++i)
+            x[k / (2 * U)][i] = mfma(__builtin_bit_cast(bf16x8_t, f[k % kRing]), qf[k % (2 * U)][i], x[k / (2 * U)][i]);
+          f[k % kRing] = from[(k + kRing) * 64];
         }
-        const float sc0 = ksc[buf][s][0], sc1 = ksc[buf][s][1];
-        const int bad = __builtin_amdgcn_readfirstlane(kbad[buf][s]);
+        __builtin_amdgcn_sched_barrier(0);
+        // exponents: scores less the row's reference
         const bool masked = bad != 0 || key + kStep - 1 > lim_lo;
         bool grown = false;
         float top[NB];
@@ -274,20 +315,26 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float y = __builtin_fmaf(x[t][i][e], t ? sc1 : sc0, -ref);
-              if (masked) {
-                const int kk = key + 16 * t + 4 * g4 + e;
-                if ((bad >> t & 1) || kk > lim[i]) y = -INFINITY;
-              }
-              x[t][i][e] = y;
+            for (int e = 0; e < 4; ++e) x[t][i][e] = __builtin_fmaf(x[t][i][e], sc[t], -ref);
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const int most = bad >> t & 1 ? -1 : lim[i] - (key + 16 * t + 4 * g4);   // last element seen
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[t][i][e] = e > most ? -INFINITY : x[t][i][e];
             }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
           top[i] = fmaxf(fmaxf(fmaxf(x[0][i][0], x[0][i][1]), fmaxf(x[0][i][2], x[0][i][3])),
                          fmaxf(fmaxf(x[1][i][0], x[1][i][1]), fmaxf(x[1][i][2], x[1][i][3])));
           grown |= top[i] > (m[i] == -INFINITY ? -INFINITY : kLazy);
         }
-        // The reference of the exponentials follows the maximum only when that has grown
-        // by 2^8: no exchange between lanes, no rescaling in most steps.
+        // The reference follows the maximum only when that has grown by 2^8: the sums hold
+        // that, no lane has to ask the others in most steps, and O is seldom rescaled.
         if (__any(grown)) {
 #pragma unroll
           for (int i = 0; i < NB; ++i) {
@@ -303,10 +350,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             for (int t = 0; t < 2; ++t) x[t][i] += shift;
           }
         }
-        bf16x8_t pf[NB];
-        const bool any_nan = masked && __builtin_amdgcn_readfirstlane(vnan[buf][s]) != 0;
-        bf16x8_t seen[NB];
-        if (any_nan) {
+        // NaN values count only in rows that see their key
+        if (masked && __builtin_amdgcn_readfirstlane(vnan[buf][s]) != 0) {
 #pragma unroll
           for (int i = 0; i < NB; ++i) {
             u32x4_t w;
@@ -314,9 +359,21 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             for (int j = 0; j < 4; ++j)
               w[j] = (x[j >> 1][i][2 * (j & 1)] == -INFINITY ? 0u : 0x3f80u) |
                      (x[j >> 1][i][2 * (j & 1) + 1] == -INFINITY ? 0u : 0x3f800000u);
-            seen[i] = __builtin_bit_cast(bf16x8_t, w);
+            const bf16x8_t seen = __builtin_bit_cast(bf16x8_t, w);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              const uint32_t bits = nans[buf][s][c / 4][lane] >> (c % 4);   // bit 4 j: key j of channel c
+              u32x4_t hit;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                hit[j] = (bits >> (8 * j) & 1) * 0x3f80u | (bits >> (8 * j + 4) & 1) * 0x3f800000u;
+              const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), seen, (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][c][e] = count[e] != 0.0f ? __builtin_nanf("") : o[i][c][e];
+            }
           }
         }
+        bf16x8_t p[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           u32x4_t w;
@@ -328,30 +385,17 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             w[2 * t] = pack2(x[t][i][0], x[t][i][1]);
             w[2 * t + 1] = pack2(x[t][i][2], x[t][i][3]);
           }
-          pf[i] = __builtin_bit_cast(bf16x8_t, w);
+          p[i] = __builtin_bit_cast(bf16x8_t, w);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          u32x4_t f = kv[buf][s][KF + c][lane];
-          if (any_nan) {     // NaN values count only in rows that see their key
-            u32x4_t hit;
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const bool lo = (f[j] & 0x7fffu) > 0x7f80u, hi = (f[j] & 0x7fff0000u) > 0x7f800000u;
-              hit[j] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
-              f[j] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-            }
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), seen[i], (f32x4_t){0, 0, 0, 0});
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (count[e] != 0.0f) o[i][c][e] = __builtin_nanf("");
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < NB; ++i) o[i][c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[i], o[i][c]);
+          for (int i = 0; i < NB; ++i) o[i][c] = mfma(__builtin_bit_cast(bf16x8_t, f[(KF + c) % kRing]), p[i], o[i][c]);
+          f[(KF + c) % kRing] = KF + c + kRing < F ? from[(KF + c + kRing) * 64] : next[(KF + c + kRing - F) * 64];
         }
+        __builtin_amdgcn_sched_barrier(0);
+        from = next;
       }
     };
 
@@ -379,11 +423,12 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
     // where its share of the weight holds no whole quantum)
     const int64_t g0 = unit0 / per, g1 = (unit0 + weight - 1) / per;
     bool done = g0 == g1;
+    asm volatile("" : "+v"(ln));
     if (!done) {
       const int parts = (int)(g1 - g0) + 1, mine_at = (int)(me - g0);
       auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
       auto put = [&](int i) {
-        float* to = partial + (int64_t)slot(i) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * lane;
+        float* to = partial + (int64_t)slot(i) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * ln;
         if (row0 >= r.rows) return;
 #pragma unroll
         for (int x = 0; x < NB; ++x) {
@@ -404,8 +449,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll
           for (int c = 0; c < C; ++c) o[x][c] = (f32x4_t){0, 0, 0, 0};
         }
+#pragma unroll 1
         for (int i = 0; i < count; ++i) {
-          const float* from = partial + (int64_t)slot(first + i * stride) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * lane;
+          const float* from = partial + (int64_t)slot(first + i * stride) * SLOT + wave * NB * (4 * C + 2) * 64 + 2 * ln;
 #pragma unroll
           for (int x = 0; x < NB; ++x) {
             float2 v[2 * C];
@@ -413,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             for (int c = 0; c < 2 * C; ++c) v[c] = get2(from + (x * (2 * C + 1) + c) * 128);
             const float2 ml = get2(from + (x * (2 * C + 1) + 2 * C) * 128);
             const float now = fmaxf(m[x], ml.x), ref = now == -INFINITY ? 0.0f : now;
-            const float keep = exp2f(m[x] - ref), f = exp2f(ml.x - ref);
+            const float keep = __builtin_amdgcn_exp2f(m[x] - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
             m[x] = now;
             l[x] = l[x] * keep + ml.y * f;
 #pragma unroll
@@ -445,10 +491,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
         if (!mine[x]) continue;
-        const int row = row0 + 16 * x + n;
+        const int row = row0 + 16 * x + (ln & 15);
         const int64_t to = (int64_t)(r.row0 + row / a.G) * a.H * a.G + h * a.G + row % a.G;
         const float f = l[x] == 0.0f ? 0.0f : 1.0f / l[x];    // no key: 0
-        u32x4_t* y = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) + to * D + 4 * C * g4);
+        u32x4_t* y = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) + to * D + 4 * C * (ln >> 4));
         // channel (4 g4 + i) C + c
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -463,12 +509,12 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
                                  pack2(o[x][2][i + 1] * f, o[x][3][i + 1] * f)};
           }
         }
-        if (a.lse != nullptr && g4 == 0)
-          a.lse[to] = l[x] == 0.0f ? -INFINITY : (m[x] + log2f(l[x])) * 0.69314718055994530942f;
+        if (a.lse != nullptr && ln < 16)
+          a.lse[to] = l[x] == 0.0f ? -INFINITY : (m[x] + __builtin_amdgcn_logf(l[x])) * 0.69314718055994530942f;
       }
     }
     __syncthreads();     // `last` and the buffers are free again
-    at = unit0 + weight;
+    at = uniform(unit0 + weight);
   }
 }
 

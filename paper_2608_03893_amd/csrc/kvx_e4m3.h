@@ -33,6 +33,9 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float x0, float x1, float x2, floa
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, w, true);
 }
 
+// The top bit of each byte that is NaN (all ones but the sign).
+__device__ __forceinline__ uint32_t e4m3_nan(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // Code i (0 .. 3) of a word, exactly.
 template <int I>
 __device__ __forceinline__ float from_e4m3(uint32_t w) { return __builtin_amdgcn_cvt_f32_fp8((int)w, I); }
