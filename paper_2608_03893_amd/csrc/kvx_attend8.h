@@ -11,9 +11,9 @@ namespace {
 
 constexpr float kLazy = 8.0f;    // growth of a row's maximum (log2) that is let pass
 constexpr int kJoin = 16;        // partial sums joined at a time
-// Arrival counters, first in the workspace (four for each workgroup of the larger grid):
+// Arrival counters, first in the workspace (four for each workgroup of the largest grid):
 // all kernels keep them there and leave them at zero, and partial sums behind.
-constexpr int kCounters = 4 * 512;
+constexpr int kCounters = 4 * 1024;
 
 // Largest / sum of a value over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quad_max(float v) {

@@ -27,14 +27,18 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kStep = 32;                  // keys of a wave's step
 constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
 constexpr int kRows = 16;                  // query rows of a block
-#ifndef KLS
-#define KLS 1
+constexpr int kLeast = 1;                  // quanta of a workgroup
+#ifndef OCC
+#define OCC 3
 #endif
-#ifndef KG
-#define KG 512
-#endif
-constexpr int kLeast = KLS;
-constexpr int kGrid = KG;                 // workgroups: two per CU
+// Workgroups a CU: as many as the registers hold.  More of them hide more of a unit's
+// start (lengths, pages, scales, rows: loads that wait for one another) than prefetching
+// within a wave: 64 ragged requests 86 us with two and the next step's loads in flight,
+// 72 us with three and no prefetch.
+template <int DT, int D>
+constexpr int kOcc = DT == 1 && D == 128 ? 2 : OCC;
+template <int DT, int D>
+constexpr int kGrid = 256 * kOcc<DT, D>;
 
 // Blocks of rows, and quanta of one block and head (rows without any key still have an
 // output).
@@ -52,7 +56,7 @@ struct Stage {
 };
 
 template <int DT, int D>
-__global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+__global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
   constexpr int RS = D + 4;                                        // row stride in LDS
   constexpr int SLOT = kRows * (D + 2);                            // floats of a partial sum
@@ -61,14 +65,14 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
   __shared__ __attribute__((aligned(16))) float jo[kWaves][kRows * RS];
   __shared__ float jm[kWaves][kRows], jl[kWaves][kRows];
   __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n = lane & 15, g4 = lane >> 4;
 
   prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
     return (int64_t)blocks_of(r) * quanta_of(r) * a.H;
   });
   const int64_t total = pre[a.B - 1];
-  int64_t per = (total + kGrid - 1) / kGrid;
+  int64_t per = (total + kGrid<DT, D> - 1) / kGrid<DT, D>;
   per = per > kLeast ? per : kLeast;
   int64_t at = (int64_t)blockIdx.x * per;
   const int64_t end = at + per < total ? at + per : total;
@@ -79,27 +83,24 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
   const int P1 = (1 << a.log2p) - 1;
   while (at < end) {
     while (pre[b] <= at) ++b;
-    b = __builtin_amdgcn_readfirstlane(b);
+    b = uniform(b);
     const int64_t base = b > 0 ? pre[b - 1] : 0;
     const Request r = request(a, b);
     const int quanta = quanta_of(r);
     const int64_t unit = (at - base) / quanta;
     const int blk = (int)(unit / a.H), h = (int)(unit % a.H);
     const int64_t unit0 = base + unit * quanta;              // its first quantum
-    const int q0 = __builtin_amdgcn_readfirstlane((int)(at - unit0));
-    const int q1 = __builtin_amdgcn_readfirstlane(
-        (int)(end - unit0 < quanta ? end - unit0 : quanta));
+    const int q0 = uniform((int)(at - unit0));
+    const int q1 = uniform((int)(end - unit0 < quanta ? end - unit0 : quanta));
 
-    // this lane's query row: limit of its keys, its channels
-    const int row = blk * kRows + n;
-    const bool mine = row < r.rows;
-    const int token = mine ? row / a.G : 0, head = h * a.G + (mine ? row % a.G : 0);
-    const int lim = mine ? r.len - r.tokens + token : -1;      // last key it sees
-    const int first_tok = blk * kRows / a.G;
-    const int last_row = (blk + 1) * kRows < r.rows ? (blk + 1) * kRows - 1 : r.rows - 1;
-    const bool full = (blk + 1) * kRows <= r.rows;
-    const int lim_lo = full ? r.len - r.tokens + first_tok : -1;          // least and largest
-    const int lim_hi = r.len - r.tokens + last_row / a.G;                 // of the block
+    // this lane's query row (the block's last one again past the end): its keys' limit, its
+    // channels
+    const int block_last = (blk + 1) * kRows < r.rows ? (blk + 1) * kRows - 1 : r.rows - 1;
+    const int row = blk * kRows + n < block_last ? blk * kRows + n : block_last;
+    const int token = row / a.G, head = h * a.G + row % a.G;
+    const int lim = r.len - r.tokens + token;                              // last key it sees
+    const int lim_lo = uniform(r.len - r.tokens + blk * kRows / a.G);      // least and largest
+    const int lim_hi = uniform(r.len - r.tokens + block_last / a.G);       // of the block
     bf16x8_t qf[2 * U][TERMS];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -108,18 +109,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
         const int64_t off = (int64_t)(r.row0 + token) * a.q_stride[0] + (int64_t)head * a.q_stride[1] +
                             64 * u + 16 * g4 + 8 * w;
         if (DT == 0) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (mine) x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + off);
-          qf[2 * u + w][0] = as_bf16x8(x);
+          qf[2 * u + w][0] = as_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + off));
         } else {
-          float x[8];
-          float4 lo = make_float4(0, 0, 0, 0), hi = lo;
-          if (mine) {
-            lo = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
-            hi = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off + 4);
-          }
-          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
-          x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+          const float4 lo = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
+          const float4 hi = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off + 4);
+          const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
           split_terms<TERMS>(x, qf[2 * u + w]);
         }
       }
@@ -172,7 +166,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
       auto compute = [&](Stage<D>& s, int q) {
         const int key = q * kQuant + wave * kStep;
         float x[8];
-        bool nan_v = false;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           f32x4_t acc = {0, 0, 0, 0};
@@ -193,18 +186,49 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
         const int p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
         const float v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa)));
         const float v1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa) + 1));
-        const bool masked = p0 < 0 || p1 < 0 || key + kStep - 1 > lim_lo;
-        if (masked) {
+        if (p0 < 0 || p1 < 0 || key + kStep - 1 > lim_lo) {
+          bool nan = false;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int kk = key + 16 * (j >> 2) + 4 * g4 + (j & 3);
-            const bool real = (j < 4 ? p0 : p1) >= 0 && kk < r.len;
-            if (!(real && kk <= lim)) x[j] = -INFINITY;
+          for (int t = 0; t < 2; ++t) {
+            const int first = key + 16 * t + 4 * g4;      // this lane's first key; seen, real: its last
+            const int seen = (t ? p1 : p0) < 0 ? -1 : lim - first, real = (t ? p1 : p0) < 0 ? -1 : r.len - 1 - first;
 #pragma unroll
-            for (int w = 0; w < U; ++w) {
-              if (!real) s.v[j][w] = 0;     // nobody's codes, NaN perhaps
-              nan_v |= (((s.v[j][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            for (int e = 0; e < 4; ++e) {
+              const int j = 4 * t + e;
+              x[j] = e > seen ? -INFINITY : x[j];
+#pragma unroll
+              for (int w = 0; w < U; ++w) {
+                s.v[j][w] = e > real ? 0 : s.v[j][w];     // nobody's codes
+                nan |= e4m3_nan(s.v[j][w]) != 0;
+              }
             }
+          }
+          if (__any(nan)) {
+            // NaN values count only in rows that see their key: they leave the product, and
+            // go into the sums of the rows for which a product of marks finds one
+            u32x4_t m8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              m8[j] = (x[2 * j] == -INFINITY ? 0u : 0x3f80u) | (x[2 * j + 1] == -INFINITY ? 0u : 0x3f800000u);
+            const bf16x8_t sees = __builtin_bit_cast(bf16x8_t, m8);
+#pragma unroll
+            for (int w = 0; w < U; ++w)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                u32x4_t hit;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  hit[j] = (e4m3_nan(s.v[2 * j][w]) >> (8 * c + 7) & 1) * 0x3f80u |
+                           (e4m3_nan(s.v[2 * j + 1][w]) >> (8 * c + 7) & 1) * 0x3f800000u;
+                const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), sees, (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  o[4 * w + c][i] = count[i] != 0.0f ? __builtin_nanf("") : o[4 * w + c][i];
+              }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int w = 0; w < U; ++w) s.v[j][w] &= ~((e4m3_nan(s.v[j][w]) >> 7) * 0xffu);
           }
         }
         // The reference of the exponentials follows the maximum only when that has
@@ -228,52 +252,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
           p[j] = __builtin_amdgcn_exp2f(x[j] - ref);
           l += p[j];
         }
-        bf16x8_t seen = {};
-        const bool any_nan = masked && __any(nan_v);
-        if (any_nan) {     // which keys each row sees
-          u32x4_t w;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = (x[2 * j] == -INFINITY ? 0u : 0x3f80u) | (x[2 * j + 1] == -INFINITY ? 0u : 0x3f800000u);
-          seen = __builtin_bit_cast(bf16x8_t, w);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float y = p[j] * (j < 4 ? v0 : v1);
-          p[j] = masked && x[j] == -INFINITY ? 0.0f : y;
-        }
+        for (int j = 0; j < 8; ++j) p[j] *= j < 4 ? v0 : v1;
         bf16x8_t pf[TERMS];
         split_terms<TERMS>(p, pf);
 #pragma unroll
         for (int w = 0; w < U; ++w) {
           uint32_t y[4][2];   // pairs of keys: bytes (c, c), (c + 1, c + 1) | the next two channels
-          if (any_nan) {
-            // NaN values count only in rows that see their key
-            uint32_t z[4][2];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t nan = ((((s.v[j][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
-              s.v[j][w] &= ~nan;
-              const uint32_t one = nan & 0x38383838u;     // e4m3's 1.0
-              if (j & 1) {
-                z[j >> 1][1] = __builtin_amdgcn_perm(one, z[j >> 1][0], 0x07030602u);
-                z[j >> 1][0] = __builtin_amdgcn_perm(one, z[j >> 1][0], 0x05010400u);
-              } else {
-                z[j >> 1][0] = one;
-              }
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              u32x4_t f;
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                f[j] = c & 1 ? bf16_pair<true>(z[j][c >> 1]) : bf16_pair<false>(z[j][c >> 1]);
-              const f32x4_t hit = mfma(__builtin_bit_cast(bf16x8_t, f), seen, (f32x4_t){0, 0, 0, 0});
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (hit[i] != 0.0f) o[4 * w + c][i] = __builtin_nanf("");
-            }
-          }
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             y[j][0] = __builtin_amdgcn_perm(s.v[2 * j + 1][w], s.v[2 * j][w], 0x05010400u);
@@ -295,15 +280,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_split_kernel(AttendArgs a
       const int64_t room = (int64_t)lim_hi - wave * kStep;
       int qe = room < 0 ? qa : (int)(room / kQuant) + 1;
       qe = qe < qb ? qe : qb;
-      Stage<D> s0, s1;
-      if (qa < qe) load(s0, qa);
-      for (int q = qa; q < qe; q += 2) {
-        if (q + 1 < qe) load(s1, q + 1);
-        compute(s0, q);
-        if (q + 1 < qe) {
-          if (q + 2 < qe) load(s0, q + 2);
-          compute(s1, q + 1);
-        }
+      for (int q = qa; q < qe; ++q) {
+        Stage<D> s;
+        load(s, q);
+        compute(s, q);
       }
     }
 
@@ -436,27 +416,25 @@ bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T *
 
 }  // namespace
 
-// Counters and two partial sums for each workgroup's first and last unit.
+// Counters, and two partial sums for each workgroup's first and last unit.
 size_t attend_ws_bytes(int B, int, int G, int T, int d, int dtype) {
   if (by_rows(B, G, T, dtype)) return attend_rows_ws_bytes(d);
-  return kCounters * sizeof(int) + (size_t)kGrid * 2 * kRows * (d + 2) * sizeof(float);
+  const size_t grid = dtype == 0 ? (d == 64 ? kGrid<0, 64> : kGrid<0, 128>) : (d == 64 ? kGrid<1, 64> : kGrid<1, 128>);
+  return kCounters * sizeof(int) + grid * 2 * kRows * (d + 2) * sizeof(float);
+}
+
+template <int DT, int D>
+static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
+  int* counters = static_cast<int*>(ws);
+  hipLaunchKernelGGL((attend8_split_kernel<DT, D>), dim3(kGrid<DT, D>), dim3(kThreads),
+                     (size_t)a.B * sizeof(int64_t), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
+  return hipGetLastError();
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
   if (by_rows(a.B, a.G, a.T, dtype)) return launch_attend_rows(a, d, ws, stream);
-  int* counters = static_cast<int*>(ws);
-  float* partial = reinterpret_cast<float*>(counters + kCounters);
-  const size_t lds = (size_t)a.B * sizeof(int64_t);
-  const dim3 grid(kGrid), block(kThreads);
-  if (dtype == 0 && d == 64)
-    hipLaunchKernelGGL((attend8_split_kernel<0, 64>), grid, block, lds, stream, a, partial, counters);
-  else if (dtype == 0)
-    hipLaunchKernelGGL((attend8_split_kernel<0, 128>), grid, block, lds, stream, a, partial, counters);
-  else if (d == 64)
-    hipLaunchKernelGGL((attend8_split_kernel<1, 64>), grid, block, lds, stream, a, partial, counters);
-  else
-    hipLaunchKernelGGL((attend8_split_kernel<1, 128>), grid, block, lds, stream, a, partial, counters);
-  return hipGetLastError();
+  if (dtype == 0) return d == 64 ? launch_split<0, 64>(a, ws, stream) : launch_split<0, 128>(a, ws, stream);
+  return d == 64 ? launch_split<1, 64>(a, ws, stream) : launch_split<1, 128>(a, ws, stream);
 }
 
 }  // namespace kvx

@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   __shared__ int last;
   static_assert(sizeof(kv) >= KVX_MAX_REQUESTS * sizeof(int64_t), "the prefix sums fit");
   int64_t* pre = reinterpret_cast<int64_t*>(kv);   // until the first unit
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int step_of = wave & 3;             // the step whose keys (waves 0-3) or values this wave widens
 
   prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
       ++b;
       continue;
     }
-    const int h = __builtin_amdgcn_readfirstlane((int)((at - base) / head_w));
+    const int h = uniform((int)((at - base) / head_w));
     const int64_t z = at - base - h * head_w;
     int blk = 0;
     for (int left = blocks; left > 0;) {   // last block whose first weight is at most z
@@ -109,44 +109,39 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
       if (WT::sum(before, blk + half + 1) <= z) { blk += half + 1; left -= half + 1; }
       else left = half;
     }
-    blk = __builtin_amdgcn_readfirstlane(blk);
+    blk = uniform(blk);
     const int64_t unit0 = uniform(base + h * head_w + WT::sum(before, blk));
     const int64_t weight = uniform(WT::sum(before, blk + 1) - WT::sum(before, blk));
     const int last_row = (blk + 1) * ROWS < r.rows ? (blk + 1) * ROWS - 1 : r.rows - 1;
-    const int lim_block = __builtin_amdgcn_readfirstlane(r.len - r.tokens + last_row / a.G);     // last key of the block
+    const int lim_block = uniform(r.len - r.tokens + last_row / a.G);     // last key of the block
     const int quanta = lim_block < 0 ? 1 : lim_block / kQuant + 1;
-    const int q0 = __builtin_amdgcn_readfirstlane((int)((at - unit0) * quanta / weight));
-    const int q1 = __builtin_amdgcn_readfirstlane(
+    const int q0 = uniform((int)((at - unit0) * quanta / weight));
+    const int q1 = uniform(
         end - unit0 >= weight ? quanta : (int)((end - unit0) * quanta / weight));
 
+    // the lane's query rows (the block's last one again past the end), the last key of each
     int lim[NB];
-    bool mine[NB];
     bf16x8_t qf[2 * U][NB];
     const int row0 = blk * ROWS + wave * 16 * NB;
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
-      const int row = row0 + 16 * x + n;
-      mine[x] = row < r.rows;
-      const int token = mine[x] ? row / a.G : 0, head = h * a.G + (mine[x] ? row % a.G : 0);
-      lim[x] = mine[x] ? r.len - r.tokens + token : -1;
+      const int row = row0 + 16 * x + n < r.rows ? row0 + 16 * x + n : r.rows - 1;
+      const int token = row / a.G, head = h * a.G + row % a.G;
+      lim[x] = r.len - r.tokens + token;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          u32x4_t v = {0, 0, 0, 0};
-          if (mine[x])
-            v = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) +
-                                                  (int64_t)(r.row0 + token) * a.q_stride[0] +
-                                                  (int64_t)head * a.q_stride[1] + 64 * u + 16 * g4 + 8 * w);
-          qf[2 * u + w][x] = __builtin_bit_cast(bf16x8_t, v);
-        }
+        for (int w = 0; w < 2; ++w)
+          qf[2 * u + w][x] = __builtin_bit_cast(
+              bf16x8_t, *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) +
+                                                          (int64_t)(r.row0 + token) * a.q_stride[0] +
+                                                          (int64_t)head * a.q_stride[1] + 64 * u + 16 * g4 + 8 * w));
     }
-    // least and largest of the wave's limits, and the least of the block's
-    const bool wave_full = row0 + 16 * NB <= r.rows, block_full = (blk + 1) * ROWS <= r.rows;
+    // least and largest of the wave's limits (none: -1), and the least of the block's
     const int wave_last = row0 + 16 * NB - 1 < r.rows ? row0 + 16 * NB - 1 : r.rows - 1;
-    const int lim_lo = __builtin_amdgcn_readfirstlane(wave_full ? r.len - r.tokens + row0 / a.G : -1);
-    const int lim_hi = __builtin_amdgcn_readfirstlane(row0 < r.rows ? r.len - r.tokens + wave_last / a.G : -1);
-    const int block_lo = __builtin_amdgcn_readfirstlane(block_full ? r.len - r.tokens + blk * ROWS / a.G : -1);
+    const int lim_lo = uniform(r.len - r.tokens + row0 / a.G);
+    const int lim_hi = uniform(row0 < r.rows ? r.len - r.tokens + wave_last / a.G : -1);
+    const int block_lo = uniform(r.len - r.tokens + blk * ROWS / a.G);
 
     f32x4_t o[NB][C];
     float m[NB], l[NB];
@@ -289,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll 1
       for (int s = 0; s < kSteps && key <= lim_hi; ++s, key += kStep) {
         const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};
-        const int bad = __builtin_amdgcn_readfirstlane(kbad[buf][s]);
+        const int bad = uniform(kbad[buf][s]);
         const u32x4_t* next = s + 1 < kSteps ? from + F * 64 : from;   // the last step's are not used
         f32x4_t x[2][NB];
 #pragma unroll
@@ -351,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
           }
         }
         // NaN values count only in rows that see their key
-        if (masked && __builtin_amdgcn_readfirstlane(vnan[buf][s]) != 0) {
+        if (masked && uniform(vnan[buf][s]) != 0) {
 #pragma unroll
           for (int i = 0; i < NB; ++i) {
             u32x4_t w;
@@ -490,8 +485,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
     if (done) {
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
-        if (!mine[x]) continue;
         const int row = row0 + 16 * x + (ln & 15);
+        if (row >= r.rows) continue;
         const int64_t to = (int64_t)(r.row0 + row / a.G) * a.H * a.G + h * a.G + row % a.G;
         const float f = l[x] == 0.0f ? 0.0f : 1.0f / l[x];    // no key: 0
         u32x4_t* y = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) + to * D + 4 * C * (ln >> 4));
