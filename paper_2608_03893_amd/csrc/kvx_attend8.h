@@ -10,7 +10,6 @@ namespace kvx {
 namespace {
 
 constexpr float kLazy = 8.0f;    // growth of a row's maximum (log2) that is let pass
-constexpr int kJoin = 16;        // partial sums joined at a time
 // Arrival counters, first in the workspace (four for each workgroup of the largest grid):
 // all kernels keep them there and leave them at zero, and partial sums behind.
 constexpr int kCounters = 4 * 1024;
@@ -96,6 +95,12 @@ __device__ __forceinline__ float2 get2(const float* from) {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)((uint64_t)(uint32_t)uniform((int)(uint32_t)v) | (uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32);
+}
+
+// a / b for a >= 0, b > 0, by 32-bit division where that does.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  if ((uint64_t)(a | b) >> 32 == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
 }
 
 // pre[b] = sum of weight(request 0 .. b), by a workgroup of THREADS; part: an entry per wave.

@@ -27,7 +27,19 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kStep = 32;                  // keys of a wave's step
 constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
 constexpr int kRows = 16;                  // query rows of a block
-constexpr int kLeast = 1;                  // quanta of a workgroup
+#ifndef KLS
+#define KLS 2
+#endif
+#ifndef KST
+#define KST 2
+#endif
+#ifndef FLY
+#define FLY 12
+#endif
+constexpr int kLeast = KLS;                // quanta of a workgroup
+constexpr int kStart = KST;                // weight of a unit's start, in quanta
+constexpr int kJoin = 64;                  // partial sums joined at a time
+constexpr int kFly = FLY;                  // of which a thread has these in flight
 #ifndef OCC
 #define OCC 3
 #endif
@@ -58,6 +70,7 @@ struct Stage {
 template <int DT, int D>
 __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
+  static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
   constexpr int RS = D + 4;                                        // row stride in LDS
   constexpr int SLOT = kRows * (D + 2);                            // floats of a partial sum
   extern __shared__ int64_t pre[];                                 // [B] quanta of requests 0 .. b
@@ -69,29 +82,34 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
   const int n = lane & 15, g4 = lane >> 4;
 
   prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
-    return (int64_t)blocks_of(r) * quanta_of(r) * a.H;
+    return (int64_t)blocks_of(r) * (quanta_of(r) + kStart) * a.H;
   });
-  const int64_t total = pre[a.B - 1];
-  int64_t per = (total + kGrid<DT, D> - 1) / kGrid<DT, D>;
-  per = per > kLeast ? per : kLeast;
+  const int64_t total = uniform(pre[a.B - 1]);
+  const int grid = gridDim.x;
+  const int64_t share_q = uniform(divide(total + grid - 1, grid));
+  const int64_t per = share_q > kLeast ? share_q : kLeast;
+  auto share_of = [&](int64_t q) { return (int)divide(q, per); };
   int64_t at = (int64_t)blockIdx.x * per;
   const int64_t end = at + per < total ? at + per : total;
   if (at >= end) return;
-  int b = find_request(pre, a.B, at);
+  int b = uniform(find_request(pre, a.B, at));
 
   const int64_t plane = ((int64_t)a.N << a.log2p) * D;
   const int P1 = (1 << a.log2p) - 1;
   while (at < end) {
-    while (pre[b] <= at) ++b;
-    b = uniform(b);
-    const int64_t base = b > 0 ? pre[b - 1] : 0;
+    while (uniform(pre[b]) <= at) ++b;
+    const int64_t base = uniform(b > 0 ? pre[b - 1] : (int64_t)0);
     const Request r = request(a, b);
     const int quanta = quanta_of(r);
-    const int64_t unit = (at - base) / quanta;
-    const int blk = (int)(unit / a.H), h = (int)(unit % a.H);
-    const int64_t unit0 = base + unit * quanta;              // its first quantum
-    const int q0 = uniform((int)(at - unit0));
-    const int q1 = uniform((int)(end - unit0 < quanta ? end - unit0 : quanta));
+    const int64_t unit = divide(at - base, quanta + kStart);
+    const int64_t unit0 = base + unit * (quanta + kStart);     // its first weight
+    const int blk = uniform((int)divide(unit, a.H)), h = uniform((int)(unit - (int64_t)blk * a.H));
+    const int64_t lo = at - unit0 - kStart, hi = end - unit0 - kStart;
+    const int q0 = uniform(lo < 0 ? 0 : (int)lo), q1 = uniform(hi < quanta ? (int)hi : quanta);
+    if (q0 >= q1) {      // only its start
+      at = unit0 + kStart + quanta < end ? unit0 + kStart + quanta : end;
+      continue;
+    }
 
     // this lane's query row (the block's last one again past the end): its keys' limit, its
     // channels
@@ -300,76 +318,134 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         *reinterpret_cast<f32x4_t*>(&jo[wave][n * RS + (4 * g4 + i) * C + c]) =
             (f32x4_t){o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     __syncthreads();
-    // thread (row, C channels) from here on
-    const int jr = tid >> 4, jc = (tid & 15) * C;
-    const int out_row = blk * kRows + jr;
-    float sum[C] = {}, top = -INFINITY, den = 0.0f;
+    // thread = (row, 4 channels) from here on, IT of them kThreads / Q rows apart
+    constexpr int Q = D / 4, IT = kRows * Q / kThreads;
+    const int valid = block_last - blk * kRows + 1;                // rows of the block
+    const int jr = tid / Q, jc = tid % Q * 4;
+    float top[IT], den[IT];
+    f32x4_t sum[IT];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, jm[w][jr]);
-    {
-      const float ref = top == -INFINITY ? 0.0f : top;
+    for (int x = 0; x < IT; ++x) {
+      const int at_row = jr + x * (kThreads / Q);
+      top[x] = fmaxf(fmaxf(jm[0][at_row], jm[1][at_row]), fmaxf(jm[2][at_row], jm[3][at_row]));
+      const float ref = top[x] == -INFINITY ? 0.0f : top[x];
+      den[x] = 0.0f;
+      sum[x] = (f32x4_t){0, 0, 0, 0};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(jm[w][jr] - ref);    // 0 for a wave that saw nothing; NaN sums stay
-        den += f * jl[w][jr];
-#pragma unroll
-        for (int c = 0; c < C; ++c) sum[c] += f * jo[w][jr * RS + jc + c];
+        const float f = __builtin_amdgcn_exp2f(jm[w][at_row] - ref);   // 0 for a wave that saw nothing; NaN sums stay
+        den[x] += f * jl[w][at_row];
+        sum[x] += f * *reinterpret_cast<const f32x4_t*>(&jo[w][at_row * RS + jc]);
       }
     }
     // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`
-    const int64_t g0 = unit0 / per, g1 = (unit0 + quanta - 1) / per;
+    const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
     bool done = g0 == g1;
     if (!done) {
-      const int parts = (int)(g1 - g0) + 1, mine_at = (int)(blockIdx.x - g0);
-      auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
+      const int parts = g1 - g0 + 1, mine_at = (int)blockIdx.x - g0;
+      auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
       // Partial sums pass between workgroups on different XCDs, each with its own L2: they
       // are written through and read past it (agent scope), which spares the write-back
       // of the whole L2 that a fence at that scope costs.
       auto put = [&](int i) {
         float* to = partial + (int64_t)slot(i) * SLOT;
-        if (out_row < r.rows) {
 #pragma unroll
-          for (int c = 0; c < C; c += 2) put2(to + jr * D + jc + c, sum[c], sum[c + 1]);
-          if ((tid & 15) == 0) put2(to + kRows * D + 2 * jr, top, den);
+        for (int x = 0; x < IT; ++x) {
+          const int at_row = jr + x * (kThreads / Q);
+          if (at_row >= valid) break;
+          put2(to + at_row * D + jc, sum[x][0], sum[x][1]);
+          put2(to + at_row * D + jc + 2, sum[x][2], sum[x][3]);
+          if (jc == 0) put2(to + kRows * D + 2 * at_row, top[x], den[x]);
         }
       };
-      // joins `count` partial sums first, first + stride, .., four in flight
+      // Joins `count` partial sums first, first + stride, ..: the parts' weights, and kFly
+      // parts of a thread's channels in flight at a time, the first with the weights.
+      // With few rows the threads share the parts of a row.
       auto join = [&](int first, int stride, int count) {
-        top = -INFINITY;
-        den = 0.0f;
+        float* weight = &jo[0][0];                                 // [kJoin][kRows]
+        f32x4_t* across = reinterpret_cast<f32x4_t*>(&jo[1][0]);   // [kThreads]
+        const int items = valid * Q, shares = kThreads / items > 1 ? kThreads / items : 1;
+        int share = 0, item = tid;
+        if (shares > 1) {
+          share = tid / items;
+          item = tid - share * items;
+        }
+        const int at_row = item / Q < valid ? item / Q : 0;       // idle threads read a row too
+        const float* from = partial + at_row * D + item % Q * 4;
+        float2 v[kFly][2];
+        auto fly = [&](int i0, int more) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum[c] = 0.0f;
-        if (out_row >= r.rows) return;
-        for (int i0 = 0; i0 < count; i0 += 4) {
-          float2 md[4], x[4][C / 2];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int at_i = i0 + i < count ? i0 + i : count - 1;
-            const float* from = partial + (int64_t)slot(first + at_i * stride) * SLOT;
-            md[i] = get2(from + kRows * D + 2 * jr);
-#pragma unroll
-            for (int c = 0; c < C / 2; ++c) x[i][c] = get2(from + jr * D + jc + 2 * c);
+          for (int i = 0; i < kFly; ++i) {
+            const int at_i = i0 + i * shares < count ? i0 + i * shares : count - 1;
+            const uint32_t off = (uint32_t)slot(first + at_i * stride) * SLOT + more;
+            v[i][0] = get2(from + off);
+            v[i][1] = get2(from + off + 2);
           }
-          float now = top;
+        };
+        auto add = [&](f32x4_t& to, int i0, int row) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) now = fmaxf(now, md[i].x);
-          const float ref = now == -INFINITY ? 0.0f : now;
-          const float keep = __builtin_amdgcn_exp2f(top - ref);
-          top = now;
-          den *= keep;
+          for (int i = 0; i < kFly; ++i) {
+            const float f = i0 + i * shares < count ? weight[(i0 + i * shares) * kRows + row] : 0.0f;
+            to += f * (f32x4_t){v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y};
+          }
+        };
+        fly(share, 0);
+        __syncthreads();                                 // jo, jm and jl have been read
+        {  // 16 lanes a row
+          const int row = tid >> 4, sub = tid & 15;
+          float2 md[kJoin / 16];
+          float most = -INFINITY, l16 = 0.0f;
 #pragma unroll
-          for (int c = 0; c < C; ++c) sum[c] *= keep;
+          for (int i = 0; i < kJoin / 16; ++i) {
+            const int at_i = sub + 16 * i < count ? sub + 16 * i : count - 1;
+            md[i] = get2(partial + (uint32_t)slot(first + at_i * stride) * SLOT + kRows * D + 2 * (row < valid ? row : 0));
+            if (sub + 16 * i >= count) md[i] = make_float2(-INFINITY, 0.0f);
+          }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (i0 + i >= count) break;
+          for (int i = 0; i < kJoin / 16; ++i) most = fmaxf(most, md[i].x);
+#pragma unroll
+          for (int n16 = 8; n16; n16 >>= 1) most = fmaxf(most, __shfl_xor(most, n16, 64));
+          const float ref = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+          for (int i = 0; i < kJoin / 16; ++i) {
             const float f = __builtin_amdgcn_exp2f(md[i].x - ref);
-            den += f * md[i].y;
-#pragma unroll
-            for (int c = 0; c < C / 2; ++c) {
-              sum[2 * c] += f * x[i][c].x;
-              sum[2 * c + 1] += f * x[i][c].y;
-            }
+            l16 += f * md[i].y;
+            weight[(sub + 16 * i) * kRows + row] = f;
           }
+#pragma unroll
+          for (int n16 = 8; n16; n16 >>= 1) l16 += __shfl_xor(l16, n16, 64);
+          if (sub == 0) {
+            jm[0][row] = most;
+            jl[0][row] = l16;
+          }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < IT; ++x) sum[x] = (f32x4_t){0, 0, 0, 0};
+        if (share < shares) {
+          add(sum[0], share, at_row);
+          for (int i0 = share + kFly * shares; i0 < count; i0 += kFly * shares) {
+            fly(i0, 0);
+            add(sum[0], i0, at_row);
+          }
+        }
+#pragma unroll
+        for (int x = 1; x < IT; ++x)                      // shares == 1 where there are such rows
+          if (jr + x * (kThreads / Q) < valid)
+            for (int i0 = 0; i0 < count; i0 += kFly) {
+              fly(i0, x * (kThreads / Q) * D);
+              add(sum[x], i0, jr + x * (kThreads / Q));
+            }
+        if (shares > 1) {
+          if (share < shares) across[tid] = sum[0];
+          __syncthreads();
+          if (tid < items)
+            for (int i = 1; i < shares; ++i) sum[0] += across[i * items + tid];
+        }
+#pragma unroll
+        for (int x = 0; x < IT; ++x) {
+          top[x] = jm[0][jr + x * (kThreads / Q)];
+          den[x] = jl[0][jr + x * (kThreads / Q)];
         }
       };
       put(mine_at);
@@ -388,23 +464,23 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         }
       }
     }
-    if (done && out_row < r.rows) {
-      const int64_t to = (int64_t)(r.row0 + out_row / a.G) * a.H * a.G + h * a.G + out_row % a.G;
-      const float f = den == 0.0f ? 0.0f : 1.0f / den;    // no key: 0
-      if (DT == 0) {
-        uint32_t* y = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + to * D + jc);
+    if (done) {
 #pragma unroll
-        for (int c = 0; c < C / 2; ++c) y[c] = pack2(sum[2 * c] * f, sum[2 * c + 1] * f);
-      } else {
-        float* y = static_cast<float*>(a.out) + to * D + jc;
-#pragma unroll
-        for (int c = 0; c < C; ++c) y[c] = sum[c] * f;
+      for (int x = 0; x < IT; ++x) {
+        const int at_row = jr + x * (kThreads / Q), out_row = blk * kRows + at_row;
+        if (at_row >= valid) break;
+        const int64_t to = (int64_t)(r.row0 + out_row / a.G) * a.H * a.G + h * a.G + out_row % a.G;
+        const f32x4_t y = sum[x] * (den[x] == 0.0f ? 0.0f : 1.0f / den[x]);    // no key: 0
+        if (DT == 0)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to * D + jc) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+        else
+          *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + to * D + jc) = y;
+        if (a.lse != nullptr && jc == 0)
+          a.lse[to] = den[x] == 0.0f ? -INFINITY : (top[x] + __builtin_amdgcn_logf(den[x])) * 0.69314718055994530942f;
       }
-      if (a.lse != nullptr && (tid & 15) == 0)
-        a.lse[to] = den == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
     }
     __syncthreads();    // the LDS arrays are free again
-    at = unit0 + q1;
+    at = unit0 + kStart + q1;
   }
 }
 
@@ -426,7 +502,11 @@ size_t attend_ws_bytes(int B, int, int G, int T, int d, int dtype) {
 template <int DT, int D>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
   int* counters = static_cast<int*>(ws);
-  hipLaunchKernelGGL((attend8_split_kernel<DT, D>), dim3(kGrid<DT, D>), dim3(kThreads),
+  // no more workgroups than the tables' pages hold quanta for
+  const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((((int64_t)a.M << a.log2p) + kQuant - 1) / kQuant + kStart);
+  const int64_t want = (most + kLeast - 1) / kLeast;
+  const unsigned grid = want < kGrid<DT, D> ? (unsigned)want : kGrid<DT, D>;
+  hipLaunchKernelGGL((attend8_split_kernel<DT, D>), dim3(grid), dim3(kThreads),
                      (size_t)a.B * sizeof(int64_t), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
   return hipGetLastError();
 }

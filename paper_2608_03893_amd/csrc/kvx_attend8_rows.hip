@@ -23,6 +23,7 @@ constexpr int kThreads = 512, kWaves = 8;
 constexpr int kSteps = 4, kStep = 32, kQuant = kSteps * kStep;
 constexpr int kGrid = 256;                 // workgroups: one per CU
 constexpr int kXcds = 8;
+constexpr int kJoin = 16;                  // partial sums joined at a time
 #ifndef RING
 #define RING 4
 #endif
