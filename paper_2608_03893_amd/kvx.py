@@ -14,6 +14,7 @@ mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple
 
@@ -621,6 +622,16 @@ def _raw_stream(stream, device):
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
+# The library's structs by their sizes; nothing writes to them after they are made.
+_pool = functools.lru_cache(maxsize=256)(Pool)
+_sizes = functools.lru_cache(maxsize=256)(AttendDims)
+
+
+@functools.lru_cache(maxsize=256)
+def _strides(*s):
+    return (ctypes.c_int64 * len(s))(*s)
+
+
 def _new(shape, dtype, device, stream):
     """An output allocated on the launch stream (see _scratch)."""
     if stream is None:
@@ -659,12 +670,16 @@ def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None,
     args = (_int32("lens", lens, (B,)), _int32("add", add, (B,)),
             _int32("block_tables", block_tables, (B, M)), _int32("free_ring", free_ring, (N,)),
             _addr("free", free))
-    if out is None:
-        out = PagePlan(*[_new(n, torch.int32, dev, stream) for n in (B, B + 1, T, T, 4)])
+    if out is None:      # one allocation; positions and slots start on 16 bytes
+        pad = -T % 4
+        pos, _, slots, _, lens_out, cu, left = _new(
+            2 * (T + pad) + 2 * B + 5, torch.int32, dev, stream).split_with_sizes(
+                (T, pad, T, pad, B, B + 1, 4))
+        out = PagePlan(lens_out, cu, pos, slots, left)
         outs = [t.data_ptr() for t in out]
     else:
         outs = [_int32(name, t, (n,)) for name, t, n in zip(PagePlan._fields, out, (B, B + 1, T, T, 4))]
-    _check(load().kvx_plan_pages(ctypes.byref(Pool(N, int(page_size), M)), B, T, *args, *outs,
+    _check(load().kvx_plan_pages(ctypes.byref(_pool(N, int(page_size), M)), B, T, *args, *outs,
                                  _raw_stream(stream, dev)))
     return out
 
@@ -678,9 +693,6 @@ def _rows_addr(name, t):
     return t.data_ptr()
 
 
-_Strides2, _Strides3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
-
-
 def _pool8(pool, scales, lead, max_pages):
     """kvx_pool of an 8-bit pool [*lead, num_slots, d] and its scales [*lead, num_pages]."""
     shape, spages = pool.shape, scales.shape
@@ -691,7 +703,7 @@ def _pool8(pool, scales, lead, max_pages):
     slots, pages = shape[-2], spages[-1]
     if pages < 1 or slots % pages:
         raise ValueError(f"{slots} slots do not divide into {pages} pages")
-    return Pool(pages, slots // pages, max_pages)
+    return _pool(pages, slots // pages, max_pages)
 
 
 def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
@@ -708,8 +720,8 @@ def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
     if pool.shape[4] != d:
         raise ValueError(f"pool rows have {pool.shape[4]} channels, k and v {d}")
     _check(load().kvx_store_cache8(
-        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_addr("k", k), _Strides3(*k.stride()[:3]),
-        _rows_addr("v", v), _Strides3(*v.stride()[:3]), _int32("slot_mapping", slot_mapping, (T,)),
+        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_addr("k", k), _strides(*k.stride()[:3]),
+        _rows_addr("v", v), _strides(*v.stride()[:3]), _int32("slot_mapping", slot_mapping, (T,)),
         _addr("pool", pool), _addr("scales", scales), _raw_stream(stream, k.device)))
     return pool
 
@@ -721,7 +733,7 @@ def _attend_dims(q, pool, block_tables):
     H = pool.shape[1]
     if heads % H or pool.shape[3] != d:
         raise ValueError(f"{heads} query heads of {d} channels on a pool of {H} heads of {pool.shape[3]}")
-    return AttendDims(block_tables.shape[0], H, heads // H, T, d)
+    return _sizes(block_tables.shape[0], H, heads // H, T, d)
 
 
 def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
@@ -752,7 +764,7 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     B, M = block_tables.shape
     p = _pool8(pool, scales, (2, dims.H), M)
     code, dev, shape = _dtype_code(q), q.device, q.shape
-    args = (_rows_addr("q", q), _Strides2(*q.stride()[:2]), _addr("pool", pool), _addr("scales", scales),
+    args = (_rows_addr("q", q), _strides(*q.stride()[:2]), _addr("pool", pool), _addr("scales", scales),
             _int32("block_tables", block_tables, (B, M)), _int32("lens", lens, (B,)),
             _int32("cu", cu, (B + 1,)))
     if out is None:
