@@ -23,7 +23,6 @@ constexpr int kThreads = 512, kWaves = 8;
 constexpr int kSteps = 4, kStep = 32, kQuant = kSteps * kStep;
 constexpr int kGrid = 256;                 // workgroups: one per CU
 constexpr int kXcds = 8;
-constexpr int kJoin = 16;                  // partial sums joined at a time
 #ifndef RING
 #define RING 4
 #endif
@@ -469,15 +468,20 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
         }
       };
       put(mine_at);
-      const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
-      const int in_group = parts - group * kJoin < kJoin ? parts - group * kJoin : kJoin;
-      if (arrive(counters + 2 * slot(group * kJoin), in_group, &last)) {
-        join(group * kJoin, 1, in_group);
+      // More than four parts are joined in two levels of about equal width, the first by
+      // several workgroups at once (one alone reads 16 parts in 35 us).
+      int width = parts;
+      if (parts > 4)
+        for (width = 3; width * width < parts;) ++width;
+      const int group = mine_at / width, groups = (parts + width - 1) / width;
+      const int in_group = parts - group * width < width ? parts - group * width : width;
+      if (arrive(counters + 2 * slot(group * width), in_group, &last)) {
+        join(group * width, 1, in_group);
         done = groups == 1;
         if (!done) {
-          put(group * kJoin);    // each wave overwrites what only it has read
+          put(group * width);    // each wave overwrites what only it has read
           if (arrive(counters + 2 * slot(0) + 1, groups, &last)) {
-            join(0, kJoin, groups);
+            join(0, width, groups);
             done = true;
           }
         }

@@ -56,88 +56,121 @@ struct Vec<1> {
   }
 };
 
-// A wave takes the pages whose first row of the call lies in its window of rows, whole:
-// the largest value over the page's rows, the scale, the codes.
-template <int DT, int D>
+// Rows s .. e - 1 of a page by one wave: the largest value, the scale, the codes.  LOADS
+// times ROWS rows stay in registers between the two; more are read again, from L2.
+template <int DT, int D, int LOADS, typename T>
+__device__ __forceinline__ void store_page(const StoreArgs& a, const T* x, int64_t ts, uint8_t* codes, float* scales,
+                                           int s, int e, uint32_t first, float old) {
+  constexpr int E = Vec<DT>::N, LANES = D / E, ROWS = 64 / LANES;   // lanes a row, rows a load
+  const int lane = threadIdx.x & 63, sub = lane / LANES;
+  const int P = 1 << a.log2p, held = first & (P - 1);               // earlier rows of the page
+  const uint32_t page = first >> a.log2p;
+  Vec<DT> v[LOADS];
+  uint32_t slot[LOADS];
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int t = t0 + i * ROWS + sub < e ? t0 + i * ROWS + sub : e - 1;   // the last row again
+      v[i].q = *reinterpret_cast<const uint4*>(x + t * ts);
+      slot[i] = (uint32_t)a.slots[t];
+    }
+  };
+  float m = 0.0f;
+  for (int t0 = s; t0 < e; t0 += LOADS * ROWS) {
+    load(t0);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) m = fmaxf(m, v[i].amax());
+  }
+  float scale = pow2_scale(wave_max(m));
+  if (held > 0) {
+    if (old < scale) {
+      const float r = old / scale;
+      uint8_t* c = codes + (int64_t)page * P * D;
+      for (int i = 16 * lane; i < held * D; i += 1024) {
+        uint4 q = *reinterpret_cast<const uint4*>(c + i);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = to_e4m3x4(from_e4m3<0>(w[j]), from_e4m3<1>(w[j]), from_e4m3<2>(w[j]), from_e4m3<3>(w[j]), r);
+        *reinterpret_cast<uint4*>(c + i) = q;
+      }
+    } else {
+      scale = old;
+    }
+  }
+  if (lane == 0) scales[page] = scale;
+  const float r = 1.0f / scale;
+  for (int t0 = s; t0 < e; t0 += LOADS * ROWS) {
+    if (e - s > LOADS * ROWS) load(t0);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      if (t0 + i * ROWS + sub < e) v[i].put(codes + (int64_t)slot[i] * D + (lane % LANES) * E, r);
+  }
+}
+
+// A wave takes the pages whose first row of the call lies in its window of rows, whole.
+// LOADS: what a page takes, up to 16; fewer registers leave room for more waves.
+template <int DT, int D, int LOADS>
 __global__ void __launch_bounds__(64 * kWaves) store8_kernel(StoreArgs a, int window, int n_windows) {
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int plane = (int)(unit / n_windows);
   if (plane >= a.L * 2 * a.H) return;
   const int h = plane % a.H, kv = plane / a.H % 2, l = plane / (2 * a.H);
-  const int t0 = (int)(unit % n_windows) * window;
+  const int t0 = (int)(unit - (int64_t)plane * n_windows) * window;
   const int t1 = t0 + window < a.T ? t0 + window : a.T;
-  constexpr int E = Vec<DT>::N, LANES = D / E, ROWS = 64 / LANES;   // lanes a row, rows a load
+  constexpr int E = Vec<DT>::N, LANES = D / E, ROWS = 64 / LANES;
   using T = typename std::conditional<DT == 0, uint16_t, float>::type;
-  const T* x = static_cast<const T*>(a.x[kv]) + l * a.stride[kv][0] + h * a.stride[kv][1] + (lane % LANES) * E;
-  const int64_t ts = a.stride[kv][2];
-  const int P = 1 << a.log2p;
-  uint8_t* codes = a.codes + (int64_t)plane * a.N * P * D;
+  const int64_t* st = a.stride[kv];
+  const T* x = static_cast<const T*>(a.x[kv]) + l * st[0] + h * st[1] + (lane % LANES) * E;
+  uint8_t* codes = a.codes + ((int64_t)plane * a.N << a.log2p) * D;
+  float* scales = a.scales + (int64_t)plane * a.N;
   const uint32_t num_slots = (uint32_t)a.N << a.log2p;
 
-  for (int s = t0; s < t1; ++s) {
-    const uint32_t slot = (uint32_t)a.slots[s];
-    if (slot >= num_slots) continue;
-    const uint32_t page = slot >> a.log2p;
-    if (s > 0) {
-      const uint32_t before = (uint32_t)a.slots[s - 1];
-      if (before < num_slots && before >> a.log2p == page) continue;
-    }
-    // rows s .. e - 1 are the page's
-    int e = s + 1;
-    for (;;) {
-      const int t = e + lane;
-      const uint32_t u = t < a.T ? (uint32_t)a.slots[t] : num_slots;
-      const uint64_t other = __ballot(!(u < num_slots && u >> a.log2p == page));
-      if (other) { e += __ffsll((unsigned long long)other) - 1; break; }
-      e += 64;
-    }
-    float m = 0.0f;
-    for (int t = s + lane / LANES; t < e; t += ROWS) {
-      Vec<DT> v;
-      v.q = *reinterpret_cast<const uint4*>(x + t * ts);
-      m = fmaxf(m, v.amax());
-    }
-    float scale = pow2_scale(wave_max(m));
-    const int held = slot & (P - 1);   // earlier rows of the page
-    float* sp = a.scales + (int64_t)plane * a.N + page;
-    if (held > 0) {
-      const float old = *sp;
-      if (old < scale) {
-        const float r = old / scale;
-        uint8_t* c = codes + (int64_t)page * P * D;
-        for (int i = 16 * lane; i < held * D; i += 1024) {
-          uint4 q = *reinterpret_cast<const uint4*>(c + i);
-          uint32_t* w = reinterpret_cast<uint32_t*>(&q);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = to_e4m3x4(from_e4m3<0>(w[j]), from_e4m3<1>(w[j]), from_e4m3<2>(w[j]), from_e4m3<3>(w[j]), r);
-          *reinterpret_cast<uint4*>(c + i) = q;
-        }
-      } else {
-        scale = old;
+  // 64 rows from c on, a lane each: its slot, and which rows go on with the page before
+  auto look = [&](int c, uint32_t& slot) {
+    const int t = c + lane;
+    slot = t < a.T ? (uint32_t)a.slots[t] : num_slots;
+    const uint32_t before = t > 0 && t <= a.T ? (uint32_t)a.slots[t - 1] : num_slots;
+    return __ballot(slot < num_slots && before < num_slots && slot >> a.log2p == before >> a.log2p);
+  };
+  for (int c = t0; c < t1; c += 64) {
+    uint32_t slot;
+    const uint64_t on = look(c, slot);
+    uint64_t starts = __ballot(slot < num_slots && c + lane < t1) & ~on;
+    while (starts) {
+      const int i = __ffsll((unsigned long long)starts) - 1;
+      starts &= starts - 1;
+      const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)slot, i);
+      const float old = scales[first >> a.log2p];
+      // rows that follow on the page, past these 64 too
+      uint64_t rest = i < 63 ? ~(on >> (i + 1)) : ~0ull;
+      int e = c + i + 1 + (rest ? __ffsll((unsigned long long)rest) - 1 : 64);
+      for (int from = c + 64; e == from; from += 64) {
+        uint32_t ignored;
+        rest = ~look(from, ignored);
+        e = from + (rest ? __ffsll((unsigned long long)rest) - 1 : 64);
       }
+      if (e - (c + i) <= ROWS) store_page<DT, D, 1>(a, x, st[2], codes, scales, c + i, e, first, old);
+      else store_page<DT, D, LOADS>(a, x, st[2], codes, scales, c + i, e, first, old);
     }
-    if (lane == 0) *sp = scale;
-    const float r = 1.0f / scale;
-    for (int t = s + lane / LANES; t < e; t += ROWS) {
-      Vec<DT> v;
-      v.q = *reinterpret_cast<const uint4*>(x + t * ts);
-      v.put(codes + (int64_t)(uint32_t)a.slots[t] * D + (lane % LANES) * E, r);
-    }
-    s = e - 1;
   }
 }
 
 template <int DT, int D>
 hipError_t launch(const StoreArgs& a, hipStream_t stream) {
+  // A wave's window is a page of rows, or less where that would leave most of the chip idle.
   const int64_t planes = (int64_t)a.L * 2 * a.H;
   int window = 1 << a.log2p;
   while (window > 1 && planes * ((a.T + window - 1) / window) < 8192) window /= 2;
   const int n = (a.T + window - 1) / window;
   const int64_t wg = (planes * n + kWaves - 1) / kWaves;
   if (wg >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((store8_kernel<DT, D>), dim3((unsigned)wg), dim3(64 * kWaves), 0, stream, a, window, n);
+  const dim3 grid((unsigned)wg), block(64 * kWaves);
+  const int loads = (D / Vec<DT>::N << a.log2p) / 64;
+  if (loads <= 4) hipLaunchKernelGGL((store8_kernel<DT, D, 4>), grid, block, 0, stream, a, window, n);
+  else if (loads <= 8) hipLaunchKernelGGL((store8_kernel<DT, D, 8>), grid, block, 0, stream, a, window, n);
+  else hipLaunchKernelGGL((store8_kernel<DT, D, 16>), grid, block, 0, stream, a, window, n);
   return hipGetLastError();
 }
 
