@@ -15,20 +15,28 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Inclusive sum over the workgroup's threads; every thread calls it.  `part`: one
-// entry per wave.
-__device__ int64_t block_scan(int64_t v, int64_t* part) {
+// Sums that stop at 2^32 - 1 instead of wrapping: still associative, and beyond any row or
+// page that a request may get.
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Exclusive sums of a pair over the workgroup's threads; every thread calls it.  `part`: one
+// pair per wave.
+__device__ uint2 block_scan(uint2 v, uint2* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint2 sum = v;
 #pragma unroll
   for (int n = 1; n < 64; n <<= 1) {
-    const int64_t u = __shfl_up(v, n, 64);
-    if (lane >= n) v += u;
+    const uint32_t x = __shfl_up(sum.x, n, 64), y = __shfl_up(sum.y, n, 64);
+    if (lane >= n) sum = make_uint2(plus(sum.x, x), plus(sum.y, y));
   }
+  if (lane == 63) part[wave] = sum;
+  uint2 before = make_uint2(__shfl_up(sum.x, 1, 64), __shfl_up(sum.y, 1, 64));
+  if (lane == 0) before = make_uint2(0, 0);
   __syncthreads();
-  if (lane == 63) part[wave] = v;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) v += part[w];
-  return v;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64 - 1; ++w)
+    if (w < wave) before = make_uint2(plus(before.x, part[w].x), plus(before.y, part[w].y));
+  return before;
 }
 
 // First b with end[b] > x, at most B (end rises).
@@ -47,18 +55,20 @@ struct Request {
   int32_t len, grow, have, ask, back;
   bool fits;
 };
-__device__ __forceinline__ Request request(const PlanArgs& a, int b, int64_t end) {
+__device__ __forceinline__ Request request(const PlanArgs& a, int32_t len, int32_t add, uint32_t end) {
   Request r;
-  r.len = a.lens[b] > 0 ? a.lens[b] : 0;
-  const int32_t add = a.add[b];
+  r.len = len > 0 ? len : 0;
   r.grow = add > 0 ? add : 0;
   const int64_t up = (1 << a.log2p) - 1;
   const int64_t have = (r.len + up) >> a.log2p, need = (r.len + (int64_t)r.grow + up) >> a.log2p;
   r.have = (int32_t)have;
-  r.fits = r.grow == 0 || (need <= a.M && end <= a.T);
+  r.fits = r.grow == 0 || (need <= a.M && end <= (uint32_t)a.T);
   r.ask = r.fits ? (int32_t)(need - have) : 0;
   r.back = add < 0 ? (int32_t)(have < a.M ? have : a.M) : 0;
   return r;
+}
+__device__ __forceinline__ Request request(const PlanArgs& a, int b, int32_t end) {
+  return request(a, a.lens[b], a.add[b], (uint32_t)end);
 }
 
 __device__ __forceinline__ int32_t least(int64_t x, int64_t most) {
@@ -67,14 +77,15 @@ __device__ __forceinline__ int32_t least(int64_t x, int64_t most) {
 
 // Every workgroup sums over all requests (a few loads a thread) and keeps the three
 // prefix sums in LDS, so one launch does it all; then the workgroups share the rows,
-// the pages and the requests.  Sums are taken in 64 bits and kept up to the first
-// value that no request may reach.
+// the pages and the requests.
+//
+// Bound by its chain of waits: lengths, two scans, table or ring, stores.
 __global__ void __launch_bounds__(kThreads) plan_pages_kernel(PlanArgs a) {
   extern __shared__ int32_t lds[];
   int32_t* end = lds;
   int32_t* pend = lds + a.B;
   int32_t* rend = lds + 2 * a.B;
-  __shared__ int64_t part[kThreads / 64];
+  __shared__ uint2 part[2][kThreads / 64];
   __shared__ int32_t refused;
   const int tid = threadIdx.x, B = a.B, T = a.T, N = a.N;
   const int chunk = (B + kThreads - 1) / kThreads;
@@ -82,32 +93,27 @@ __global__ void __launch_bounds__(kThreads) plan_pages_kernel(PlanArgs a) {
   int32_t count = a.free_in[1];
   count = count < 0 ? 0 : count > N ? N : count;
   const int32_t head = (int32_t)((uint32_t)a.free_in[0] % (uint32_t)N);
-
-  int64_t rows = 0;
-  for (int b = b0; b < b1; ++b) rows += a.add[b] > 0 ? a.add[b] : 0;
-  int64_t at = block_scan(rows, part) - rows;
-  int64_t asks = 0, backs = 0;
-  for (int b = b0; b < b1; ++b) {
-    at += a.add[b] > 0 ? a.add[b] : 0;
-    end[b] = least(at, (int64_t)T + 1);
-    const Request r = request(a, b, at);
-    asks += r.ask;
-    backs += r.back;
-  }
-  int64_t pat = block_scan(asks, part) - asks;
-  int64_t rat = block_scan(backs, part) - backs;
-  at = block_scan(rows, part) - rows;
-  int32_t bad = 0;
   if (tid == 0) refused = 0;
-  __syncthreads();
+
+  uint32_t rows = 0;
+  for (int b = b0; b < b1; ++b) rows = plus(rows, a.add[b] > 0 ? a.add[b] : 0);
+  const uint32_t row0 = block_scan(make_uint2(rows, 0), part[0]).x;
+  uint32_t at = row0;
+  uint2 pages = make_uint2(0, 0);     // asked for, given back
   for (int b = b0; b < b1; ++b) {
-    at += a.add[b] > 0 ? a.add[b] : 0;
-    const Request r = request(a, b, at);
-    pat += r.ask;
-    rat += r.back;
-    pend[b] = least(pat, (int64_t)N + 1);
-    rend[b] = least(rat, (int64_t)N + 1);
-    bad += !r.fits || (r.ask > 0 && pat > count);
+    at = plus(at, a.add[b] > 0 ? a.add[b] : 0);
+    end[b] = least(at, (int64_t)T + 1);
+    const Request r = request(a, b, end[b]);
+    pages = make_uint2(plus(pages.x, r.ask), plus(pages.y, r.back));
+  }
+  pages = block_scan(pages, part[1]);
+  int32_t bad = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Request r = request(a, b, end[b]);
+    pages = make_uint2(plus(pages.x, r.ask), plus(pages.y, r.back));
+    pend[b] = least(pages.x, (int64_t)N + 1);
+    rend[b] = least(pages.y, (int64_t)N + 1);
+    bad += !r.fits || (r.ask > 0 && pend[b] > count);
   }
   if (bad) atomicAdd(&refused, bad);
   __syncthreads();
