@@ -103,14 +103,14 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return a / b;
 }
 
-// pre[b] = sum of weight(request 0 .. b), by a workgroup of THREADS; part: an entry per wave.
+// pre[b] = sum of weight(request, number) over requests 0 .. b, by a workgroup of THREADS; part: an entry per wave.
 template <int THREADS, typename W>
 __device__ __forceinline__ void prefix_requests(const AttendArgs& a, int64_t* pre, int64_t* part, W weight) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int chunk = (a.B + THREADS - 1) / THREADS;
   const int b0 = tid * chunk < a.B ? tid * chunk : a.B, b1 = b0 + chunk < a.B ? b0 + chunk : a.B;
   int64_t sum = 0;
-  for (int b = b0; b < b1; ++b) sum += weight(request(a, b));
+  for (int b = b0; b < b1; ++b) sum += weight(request(a, b), b);
   int64_t v = sum;
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) {
@@ -122,7 +122,7 @@ __device__ __forceinline__ void prefix_requests(const AttendArgs& a, int64_t* pr
   for (int w = 0; w < tid >> 6; ++w) v += part[w];
   v -= sum;
   for (int b = b0; b < b1; ++b) {
-    v += weight(request(a, b));
+    v += weight(request(a, b), b);
     pre[b] = v;
   }
   __syncthreads();

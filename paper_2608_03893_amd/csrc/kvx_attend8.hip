@@ -23,40 +23,32 @@
 namespace kvx {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kStep = 32;                  // keys of a wave's step
-constexpr int kQuant = kWaves * kStep;     // keys of a workgroup's step
 constexpr int kRows = 16;                  // query rows of a block
-#ifndef KLS
-#define KLS 2
+#ifndef KLB
+#define KLB 1
 #endif
-#ifndef KST
-#define KST 2
+template <int W>
+constexpr int kLeast = W > 4 ? KLB : 2;    // least quanta of a workgroup
+#ifndef KSM
+#define KSM 10
 #endif
-#ifndef FLY
-#define FLY 12
-#endif
-constexpr int kLeast = KLS;                // quanta of a workgroup
-constexpr int kStart = KST;                // weight of a unit's start, in quanta
+constexpr int kStart = 2;                  // weight of a unit's start, in quanta
+constexpr int kSmall = KSM;                // most weight of a unit that is not split
 constexpr int kJoin = 64;                  // partial sums joined at a time
-constexpr int kFly = FLY;                  // of which a thread has these in flight
-#ifndef OCC
-#define OCC 3
-#endif
-// Workgroups a CU: as many as the registers hold.  More of them hide more of a unit's
-// start (lengths, pages, scales, rows: loads that wait for one another) than prefetching
+constexpr int kFly = 12;                   // of which a thread has these in flight
+// Waves a SIMD: as many as the registers hold.  More of them hide more of a unit's start
+// (lengths, pages, scales, rows: loads that wait for one another) than prefetching
 // within a wave: 64 ragged requests 86 us with two and the next step's loads in flight,
 // 72 us with three and no prefetch.
 template <int DT, int D>
-constexpr int kOcc = DT == 1 && D == 128 ? 2 : OCC;
-template <int DT, int D>
-constexpr int kGrid = 256 * kOcc<DT, D>;
+constexpr int kOcc = DT == 1 && D == 128 ? 2 : 3;
 
-// Blocks of rows, and quanta of one block and head (rows without any key still have an
-// output).
+// Blocks of rows, and quanta (of `quant` keys) of one block and head (rows without any key
+// still have an output).
 __device__ __forceinline__ int blocks_of(const Request& r) { return (r.rows + kRows - 1) / kRows; }
-__device__ __forceinline__ int quanta_of(const Request& r) {
-  return r.len > kQuant ? (int)(((int64_t)r.len + kQuant - 1) / kQuant) : 1;
+__device__ __forceinline__ int quanta_of(const Request& r, int quant) {
+  return r.len > quant ? (int)(((int64_t)r.len + quant - 1) / quant) : 1;
 }
 
 // A step's keys and values, as loaded.
@@ -67,8 +59,10 @@ struct Stage {
   uint32_t v[8][V];         // key (lane >> 4) * 4 + (j & 3) of tile j >> 2, bytes (lane & 15) * 4 V ..
 };
 
-template <int DT, int D>
-__global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+// W waves: 4, and kOcc workgroups a CU; or 4 kOcc, and one.
+template <int DT, int D, int W>
+__global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+  constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep;
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
   static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
   constexpr int RS = D + 4;                                        // row stride in LDS
@@ -81,16 +75,28 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n = lane & 15, g4 = lane >> 4;
 
-  prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
-    return (int64_t)blocks_of(r) * (quanta_of(r) + kStart) * a.H;
+  int32_t* weight = reinterpret_cast<int32_t*>(pre + a.B);         // [B] of a unit
+  prefix_requests<kThreads>(a, pre, part, [&](const Request& r, int b) {
+    weight[b] = quanta_of(r, kQuant) + kStart;
+    return (int64_t)blocks_of(r) * weight[b] * a.H;
   });
   const int64_t total = uniform(pre[a.B - 1]);
   const int grid = gridDim.x;
   const int64_t share_q = uniform(divide(total + grid - 1, grid));
-  const int64_t per = share_q > kLeast ? share_q : kLeast;
+  const int64_t per = share_q > kLeast<W> ? share_q : kLeast<W>;
   auto share_of = [&](int64_t q) { return (int)divide(q, per); };
-  int64_t at = (int64_t)blockIdx.x * per;
-  const int64_t end = at + per < total ? at + per : total;
+  // A share ends where its weight does, or at the nearer end of the unit there if that is
+  // small: to split it would cost more, in its second start and the join, than it levels.
+  auto share_end = [&](int64_t x) {
+    if (x >= total) return total;
+    const int b = uniform(find_request(pre, a.B, x));
+    const int64_t in_request = x - (b > 0 ? pre[b - 1] : (int64_t)0), w = weight[b];
+    if (w > kSmall) return x;
+    const int64_t in_unit = in_request - divide(in_request, w) * w;
+    return 2 * in_unit < w ? x - in_unit : x - in_unit + w;
+  };
+  int64_t at = uniform(share_end((int64_t)blockIdx.x * per));
+  const int64_t end = uniform(share_end((int64_t)(blockIdx.x + 1) * per));
   if (at >= end) return;
   int b = uniform(find_request(pre, a.B, at));
 
@@ -100,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
     while (uniform(pre[b]) <= at) ++b;
     const int64_t base = uniform(b > 0 ? pre[b - 1] : (int64_t)0);
     const Request r = request(a, b);
-    const int quanta = quanta_of(r);
+    const int quanta = quanta_of(r, kQuant);
     const int64_t unit = divide(at - base, quanta + kStart);
     const int64_t unit0 = base + unit * (quanta + kStart);     // its first weight
     const int blk = uniform((int)divide(unit, a.H)), h = uniform((int)(unit - (int64_t)blk * a.H));
@@ -319,18 +325,21 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
             (f32x4_t){o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     __syncthreads();
     // thread = (row, 4 channels) from here on, IT of them kThreads / Q rows apart
-    constexpr int Q = D / 4, IT = kRows * Q / kThreads;
+    constexpr int Q = D / 4, STRIDE = kThreads / Q, IT = kRows / STRIDE > 1 ? kRows / STRIDE : 1;
     const int valid = block_last - blk * kRows + 1;                // rows of the block
     const int jr = tid / Q, jc = tid % Q * 4;
     float top[IT], den[IT];
     f32x4_t sum[IT];
 #pragma unroll
     for (int x = 0; x < IT; ++x) {
-      const int at_row = jr + x * (kThreads / Q);
-      top[x] = fmaxf(fmaxf(jm[0][at_row], jm[1][at_row]), fmaxf(jm[2][at_row], jm[3][at_row]));
-      const float ref = top[x] == -INFINITY ? 0.0f : top[x];
+      const int at_row = jr + x * STRIDE;
+      top[x] = -INFINITY;
       den[x] = 0.0f;
       sum[x] = (f32x4_t){0, 0, 0, 0};
+      if (at_row >= valid) continue;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top[x] = fmaxf(top[x], jm[w][at_row]);
+      const float ref = top[x] == -INFINITY ? 0.0f : top[x];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float f = __builtin_amdgcn_exp2f(jm[w][at_row] - ref);   // 0 for a wave that saw nothing; NaN sums stay
@@ -338,9 +347,10 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         sum[x] += f * *reinterpret_cast<const f32x4_t*>(&jo[w][at_row * RS + jc]);
       }
     }
-    // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`
+    // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`; small
+    // units have one
     const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
-    bool done = g0 == g1;
+    bool done = g0 == g1 || quanta + kStart <= kSmall;
     if (!done) {
       const int parts = g1 - g0 + 1, mine_at = (int)blockIdx.x - g0;
       auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
@@ -351,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         float* to = partial + (int64_t)slot(i) * SLOT;
 #pragma unroll
         for (int x = 0; x < IT; ++x) {
-          const int at_row = jr + x * (kThreads / Q);
+          const int at_row = jr + x * STRIDE;
           if (at_row >= valid) break;
           put2(to + at_row * D + jc, sum[x][0], sum[x][1]);
           put2(to + at_row * D + jc + 2, sum[x][2], sum[x][3]);
@@ -391,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         };
         fly(share, 0);
         __syncthreads();                                 // jo, jm and jl have been read
-        {  // 16 lanes a row
+        if (tid < 16 * kRows) {  // 16 lanes a row
           const int row = tid >> 4, sub = tid & 15;
           float2 md[kJoin / 16];
           float most = -INFINITY, l16 = 0.0f;
@@ -431,10 +441,10 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         }
 #pragma unroll
         for (int x = 1; x < IT; ++x)                      // shares == 1 where there are such rows
-          if (jr + x * (kThreads / Q) < valid)
+          if (jr + x * STRIDE < valid)
             for (int i0 = 0; i0 < count; i0 += kFly) {
-              fly(i0, x * (kThreads / Q) * D);
-              add(sum[x], i0, jr + x * (kThreads / Q));
+              fly(i0, x * STRIDE * D);
+              add(sum[x], i0, jr + x * STRIDE);
             }
         if (shares > 1) {
           if (share < shares) across[tid] = sum[0];
@@ -444,8 +454,9 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
         }
 #pragma unroll
         for (int x = 0; x < IT; ++x) {
-          top[x] = jm[0][jr + x * (kThreads / Q)];
-          den[x] = jl[0][jr + x * (kThreads / Q)];
+          if (jr + x * STRIDE >= valid) break;
+          top[x] = jm[0][jr + x * STRIDE];
+          den[x] = jl[0][jr + x * STRIDE];
         }
       };
       put(mine_at);
@@ -467,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
     if (done) {
 #pragma unroll
       for (int x = 0; x < IT; ++x) {
-        const int at_row = jr + x * (kThreads / Q), out_row = blk * kRows + at_row;
+        const int at_row = jr + x * STRIDE, out_row = blk * kRows + at_row;
         if (at_row >= valid) break;
         const int64_t to = (int64_t)(r.row0 + out_row / a.G) * a.H * a.G + h * a.G + out_row % a.G;
         const f32x4_t y = sum[x] * (den[x] == 0.0f ? 0.0f : 1.0f / den[x]);    // no key: 0
@@ -490,25 +501,43 @@ __global__ void __launch_bounds__(kThreads, (kOcc<DT, D>)) attend8_split_kernel(
 #endif
 bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G > (int64_t)B * BR; }
 
+// Few units: one large workgroup a CU, so that a unit has fewer partial sums; many: small
+// ones, whose starts and ends overlap.
+#ifndef FEW
+#define FEW 64
+#endif
+#ifndef FEWK
+#define FEWK 1048576
+#endif
+bool few_units(const AttendArgs& a) {
+  return ((int64_t)a.T * a.G / kRows + a.B) * a.H <= FEW &&
+         (int64_t)a.B * a.H * ((int64_t)a.M << a.log2p) >= FEWK;
+}
+
 }  // namespace
 
 // Counters, and two partial sums for each workgroup's first and last unit.
-size_t attend_ws_bytes(int B, int, int G, int T, int d, int dtype) {
+size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
   if (by_rows(B, G, T, dtype)) return attend_rows_ws_bytes(d);
-  const size_t grid = dtype == 0 ? (d == 64 ? kGrid<0, 64> : kGrid<0, 128>) : (d == 64 ? kGrid<1, 64> : kGrid<1, 128>);
-  return kCounters * sizeof(int) + grid * 2 * kRows * (d + 2) * sizeof(float);
+  return kCounters * sizeof(int) + (size_t)256 * 3 * 2 * kRows * (d + 2) * sizeof(float);
+}
+
+template <int DT, int D, int W>
+static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
+  // no more workgroups than the tables' pages hold quanta for
+  const int64_t keys = (int64_t)a.M << a.log2p, quant = W * kStep;
+  const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
+  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>, fill = 256 * (4 * kOcc<DT, D> / W);
+  int* counters = static_cast<int*>(ws);
+  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W>), dim3((unsigned)(want < fill ? want : fill)), dim3(64 * W),
+                     (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
+  return hipGetLastError();
 }
 
 template <int DT, int D>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  int* counters = static_cast<int*>(ws);
-  // no more workgroups than the tables' pages hold quanta for
-  const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((((int64_t)a.M << a.log2p) + kQuant - 1) / kQuant + kStart);
-  const int64_t want = (most + kLeast - 1) / kLeast;
-  const unsigned grid = want < kGrid<DT, D> ? (unsigned)want : kGrid<DT, D>;
-  hipLaunchKernelGGL((attend8_split_kernel<DT, D>), dim3(grid), dim3(kThreads),
-                     (size_t)a.B * sizeof(int64_t), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
-  return hipGetLastError();
+  return few_units(a) ? launch_split<DT, D, 4 * kOcc<DT, D>>(a, ws, stream)
+                                       : launch_split<DT, D, 4>(a, ws, stream);
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {

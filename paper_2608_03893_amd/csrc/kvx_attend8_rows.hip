@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int step_of = wave & 3;             // the step whose keys (waves 0-3) or values this wave widens
 
-  prefix_requests<kThreads>(a, pre, part, [&](const Request& r) {
+  prefix_requests<kThreads>(a, pre, part, [&](const Request& r, int) {
     return a.H * WT::sum(WT::before(r, a.G), WT::blocks(r));
   });
   const int64_t total = uniform(pre[a.B - 1]);

@@ -48,7 +48,7 @@ struct AttendArgs {
   int32_t B, H, G, T, M, N, log2p;
 };
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream);
-size_t attend_ws_bytes(int B, int H, int G, int T, int d, int dtype);
+size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);
 // Its kernel for many query rows a request (bf16).
 hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream);
 size_t attend_rows_ws_bytes(int d);

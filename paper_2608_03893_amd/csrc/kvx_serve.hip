@@ -222,8 +222,7 @@ static kvx_status check_attend(const kvx_attend_dims* dims, kvx_dtype dtype) {
 
 size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype) {
   if (check_attend(dims, dtype) != KVX_OK || dims->B == 0 || dims->T == 0) return 0;
-  return kvx::attend_ws_bytes(dims->B, dims->H, dims->G, dims->T, dims->d,
-                              dtype == KVX_BF16 ? 0 : 1);
+  return kvx::attend_ws_bytes(dims->B, dims->G, dims->T, dims->d, dtype == KVX_BF16 ? 0 : 1);
 }
 
 kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype,
@@ -244,7 +243,7 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
   if ((st = check_strides("q", q_strides, n, 2, es, m.d, &qb)) != KVX_OK) return st;
   const uint64_t pages = (uint64_t)2 * m.H * pool->num_pages, b4 = (uint64_t)m.B * 4;
   const uint64_t rows = (uint64_t)m.T * m.H * m.G;
-  const uint64_t need = kvx::attend_ws_bytes(m.B, m.H, m.G, m.T, m.d, dt);
+  const uint64_t need = kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt);
   const Span in[] = {{q, qb, "q"},
                      {codes, pages * pool->page_size * m.d, "codes"},
                      {scales, pages * 4, "scales"},
