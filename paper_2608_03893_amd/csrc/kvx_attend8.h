@@ -10,6 +10,13 @@ namespace kvx {
 namespace {
 
 constexpr float kLazy = 8.0f;    // growth of a row's maximum (log2) that is let pass
+constexpr int kXcds = 8;
+// Share of workgroup `block` of `grid` (a multiple of the XCDs, which take workgroups in
+// turn): neighbouring shares on one XCD, whose L2 then serves a head's keys to all of its
+// blocks of rows.
+__device__ __forceinline__ int xcd_order(int block, int grid) {
+  return block % kXcds * (grid / kXcds) + block / kXcds;
+}
 // Arrival counters, first in the workspace (four for each workgroup of the largest grid):
 // all kernels keep them there and leave them at zero, and partial sums behind.
 constexpr int kCounters = 4 * 1024;

@@ -25,16 +25,10 @@ namespace {
 
 constexpr int kStep = 32;                  // keys of a wave's step
 constexpr int kRows = 16;                  // query rows of a block
-#ifndef KLB
-#define KLB 1
-#endif
 template <int W>
-constexpr int kLeast = W > 4 ? KLB : 2;    // least quanta of a workgroup
-#ifndef KSM
-#define KSM 10
-#endif
+constexpr int kLeast = W > 4 ? 1 : 2;      // least quanta of a workgroup
 constexpr int kStart = 2;                  // weight of a unit's start, in quanta
-constexpr int kSmall = KSM;                // most weight of a unit that is not split
+constexpr int kSmall = 10;                 // most weight of a unit that is not split
 constexpr int kJoin = 64;                  // partial sums joined at a time
 constexpr int kFly = 12;                   // of which a thread has these in flight
 // Waves a SIMD: as many as the registers hold.  More of them hide more of a unit's start
@@ -95,8 +89,9 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
     const int64_t in_unit = in_request - divide(in_request, w) * w;
     return 2 * in_unit < w ? x - in_unit : x - in_unit + w;
   };
-  int64_t at = uniform(share_end((int64_t)blockIdx.x * per));
-  const int64_t end = uniform(share_end((int64_t)(blockIdx.x + 1) * per));
+  const int me = xcd_order(blockIdx.x, grid);
+  int64_t at = uniform(share_end(me * per));
+  const int64_t end = uniform(share_end((me + 1) * per));
   if (at >= end) return;
   int b = uniform(find_request(pre, a.B, at));
 
@@ -109,7 +104,8 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
     const int quanta = quanta_of(r, kQuant);
     const int64_t unit = divide(at - base, quanta + kStart);
     const int64_t unit0 = base + unit * (quanta + kStart);     // its first weight
-    const int blk = uniform((int)divide(unit, a.H)), h = uniform((int)(unit - (int64_t)blk * a.H));
+    const int blocks = blocks_of(r);       // of a head, which share its keys: on one XCD mostly
+    const int h = uniform((int)divide(unit, blocks)), blk = uniform((int)(unit - (int64_t)h * blocks));
     const int64_t lo = at - unit0 - kStart, hi = end - unit0 - kStart;
     const int q0 = uniform(lo < 0 ? 0 : (int)lo), q1 = uniform(hi < quanta ? (int)hi : quanta);
     if (q0 >= q1) {      // only its start
@@ -352,7 +348,7 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
     const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
     bool done = g0 == g1 || quanta + kStart <= kSmall;
     if (!done) {
-      const int parts = g1 - g0 + 1, mine_at = (int)blockIdx.x - g0;
+      const int parts = g1 - g0 + 1, mine_at = me - g0;
       auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
       // Partial sums pass between workgroups on different XCDs, each with its own L2: they
       // are written through and read past it (agent scope), which spares the write-back
@@ -495,31 +491,38 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
   }
 }
 
-// Which kernel: many rows a request share the widened codes over eight waves.
-#ifndef BR
-#define BR 32
-#endif
-bool by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G > (int64_t)B * BR; }
+// Which kernel.  By rows (bf16 only), blocks of 256 rows share the widened codes, which pays
+// where requests bring 64 rows or more on average and there is work enough to fill the
+// chip with such blocks: 2^32 / d pairs of a query row and a key, by the tables' length.
+// Measured, us, split / by rows, 8 KV heads, B requests of n new tokens after `old`:
+//   d = 128  B = 64, old 1000   G = 8, n = 4: 42 / 56    n = 8: 70 / 59     n = 64: 566 / 189
+//            B = 8,  old 1000   G = 8, n = 16: 25 / 38   n = 32: 44 / 58    n = 64: 72 / 53
+//            B = 8,  old 8000   G = 8, n = 8: 63 / 67    n = 16: 118 / 76
+//            B = 1,  old 5000   G = 8, n = 64: 44 / 55   n = 128: 77 / 62
+//   d = 64   B = 64, old 1000   G = 8, n = 8: 41 / 47    n = 16: 71 / 50
+//            B = 1,  old 5000   G = 8, n = 128: 42 / 42
+bool may_go_by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G >= (int64_t)B * 64; }
+bool by_rows(const AttendArgs& a, int dtype, int d) {
+  const double pairs = (double)a.T * a.G * a.H * ((int64_t)a.M << a.log2p);
+  return may_go_by_rows(a.B, a.G, a.T, dtype) && pairs * d >= 4294967296.0;
+}
 
-// Few units: one large workgroup a CU, so that a unit has fewer partial sums; many: small
-// ones, whose starts and ends overlap.
-#ifndef FEW
-#define FEW 64
-#endif
-#ifndef FEWK
-#define FEWK 1048576
-#endif
+// One large workgroup a CU, so that a unit has fewer partial sums, where few units span
+// much cache (4096 keys a CU by the tables' length): a few contexts of some 100000 keys 104
+// -> 90 us.  Elsewhere small ones, whose starts and ends overlap: 512 requests of 100
+// keys 37 us against 64.
 bool few_units(const AttendArgs& a) {
-  return ((int64_t)a.T * a.G / kRows + a.B) * a.H <= FEW &&
-         (int64_t)a.B * a.H * ((int64_t)a.M << a.log2p) >= FEWK;
+  return ((int64_t)a.T * a.G / kRows + a.B) * a.H <= 64 &&
+         (int64_t)a.B * a.H * ((int64_t)a.M << a.log2p) >= 256 * 4096;
 }
 
 }  // namespace
 
 // Counters, and two partial sums for each workgroup's first and last unit.
 size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
-  if (by_rows(B, G, T, dtype)) return attend_rows_ws_bytes(d);
-  return kCounters * sizeof(int) + (size_t)256 * 3 * 2 * kRows * (d + 2) * sizeof(float);
+  const size_t split = kCounters * sizeof(int) + (size_t)256 * 3 * 2 * kRows * (d + 2) * sizeof(float);
+  const size_t rows = may_go_by_rows(B, G, T, dtype) ? attend_rows_ws_bytes(d) : 0;
+  return split > rows ? split : rows;
 }
 
 template <int DT, int D, int W>
@@ -529,7 +532,8 @@ static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream
   const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
   const int64_t want = (most + kLeast<W> - 1) / kLeast<W>, fill = 256 * (4 * kOcc<DT, D> / W);
   int* counters = static_cast<int*>(ws);
-  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W>), dim3((unsigned)(want < fill ? want : fill)), dim3(64 * W),
+  const unsigned grid = (unsigned)((want < fill ? want : fill) + kXcds - 1) / kXcds * kXcds;
+  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W>), dim3(grid), dim3(64 * W),
                      (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
   return hipGetLastError();
 }
@@ -541,7 +545,7 @@ static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
-  if (by_rows(a.B, a.G, a.T, dtype)) return launch_attend_rows(a, d, ws, stream);
+  if (by_rows(a, dtype, d)) return launch_attend_rows(a, d, ws, stream);
   if (dtype == 0) return d == 64 ? launch_split<0, 64>(a, ws, stream) : launch_split<0, 128>(a, ws, stream);
   return d == 64 ? launch_split<1, 64>(a, ws, stream) : launch_split<1, 128>(a, ws, stream);
 }

@@ -22,15 +22,7 @@ namespace {
 constexpr int kThreads = 512, kWaves = 8;
 constexpr int kSteps = 4, kStep = 32, kQuant = kSteps * kStep;
 constexpr int kGrid = 256;                 // workgroups: one per CU
-constexpr int kXcds = 8;
-#ifndef RING
-#define RING 4
-#endif
-constexpr int kRing = RING;                   // operands on their way from LDS
-#ifndef KL
-#define KL 1
-#endif
-constexpr int kLeast = KL;
+constexpr int kRing = 4;                   // operands on their way from LDS
 
 // Codes 2 HALF and 2 HALF + 1 of a word times a power of two, as bf16.
 template <bool HALF>
@@ -74,10 +66,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   });
   const int64_t total = uniform(pre[a.B - 1]);
   int64_t per = uniform((total + kGrid - 1) / kGrid);
-  const int64_t least = (int64_t)a.G * kLeast;
-  per = per > least ? per : least;
-  const int me = (blockIdx.x % kXcds) * (kGrid / kXcds) + blockIdx.x / kXcds;   // share `me`
-  int64_t at = uniform(me * per);
+  per = per > a.G ? per : a.G;      // a quantum at least
+  const int me = xcd_order(blockIdx.x, kGrid);
+  int64_t at = uniform((int64_t)me * per);
   const int64_t end = uniform(at + per < total ? at + per : total);
   if (at >= end) return;
   int b = uniform(find_request(pre, a.B, at));
