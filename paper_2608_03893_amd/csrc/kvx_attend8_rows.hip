@@ -51,8 +51,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   constexpr int SLOT = kWaves * NB * (4 * C + 2) * 64;            // floats of a partial sum
   __shared__ __attribute__((aligned(16))) u32x4_t kv[2][kSteps][F][64];
   __shared__ float ksc[2][kSteps][2];       // scale of the scores of a 16-key tile
-  __shared__ int kbad[2][kSteps];           // bit t: tile t has no page
-  __shared__ int vnan[2][kSteps];           // some value is NaN (where rows differ in what they see)
+  // [0], bit t: tile t has no page; [1]: some value is NaN (where rows of the block differ
+  // in what they see)
+  __shared__ int flags[2][kSteps][2];
   __shared__ uint32_t nans[2][kSteps][U][64];   // which
   __shared__ int64_t part[kWaves];
   __shared__ int last;
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
         if (lane == 0) {
           ksc[buf][step_of][0] = s0 * a.scale_log2;
           ksc[buf][step_of][1] = s1 * a.scale_log2;
-          kbad[buf][step_of] = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
+          flags[buf][step_of][0] = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
         }
       } else {
         bool nan = false;
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
           }
         }
         nan = __any(nan);
-        if (lane == 0) vnan[buf][step_of] = nan;
+        if (lane == 0) flags[buf][step_of][1] = nan;
         if (nan) {      // kept apart where rows differ in what they see: bit 4 j + i is key j, byte i
 #pragma unroll
           for (int w = 0; w < U; ++w) {
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll 1
       for (int s = 0; s < kSteps && key <= lim_hi; ++s, key += kStep) {
         const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};
-        const int bad = uniform(kbad[buf][s]);
+        const int bad = uniform(flags[buf][s][0]), nan = uniform(flags[buf][s][1]);
         const u32x4_t* next = s + 1 < kSteps ? from + F * 64 : from;   // the last step's are not used
         f32x4_t x[2][NB];
 #pragma unroll
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
         }
         __builtin_amdgcn_sched_barrier(0);
         // exponents: scores less the row's reference
-        const bool masked = bad != 0 || key + kStep - 1 > lim_lo;
+        const bool masked = (bad | nan) != 0 || key + kStep - 1 > lim_lo;
         bool grown = false;
         float top[NB];
 #pragma unroll
@@ -312,6 +313,29 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[t][i][e] = e > most ? -INFINITY : x[t][i][e];
             }
+          // NaN values count only in rows that see their key
+          if (nan != 0) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              u32x4_t w;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                w[j] = (x[j >> 1][i][2 * (j & 1)] == -INFINITY ? 0u : 0x3f80u) |
+                       (x[j >> 1][i][2 * (j & 1) + 1] == -INFINITY ? 0u : 0x3f800000u);
+              const bf16x8_t seen = __builtin_bit_cast(bf16x8_t, w);
+#pragma unroll
+              for (int c = 0; c < C; ++c) {
+                const uint32_t bits = nans[buf][s][c / 4][lane] >> (c % 4);   // bit 4 j: key j of channel c
+                u32x4_t hit;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  hit[j] = (bits >> (8 * j) & 1) * 0x3f80u | (bits >> (8 * j + 4) & 1) * 0x3f800000u;
+                const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), seen, (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][c][e] = count[e] != 0.0f ? __builtin_nanf("") : o[i][c][e];
+              }
+            }
+          }
         }
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -334,29 +358,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             for (int c = 0; c < C; ++c) o[i][c] *= keep;
 #pragma unroll
             for (int t = 0; t < 2; ++t) x[t][i] += shift;
-          }
-        }
-        // NaN values count only in rows that see their key
-        if (masked && uniform(vnan[buf][s]) != 0) {
-#pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            u32x4_t w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              w[j] = (x[j >> 1][i][2 * (j & 1)] == -INFINITY ? 0u : 0x3f80u) |
-                     (x[j >> 1][i][2 * (j & 1) + 1] == -INFINITY ? 0u : 0x3f800000u);
-            const bf16x8_t seen = __builtin_bit_cast(bf16x8_t, w);
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-              const uint32_t bits = nans[buf][s][c / 4][lane] >> (c % 4);   // bit 4 j: key j of channel c
-              u32x4_t hit;
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                hit[j] = (bits >> (8 * j) & 1) * 0x3f80u | (bits >> (8 * j + 4) & 1) * 0x3f800000u;
-              const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), seen, (f32x4_t){0, 0, 0, 0});
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][c][e] = count[e] != 0.0f ? __builtin_nanf("") : o[i][c][e];
-            }
           }
         }
         bf16x8_t p[NB];
