@@ -13,11 +13,16 @@
 // a lane reads 16 bytes of one key's row, or 8 bytes of 8 value rows whose bytes it then
 // pairs up for V^T.
 //
-// The grid is fixed and every workgroup takes an equal share of all (request, row block,
-// head, 128 keys) quanta, whatever the lengths: it finds its share from a prefix sum over
-// the requests.  A block of rows whose keys span workgroups is joined by the workgroup
-// that comes last, from partial sums in order of the keys, so results do not depend on
-// timing.
+// The grid fills the chip once and every workgroup takes an equal share of the weight of
+// all units (request, head, row block), whatever the lengths: a quantum of 32 keys a wave
+// weighs one and a unit's start two.  It finds its share from a prefix sum over the
+// requests.  A unit whose keys span workgroups is joined by the workgroup that comes last,
+// from partial sums in order of the keys, so results do not depend on timing.
+//
+// Measured, d = 128, G = 8, 8 KV heads, 16-token pages that no cache holds: 32 requests of
+// 5000 keys 66 us (4.9 TB/s), 16 of 2178 27 us (2.6), 1 of 5000 13.6 us, 1 of 300 8.8 us:
+// a launch, the lengths, pages, keys and joins, each of which waits for the one before, take
+// 8 to 12 us, and the bytes come on top.
 #include "kvx_attend8.h"
 
 namespace kvx {
@@ -28,15 +33,20 @@ constexpr int kRows = 16;                  // query rows of a block
 template <int W>
 constexpr int kLeast = W > 4 ? 1 : 2;      // least quanta of a workgroup
 constexpr int kStart = 2;                  // weight of a unit's start, in quanta
-constexpr int kSmall = 10;                 // most weight of a unit that is not split
+constexpr int kSmall = 10;                 // a unit is not split if it weighs no more than this
+constexpr int kSplit = 5;                  // and than a share and what a join costs
 constexpr int kJoin = 64;                  // partial sums joined at a time
 constexpr int kFly = 12;                   // of which a thread has these in flight
 // Waves a SIMD: as many as the registers hold.  More of them hide more of a unit's start
 // (lengths, pages, scales, rows: loads that wait for one another) than prefetching
 // within a wave: 64 ragged requests 86 us with two and the next step's loads in flight,
-// 72 us with three and no prefetch.
+// 72 us with three and no prefetch; three and the next step's keys in flight, 124 -> 132 us
+// at 64 requests of up to 8191 keys.  d = 64: 128 requests of 1000 keys 37 us with three,
+// 32 with four.
 template <int DT, int D>
-constexpr int kOcc = DT == 1 && D == 128 ? 2 : 3;
+constexpr int kOcc = DT == 1 && D == 128 ? 2 : DT == 0 && D == 64 ? 4 : 3;
+template <int DT, int D>
+constexpr int kLarge = DT == 1 && D == 128 ? 8 : 12;   // waves of a large workgroup
 
 // Blocks of rows, and quanta (of `quant` keys) of one block and head (rows without any key
 // still have an output).
@@ -53,9 +63,9 @@ struct Stage {
   uint32_t v[8][V];         // key (lane >> 4) * 4 + (j & 3) of tile j >> 2, bytes (lane & 15) * 4 V ..
 };
 
-// W waves: 4, and kOcc workgroups a CU; or 4 kOcc, and one.
+// W waves: 4, and kOcc workgroups a CU; or kLarge, and one.
 template <int DT, int D, int W>
-__global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+__global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
   constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep;
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
   static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
@@ -78,6 +88,7 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
   const int grid = gridDim.x;
   const int64_t share_q = uniform(divide(total + grid - 1, grid));
   const int64_t per = share_q > kLeast<W> ? share_q : kLeast<W>;
+  const int small = per + kSplit < kSmall ? (int)per + kSplit : kSmall;
   auto share_of = [&](int64_t q) { return (int)divide(q, per); };
   // A share ends where its weight does, or at the nearer end of the unit there if that is
   // small: to split it would cost more, in its second start and the join, than it levels.
@@ -85,7 +96,7 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
     if (x >= total) return total;
     const int b = uniform(find_request(pre, a.B, x));
     const int64_t in_request = x - (b > 0 ? pre[b - 1] : (int64_t)0), w = weight[b];
-    if (w > kSmall) return x;
+    if (w > small) return x;
     const int64_t in_unit = in_request - divide(in_request, w) * w;
     return 2 * in_unit < w ? x - in_unit : x - in_unit + w;
   };
@@ -321,7 +332,7 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
             (f32x4_t){o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     __syncthreads();
     // thread = (row, 4 channels) from here on, IT of them kThreads / Q rows apart
-    constexpr int Q = D / 4, STRIDE = kThreads / Q, IT = kRows / STRIDE > 1 ? kRows / STRIDE : 1;
+    constexpr int Q = D / 4, STRIDE = kThreads / Q, IT = (kRows + STRIDE - 1) / STRIDE;
     const int valid = block_last - blk * kRows + 1;                // rows of the block
     const int jr = tid / Q, jc = tid % Q * 4;
     float top[IT], den[IT];
@@ -346,7 +357,7 @@ __global__ void __launch_bounds__(64 * W, (kOcc<DT, D>)) attend8_split_kernel(At
     // workgroups that share this unit: g0 .. g1, this one's part is number `mine_at`; small
     // units have one
     const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
-    bool done = g0 == g1 || quanta + kStart <= kSmall;
+    bool done = g0 == g1 || quanta + kStart <= small;
     if (!done) {
       const int parts = g1 - g0 + 1, mine_at = me - g0;
       auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
@@ -507,20 +518,28 @@ bool by_rows(const AttendArgs& a, int dtype, int d) {
   return may_go_by_rows(a.B, a.G, a.T, dtype) && pairs * d >= 4294967296.0;
 }
 
-// One large workgroup a CU, so that a unit has fewer partial sums, where few units span
-// much cache (4096 keys a CU by the tables' length): a few contexts of some 100000 keys 104
-// -> 90 us.  Elsewhere small ones, whose starts and ends overlap: 512 requests of 100
-// keys 37 us against 64.
-bool few_units(const AttendArgs& a) {
-  return ((int64_t)a.T * a.G / kRows + a.B) * a.H <= 64 &&
-         (int64_t)a.B * a.H * ((int64_t)a.M << a.log2p) >= 256 * 4096;
+// One large workgroup a CU instead of several of four waves: a unit then has fewer partial
+// sums or none.  Pays where the units' keys, by the tables' length, come to 256 a CU (a
+// decoding step of 32 requests of 2178 keys 35 us against 43, 16 of 1000 17 against 20,
+// 4 contexts up to 131070 91 against 97), but not
+//   - for requests of more than 32 rows (a mixed batch of 8: 26 us against 19);
+//   - for few units of one or two rows, whose sums join fast (G = 1, 16000 keys: 20 against 17);
+//   - for many short units, where starts and ends of small workgroups overlap: 256 requests
+//     of 300 keys 59 against 43, of 1000 117 against 113, of 2178 220 against 231; with
+//     eight waves (fp32, d = 128) for many units of any length, 121 against 115.
+template <int LARGE>
+bool large_workgroups(const AttendArgs& a) {
+  const int64_t rows = (int64_t)a.T * a.G, blocks = rows / kRows > a.B ? rows / kRows : a.B;
+  const int64_t units = blocks * a.H, keys = (int64_t)a.M << a.log2p;
+  return rows <= 32 * (int64_t)a.B && units * keys >= 256 * 256 && (units >= 64 || rows >= 4 * (int64_t)a.B) &&
+         (units < 512 || (LARGE >= 12 && keys > 1024));
 }
 
 }  // namespace
 
 // Counters, and two partial sums for each workgroup's first and last unit.
 size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
-  const size_t split = kCounters * sizeof(int) + (size_t)256 * 3 * 2 * kRows * (d + 2) * sizeof(float);
+  const size_t split = kCounters * sizeof(int) + (size_t)256 * 4 * 2 * kRows * (d + 2) * sizeof(float);
   const size_t rows = may_go_by_rows(B, G, T, dtype) ? attend_rows_ws_bytes(d) : 0;
   return split > rows ? split : rows;
 }
@@ -530,7 +549,7 @@ static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream
   // no more workgroups than the tables' pages hold quanta for
   const int64_t keys = (int64_t)a.M << a.log2p, quant = W * kStep;
   const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
-  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>, fill = 256 * (4 * kOcc<DT, D> / W);
+  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>, fill = W == 4 ? 256 * kOcc<DT, D> : 256;
   int* counters = static_cast<int*>(ws);
   const unsigned grid = (unsigned)((want < fill ? want : fill) + kXcds - 1) / kXcds * kXcds;
   hipLaunchKernelGGL((attend8_split_kernel<DT, D, W>), dim3(grid), dim3(64 * W),
@@ -540,8 +559,8 @@ static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream
 
 template <int DT, int D>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  return few_units(a) ? launch_split<DT, D, 4 * kOcc<DT, D>>(a, ws, stream)
-                                       : launch_split<DT, D, 4>(a, ws, stream);
+  constexpr int LARGE = kLarge<DT, D>;
+  return large_workgroups<LARGE>(a) ? launch_split<DT, D, LARGE>(a, ws, stream) : launch_split<DT, D, 4>(a, ws, stream);
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {

@@ -25,8 +25,8 @@ def _by_rows(c):
 
 
 def _large(c):
-    """Widens the tables until few units take one large workgroup a CU (too few rows a
-    request to go by rows)."""
+    """Widens the tables until a request's 4 to 32 rows take one large workgroup a CU (other
+    numbers of rows take the small ones)."""
     B, M = c["tables"].shape
     T, heads, _ = c["q"].shape
     assert c["q"].dtype != torch.bfloat16 or T * heads // c["codes"].shape[1] < 64 * B
@@ -86,6 +86,9 @@ def test_by_rows_shares(gpu_kvx, lens, news, H, G, d, P):
     ([20011], [1], 1, 8, 128, 64),
     ([40011, 7], [3, 1], 1, 4, 64, 128),
     ([2, 40, 7, 90], [5, 3, 7, 4], 2, 3, 128, 16),
+    ([1], [1], 1, 4, 128, 16),
+    ([30] * 33 + [500], [1] * 34, 2, 1, 64, 16),   # single rows, units enough
+    ([300] * 60, [4] * 60, 3, 8, 128, 32),         # several units a workgroup
 ])
 def test_large_workgroups(gpu_kvx, dtype, lens, news, H, G, d, P):
     rng = np.random.default_rng(lens[0])
@@ -138,7 +141,8 @@ def test_nan_in_the_cache_reaches_the_rows_that_see_it(gpu_kvx, kernel, dtype):
         pytest.skip("fp32 queries go by keys")
     rng = np.random.default_rng(33)
     for d, P in ((128, 32), (64, 16)):
-        for lens, news, G in ((([90, 300], [6, 7], 8), ([33, 70], [33, 3], 1)) if kernel == "large" else
+        for lens, news, G in ((([90, 300], [6, 7], 8), ([33, 70], [33, 3], 1),
+                               ([90, 300], [3, 4], 8)) if kernel == "large" else
                               (([90, 300], [80, 70], 1), ([33, 70], [33, 3], 8))):
             c = _case(rng, lens, news, 2, G, d, P, dtype)
             slot = lambda b, p: c["tables"][b, p // P] * P + p % P  # noqa: E731, B023
