@@ -29,28 +29,29 @@ namespace kvx {
 namespace {
 
 constexpr int kStep = 32;                  // keys of a wave's step
-constexpr int kRows = 16;                  // query rows of a block
 template <int W>
 constexpr int kLeast = W > 4 ? 1 : 2;      // least quanta of a workgroup
 constexpr int kStart = 2;                  // weight of a unit's start, in quanta
 constexpr int kSmall = 10;                 // a unit is not split if it weighs no more than this
 constexpr int kSplit = 5;                  // and than a share and what a join costs
 constexpr int kJoin = 64;                  // partial sums joined at a time
-constexpr int kFly = 12;                   // of which a thread has these in flight
+template <int NB>
+constexpr int kFlying = NB == 2 ? 8 : 12;  // of which a thread has these in flight
 // Waves a SIMD: as many as the registers hold.  More of them hide more of a unit's start
 // (lengths, pages, scales, rows: loads that wait for one another) than prefetching
 // within a wave: 64 ragged requests 86 us with two and the next step's loads in flight,
 // 72 us with three and no prefetch; three and the next step's keys in flight, 124 -> 132 us
 // at 64 requests of up to 8191 keys.  d = 64: 128 requests of 1000 keys 37 us with three,
 // 32 with four.
-template <int DT, int D>
-constexpr int kOcc = DT == 1 && D == 128 ? 2 : DT == 0 && D == 64 ? 4 : 3;
-template <int DT, int D>
-constexpr int kLarge = DT == 1 && D == 128 ? 8 : 12;   // waves of a large workgroup
+template <int DT, int D, int NB>
+constexpr int kOcc = D == 64 ? 5 - NB : DT == 1 ? 2 : 4 - NB;
+template <int DT, int D, int NB>
+constexpr int kLarge = kOcc<DT, D, NB> > 2 ? 12 : 8;   // waves of a large workgroup
 
 // Blocks of rows, and quanta (of `quant` keys) of one block and head (rows without any key
 // still have an output).
-__device__ __forceinline__ int blocks_of(const Request& r) { return (r.rows + kRows - 1) / kRows; }
+template <int R>
+__device__ __forceinline__ int blocks_of(const Request& r) { return (r.rows + R - 1) / R; }
 __device__ __forceinline__ int quanta_of(const Request& r, int quant) {
   return r.len > quant ? (int)(((int64_t)r.len + quant - 1) / quant) : 1;
 }
@@ -64,9 +65,10 @@ struct Stage {
 };
 
 // W waves: 4, and kOcc workgroups a CU; or kLarge, and one.
-template <int DT, int D, int W>
-__global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
-  constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep;
+template <int DT, int D, int W, int NB>
+__global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
+  constexpr int kFly = kFlying<NB>;
+  constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep, kRows = 16 * NB;
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
   static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
   constexpr int RS = D + 4;                                        // row stride in LDS
@@ -82,7 +84,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
   int32_t* weight = reinterpret_cast<int32_t*>(pre + a.B);         // [B] of a unit
   prefix_requests<kThreads>(a, pre, part, [&](const Request& r, int b) {
     weight[b] = quanta_of(r, kQuant) + kStart;
-    return (int64_t)blocks_of(r) * weight[b] * a.H;
+    return (int64_t)blocks_of<kRows>(r) * weight[b] * a.H;
   });
   const int64_t total = uniform(pre[a.B - 1]);
   const int grid = gridDim.x;
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
     const int quanta = quanta_of(r, kQuant);
     const int64_t unit = divide(at - base, quanta + kStart);
     const int64_t unit0 = base + unit * (quanta + kStart);     // its first weight
-    const int blocks = blocks_of(r);       // of a head, which share its keys: on one XCD mostly
+    const int blocks = blocks_of<kRows>(r);       // of a head, which share its keys: on one XCD mostly
     const int h = uniform((int)divide(unit, blocks)), blk = uniform((int)(unit - (int64_t)h * blocks));
     const int64_t lo = at - unit0 - kStart, hi = end - unit0 - kStart;
     const int q0 = uniform(lo < 0 ? 0 : (int)lo), q1 = uniform(hi < quanta ? (int)hi : quanta);
@@ -127,35 +129,44 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
     // this lane's query row (the block's last one again past the end): its keys' limit, its
     // channels
     const int block_last = (blk + 1) * kRows < r.rows ? (blk + 1) * kRows - 1 : r.rows - 1;
-    const int row = blk * kRows + n < block_last ? blk * kRows + n : block_last;
-    const int token = row / a.G, head = h * a.G + row % a.G;
-    const int lim = r.len - r.tokens + token;                              // last key it sees
+    int lim[NB];                                                           // last key a row sees
     const int lim_lo = uniform(r.len - r.tokens + blk * kRows / a.G);      // least and largest
     const int lim_hi = uniform(r.len - r.tokens + block_last / a.G);       // of the block
-    bf16x8_t qf[2 * U][TERMS];
+    bf16x8_t qf[NB][2 * U][TERMS];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int i = 0; i < NB; ++i) {
+      const int at_row = blk * kRows + 16 * i + n, row = at_row < block_last ? at_row : block_last;
+      const int token = row / a.G, head = h * a.G + row % a.G;
+      lim[i] = r.len - r.tokens + token;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const int64_t off = (int64_t)(r.row0 + token) * a.q_stride[0] + (int64_t)head * a.q_stride[1] +
-                            64 * u + 16 * g4 + 8 * w;
-        if (DT == 0) {
-          qf[2 * u + w][0] = as_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + off));
-        } else {
-          const float4 lo = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
-          const float4 hi = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off + 4);
-          const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-          split_terms<TERMS>(x, qf[2 * u + w]);
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int64_t off = (int64_t)(r.row0 + token) * a.q_stride[0] + (int64_t)head * a.q_stride[1] +
+                              64 * u + 16 * g4 + 8 * w;
+          if (DT == 0) {
+            qf[i][2 * u + w][0] = as_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + off));
+          } else {
+            const float4 lo = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
+            const float4 hi = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off + 4);
+            const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            split_terms<TERMS>(x, qf[i][2 * u + w]);
+          }
         }
-      }
+    }
 
     const uint8_t* kc = a.codes + h * plane;
     const uint8_t* vc = a.codes + (a.H + h) * plane;
     const uint32_t k_lane = (uint32_t)n * D + 16 * g4, v_lane = (uint32_t)g4 * 4 * D + n * (D / 16);
-    float m = -INFINITY, l = 0.0f;
-    f32x4_t o[C];
+    float m[NB], l[NB];
+    f32x4_t o[NB][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = (f32x4_t){0, 0, 0, 0};
+    for (int i = 0; i < NB; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[i][c] = (f32x4_t){0, 0, 0, 0};
+    }
 
     // pages of this wave's next 32 steps: lane 2 s + t has tile t of step s
     for (int qa = q0; qa < q1; qa += 32) {
@@ -196,22 +207,28 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
       };
       auto compute = [&](Stage<D>& s, int q) {
         const int key = q * kQuant + wave * kStep;
-        float x[8];
+        float x[NB][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          f32x4_t acc = {0, 0, 0, 0};
+          f32x4_t acc[NB];
+#pragma unroll
+          for (int i = 0; i < NB; ++i) acc[i] = (f32x4_t){0, 0, 0, 0};
 #pragma unroll
           for (int u = 0; u < U; ++u) {
             const bf16x8_t k0 = bf16_octet(s.k[t][u].x, s.k[t][u].y), k1 = bf16_octet(s.k[t][u].z, s.k[t][u].w);
 #pragma unroll
-            for (int e = 0; e < TERMS; ++e) {
-              acc = mfma(k0, qf[2 * u][e], acc);
-              acc = mfma(k1, qf[2 * u + 1][e], acc);
-            }
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) {
+                acc[i] = mfma(k0, qf[i][2 * u][e], acc[i]);
+                acc[i] = mfma(k1, qf[i][2 * u + 1][e], acc[i]);
+              }
           }
           const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ksc), 2 * (q - qa) + t));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[4 * t + i] = acc[i] * sc;
+          for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][4 * t + e] = acc[i][e] * sc;
         }
         const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa));
         const int p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
@@ -221,41 +238,47 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
           bool nan = false;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const int first = key + 16 * t + 4 * g4;      // this lane's first key; seen, real: its last
-            const int seen = (t ? p1 : p0) < 0 ? -1 : lim - first, real = (t ? p1 : p0) < 0 ? -1 : r.len - 1 - first;
+            const int first = key + 16 * t + 4 * g4;      // this lane's first key; real, seen: its last
+            const int real = (t ? p1 : p0) < 0 ? -1 : r.len - 1 - first;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = 4 * t + e;
-              x[j] = e > seen ? -INFINITY : x[j];
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
               for (int w = 0; w < U; ++w) {
-                s.v[j][w] = e > real ? 0 : s.v[j][w];     // nobody's codes
-                nan |= e4m3_nan(s.v[j][w]) != 0;
+                s.v[4 * t + e][w] = e > real ? 0 : s.v[4 * t + e][w];     // nobody's codes
+                nan |= e4m3_nan(s.v[4 * t + e][w]) != 0;
               }
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const int seen = (t ? p1 : p0) < 0 ? -1 : lim[i] - first;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[i][4 * t + e] = e > seen ? -INFINITY : x[i][4 * t + e];
             }
           }
           if (__any(nan)) {
             // NaN values count only in rows that see their key: they leave the product, and
             // go into the sums of the rows for which a product of marks finds one
-            u32x4_t m8;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              m8[j] = (x[2 * j] == -INFINITY ? 0u : 0x3f80u) | (x[2 * j + 1] == -INFINITY ? 0u : 0x3f800000u);
-            const bf16x8_t sees = __builtin_bit_cast(bf16x8_t, m8);
+            for (int i = 0; i < NB; ++i) {
+              u32x4_t m8;
 #pragma unroll
-            for (int w = 0; w < U; ++w)
+              for (int j = 0; j < 4; ++j)
+                m8[j] = (x[i][2 * j] == -INFINITY ? 0u : 0x3f80u) | (x[i][2 * j + 1] == -INFINITY ? 0u : 0x3f800000u);
+              const bf16x8_t sees = __builtin_bit_cast(bf16x8_t, m8);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                u32x4_t hit;
+              for (int w = 0; w < U; ++w)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  hit[j] = (e4m3_nan(s.v[2 * j][w]) >> (8 * c + 7) & 1) * 0x3f80u |
-                           (e4m3_nan(s.v[2 * j + 1][w]) >> (8 * c + 7) & 1) * 0x3f800000u;
-                const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), sees, (f32x4_t){0, 0, 0, 0});
+                for (int c = 0; c < 4; ++c) {
+                  u32x4_t hit;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  o[4 * w + c][i] = count[i] != 0.0f ? __builtin_nanf("") : o[4 * w + c][i];
-              }
+                  for (int j = 0; j < 4; ++j)
+                    hit[j] = (e4m3_nan(s.v[2 * j][w]) >> (8 * c + 7) & 1) * 0x3f80u |
+                             (e4m3_nan(s.v[2 * j + 1][w]) >> (8 * c + 7) & 1) * 0x3f800000u;
+                  const f32x4_t count = mfma(__builtin_bit_cast(bf16x8_t, hit), sees, (f32x4_t){0, 0, 0, 0});
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    o[i][4 * w + c][e] = count[e] != 0.0f ? __builtin_nanf("") : o[i][4 * w + c][e];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -265,28 +288,40 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
         // The reference of the exponentials follows the maximum only when that has
         // grown by 2^8: the sums hold that, no lane has to ask the others in most
         // steps, and O is seldom rescaled.
-        float top = x[0];
+        float top[NB];
+        bool grown = false;
 #pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-        if (__any(top > m + kLazy)) {
-          const float now = fmaxf(m, quad_max(top));
-          const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-          m = now;
-          l *= keep;
+        for (int i = 0; i < NB; ++i) {
+          top[i] = x[i][0];
 #pragma unroll
-          for (int c = 0; c < C; ++c) o[c] *= keep;
+          for (int j = 1; j < 8; ++j) top[i] = fmaxf(top[i], x[i][j]);
+          grown |= top[i] > m[i] + kLazy;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float p[8];
+        if (__any(grown)) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[j] = __builtin_amdgcn_exp2f(x[j] - ref);
-          l += p[j];
+          for (int i = 0; i < NB; ++i) {
+            const float now = fmaxf(m[i], quad_max(top[i]));
+            const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[i] - now);
+            m[i] = now;
+            l[i] *= keep;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[i][c] *= keep;
+          }
         }
+        bf16x8_t pf[NB][TERMS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] *= j < 4 ? v0 : v1;
-        bf16x8_t pf[TERMS];
-        split_terms<TERMS>(p, pf);
+        for (int i = 0; i < NB; ++i) {
+          const float ref = m[i] == -INFINITY ? 0.0f : m[i];
+          float p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(x[i][j] - ref);
+            l[i] += p[j];
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] *= j < 4 ? v0 : v1;
+          split_terms<TERMS>(p, pf[i]);
+        }
 #pragma unroll
         for (int w = 0; w < U; ++w) {
           uint32_t y[4][2];   // pairs of keys: bytes (c, c), (c + 1, c + 1) | the next two channels
@@ -302,8 +337,10 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
             for (int j = 0; j < 4; ++j)
               f[j] = c & 1 ? bf16_pair<true>(y[j][c >> 1]) : bf16_pair<false>(y[j][c >> 1]);
 #pragma unroll
-            for (int e = 0; e < TERMS; ++e)
-              o[4 * w + c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[e], o[4 * w + c]);
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e)
+                o[i][4 * w + c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[i][e], o[i][4 * w + c]);
           }
         }
       };
@@ -318,23 +355,29 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
       }
     }
 
-    // the four waves' sums: lane (n, g4) has of row n the channels (4 g4 + i) C + c
-    l = quad_sum(l);
-    if (g4 == 0) {
-      jm[wave][n] = m;
-      jl[wave][n] = l;
+    // the waves' sums: lane (n, g4) has of row 16 i + n the channels (4 g4 + e) C + c
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const float sum16 = quad_sum(l[i]);
+      if (g4 == 0) {
+        jm[wave][16 * i + n] = m[i];
+        jl[wave][16 * i + n] = sum16;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < C; c += 4)
+          *reinterpret_cast<f32x4_t*>(&jo[wave][(16 * i + n) * RS + (4 * g4 + e) * C + c]) =
+              (f32x4_t){o[i][c][e], o[i][c + 1][e], o[i][c + 2][e], o[i][c + 3][e]};
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < C; c += 4)
-        *reinterpret_cast<f32x4_t*>(&jo[wave][n * RS + (4 * g4 + i) * C + c]) =
-            (f32x4_t){o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     __syncthreads();
-    // thread = (row, 4 channels) from here on, IT of them kThreads / Q rows apart
+    // thread = (row, 4 channels) from here on, IT of them kThreads / Q rows apart (its number
+    // again, opaquely: what depends on it would be held in registers through the loop above)
+    int at_thread = tid;
+    asm volatile("" : "+v"(at_thread));
     constexpr int Q = D / 4, STRIDE = kThreads / Q, IT = (kRows + STRIDE - 1) / STRIDE;
     const int valid = block_last - blk * kRows + 1;                // rows of the block
-    const int jr = tid / Q, jc = tid % Q * 4;
+    const int jr = at_thread / Q, jc = at_thread % Q * 4;
     float top[IT], den[IT];
     f32x4_t sum[IT];
 #pragma unroll
@@ -382,10 +425,10 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
         float* weight = &jo[0][0];                                 // [kJoin][kRows]
         f32x4_t* across = reinterpret_cast<f32x4_t*>(&jo[1][0]);   // [kThreads]
         const int items = valid * Q, shares = kThreads / items > 1 ? kThreads / items : 1;
-        int share = 0, item = tid;
+        int share = 0, item = at_thread;
         if (shares > 1) {
-          share = tid / items;
-          item = tid - share * items;
+          share = at_thread / items;
+          item = at_thread - share * items;
         }
         const int at_row = item / Q < valid ? item / Q : 0;       // idle threads read a row too
         const float* from = partial + at_row * D + item % Q * 4;
@@ -408,8 +451,8 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
         };
         fly(share, 0);
         __syncthreads();                                 // jo, jm and jl have been read
-        if (tid < 16 * kRows) {  // 16 lanes a row
-          const int row = tid >> 4, sub = tid & 15;
+        for (int row = at_thread >> 4; row < kRows; row += kThreads / 16) {   // 16 lanes a row
+          const int sub = at_thread & 15;
           float2 md[kJoin / 16];
           float most = -INFINITY, l16 = 0.0f;
 #pragma unroll
@@ -454,10 +497,10 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
               add(sum[x], i0, jr + x * STRIDE);
             }
         if (shares > 1) {
-          if (share < shares) across[tid] = sum[0];
+          if (share < shares) across[at_thread] = sum[0];
           __syncthreads();
-          if (tid < items)
-            for (int i = 1; i < shares; ++i) sum[0] += across[i * items + tid];
+          if (at_thread < items)
+            for (int i = 1; i < shares; ++i) sum[0] += across[i * items + at_thread];
         }
 #pragma unroll
         for (int x = 0; x < IT; ++x) {
@@ -502,71 +545,91 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D> : W / 4)) attend
   }
 }
 
-// Which kernel.  By rows (bf16 only), blocks of 256 rows share the widened codes, which pays
-// where requests bring 64 rows or more on average and there is work enough to fill the
-// chip with such blocks: 2^32 / d pairs of a query row and a key, by the tables' length.
-// Measured, us, split / by rows, 8 KV heads, B requests of n new tokens after `old`:
-//   d = 128  B = 64, old 1000   G = 8, n = 4: 42 / 56    n = 8: 70 / 59     n = 64: 566 / 189
-//            B = 8,  old 1000   G = 8, n = 16: 25 / 38   n = 32: 44 / 58    n = 64: 72 / 53
-//            B = 8,  old 8000   G = 8, n = 8: 63 / 67    n = 16: 118 / 76
-//            B = 1,  old 5000   G = 8, n = 64: 44 / 55   n = 128: 77 / 62
-//   d = 64   B = 64, old 1000   G = 8, n = 8: 41 / 47    n = 16: 71 / 50
-//            B = 1,  old 5000   G = 8, n = 128: 42 / 42
-bool may_go_by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G >= (int64_t)B * 64; }
+// Which kernel: by what the host knows, rows, requests and the tables' length, which is at
+// least the longest request's.  Measured, us, with 8 KV heads, pages that no cache holds, B
+// requests of `rows` query rows a head over `keys` keys.
+
+// By rows (bf16 only): blocks of 256 rows share the widened codes.  Pays from 96 rows a
+// request on where blocks are enough for the CUs or the work is, else its joins cost more.
+//   d = 128, split / by rows    B = 64, 64 rows, 1000 keys 58 / 58    96 rows 80 / 61
+//     B = 32, 128 rows, 300 keys 27 / 19     B = 16, 160 rows, 5000 keys 131 / 93
+//     B = 8,  256 rows, 5000 keys 77 / 84, 16000 keys 211 / 188
+//     B = 1,  2048 rows, 2178 keys 37 / 63, 16000 keys 198 / 167
+//   d = 64   B = 64, 64 rows, 1000 keys 35 / 46    128 rows 59 / 47
+bool may_go_by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G >= (int64_t)B * 96; }
 bool by_rows(const AttendArgs& a, int dtype, int d) {
-  const double pairs = (double)a.T * a.G * a.H * ((int64_t)a.M << a.log2p);
-  return may_go_by_rows(a.B, a.G, a.T, dtype) && pairs * d >= 4294967296.0;
+  const int64_t rows = (int64_t)a.T * a.G, units = (rows / 256 > a.B ? rows / 256 : a.B) * a.H;
+  const double work = (double)rows * a.H * ((int64_t)a.M << a.log2p) * d;
+  return may_go_by_rows(a.B, a.G, a.T, dtype) && (units >= 192 || work >= (units >= 128 ? 8589934592.0 : 17179869184.0));
+}
+
+// Blocks of 32 rows (bf16 only), whose codes are loaded and widened once for two row tiles,
+// where a request brings more than one tile and the blocks' keys come to 512 a CU:
+//   d = 128, 16 / 32 rows a block    B = 64, 32 rows, 1000 keys 47 / 36, 5000 keys 229 / 131
+//     B = 8, 128 rows, 5000 keys 70 / 45     B = 2, 24 rows, 1000 keys 14 / 16
+//   d = 64   B = 32, 32 rows, 5000 keys 50 / 40
+bool two_tiles(const AttendArgs& a, int dtype) {
+  const int64_t rows = (int64_t)a.T * a.G, blocks = rows / 32 > a.B ? rows / 32 : a.B;
+  return dtype == 0 && rows > 16 * (int64_t)a.B && blocks * a.H * ((int64_t)a.M << a.log2p) >= 256 * 512;
 }
 
 // One large workgroup a CU instead of several of four waves: a unit then has fewer partial
-// sums or none.  Pays where the units' keys, by the tables' length, come to 256 a CU (a
-// decoding step of 32 requests of 2178 keys 35 us against 43, 16 of 1000 17 against 20,
-// 4 contexts up to 131070 91 against 97), but not
-//   - for requests of more than 32 rows (a mixed batch of 8: 26 us against 19);
-//   - for few units of one or two rows, whose sums join fast (G = 1, 16000 keys: 20 against 17);
+// sums or none.
+//   Blocks of 32 rows: fewer than two units a CU (32 requests of 24 rows and 2178 keys 44 ->
+//   35, 64 of 1000 33 against 38) of 1024 keys and more (a prompt of 195 tokens 17 against 19).
+//   Blocks of 16: where the units' keys come to 256 a CU (a decoding step of 32 requests of
+//   2178 keys 43 -> 35, 16 of 1000 20 -> 17, 4 contexts up to 131070 97 -> 91), but not
+//   - for requests of more than 32 rows (a mixed batch of 8: 26 against 18);
+//   - for few units of one to three rows, whose sums join fast, until their keys come to
+//     2048 a CU (G = 1, 16000 keys 17 against 20; two heads, 16 contexts up to 24900 23 -> 20);
 //   - for many short units, where starts and ends of small workgroups overlap: 256 requests
-//     of 300 keys 59 against 43, of 1000 117 against 113, of 2178 220 against 231; with
-//     eight waves (fp32, d = 128) for many units of any length, 121 against 115.
-template <int LARGE>
+//     of 300 keys 43 against 59, of 1000 113 against 117, of 2178 231 -> 220; with eight
+//     waves (fp32, d = 128) for many units of any length, 115 against 121.
+template <int NB, int LARGE>
 bool large_workgroups(const AttendArgs& a) {
-  const int64_t rows = (int64_t)a.T * a.G, blocks = rows / kRows > a.B ? rows / kRows : a.B;
+  const int64_t rows = (int64_t)a.T * a.G, B = a.B, blocks = rows / (16 * NB) > B ? rows / (16 * NB) : B;
   const int64_t units = blocks * a.H, keys = (int64_t)a.M << a.log2p;
-  return rows <= 32 * (int64_t)a.B && units * keys >= 256 * 256 && (units >= 64 || rows >= 4 * (int64_t)a.B) &&
-         (units < 512 || (LARGE >= 12 && keys > 1024));
+  if (NB == 2) return units < 512 && keys >= 1024;
+  const int64_t least = units < 64 && rows < 4 * B ? 256 * 2048 : 256 * 256;
+  return rows <= 32 * B && units * keys >= least && (units < 512 || (LARGE >= 12 && keys > 1024));
 }
 
 }  // namespace
 
-// Counters, and two partial sums for each workgroup's first and last unit.
+// Counters, and two partial sums for each workgroup's first and last unit: most rows with
+// blocks of 32 rows and three workgroups a CU.
 size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
-  const size_t split = kCounters * sizeof(int) + (size_t)256 * 4 * 2 * kRows * (d + 2) * sizeof(float);
+  const size_t split = kCounters * sizeof(int) + (size_t)256 * 3 * 2 * 32 * (d + 2) * sizeof(float);
   const size_t rows = may_go_by_rows(B, G, T, dtype) ? attend_rows_ws_bytes(d) : 0;
   return split > rows ? split : rows;
 }
 
-template <int DT, int D, int W>
+template <int DT, int D, int W, int NB>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
   // no more workgroups than the tables' pages hold quanta for
   const int64_t keys = (int64_t)a.M << a.log2p, quant = W * kStep;
-  const int64_t most = ((int64_t)a.T * a.G / kRows + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
-  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>, fill = W == 4 ? 256 * kOcc<DT, D> : 256;
+  const int64_t most = ((int64_t)a.T * a.G / (16 * NB) + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
+  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>;
+  const int64_t fill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
   int* counters = static_cast<int*>(ws);
   const unsigned grid = (unsigned)((want < fill ? want : fill) + kXcds - 1) / kXcds * kXcds;
-  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W>), dim3(grid), dim3(64 * W),
+  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W, NB>), dim3(grid), dim3(64 * W),
                      (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
   return hipGetLastError();
 }
 
-template <int DT, int D>
+template <int DT, int D, int NB>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  constexpr int LARGE = kLarge<DT, D>;
-  return large_workgroups<LARGE>(a) ? launch_split<DT, D, LARGE>(a, ws, stream) : launch_split<DT, D, 4>(a, ws, stream);
+  constexpr int LARGE = kLarge<DT, D, NB>;
+  return large_workgroups<NB, LARGE>(a) ? launch_split<DT, D, LARGE, NB>(a, ws, stream)
+                                        : launch_split<DT, D, 4, NB>(a, ws, stream);
 }
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
   if (by_rows(a, dtype, d)) return launch_attend_rows(a, d, ws, stream);
-  if (dtype == 0) return d == 64 ? launch_split<0, 64>(a, ws, stream) : launch_split<0, 128>(a, ws, stream);
-  return d == 64 ? launch_split<1, 64>(a, ws, stream) : launch_split<1, 128>(a, ws, stream);
+  if (two_tiles(a, dtype)) return d == 64 ? launch_split<0, 64, 2>(a, ws, stream) : launch_split<0, 128, 2>(a, ws, stream);
+  if (dtype == 0) return d == 64 ? launch_split<0, 64, 1>(a, ws, stream) : launch_split<0, 128, 1>(a, ws, stream);
+  return d == 64 ? launch_split<1, 64, 1>(a, ws, stream) : launch_split<1, 128, 1>(a, ws, stream);
 }
 
 }  // namespace kvx

@@ -20,8 +20,8 @@ def _by_rows(c):
     T, heads, d = c["q"].shape
     B, M = c["tables"].shape
     P = c["codes"].shape[2] // c["scales"].shape[2]
-    assert T * heads // c["codes"].shape[1] >= 64 * B and c["q"].dtype == torch.bfloat16
-    return _wide(c, -(-2 ** 32 // (T * heads * d * P)))
+    assert c["q"].dtype == torch.bfloat16     # requests of 96 rows and more; others go in blocks of 32
+    return _wide(c, -(-2 ** 34 // (T * heads * d * P)))
 
 
 def _large(c):
@@ -32,6 +32,17 @@ def _large(c):
     assert c["q"].dtype != torch.bfloat16 or T * heads // c["codes"].shape[1] < 64 * B
     P = c["codes"].shape[2] // c["scales"].shape[2]
     return _wide(c, -(-2 ** 20 // (B * c["codes"].shape[1] * P)))
+
+
+def _two_tiles(c):
+    """Widens the tables until requests of 17 to 95 rows take blocks of 32, in large
+    workgroups where those are few."""
+    B, M = c["tables"].shape
+    T, heads, _ = c["q"].shape
+    H = c["codes"].shape[1]
+    assert c["q"].dtype == torch.bfloat16 and 16 * B < T * heads // H < 96 * B
+    P = c["codes"].shape[2] // c["scales"].shape[2]
+    return _wide(c, -(-2 ** 17 // (B * H * P)))
 
 
 def _wide(c, M):
@@ -51,6 +62,7 @@ CHUNKS = [   # tokens in the pool, new ones, KV heads, query heads each
     ([300, 40], [20, 17], 3, 16),
     ([90, 33], [30, 33], 2, 17),
     ([200], [10], 1, 40),
+    ([64], [64], 1, 2),
 ]
 
 
@@ -66,9 +78,11 @@ def test_by_rows(gpu_kvx, d, P):
 @pytest.mark.parametrize("lens,news,H,G,d,P", [
     ([3000, 5], [130, 1], 1, 4, 128, 32),          # a unit over many workgroups: two-level joins
     ([20011], [64], 1, 1, 64, 128),
+    ([20011], [64], 1, 2, 64, 128),
     ([9001], [65], 1, 5, 128, 16),
     ([700] * 40, [33] * 40, 1, 4, 64, 16),         # several units a workgroup
     (list(range(64, 364, 3)), [64] * 100, 1, 1, 64, 16),
+    (list(range(64, 364, 3)), [64] * 100, 1, 2, 64, 16),
 ])
 def test_by_rows_shares(gpu_kvx, lens, news, H, G, d, P):
     rng = np.random.default_rng(len(lens) + d)
@@ -98,12 +112,41 @@ def test_large_workgroups(gpu_kvx, dtype, lens, news, H, G, d, P):
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
-KERNELS = {"split": lambda c: c, "large": _large, "by rows": _by_rows}
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,news,H,G,P", [
+    ([17], [17], 1, 1, 16),
+    ([60, 5, 300], [3, 5, 40], 2, 3, 32),            # rows past a block's end, blocks of one tile
+    ([0, 33, 9], [7, 33, 12], 2, 2, 16),             # a request without keys, more rows than tokens
+    ([20011], [3], 1, 8, 64),                        # a unit over many workgroups
+    ([40011, 7], [5, 1], 1, 8, 128),
+    ([255, 256, 257, 383, 384, 385], [5] * 6, 1, 8, 16),
+    ([31] * 40 + [700], [20] * 41, 2, 1, 16),        # several units a workgroup
+    ([300] * 130, [3] * 130, 4, 8, 32),              # many units: small workgroups
+    ([90] * 700, [6] * 700, 1, 3, 16),
+])
+def test_blocks_of_32_rows(gpu_kvx, lens, news, H, G, P, d):
+    rng = np.random.default_rng(lens[0] + len(lens))
+    c = _two_tiles(_case(rng, lens, news, H, G, d, P, "bf16"))
+    first = _check(gpu_kvx, c, f"blocks of 32 lens={lens[:6]} H={H} G={G} d={d}")
+    again = gpu_kvx.attend_cache8(*_gpu(c), with_lse=True)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_most_requests_in_large_workgroups(gpu_kvx):
+    """4096 requests' prefix sums beside the largest arrays of a workgroup."""
+    rng = np.random.default_rng(36)
+    lens = rng.integers(0, 40, 4096).tolist()
+    for G, d in ((1, 128), (2, 64)):
+        c = _case(rng, lens, [int(n > 0) for n in lens], 1, G, d, 16, "bf16")
+        _check(gpu_kvx, _wide(c, 65), f"4096 requests, G={G} d={d}")
+
+
+KERNELS = {"split": lambda c: c, "large": _large, "two tiles": _two_tiles, "by rows": _by_rows}
 
 
 def _news(kernel, few, many):
-    """New tokens: few for the large workgroups, many else."""
-    return few if kernel == "large" else many
+    """New tokens: few for the large workgroups, more for blocks of 32 rows, many else."""
+    return few if kernel == "large" else [4 * n for n in few] if kernel == "two tiles" else many
 
 
 @pytest.mark.parametrize("kernel", KERNELS)
@@ -137,12 +180,13 @@ def test_missing_pages_and_lengths_out_of_range(gpu_kvx, kernel):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_nan_in_the_cache_reaches_the_rows_that_see_it(gpu_kvx, kernel, dtype):
     """NaN keys and values among the newest tokens: rows before them are as without."""
-    if kernel == "by rows" and dtype == "f32":
-        pytest.skip("fp32 queries go by keys")
+    if kernel in ("by rows", "two tiles") and dtype == "f32":
+        pytest.skip("fp32 queries go by keys, in blocks of 16 rows")
     rng = np.random.default_rng(33)
     for d, P in ((128, 32), (64, 16)):
         for lens, news, G in ((([90, 300], [6, 7], 8), ([33, 70], [33, 3], 1),
                                ([90, 300], [3, 4], 8)) if kernel == "large" else
+                              (([33, 70], [33, 3], 1), ([90, 300], [3, 4], 8)) if kernel == "two tiles" else
                               (([90, 300], [80, 70], 1), ([33, 70], [33, 3], 8))):
             c = _case(rng, lens, news, 2, G, d, P, dtype)
             slot = lambda b, p: c["tables"][b, p // P] * P + p % P  # noqa: E731, B023
@@ -184,7 +228,7 @@ def test_scales_that_are_no_powers_of_two(gpu_kvx, kernel):
     assert np.all(np.abs(lse.double().cpu().numpy() - wl) <= E[..., 0] + 2.0 ** -22 * np.abs(wl))
 
 
-@pytest.mark.parametrize("kernel", ["large", "by rows"])
+@pytest.mark.parametrize("kernel", ["large", "two tiles", "by rows"])
 def test_far_pages_strides_streams_and_graphs(gpu_kvx, kernel):
     rng = np.random.default_rng(35)
     c = KERNELS[kernel](_case(rng, [500, 230], _news(kernel, [1, 5], [1, 230]), 2, 4, 128, 16, "bf16"))
