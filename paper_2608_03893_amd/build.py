@@ -1,4 +1,5 @@
-"""Build libkvx.so (HIP for gfx950) in the package directory.
+"""Build libkvx.so (HIP for gfx950) and the binding's compiled part, _kvx_bind.so (host
+C++), in the package directory.
 
 Run ``python -m paper_2608_03893_amd.build``.  Every call recompiles.
 """
@@ -8,6 +9,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 import time
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -15,6 +17,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libkvx.so")
+BIND = os.path.join(PKG, "_kvx_bind.so")
 SOURCES = ["kvx_api.hip", "kvx_kernels.hip", "kvx_map_bf16.hip", "kvx_map_sweep.hip",
            "kvx_map_ks.hip", "kvx_map_ks_raw.hip", "kvx_map_tile.hip", "kvx_map_short.hip",
            "kvx_map_ks2.hip", "kvx_map_ks2_raw.hip", "kvx_xhead.hip", "kvx_noalloc.hip",
@@ -33,11 +36,29 @@ def hipcc() -> str:
     return os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
+def bind_command(out: str) -> list:
+    """Compiles kvx_bind.cpp against the installed torch, which a process that imports the
+    module has loaded."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+            "-isystem", os.path.join(at, "include"),
+            "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "kvx_bind.cpp"),
+            "-L", os.path.join(at, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python", "-o", out]
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source and link libkvx.so; returns the library path."""
+    """Compile every source, link libkvx.so and the binding's compiled part; returns the
+    library path."""
     t0 = time.time()
     objs = []
-    procs = []
+    cmd = bind_command(BIND + ".tmp")
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    procs = [(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True),
+              "kvx_bind.cpp")]
     for src in SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
         cmd = [hipcc(), *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c",
@@ -58,7 +79,8 @@ def build(verbose: bool = False) -> str:
         if p.returncode:
             failed.append(src)
     if failed:
-        raise RuntimeError(f"hipcc failed for {failed}")
+        raise RuntimeError(f"compilation failed for {failed}")
+    os.replace(BIND + ".tmp", BIND)
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp]
     subprocess.run(cmd, check=True)

@@ -1,4 +1,5 @@
-"""ctypes binding of libkvx.so (argument marshalling only).
+"""Binding of libkvx.so (argument marshalling only): ctypes, and compiled for the
+serving calls.
 
 Every step of the mapping runs in the library's HIP kernels.  This module
 checks tensor placement, dtype and contiguity, derives the problem sizes from
@@ -14,7 +15,6 @@ mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from typing import NamedTuple
 
@@ -112,6 +112,10 @@ _LIB = None
 
 def lib_path() -> str:
     return os.path.join(_PKG, "libkvx.so")
+
+
+def bind_path() -> str:
+    return os.path.join(_PKG, "_kvx_bind.so")
 
 
 def load():
@@ -605,8 +609,9 @@ def mlp_map_layer(l_t, src, idx, mlp_K, mlp_V, rope_src, rope_tgt, positions, ou
 
 # ------------------------------------------------- serving from the mapped cache
 #
-# These calls take a few microseconds on the GPU, so the binding keeps its own work small:
-# plain integers for pointers, the raw stream handle, no stream context for the default.
+# These calls take a few microseconds on the GPU, so their checks, outputs and marshalling
+# are compiled (csrc/kvx_bind.cpp): the host's part of an attention call is 5 us instead of
+# 13.
 
 class PagePlan(NamedTuple):
     """What plan_pages computes (device int32 tensors)."""
@@ -618,40 +623,24 @@ class PagePlan(NamedTuple):
                               # refused requests, rows
 
 
-def _raw_stream(stream, device):
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+_BIND = None
 
 
-# The library's structs by their sizes; nothing writes to them after they are made.
-_pool = functools.lru_cache(maxsize=256)(Pool)
-_sizes = functools.lru_cache(maxsize=256)(AttendDims)
-
-
-@functools.lru_cache(maxsize=256)
-def _strides(*s):
-    return (ctypes.c_int64 * len(s))(*s)
-
-
-def _new(shape, dtype, device, stream):
-    """An output allocated on the launch stream (see _scratch)."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _addr(name, t):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
-
-
-def _int32(name, t, shape):
-    if t.dtype != torch.int32 or t.shape != shape:
-        raise ValueError(f"{name} must be int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _addr(name, t)
+def _native():
+    """The compiled marshalling, with the library's entry points."""
+    global _BIND
+    if _BIND is None:
+        lib = load()
+        try:
+            from . import _kvx_bind
+        except ImportError as e:
+            raise KvxNotBuilt(f"{bind_path()}: {e}; run python -m paper_2608_03893_amd.build") from e
+        entry = [ctypes.cast(f, ctypes.c_void_p).value
+                 for f in (lib.kvx_plan_pages, lib.kvx_store_cache8, lib.kvx_attend_cache8,
+                           lib.kvx_attend_workspace_bytes)]
+        _kvx_bind.bind(*entry, _check, PagePlan, torch._C._cuda_getCurrentRawStream)
+        _BIND = _kvx_bind
+    return _BIND
 
 
 def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None, stream=None):
@@ -661,49 +650,11 @@ def plan_pages(lens, add, block_tables, free_ring, free, T, page_size, out=None,
     lens, add [B] int32 (add < 0: the request has ended), block_tables
     [B, max_pages] and free_ring [num_pages] int32, updated in place; free: int32,
     the ring's first place and count (the last plan's ``free``); T rows."""
-    if block_tables.dim() != 2 or free_ring.dim() != 1:
-        raise ValueError("block_tables must be [B, max_pages], free_ring [num_pages]")
-    if free.dtype != torch.int32 or free.dim() != 1 or free.shape[0] < 2:
-        raise ValueError("free must be int32 with the ring's first place and count")
-    B, M = block_tables.shape
-    N, T, dev = free_ring.shape[0], int(T), lens.device
-    args = (_int32("lens", lens, (B,)), _int32("add", add, (B,)),
-            _int32("block_tables", block_tables, (B, M)), _int32("free_ring", free_ring, (N,)),
-            _addr("free", free))
-    if out is None:      # one allocation; positions and slots start on 16 bytes
-        pad = -T % 4
-        pos, _, slots, _, lens_out, cu, left = _new(
-            2 * (T + pad) + 2 * B + 5, torch.int32, dev, stream).split_with_sizes(
-                (T, pad, T, pad, B, B + 1, 4))
-        out = PagePlan(lens_out, cu, pos, slots, left)
-        outs = [t.data_ptr() for t in out]
-    else:
-        outs = [_int32(name, t, (n,)) for name, t, n in zip(PagePlan._fields, out, (B, B + 1, T, T, 4))]
-    _check(load().kvx_plan_pages(ctypes.byref(_pool(N, int(page_size), M)), B, T, *args, *outs,
-                                 _raw_stream(stream, dev)))
-    return out
-
-
-def _rows_addr(name, t):
-    """Address of a tensor whose last dimension is dense, whatever the other strides."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{name} must be dense in its last dimension")
-    return t.data_ptr()
-
-
-def _pool8(pool, scales, lead, max_pages):
-    """kvx_pool of an 8-bit pool [*lead, num_slots, d] and its scales [*lead, num_pages]."""
-    shape, spages = pool.shape, scales.shape
-    if pool.dtype != torch.float8_e4m3fn or len(shape) != len(lead) + 2 or shape[:-2] != lead:
-        raise ValueError(f"pool must be float8_e4m3fn {tuple(lead)} + [num_slots, d]")
-    if scales.dtype != torch.float32 or len(spages) != len(lead) + 1 or spages[:-1] != lead:
-        raise ValueError(f"scales must be float32 {tuple(lead)} + [num_pages]")
-    slots, pages = shape[-2], spages[-1]
-    if pages < 1 or slots % pages:
-        raise ValueError(f"{slots} slots do not divide into {pages} pages")
-    return _pool(pages, slots // pages, max_pages)
+    f, T, page_size = (_BIND or _native()).plan_pages, int(T), int(page_size)
+    if stream is None:
+        return f(lens, add, block_tables, free_ring, free, T, page_size, out, None)
+    with torch.cuda.stream(stream):      # outputs are allocated on it (see _scratch)
+        return f(lens, add, block_tables, free_ring, free, T, page_size, out, stream.cuda_stream)
 
 
 def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
@@ -713,17 +664,8 @@ def store_cache8(k, v, slot_mapping, pool, scales, stream=None):
     cache's out[:, 0] and out[:, 1], or a projection's [T, H, d] transposed);
     slot_mapping int32 [T]; pool [L, 2, H, num_slots, d] float8_e4m3fn and scales
     [L, 2, H, num_pages] float32, updated in place."""
-    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("k and v must be [L, H, T, d] of one dtype")
-    L, H, T, d = k.shape
-    p = _pool8(pool, scales, (L, 2, H), 1)
-    if pool.shape[4] != d:
-        raise ValueError(f"pool rows have {pool.shape[4]} channels, k and v {d}")
-    _check(load().kvx_store_cache8(
-        ctypes.byref(p), _dtype_code(k), L, H, T, d, _rows_addr("k", k), _strides(*k.stride()[:3]),
-        _rows_addr("v", v), _strides(*v.stride()[:3]), _int32("slot_mapping", slot_mapping, (T,)),
-        _addr("pool", pool), _addr("scales", scales), _raw_stream(stream, k.device)))
-    return pool
+    return (_BIND or _native()).store_cache8(k, v, slot_mapping, pool, scales,
+                                             None if stream is None else stream.cuda_stream)
 
 
 def _attend_dims(q, pool, block_tables):
@@ -731,9 +673,9 @@ def _attend_dims(q, pool, block_tables):
         raise ValueError("q must be [T, H*G, d], pool [2, H, num_slots, d], block_tables [B, max_pages]")
     T, heads, d = q.shape
     H = pool.shape[1]
-    if heads % H or pool.shape[3] != d:
+    if H < 1 or heads % H or pool.shape[3] != d:
         raise ValueError(f"{heads} query heads of {d} channels on a pool of {H} heads of {pool.shape[3]}")
-    return _sizes(block_tables.shape[0], H, heads // H, T, d)
+    return AttendDims(block_tables.shape[0], H, heads // H, T, d)
 
 
 def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
@@ -760,23 +702,8 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     [2, H, num_pages]; block_tables [B, max_pages], lens [B] (tokens in the pool,
     the new ones included), cu [B + 1] (their rows in q) int32; scale: factor of
     the scores, 1 / sqrt(d) by default."""
-    dims = _attend_dims(q, pool, block_tables)
-    B, M = block_tables.shape
-    p = _pool8(pool, scales, (2, dims.H), M)
-    code, dev, shape = _dtype_code(q), q.device, q.shape
-    args = (_rows_addr("q", q), _strides(*q.stride()[:2]), _addr("pool", pool), _addr("scales", scales),
-            _int32("block_tables", block_tables, (B, M)), _int32("lens", lens, (B,)),
-            _int32("cu", cu, (B + 1,)))
-    if out is None:
-        out = _new(shape, q.dtype, dev, stream)
-    elif out.shape != shape or out.dtype != q.dtype:
-        raise ValueError("out must have q's shape and dtype")
-    lse = _new(shape[:2], torch.float32, dev, stream) if with_lse else None
-    if workspace is None:
-        workspace = attend_workspace(q, pool, block_tables, stream)
-    _check(load().kvx_attend_cache8(
-        ctypes.byref(dims), ctypes.byref(p), code, *args,
-        dims.d ** -0.5 if scale is None else float(scale), _addr("out", out),
-        None if lse is None else lse.data_ptr(), _addr("workspace", workspace),
-        workspace.numel(), _raw_stream(stream, dev)))
-    return (out, lse) if with_lse else out
+    f = (_BIND or _native()).attend_cache8
+    if stream is None:
+        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, None)
+    with torch.cuda.stream(stream):
+        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, stream.cuda_stream)
