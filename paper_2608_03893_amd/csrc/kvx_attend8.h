@@ -74,7 +74,7 @@ struct Request {
   int32_t row0, tokens, rows;   // first query row, new tokens, rows of a KV head (tokens * G)
   int32_t len;                  // keys
 };
-__device__ __forceinline__ Request request(const AttendArgs& a, int b) {
+__device__ __forceinline__ Request request(const AttendArgs& a, int b, int len) {
   Request r;
   int c0 = a.cu[b], c1 = a.cu[b + 1];
   c0 = c0 < 0 ? 0 : c0;
@@ -82,10 +82,11 @@ __device__ __forceinline__ Request request(const AttendArgs& a, int b) {
   r.row0 = c0;
   r.tokens = c1 > c0 ? c1 - c0 : 0;
   const int64_t cap = (int64_t)a.M << a.log2p;
-  r.len = a.lens[b] < 0 ? 0 : a.lens[b] < cap ? a.lens[b] : (int)cap;
+  r.len = len < 0 ? 0 : len < cap ? len : (int)cap;
   r.rows = r.tokens * a.G;
   return r;
 }
+__device__ __forceinline__ Request request(const AttendArgs& a, int b) { return request(a, b, a.lens[b]); }
 
 // Two floats written through to memory / read from there, past this XCD's L2.
 __device__ __forceinline__ void put2(float* to, float x, float y) {

@@ -52,9 +52,10 @@ constexpr int kLarge = kOcc<DT, D, NB> > 2 ? 12 : 8;   // waves of a large workg
 // still have an output).
 template <int R>
 __device__ __forceinline__ int blocks_of(const Request& r) { return (r.rows + R - 1) / R; }
-__device__ __forceinline__ int quanta_of(const Request& r, int quant) {
-  return r.len > quant ? (int)(((int64_t)r.len + quant - 1) / quant) : 1;
+__device__ __forceinline__ int quanta_of(int len, int quant) {
+  return len > quant ? (int)(((uint32_t)len + quant - 1) / quant) : 1;
 }
+__device__ __forceinline__ int quanta_of(const Request& r, int quant) { return quanta_of(r.len, quant); }
 
 // A step's keys and values, as loaded.
 template <int D>
@@ -82,11 +83,41 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
   const int n = lane & 15, g4 = lane >> 4;
 
   int32_t* weight = reinterpret_cast<int32_t*>(pre + a.B);         // [B] of a unit
-  prefix_requests<kThreads>(a, pre, part, [&](const Request& r, int b) {
-    weight[b] = quanta_of(r, kQuant) + kStart;
-    return (int64_t)blocks_of<kRows>(r) * weight[b] * a.H;
-  });
-  const int64_t total = uniform(pre[a.B - 1]);
+  // Up to 64 requests: every wave has them in its lanes, and neither LDS nor barriers come
+  // before its first loads (three requests of 100 to 250 keys 6.9 -> 6.4 us).
+  uint32_t pre_lane = 0;
+  int len_lane = 0;
+  int64_t total = 0;
+  bool lanes = a.B <= 64;
+  if (lanes) {
+    const Request r = request(a, lane < a.B ? lane : a.B - 1);
+    len_lane = r.len;
+    const int64_t w = lane < a.B ? (int64_t)blocks_of<kRows>(r) * (quanta_of(r, kQuant) + kStart) * a.H : 0;
+    pre_lane = w < UINT32_MAX ? (uint32_t)w : UINT32_MAX;
+#pragma unroll
+    for (int n = 1; n < 64; n <<= 1) {
+      const uint32_t x = __shfl_up(pre_lane, n, 64);
+      if (lane >= n) pre_lane = __builtin_elementwise_add_sat(pre_lane, x);
+    }
+    total = (uint32_t)__builtin_amdgcn_readlane(pre_lane, 63);
+    lanes = total < UINT32_MAX;        // else the sums may not fit
+  }
+  if (!lanes) {
+    prefix_requests<kThreads>(a, pre, part, [&](const Request& r, int b) {
+      weight[b] = quanta_of(r, kQuant) + kStart;
+      return (int64_t)blocks_of<kRows>(r) * weight[b] * a.H;
+    });
+    total = uniform(pre[a.B - 1]);
+  }
+  // the request that has weight x, the weight before it, its units' weight
+  auto find = [&](int64_t x) {
+    return lanes ? __builtin_ctzll(__ballot(pre_lane > (uint32_t)x)) : uniform(find_request(pre, a.B, x));
+  };
+  auto before = [&](int b) {
+    return b == 0 ? (int64_t)0
+           : lanes ? (int64_t)(uint32_t)__builtin_amdgcn_readlane(pre_lane, b - 1) : uniform(pre[b - 1]);
+  };
+  auto length = [&](int b) { return __builtin_amdgcn_readlane(len_lane, b); };
   const int grid = gridDim.x;
   const int64_t share_q = uniform(divide(total + grid - 1, grid));
   const int64_t per = share_q > kLeast<W> ? share_q : kLeast<W>;
@@ -96,8 +127,8 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
   // small: to split it would cost more, in its second start and the join, than it levels.
   auto share_end = [&](int64_t x) {
     if (x >= total) return total;
-    const int b = uniform(find_request(pre, a.B, x));
-    const int64_t in_request = x - (b > 0 ? pre[b - 1] : (int64_t)0), w = weight[b];
+    const int b = find(x);
+    const int64_t in_request = x - before(b), w = lanes ? quanta_of(length(b), kQuant) + kStart : weight[b];
     if (w > small) return x;
     const int64_t in_unit = in_request - divide(in_request, w) * w;
     return 2 * in_unit < w ? x - in_unit : x - in_unit + w;
@@ -106,14 +137,13 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
   int64_t at = uniform(share_end(me * per));
   const int64_t end = uniform(share_end((me + 1) * per));
   if (at >= end) return;
-  int b = uniform(find_request(pre, a.B, at));
 
   const int64_t plane = ((int64_t)a.N << a.log2p) * D;
   const int P1 = (1 << a.log2p) - 1;
   while (at < end) {
-    while (uniform(pre[b]) <= at) ++b;
-    const int64_t base = uniform(b > 0 ? pre[b - 1] : (int64_t)0);
-    const Request r = request(a, b);
+    const int b = find(at);
+    const int64_t base = before(b);
+    const Request r = lanes ? request(a, b, length(b)) : request(a, b);
     const int quanta = quanta_of(r, kQuant);
     const int64_t unit = divide(at - base, quanta + kStart);
     const int64_t unit0 = base + unit * (quanta + kStart);     // its first weight
