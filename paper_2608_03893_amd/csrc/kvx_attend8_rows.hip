@@ -9,7 +9,10 @@
 // the next are in flight.  The products are those of the split kernel (kvx_attend8.hip).
 // A value's scale is applied as the code is widened (a power of two is exact there).
 //
-// Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them.
+// Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them:
+// 2048 new tokens of 64 heads over 10240 keys, d = 128, 615 us, 1000 TFLOP/s, where a large
+// product of the library reaches 1230.  To form a step's scores beside the exponentials of
+// the step before took as long (a quarter more products of keys, and 8% more time).
 //
 // One workgroup a CU; each takes an equal share of the weight of all (request, head, block
 // of rows), a block's weight being the keys that its last row sees.  Neighbouring
@@ -275,6 +278,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
       for (int i = 0; i < kRing; ++i) f[i] = from[i * 64];
 #pragma unroll 1
       for (int s = 0; s < kSteps && key <= lim_hi; ++s, key += kStep) {
+        // A SIMD's two waves take turns at going first, two steps each: left alone, one always
+        // does, and waits at the barrier for a third of the time (631 -> 615 us).
+        if ((s >> 1 ^ wave >> 2) & 1) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
         const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};
         const int bad = uniform(flags[buf][s][0]), nan = uniform(flags[buf][s][1]);
         const u32x4_t* next = s + 1 < kSteps ? from + F * 64 : from;   // the last step's are not used
