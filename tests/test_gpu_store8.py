@@ -210,3 +210,24 @@ def test_store_on_another_stream_and_in_a_graph(gpu_kvx):
         wc, ws = codes.copy(), scales.astype(np.float64)
         S.store_cache8(k.double().cpu().numpy(), v.double().cpu().numpy(), slots, wc, ws)
         assert np.array_equal(pool.cpu().numpy(), wc) and np.array_equal(sc.double().cpu().numpy(), ws), n
+
+
+@pytest.mark.parametrize("d,P,T", [(64, 16, 2500), (64, 16, 4096 + 37), (128, 128, 700)])
+def test_a_large_call_equals_its_layers_one_by_one(gpu_kvx, d, P, T):
+    """Waves that take several small pages, or a long one whole, against calls of one layer."""
+    rng = np.random.default_rng(T)
+    L, H, turns = 64, 8, [(9, T // 2), (0, 5), (P, T - T // 2 - 5 - 61), (3, 61)]
+    N = sum(-(-(a + b) // P) for a, b in turns) + 2
+    slots = torch.from_numpy(_slots(rng, turns, P, N).astype(np.int32)).to(DEV)
+    slots[T // 2:T // 2 + 5] = -1               # a refused request's
+    k, v = (torch.randn((L, H, T, d), device=DEV).to(torch.bfloat16) for _ in range(2))
+    k[:, :, T // 2:] *= 40
+    pool = torch.randint(0, 0x60, (L, 2, H, N * P, d), dtype=torch.uint8, device=DEV)
+    scales = torch.full((L, 2, H, N), 2.0 ** -8, device=DEV)
+    one, one_scales = pool.clone(), scales.clone()
+    gpu_kvx.store_cache8(k, v, slots, pool.view(torch.float8_e4m3fn), scales)
+    for l in range(L):
+        gpu_kvx.store_cache8(k[l:l + 1], v[l:l + 1], slots, one[l:l + 1].view(torch.float8_e4m3fn), one_scales[l:l + 1])
+    assert torch.equal(pool, one) and torch.equal(scales, one_scales)
+    codes, ws = _pool(rng, 1, H, N, P, d)       # and one layer against the definition
+    _check(gpu_kvx, k[:1, :, :300], v[:1, :, :300], slots[:300].cpu().numpy().astype(int), codes, ws)
