@@ -526,9 +526,12 @@ kvx_status kvx_store_cache8(const kvx_pool* pool, kvx_dtype dtype, int32_t L, in
 
 /* Sizes of an attention call: B requests, H KV heads with G query heads each
  * (query head h * G + g reads KV head h), T packed query rows, head dimension d
- * (64 or 128). */
+ * (64 or 128).  longest: the most keys that a request has, 0 for as many as its
+ * row of the tables holds.  Only the choice of kernel goes by it (the lengths
+ * are on the device): a call is right whatever it says, and a close bound saves
+ * up to two thirds of a short one's time where the tables are long. */
 typedef struct kvx_attend_dims {
-  int32_t B, H, G, T, d;
+  int32_t B, H, G, T, d, longest;
 } kvx_attend_dims;
 
 /* Bytes of workspace kvx_attend_cache8 needs (0 for B == 0, T == 0 or invalid

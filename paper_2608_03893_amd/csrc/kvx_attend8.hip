@@ -575,9 +575,9 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
   }
 }
 
-// Which kernel: by what the host knows, rows, requests and the tables' length, which is at
-// least the longest request's.  Measured, us, with 8 KV heads, pages that no cache holds, B
-// requests of `rows` query rows a head over `keys` keys.
+// Which kernel: by what the host knows, rows, requests and a bound of the longest one (the
+// tables' length if the caller states none).  Measured, us, with 8 KV heads, pages that no
+// cache holds, B requests of `rows` query rows a head over `keys` keys.
 
 // By rows (bf16 only): blocks of 256 rows share the widened codes.  Pays from 96 rows a
 // request on where blocks are enough for the CUs or the work is, else its joins cost more.
@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
 bool may_go_by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G >= (int64_t)B * 96; }
 bool by_rows(const AttendArgs& a, int dtype, int d) {
   const int64_t rows = (int64_t)a.T * a.G, units = (rows / 256 > a.B ? rows / 256 : a.B) * a.H;
-  const double work = (double)rows * a.H * ((int64_t)a.M << a.log2p) * d;
+  const double work = (double)rows * a.H * a.keys * d;
   return may_go_by_rows(a.B, a.G, a.T, dtype) && (units >= 192 || work >= (units >= 128 ? 8589934592.0 : 17179869184.0));
 }
 
@@ -600,7 +600,7 @@ bool by_rows(const AttendArgs& a, int dtype, int d) {
 //   d = 64   B = 32, 32 rows, 5000 keys 50 / 40
 bool two_tiles(const AttendArgs& a, int dtype) {
   const int64_t rows = (int64_t)a.T * a.G, blocks = rows / 32 > a.B ? rows / 32 : a.B;
-  return dtype == 0 && rows > 16 * (int64_t)a.B && blocks * a.H * ((int64_t)a.M << a.log2p) >= 256 * 512;
+  return dtype == 0 && rows > 16 * (int64_t)a.B && (double)blocks * a.H * a.keys >= 256 * 512;
 }
 
 // One large workgroup a CU instead of several of four waves: a unit then has fewer partial
@@ -618,10 +618,10 @@ bool two_tiles(const AttendArgs& a, int dtype) {
 template <int NB, int LARGE>
 bool large_workgroups(const AttendArgs& a) {
   const int64_t rows = (int64_t)a.T * a.G, B = a.B, blocks = rows / (16 * NB) > B ? rows / (16 * NB) : B;
-  const int64_t units = blocks * a.H, keys = (int64_t)a.M << a.log2p;
+  const int64_t units = blocks * a.H, keys = a.keys;
   if (NB == 2) return units < 512 && keys >= 1024;
-  const int64_t least = units < 64 && rows < 4 * B ? 256 * 2048 : 256 * 256;
-  return rows <= 32 * B && units * keys >= least && (units < 512 || (LARGE >= 12 && keys > 1024));
+  const double least = units < 64 && rows < 4 * B ? 256 * 2048 : 256 * 256;
+  return rows <= 32 * B && (double)units * keys >= least && (units < 512 || (LARGE >= 12 && keys > 1024));
 }
 
 }  // namespace
@@ -636,13 +636,12 @@ size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
 
 template <int DT, int D, int W, int NB>
 static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  // no more workgroups than the tables' pages hold quanta for
-  const int64_t keys = (int64_t)a.M << a.log2p, quant = W * kStep;
-  const int64_t most = ((int64_t)a.T * a.G / (16 * NB) + a.B) * a.H * ((keys + quant - 1) / quant + kStart);
-  const int64_t want = (most + kLeast<W> - 1) / kLeast<W>;
-  const int64_t fill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
+  // no more workgroups than there can be quanta
+  constexpr int kFill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
+  const double units = ((double)a.T * a.G / (16 * NB) + a.B) * a.H, quant = W * kStep;
+  const double want = units * (a.keys / quant + 1 + kStart) / kLeast<W> + 1;
   int* counters = static_cast<int*>(ws);
-  const unsigned grid = (unsigned)((want < fill ? want : fill) + kXcds - 1) / kXcds * kXcds;
+  const unsigned grid = ((want < kFill ? (unsigned)want : kFill) + kXcds - 1) / kXcds * kXcds;
   hipLaunchKernelGGL((attend8_split_kernel<DT, D, W, NB>), dim3(grid), dim3(64 * W),
                      (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
   return hipGetLastError();

@@ -189,10 +189,10 @@ PyObject* store_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 // attend_cache8(q, pool, scales, block_tables, lens, cu, scale or None, out or None, with_lse,
-//               workspace or None, stream or None)
+//               workspace or None, stream or None, longest)
 PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  arguments(nargs, 11);
+  arguments(nargs, 12);
   const at::Tensor &q = tensor(args[0], "q"), &codes = tensor(args[1], "pool"), &scales = tensor(args[2], "scales");
   const at::Tensor &tables = tensor(args[3], "block_tables"), &lens = tensor(args[4], "lens"), &cu = tensor(args[5], "cu");
   TORCH_CHECK_VALUE(q.dim() == 3 && codes.dim() == 4 && tables.dim() == 2,
@@ -201,7 +201,8 @@ PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   TORCH_CHECK_VALUE(H >= 1 && heads % H == 0 && codes.size(3) == d, heads, " query heads of ", d,
                     " channels on a pool of ", H, " heads of ", codes.size(3));
   const kvx_pool pool = pool_of(codes, scales, {2, H}, size32(M));
-  const kvx_attend_dims dims{size32(B), size32(H), size32(heads / H), size32(T), size32(d)};
+  const kvx_attend_dims dims{size32(B), size32(H), size32(heads / H), size32(T), size32(d),
+                             size32(PyLong_AsLongLong(args[11]))};
   const kvx_dtype dtype = dtype_of(q);
   const void* q_at = rows_address(q, "q");
   const int64_t strides[2] = {q.stride(0), q.stride(1)};

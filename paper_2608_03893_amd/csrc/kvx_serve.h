@@ -46,6 +46,7 @@ struct AttendArgs {
   float* lse;               // [T, H * G] or nullptr
   float scale_log2;         // score factor times log2(e): softmax in powers of two
   int32_t B, H, G, T, M, N, log2p;
+  int64_t keys;             // most a request has, as far as the host knows: for the choice of kernel
 };
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream);
 size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);

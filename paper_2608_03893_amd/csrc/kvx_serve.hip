@@ -214,6 +214,7 @@ static kvx_status check_attend(const kvx_attend_dims* dims, kvx_dtype dtype) {
   if ((st = check_requests(dims->B, dims->T)) != KVX_OK) return st;
   if (dims->H < 1 || dims->G < 1)
     return set_error(KVX_ERR_SHAPE, "H=%d and G=%d must be at least 1", dims->H, dims->G);
+  if (dims->longest < 0) return set_error(KVX_ERR_SHAPE, "longest=%d is negative", dims->longest);
   if ((int64_t)dims->H * dims->G > 65535 || (int64_t)dims->T * dims->G >= ((int64_t)1 << 30))
     return set_error(KVX_ERR_UNSUPPORTED, "H*G=%lld exceeds 65535 or T*G=%lld reaches 2^30",
                      (long long)dims->H * dims->G, (long long)dims->T * dims->G);
@@ -287,6 +288,8 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
   a.M = pool->max_pages;
   a.N = pool->num_pages;
   a.log2p = log2p;
+  a.keys = (int64_t)a.M << log2p;
+  if (m.longest > 0 && m.longest < a.keys) a.keys = m.longest;
   const hipError_t e = kvx::launch_attend(a, dt, m.d, workspace, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
   return ok();

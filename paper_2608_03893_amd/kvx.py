@@ -85,7 +85,7 @@ class Pool(ctypes.Structure):
 class AttendDims(ctypes.Structure):
     """kvx_attend_dims: sizes of an attention call over the 8-bit pool."""
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("G", ctypes.c_int32),
-                ("T", ctypes.c_int32), ("d", ctypes.c_int32)]
+                ("T", ctypes.c_int32), ("d", ctypes.c_int32), ("longest", ctypes.c_int32)]
 
 
 class Rope(ctypes.Structure):
@@ -675,7 +675,7 @@ def _attend_dims(q, pool, block_tables):
     H = pool.shape[1]
     if H < 1 or heads % H or pool.shape[3] != d:
         raise ValueError(f"{heads} query heads of {d} channels on a pool of {H} heads of {pool.shape[3]}")
-    return AttendDims(block_tables.shape[0], H, heads // H, T, d)
+    return AttendDims(block_tables.shape[0], H, heads // H, T, d, 0)
 
 
 def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
@@ -694,16 +694,18 @@ def attend_workspace(q, pool, block_tables, stream=None):
 
 
 def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None, with_lse=False,
-                  workspace=None, stream=None):
+                  workspace=None, stream=None, longest=0):
     """Causal attention of the newest tokens over one layer of the 8-bit pool
     (enqueued on the stream); returns out [T, H*G, d], with_lse also lse [T, H*G].
 
     q [T, H*G, d] bf16 or fp32 (d dense); pool [2, H, num_slots, d], scales
     [2, H, num_pages]; block_tables [B, max_pages], lens [B] (tokens in the pool,
     the new ones included), cu [B + 1] (their rows in q) int32; scale: factor of
-    the scores, 1 / sqrt(d) by default."""
+    the scores, 1 / sqrt(d) by default; longest: the most keys of a request, if the
+    host knows it (only the kernel's choice goes by it, else by max_pages)."""
     f = (_BIND or _native()).attend_cache8
     if stream is None:
-        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, None)
+        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, None, longest)
     with torch.cuda.stream(stream):
-        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, stream.cuda_stream)
+        return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, stream.cuda_stream,
+                 longest)

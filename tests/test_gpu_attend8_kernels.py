@@ -268,6 +268,20 @@ def test_far_pages_strides_streams_and_graphs(gpu_kvx, kernel):
     _compare(c, out, lse, 128 ** -0.5, f"{kernel} far pages")
 
 
+@pytest.mark.parametrize("lens,news,H,G", [([300, 40, 7], [1, 1, 1], 8, 4), ([300, 140], [2, 9], 2, 4),
+                                           ([300, 140], [130, 140], 2, 4), ([3, 0, 2000], [3, 1, 700], 4, 8)])
+def test_a_stated_bound_changes_the_kernel_only(gpu_kvx, lens, news, H, G):
+    """Whatever bound is stated, one that a request passes too."""
+    rng = np.random.default_rng(37)
+    c = _wide(_case(rng, lens, news, H, G, 64, 16, "bf16"), 2 ** 16)
+    for longest in (max(lens), 1, 2 ** 31 - 1, 0):
+        out, lse = gpu_kvx.attend_cache8(*_gpu(c), with_lse=True, longest=longest)
+        torch.cuda.synchronize()
+        _compare(c, out, lse, 0.125, f"longest={longest} lens={lens}")
+    with pytest.raises(gpu_kvx.KvxError):
+        gpu_kvx.attend_cache8(*_gpu(c), longest=-1)
+
+
 def test_a_workspace_serves_all_kernels(gpu_kvx):
     rng = np.random.default_rng(36)
     cases = [KERNELS[k](_case(rng, [900, 230], _news(k, [1, 2], [1, 130]), 2, 4, 128, 16, "bf16")) for k in KERNELS]
