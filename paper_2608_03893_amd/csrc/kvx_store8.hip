@@ -162,14 +162,16 @@ __global__ void __launch_bounds__(64 * kWaves) store8_kernel(StoreArgs a, int wi
 
 template <int DT, int D>
 hipError_t launch(const StoreArgs& a, hipStream_t stream) {
-  // A wave's window is a page of rows, or less where that would leave most of the chip idle;
+  // A wave's window is a page of rows, or less where waves would be fewer than 8 a CU (rows of
+  // one page each would wait for one another: 512 single rows of 8 heads 10.0 us with 4 a CU,
+  // 7.4 with 8, 6.5 with 32; but waves without a page cost too: 2048 rows 7.2, 8.5, 14.3);
   // up to eight pages of 2 KB or less, where waves are many (d = 64, 16-token pages, 8192 rows
   // of 64 layers 455 -> 400 us; pages of 4 KB 608 -> 623).
   const int64_t planes = (int64_t)a.L * 2 * a.H;
   const int loads = (D / Vec<DT>::N << a.log2p) / 64;
   int window = 1 << a.log2p;
   for (int i = 0; i < 3 && loads <= 2 && planes * (a.T / (2 * window)) >= 32768; ++i) window *= 2;
-  while (window > 1 && planes * ((a.T + window - 1) / window) < 8192) window /= 2;
+  while (window > 1 && planes * ((a.T + window - 1) / window) < 2048) window /= 2;
   const int n = (a.T + window - 1) / window;
   const int64_t wg = (planes * n + kWaves - 1) / kWaves;
   if (wg >= (int64_t)1 << 31) return hipErrorInvalidValue;
