@@ -34,9 +34,9 @@ constexpr int kLeast = W > 4 ? 1 : 2;      // least quanta of a workgroup
 constexpr int kStart = 2;                  // weight of a unit's start, in quanta
 constexpr int kSmall = 10;                 // a unit is not split if it weighs no more than this
 constexpr int kSplit = 5;                  // and than a share and what a join costs
-constexpr int kJoin = 64;                  // partial sums joined at a time
-template <int NB>
-constexpr int kFlying = NB == 2 ? 8 : 12;  // of which a thread has these in flight
+constexpr int kJoin = 64;                  // most partial sums joined at a time
+template <int D, int NB>
+constexpr int kFlying = NB == 2 ? 8 : D == 64 ? 10 : 12;  // of which a thread has these in flight
 // Waves a SIMD: as many as the registers hold.  More of them hide more of a unit's start
 // (lengths, pages, scales, rows: loads that wait for one another) than prefetching
 // within a wave: 64 ragged requests 86 us with two and the next step's loads in flight,
@@ -68,7 +68,7 @@ struct Stage {
 // W waves: 4, and kOcc workgroups a CU; or kLarge, and one.
 template <int DT, int D, int W, int NB>
 __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
-  constexpr int kFly = kFlying<NB>;
+  constexpr int kFly = kFlying<D, NB>;
   constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep, kRows = 16 * NB;
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
   static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
     const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
     bool done = g0 == g1 || quanta + kStart <= small;
     if (!done) {
-      const int parts = g1 - g0 + 1, mine_at = me - g0;
+      const int parts = uniform(g1 - g0) + 1, mine_at = uniform(me - g0);
       auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
       // Partial sums pass between workgroups on different XCDs, each with its own L2: they
       // are written through and read past it (agent scope), which spares the write-back
@@ -540,16 +540,21 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
         }
       };
       put(mine_at);
-      const int group = mine_at / kJoin, groups = (parts + kJoin - 1) / kJoin;
-      const int in_group = parts - group * kJoin < kJoin ? parts - group * kJoin : kJoin;
-      if (arrive(counters + 2 * slot(group * kJoin), in_group, &last)) {
-        join(group * kJoin, 1, in_group);
+      // Many partial sums are joined in two levels, by groups side by side, where one workgroup
+      // would read 128 KB or more (16 rows of 16000 keys 29 -> 22 us; one row 12 against 15).
+      int width = uniform(parts);
+      if (width > kJoin || (width > kJoin / 2 && width * uniform(valid) * D > 32768))
+        for (width = 6; width * width < parts; ++width) {}
+      const int group = mine_at / width, groups = (parts + width - 1) / width;
+      const int in_group = parts - group * width < width ? parts - group * width : width;
+      if (arrive(counters + 2 * slot(group * width), in_group, &last)) {
+        join(group * width, 1, in_group);
         done = groups == 1;
         if (!done) {
           __syncthreads();       // all have read the partial sums that put overwrites
-          put(group * kJoin);
+          put(group * width);
           if (arrive(counters + 2 * slot(0) + 1, groups, &last)) {
-            join(0, kJoin, groups);
+            join(0, width, groups);
             done = true;
           }
         }
