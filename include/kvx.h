@@ -558,11 +558,11 @@ size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
  *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned; filled with
  *                  zeros before its first use (it holds counters, which every call
  *                  leaves at zero); calls of any sizes may follow one another in it
- * Scores, softmax statistics and sums are held in fp32.  For bf16 queries the
- * probabilities (times the page's value scale) are rounded to bf16 before their
- * product with the values, and in large chunks so may be the values where their
- * scale is no power of two; for fp32 queries both products carry the operands'
- * 24 bits.  Codes enter exactly. */
+ * Scores, softmax statistics and sums are held in fp32.  The probabilities (times
+ * the page's value scale) enter their product with the values with 16 bits for
+ * bf16 queries, so that the output's own rounding is the only one that counts, and
+ * with 24 for fp32 queries; in large chunks of bf16 queries values are rounded to
+ * bf16 where their scale is no power of two.  Codes enter exactly. */
 kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype,
                              const void* q, const int64_t* q_strides, const uint8_t* codes,
                              const float* scales, const int32_t* block_tables,

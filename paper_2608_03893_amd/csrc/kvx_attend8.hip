@@ -6,8 +6,8 @@
 // row's scores for 4 keys, so the softmax needs no exchange but the maximum over four
 // lanes, and P^T has the layout that O^T = V^T P^T takes as its second operand.  e4m3
 // codes are bf16 numbers, so K and V enter exactly; a page's scales multiply the scores
-// and the probabilities.  fp32 queries and probabilities enter as three bf16 terms, which
-// hold all 24 bits.
+// and the probabilities.  fp32 queries and their probabilities enter as three bf16 terms, which
+// hold all 24 bits, the probabilities of bf16 queries as two.
 //
 // Bound by the bytes of K and V, which go from memory straight to registers, each once:
 // a lane reads 16 bytes of one key's row, or 8 bytes of 8 value rows whose bytes it then
@@ -70,7 +70,8 @@ template <int DT, int D, int W, int NB>
 __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
   constexpr int kFly = kFlying<D, NB>;
   constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep, kRows = 16 * NB;
-  constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, C = D / 16;   // C: channel tiles
+  constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, PT = kTerms<DT>;    // terms of queries, probabilities
+  constexpr int C = D / 16;                                        // channel tiles
   static_assert(kJoin % 16 == 0 && kJoin * kRows <= kRows * (D + 4), "weights of a join fit one wave's sums");
   constexpr int RS = D + 4;                                        // row stride in LDS
   constexpr int SLOT = kRows * (D + 2);                            // floats of a partial sum
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
             for (int c = 0; c < C; ++c) o[i][c] *= keep;
           }
         }
-        bf16x8_t pf[NB][TERMS];
+        bf16x8_t pf[NB][PT];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           const float ref = m[i] == -INFINITY ? 0.0f : m[i];
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] *= j < 4 ? v0 : v1;
-          split_terms<TERMS>(p, pf[i]);
+          split_terms<PT>(p, pf[i]);
         }
 #pragma unroll
         for (int w = 0; w < U; ++w) {
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
-              for (int e = 0; e < TERMS; ++e)
+              for (int e = 0; e < PT; ++e)
                 o[i][4 * w + c] = mfma(__builtin_bit_cast(bf16x8_t, f), pf[i][e], o[i][4 * w + c]);
           }
         }

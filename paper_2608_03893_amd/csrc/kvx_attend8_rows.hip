@@ -10,9 +10,10 @@
 // A value's scale is applied as the code is widened (a power of two is exact there).
 //
 // Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them:
-// 2048 new tokens of 64 heads over 10240 keys, d = 128, 615 us, 1000 TFLOP/s, where a large
-// product of the library reaches 1230.  To form a step's scores beside the exponentials of
-// the step before took as long (a quarter more products of keys, and 8% more time).
+// 2048 new tokens of 64 heads over 10240 keys, d = 128, 815 us: 760 TFLOP/s, and 1140 with the
+// products of the probabilities' second term, where a large product of the library reaches
+// 1230.  With one term, to form a step's scores beside the exponentials of the step before took
+// as long (a quarter more products of keys, and 8% more time).
 //
 // One workgroup a CU; each takes an equal share of the weight of all (request, head, block
 // of rows), a block's weight being the keys that its last row sees.  Neighbouring
@@ -367,25 +368,25 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
             for (int t = 0; t < 2; ++t) x[t][i] += shift;
           }
         }
-        bf16x8_t p[NB];
+        bf16x8_t p[NB][kTerms<0>];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          u32x4_t w;
+          float y[8];
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[t][i][e] = __builtin_amdgcn_exp2f(x[t][i][e]);
-            l[i] += (x[t][i][0] + x[t][i][1]) + (x[t][i][2] + x[t][i][3]);
-            w[2 * t] = pack2(x[t][i][0], x[t][i][1]);
-            w[2 * t + 1] = pack2(x[t][i][2], x[t][i][3]);
+            for (int e = 0; e < 4; ++e) y[4 * t + e] = __builtin_amdgcn_exp2f(x[t][i][e]);
+            l[i] += (y[4 * t] + y[4 * t + 1]) + (y[4 * t + 2] + y[4 * t + 3]);
           }
-          p[i] = __builtin_bit_cast(bf16x8_t, w);
+          split_terms<kTerms<0>>(y, p[i]);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int i = 0; i < NB; ++i) o[i][c] = mfma(__builtin_bit_cast(bf16x8_t, f[(KF + c) % kRing]), p[i], o[i][c]);
+          for (int e = 0; e < kTerms<0>; ++e)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) o[i][c] = mfma(__builtin_bit_cast(bf16x8_t, f[(KF + c) % kRing]), p[i][e], o[i][c]);
           f[(KF + c) % kRing] = KF + c + kRing < F ? from[(KF + c + kRing) * 64] : next[(KF + c + kRing - F) * 64];
         }
         __builtin_amdgcn_sched_barrier(0);
