@@ -7,7 +7,8 @@
 // LDS, whole operands one after another, so that reads and writes of LDS are 16 bytes a
 // lane without conflicts.  Two such buffers: while the waves compute on one, the loads of
 // the next are in flight.  The products are those of the split kernel (kvx_attend8.hip).
-// A value's scale is applied as the code is widened (a power of two is exact there).
+// A value's scale is applied as the code is widened where it is a power of two, which is exact
+// there, and else to the probabilities.
 //
 // Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them:
 // 2048 new tokens of 64 heads over 10240 keys, d = 128, 815 us: 760 TFLOP/s, and 1140 with the
@@ -55,8 +56,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
   constexpr int SLOT = kWaves * NB * (4 * C + 2) * 64;            // floats of a partial sum
   __shared__ __attribute__((aligned(16))) u32x4_t kv[2][kSteps][F][64];
   __shared__ float ksc[2][kSteps][2];       // scale of the scores of a 16-key tile
-  // [0], bit t: tile t has no page; [1]: some value is NaN (where rows of the block differ
-  // in what they see)
+  __shared__ float vsc[2][kSteps][2];       // what its probabilities have yet to be multiplied by
+  // [0], bit t: tile t has no page; [1], bit 0: some value is NaN (where rows of the block
+  // differ in what they see), bit 1: vsc is not one
   __shared__ int flags[2][kSteps][2];
   __shared__ uint32_t nans[2][kSteps][U][64];   // which
   __shared__ int64_t part[kWaves];
@@ -222,7 +224,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
           }
         }
         nan = __any(nan);
-        if (lane == 0) flags[buf][step_of][1] = nan;
         if (nan) {      // kept apart where rows differ in what they see: bit 4 j + i is key j, byte i
 #pragma unroll
           for (int w = 0; w < U; ++w) {
@@ -237,33 +238,29 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
           }
         }
         // powers of two, normal and positive, are applied with the conversion
-        const bool exact = ((__float_as_uint(s0) | __float_as_uint(s1)) & 0x807fffffu) == 0 &&
-                           fminf(s0, s1) >= 0x1p-126f;
-        auto operands = [&](auto by) {
+        auto exact = [](float s) { return (__float_as_uint(s) & 0x807fffffu) == 0 && s >= 0x1p-126f; };
+        const float f0 = exact(s0) ? s0 : 1.0f, f1 = exact(s1) ? s1 : 1.0f;
+        if (lane == 0) {
+          vsc[buf][step_of][0] = exact(s0) ? 1.0f : s0;
+          vsc[buf][step_of][1] = exact(s1) ? 1.0f : s1;
+          flags[buf][step_of][1] = (nan ? 1 : 0) | (exact(s0) && exact(s1) ? 0 : 2);
+        }
 #pragma unroll
-          for (int w = 0; w < U; ++w) {
-            uint32_t y[4][2];   // keys 2 j, 2 j + 1 of channels (c, c + 1 | c + 2, c + 3)
+        for (int w = 0; w < U; ++w) {
+          uint32_t y[4][2];   // keys 2 j, 2 j + 1 of channels (c, c + 1 | c + 2, c + 3)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              y[j][0] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x05010400u);
-              y[j][1] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x07030602u);
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              u32x4_t f;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) f[j] = by(y[j][c >> 1], c & 1, j < 2 ? s0 : s1);
-              kv[buf][step_of][KF + 4 * w + c][lane] = f;
-            }
+          for (int j = 0; j < 4; ++j) {
+            y[j][0] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x05010400u);
+            y[j][1] = __builtin_amdgcn_perm(st[(2 * j + 1) * U + w], st[2 * j * U + w], 0x07030602u);
           }
-        };
-        if (exact) {
-          operands([](uint32_t w, bool half, float s) { return half ? bf16_pair_by<true>(w, s) : bf16_pair_by<false>(w, s); });
-        } else {   // a caller's own scale: rounded to bf16 once more
-          operands([](uint32_t w, bool half, float s) {
-            const uint32_t f = half ? bf16_pair<true>(w) : bf16_pair<false>(w);
-            return pack2(lo_bf16(f) * s, hi_bf16(f) * s);
-          });
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            u32x4_t f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              f[j] = c & 1 ? bf16_pair_by<true>(y[j][c >> 1], j < 2 ? f0 : f1) : bf16_pair_by<false>(y[j][c >> 1], j < 2 ? f0 : f1);
+            kv[buf][step_of][KF + 4 * w + c][lane] = f;
+          }
         }
       }
     };
@@ -284,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
         if ((s >> 1 ^ wave >> 2) & 1) __builtin_amdgcn_s_setprio(1);
         else __builtin_amdgcn_s_setprio(0);
         const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};
-        const int bad = uniform(flags[buf][s][0]), nan = uniform(flags[buf][s][1]);
+        const int bad = uniform(flags[buf][s][0]), vflags = uniform(flags[buf][s][1]), nan = vflags & 1;
         const u32x4_t* next = s + 1 < kSteps ? from + F * 64 : from;   // the last step's are not used
         f32x4_t x[2][NB];
 #pragma unroll
@@ -377,6 +374,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[4 * t + e] = __builtin_amdgcn_exp2f(x[t][i][e]);
             l[i] += (y[4 * t] + y[4 * t + 1]) + (y[4 * t + 2] + y[4 * t + 3]);
+          }
+          if (vflags & 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] *= vsc[buf][s][j >> 2];
           }
           split_terms<kTerms<0>>(y, p[i]);
         }

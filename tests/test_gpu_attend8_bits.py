@@ -52,3 +52,19 @@ def test_outputs_are_rounded_once(gpu_kvx, kernel, d):
     out = gpu_kvx.attend_cache8(*_gpu(c))
     torch.cuda.synchronize()
     _rounded_once(c, out, d ** -0.5, f"rounded once, {kernel} d={d}")
+
+
+@pytest.mark.parametrize("kernel", SHAPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_own_scales_are_not_rounded(gpu_kvx, kernel, d):
+    """A caller's scales that are no powers of two, with equal probabilities, so that nothing
+    else is rounded before the output is."""
+    lens, news, G, M = SHAPES[kernel]
+    rng = np.random.default_rng(500 + d)
+    c = _case(rng, lens, news, 2, G, d, 16, "bf16", q_scale=0.0)
+    own = rng.integers(0, 2, c["scales"].shape)      # beside powers of two
+    c["scales"] = (c["scales"] * (1 + own * rng.uniform(0, 1, own.shape))).astype(np.float32).astype(np.float64)
+    c = c if M is None else _wide(c, M)
+    out = gpu_kvx.attend_cache8(*_gpu(c))
+    torch.cuda.synchronize()
+    _rounded_once(c, out, d ** -0.5, f"own scales, {kernel} d={d}")
