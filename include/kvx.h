@@ -561,7 +561,9 @@ size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
  * Scores, softmax statistics and sums are held in fp32.  The probabilities (times
  * the page's value scale) enter their product with the values with 16 bits for
  * bf16 queries, so that the output's own rounding is the only one that counts, and
- * with 24 for fp32 queries.  Codes enter exactly. */
+ * with 24 for fp32 queries.  Codes enter exactly.  A NaN code, and a value scale
+ * that is NaN or infinite, make NaN in the rows that see a key of theirs, and leave
+ * the other rows as they are. */
 kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype,
                              const void* q, const int64_t* q_strides, const uint8_t* codes,
                              const float* scales, const int32_t* block_tables,

@@ -263,9 +263,13 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
         }
         const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa));
         const int p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
-        const float v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa)));
-        const float v1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa) + 1));
+        float v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa)));
+        float v1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa) + 1));
         if (p0 < 0 || p1 < 0 || key + kStep - 1 > lim_lo) {
+          // values under a scale that is infinite or NaN are NaN
+          const bool lost[2] = {!finite(v0), !finite(v1)};
+          v0 = lost[0] ? 1.0f : v0;
+          v1 = lost[1] ? 1.0f : v1;
           bool nan = false;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -275,6 +279,7 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
             for (int e = 0; e < 4; ++e)
 #pragma unroll
               for (int w = 0; w < U; ++w) {
+                if (lost[t]) s.v[4 * t + e][w] = kNan4;
                 s.v[4 * t + e][w] = e > real ? 0 : s.v[4 * t + e][w];     // nobody's codes
                 nan |= e4m3_nan(s.v[4 * t + e][w]) != 0;
               }

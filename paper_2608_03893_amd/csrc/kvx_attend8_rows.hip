@@ -197,8 +197,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
     auto widen = [&](int q, int buf) {
       const int key = q * kQuant + step_of * kStep;
       const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa)), p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
-      const float s0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa)));
-      const float s1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa) + 1));
+      float s0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa)));
+      float s1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), 2 * (q - qa) + 1));
       if (wave < 4) {
 #pragma unroll
         for (int i = 0; i < 2 * U; ++i) {
@@ -213,11 +213,16 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
       } else {
         bool nan = false;
         if (p0 < 0 || p1 < 0 || key + kStep - 1 > block_lo) {
+          // values under a scale that is infinite or NaN are NaN
+          const bool lost0 = !finite(s0), lost1 = !finite(s1);
+          s0 = lost0 ? 1.0f : s0;
+          s1 = lost1 ? 1.0f : s1;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const bool real = (j < 4 ? p0 : p1) >= 0 && key + 16 * (j >> 2) + 4 * g4 + (j & 3) < r.len;
 #pragma unroll
             for (int w = 0; w < U; ++w) {
+              if (j < 4 ? lost0 : lost1) st[j * U + w] = kNan4;
               if (!real) st[j * U + w] = 0;
               nan |= e4m3_nan(st[j * U + w]) != 0;
             }
@@ -238,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
           }
         }
         // powers of two, normal and positive, are applied with the conversion
-        auto exact = [](float s) { return (__float_as_uint(s) & 0x807fffffu) == 0 && s >= 0x1p-126f; };
+        auto exact = [](float s) { return (__float_as_uint(s) & 0x807fffffu) == 0 && s >= 0x1p-126f && finite(s); };
         const float f0 = exact(s0) ? s0 : 1.0f, f1 = exact(s1) ? s1 : 1.0f;
         if (lane == 0) {
           vsc[buf][step_of][0] = exact(s0) ? 1.0f : s0;

@@ -33,6 +33,10 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float x0, float x1, float x2, floa
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, w, true);
 }
 
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+constexpr uint32_t kNan4 = 0x7f7f7f7fu;   // four NaN codes
+
 // The top bit of each byte that is NaN (all ones but the sign).
 __device__ __forceinline__ uint32_t e4m3_nan(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
