@@ -535,7 +535,8 @@ typedef struct kvx_attend_dims {
 } kvx_attend_dims;
 
 /* Bytes of workspace kvx_attend_cache8 needs (0 for B == 0, T == 0 or invalid
- * arguments). */
+ * arguments), and how many of them, the first, have to be zero once. */
+#define KVX_ATTEND_COUNTER_BYTES 16384
 size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
 
 /* Causal attention of each request's newest tokens over its keys and values in
@@ -555,9 +556,10 @@ size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
  *   scale          factor of the scores (1 / sqrt(d) in most models), finite
  *   out            [T, H * G, d] in q's type
  *   lse            fp32 [T, H * G] or NULL
- *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned; filled with
- *                  zeros before its first use (it holds counters, which every call
- *                  leaves at zero); calls of any sizes may follow one another in it
+ *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned; its first
+ *                  KVX_ATTEND_COUNTER_BYTES are zero before its first use (counters,
+ *                  which every call leaves at zero; the rest may hold anything);
+ *                  calls of any sizes may follow one another in it
  * Scores, softmax statistics and sums are held in fp32.  The probabilities (times
  * the page's value scale) enter their product with the values with 16 bits for
  * bf16 queries, so that the output's own rounding is the only one that counts, and

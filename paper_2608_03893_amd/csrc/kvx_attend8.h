@@ -20,6 +20,7 @@ __device__ __forceinline__ int xcd_order(int block, int grid) {
 // Arrival counters, first in the workspace (four for each workgroup of the largest grid):
 // all kernels keep them there and leave them at zero, and partial sums behind.
 constexpr int kCounters = 4 * 1024;
+static_assert(kCounters * sizeof(int) == KVX_ATTEND_COUNTER_BYTES, "what a caller clears");
 
 // Largest / sum of a value over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quad_max(float v) {

@@ -8,7 +8,6 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
-#include <ATen/ops/zeros.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -215,8 +214,9 @@ PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (PyErr_Occurred()) throw python_error();
   at::Tensor out, lse, workspace;
   if (args[9] == Py_None) {
-    const size_t need = attend_workspace_bytes_entry(&dims, dtype);
-    workspace = at::zeros({(int64_t)(need > 0 ? need : 1)}, q.options().dtype(at::kByte));
+    const int64_t need = (int64_t)attend_workspace_bytes_entry(&dims, dtype);
+    workspace = at::empty({need > 0 ? need : 1}, q.options().dtype(at::kByte));
+    if (need > 0) workspace.narrow(0, 0, KVX_ATTEND_COUNTER_BYTES).zero_();
   } else {
     workspace = tensor(args[9], "workspace");
   }

@@ -38,6 +38,7 @@ FLAG_WEIGHTS_PACKED = 2
 FLAG_KEYS_STRIPPED = 4
 FLAG_PLANES_READY = 8
 SCRATCH_MAX_BYTES = 256 << 20   # KVX_SCRATCH_MAX_BYTES of include/kvx.h
+ATTEND_COUNTER_BYTES = 16384    # KVX_ATTEND_COUNTER_BYTES
 
 STATUS = {
     0: "KVX_OK", 1: "KVX_ERR_NULL", 2: "KVX_ERR_SHAPE", 3: "KVX_ERR_INDEX",
@@ -686,11 +687,13 @@ def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
 
 def attend_workspace(q, pool, block_tables, stream=None):
     """A workspace for attend_cache8 calls of these shapes, to be kept between them
-    (zeros, as its first use needs)."""
+    (its counters cleared, as the first use needs)."""
     need = int(load().kvx_attend_workspace_bytes(
         ctypes.byref(_attend_dims(q, pool, block_tables)), _dtype_code(q)))
     with torch.cuda.stream(_torch_stream(stream, q.device)):
-        return torch.zeros(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace[:ATTEND_COUNTER_BYTES].zero_()
+        return workspace
 
 
 def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None, with_lse=False,
@@ -702,7 +705,8 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     [2, H, num_pages]; block_tables [B, max_pages], lens [B] (tokens in the pool,
     the new ones included), cu [B + 1] (their rows in q) int32; scale: factor of
     the scores, 1 / sqrt(d) by default; longest: the most keys of a request, if the
-    host knows it (only the kernel's choice goes by it, else by max_pages)."""
+    host knows it (only the kernel's choice goes by it, else by max_pages); workspace:
+    an attend_workspace that calls on one stream share, else one is made for the call."""
     f = (_BIND or _native()).attend_cache8
     if stream is None:
         return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, None, longest)
