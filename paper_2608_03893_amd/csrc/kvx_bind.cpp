@@ -8,6 +8,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -36,23 +37,32 @@ int32_t size32(int64_t n) {
   return (int32_t)n;
 }
 
-void* address(const at::Tensor& t, const char* name) {
-  TORCH_CHECK_VALUE(t.is_cuda(), name, " must live on the GPU");
+// The device of a call, that of one of its tensors; the others have to live there too.
+struct Place {
+  at::Device device;
+  void check(const at::Tensor& t, const char* name) const {
+    TORCH_CHECK_VALUE(t.is_cuda(), name, " must live on the GPU");
+    TORCH_CHECK_VALUE(t.device() == device, name, " lives on ", t.device(), ", other operands on ", device);
+  }
+};
+
+void* address(const Place& place, const at::Tensor& t, const char* name) {
+  place.check(t, name);
   TORCH_CHECK_VALUE(t.is_contiguous(), name, " must be contiguous");
   return t.data_ptr();
 }
 
 // A tensor whose last dimension is dense, whatever its other strides.
-const void* rows_address(const at::Tensor& t, const char* name) {
-  TORCH_CHECK_VALUE(t.is_cuda(), name, " must live on the GPU");
+const void* rows_address(const Place& place, const at::Tensor& t, const char* name) {
+  place.check(t, name);
   TORCH_CHECK_VALUE(t.stride(-1) == 1 || t.size(-1) <= 1, name, " must be dense in its last dimension");
   return t.data_ptr();
 }
 
-int32_t* int32_at(const at::Tensor& t, const char* name, at::IntArrayRef shape) {
+int32_t* int32_at(const Place& place, const at::Tensor& t, const char* name, at::IntArrayRef shape) {
   TORCH_CHECK_VALUE(t.scalar_type() == at::kInt && t.sizes() == shape, name, " must be int32 ", shape, ", got ",
                     t.scalar_type(), ' ', t.sizes());
-  return static_cast<int32_t*>(address(t, name));
+  return static_cast<int32_t*>(address(place, t, name));
 }
 
 kvx_dtype dtype_of(const at::Tensor& t) {
@@ -84,8 +94,11 @@ void* stream_of(PyObject* raw, const at::Tensor& t) {
   return s;
 }
 
+// On the operands' device: a launch on its default stream, whose handle is 0, would go to the
+// current device else.
 template <typename F, typename... A>
-void call(F entry, A... a) {
+void call(const Place& place, F entry, A... a) {
+  const c10::DeviceGuard guard(place.device);
   kvx_status status;
   Py_BEGIN_ALLOW_THREADS
   status = entry(a...);
@@ -123,9 +136,10 @@ PyObject* plan_pages(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (PyErr_Occurred()) throw python_error();
   const int64_t B = tables.size(0), M = tables.size(1), N = ring.size(0);
   const kvx_pool pool{size32(N), size32(page_size), size32(M)};
-  const int32_t *lens_at = int32_at(lens, "lens", {B}), *add_at = int32_at(add, "add", {B});
-  int32_t *tables_at = int32_at(tables, "block_tables", {B, M}), *ring_at = int32_at(ring, "free_ring", {N});
-  const int32_t* free_at = static_cast<const int32_t*>(address(free, "free"));
+  const Place place{lens.device()};
+  const int32_t *lens_at = int32_at(place, lens, "lens", {B}), *add_at = int32_at(place, add, "add", {B});
+  int32_t *tables_at = int32_at(place, tables, "block_tables", {B, M}), *ring_at = int32_at(place, ring, "free_ring", {N});
+  const int32_t* free_at = static_cast<const int32_t*>(address(place, free, "free"));
   int32_t* outs[5];   // lens, cu, positions, slots, free
   const int64_t shape[5] = {B, B + 1, T, T, 4};
   PyObject* result = nullptr;
@@ -148,12 +162,12 @@ PyObject* plan_pages(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   } else {
     static const char* const names[5] = {"lens", "cu", "positions", "slots", "free"};
     TORCH_CHECK_TYPE(PyTuple_Check(args[7]) && PyTuple_GET_SIZE(args[7]) == 5, "out must be a PagePlan");
-    for (int i = 0; i < 5; ++i) outs[i] = int32_at(tensor(PyTuple_GET_ITEM(args[7], i), names[i]), names[i], {shape[i]});
+    for (int i = 0; i < 5; ++i) outs[i] = int32_at(place, tensor(PyTuple_GET_ITEM(args[7], i), names[i]), names[i], {shape[i]});
     result = args[7];
     Py_INCREF(result);
   }
   try {
-    call(plan_pages_entry, &pool, size32(B), size32(T), lens_at, add_at, tables_at, ring_at, free_at, outs[0], outs[1],
+    call(place, plan_pages_entry, &pool, size32(B), size32(T), lens_at, add_at, tables_at, ring_at, free_at, outs[0], outs[1],
          outs[2], outs[3], outs[4], stream_of(args[8], lens));
   } catch (...) {
     Py_DECREF(result);
@@ -174,13 +188,14 @@ PyObject* store_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t L = k.size(0), H = k.size(1), T = k.size(2), d = k.size(3);
   const kvx_pool pool = pool_of(codes, scales, {L, 2, H}, 1);
   TORCH_CHECK_VALUE(codes.size(4) == d, "pool rows have ", codes.size(4), " channels, k and v ", d);
+  const Place place{k.device()};
   const int64_t ks[3] = {k.stride(0), k.stride(1), k.stride(2)}, vs[3] = {v.stride(0), v.stride(1), v.stride(2)};
   const kvx_dtype dtype = dtype_of(k);
-  const void *k_at = rows_address(k, "k"), *v_at = rows_address(v, "v");
-  const int32_t* slots_at = int32_at(slots, "slot_mapping", {T});
-  uint8_t* codes_at = static_cast<uint8_t*>(address(codes, "pool"));
-  float* scales_at = static_cast<float*>(address(scales, "scales"));
-  call(store_cache8_entry, &pool, dtype, size32(L), size32(H), size32(T), size32(d), k_at, ks, v_at, vs, slots_at,
+  const void *k_at = rows_address(place, k, "k"), *v_at = rows_address(place, v, "v");
+  const int32_t* slots_at = int32_at(place, slots, "slot_mapping", {T});
+  uint8_t* codes_at = static_cast<uint8_t*>(address(place, codes, "pool"));
+  float* scales_at = static_cast<float*>(address(place, scales, "scales"));
+  call(place, store_cache8_entry, &pool, dtype, size32(L), size32(H), size32(T), size32(d), k_at, ks, v_at, vs, slots_at,
        codes_at, scales_at, stream_of(args[5], k));
   Py_INCREF(args[3]);
   return args[3];
@@ -203,12 +218,13 @@ PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const kvx_attend_dims dims{size32(B), size32(H), size32(heads / H), size32(T), size32(d),
                              size32(PyLong_AsLongLong(args[11]))};
   const kvx_dtype dtype = dtype_of(q);
-  const void* q_at = rows_address(q, "q");
+  const Place place{q.device()};
+  const void* q_at = rows_address(place, q, "q");
   const int64_t strides[2] = {q.stride(0), q.stride(1)};
-  const uint8_t* codes_at = static_cast<const uint8_t*>(address(codes, "pool"));
-  const float* scales_at = static_cast<const float*>(address(scales, "scales"));
-  const int32_t *tables_at = int32_at(tables, "block_tables", {B, M}), *lens_at = int32_at(lens, "lens", {B});
-  const int32_t* cu_at = int32_at(cu, "cu", {B + 1});
+  const uint8_t* codes_at = static_cast<const uint8_t*>(address(place, codes, "pool"));
+  const float* scales_at = static_cast<const float*>(address(place, scales, "scales"));
+  const int32_t *tables_at = int32_at(place, tables, "block_tables", {B, M}), *lens_at = int32_at(place, lens, "lens", {B});
+  const int32_t* cu_at = int32_at(place, cu, "cu", {B + 1});
   const double scale = args[6] == Py_None ? 1.0 / std::sqrt((double)d) : PyFloat_AsDouble(args[6]);
   const int with_lse = PyObject_IsTrue(args[8]);
   if (PyErr_Occurred()) throw python_error();
@@ -227,9 +243,9 @@ PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out must have q's shape and dtype");
   }
   if (with_lse) lse = at::empty({T, heads}, q.options().dtype(at::kFloat));
-  call(attend_cache8_entry, &dims, &pool, dtype, q_at, strides, codes_at, scales_at, tables_at, lens_at, cu_at,
-       (float)scale, address(out, "out"), with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
-       address(workspace, "workspace"), (size_t)workspace.numel(), stream_of(args[10], q));
+  call(place, attend_cache8_entry, &dims, &pool, dtype, q_at, strides, codes_at, scales_at, tables_at, lens_at, cu_at,
+       (float)scale, address(place, out, "out"), with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
+       address(place, workspace, "workspace"), (size_t)workspace.numel(), stream_of(args[10], q));
   PyObject* result = args[7];
   if (result == Py_None) result = THPVariable_Wrap(std::move(out));
   else Py_INCREF(result);
