@@ -51,14 +51,20 @@ def bind_command(out: str) -> list:
 
 def build(verbose: bool = False) -> str:
     """Compile every source, link libkvx.so and the binding's compiled part; returns the
-    library path."""
+    library path.  libkvx.so needs hipcc alone: where the binding's part, which needs torch
+    and a host compiler, cannot be built, it is linked all the same before the error."""
     t0 = time.time()
     objs = []
-    cmd = bind_command(BIND + ".tmp")
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    procs = [(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True),
-              "kvx_bind.cpp")]
+    procs = []
+    bind = "kvx_bind.cpp"
+    bind_failed = None
+    try:
+        cmd = bind_command(BIND + ".tmp")
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        procs.append((subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True), bind))
+    except (ImportError, OSError) as e:      # no torch, no compiler
+        bind_failed = str(e)
     for src in SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
         cmd = [hipcc(), *HIP_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c",
@@ -76,17 +82,23 @@ def build(verbose: bool = False) -> str:
                  if "packed-fp32-ops" not in ln]
         if lines and (verbose or p.returncode):
             print("\n".join(lines), file=sys.stderr)
-        if p.returncode:
+        if p.returncode and src == bind:
+            bind_failed = f"exit status {p.returncode}"
+        elif p.returncode:
             failed.append(src)
     if failed:
         raise RuntimeError(f"compilation failed for {failed}")
-    os.replace(BIND + ".tmp", BIND)
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
     for o in objs:
         os.remove(o)
+    if bind_failed is not None:
+        if os.path.exists(BIND):      # an earlier library's
+            os.remove(BIND)
+        raise RuntimeError(f"compilation failed for {bind}: {bind_failed} ({LIB} is built)")
+    os.replace(BIND + ".tmp", BIND)
     if verbose:
         print(f"built {LIB} in {time.time() - t0:.1f}s", flush=True)
     return LIB
