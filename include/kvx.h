@@ -464,7 +464,8 @@ typedef struct kvx_pool {
   int32_t max_pages;   /* entries of one row of block_tables                 */
 } kvx_pool;
 
-/* Most requests of a kvx_plan_pages or kvx_attend_cache8 call. */
+/* Most requests of a kvx_plan_pages or kvx_attend_cache8 call.  These and
+ * kvx_store_cache8 take up to 2^30 rows (KVX_ERR_UNSUPPORTED beyond). */
 #define KVX_MAX_REQUESTS 4096
 
 /* Pages, slots and positions of a step's new tokens, from request lengths.

@@ -58,12 +58,17 @@ kvx_status check_pool(const kvx_pool* pool, bool tables, int* log2p) {
   return KVX_OK;
 }
 
+// Row numbers step past the last one in 32 bits.
+kvx_status check_rows(int32_t T) {
+  if (T > 1 << 30) return set_error(KVX_ERR_UNSUPPORTED, "T=%d exceeds 2^30 rows", T);
+  return KVX_OK;
+}
+
 kvx_status check_requests(int32_t B, int32_t T) {
   if (B < 0 || T < 0) return set_error(KVX_ERR_SHAPE, "B=%d and T=%d must not be negative", B, T);
   if (B > KVX_MAX_REQUESTS)
     return set_error(KVX_ERR_UNSUPPORTED, "B=%d exceeds %d requests", B, KVX_MAX_REQUESTS);
-  if (T > 1 << 30) return set_error(KVX_ERR_UNSUPPORTED, "T=%d exceeds 2^30 rows", T);
-  return KVX_OK;
+  return check_rows(T);
 }
 
 kvx_status check_dtype(kvx_dtype dtype) {
@@ -167,6 +172,7 @@ kvx_status kvx_store_cache8(const kvx_pool* pool, kvx_dtype dtype, int32_t L, in
   if ((st = check_d(d)) != KVX_OK) return st;
   if (L < 1 || H < 1 || T < 0)
     return set_error(KVX_ERR_SHAPE, "L=%d H=%d T=%d out of range (L, H >= 1, T >= 0)", L, H, T);
+  if ((st = check_rows(T)) != KVX_OK) return st;
   if ((int64_t)L * H * 2 > 65535)
     return set_error(KVX_ERR_UNSUPPORTED, "L*H*2=%lld exceeds 65535 planes", (long long)L * H * 2);
   if (T == 0) return ok();
