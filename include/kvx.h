@@ -573,6 +573,13 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
                              const int32_t* lens, const int32_t* cu, float scale, void* out,
                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Name of the kernel that kvx_attend_cache8 would launch for these sizes and
+ * type, as a trace shows it: "attend8_rows_kernel<d, 2>" for chunks of bf16
+ * queries, else "attend8_split_kernel<t, d, w, n>", t = 0 for bf16 and 1 for fp32
+ * queries, w waves a workgroup, 16 n rows a block.  For profiling and tests; a
+ * static string, NULL for invalid arguments and for calls that launch nothing. */
+const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype);
+
 /* Text for the last non-OK status returned on the calling thread ("" if
  * none).  The pointer stays valid until the next kvx call on that thread. */
 const char* kvx_last_error(void);

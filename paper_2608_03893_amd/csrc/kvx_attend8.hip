@@ -25,6 +25,8 @@
 // 8 to 12 us, and the bytes come on top.
 #include "kvx_attend8.h"
 
+#include <cstdio>
+
 namespace kvx {
 namespace {
 
@@ -645,31 +647,59 @@ size_t attend_ws_bytes(int B, int G, int T, int d, int dtype) {
   return split > rows ? split : rows;
 }
 
+namespace {
+
 template <int DT, int D, int W, int NB>
-static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  // no more workgroups than there can be quanta
-  constexpr int kFill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
-  const double units = ((double)a.T * a.G / (16 * NB) + a.B) * a.H, quant = W * kStep;
-  const double want = units * (a.keys / quant + 1 + kStart) / kLeast<W> + 1;
-  int* counters = static_cast<int*>(ws);
-  const unsigned grid = ((want < kFill ? (unsigned)want : kFill) + kXcds - 1) / kXcds * kXcds;
-  hipLaunchKernelGGL((attend8_split_kernel<DT, D, W, NB>), dim3(grid), dim3(64 * W),
-                     (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
-  return hipGetLastError();
+struct Split {
+  static hipError_t launch(const AttendArgs& a, void* ws, hipStream_t stream) {
+    // no more workgroups than there can be quanta
+    constexpr int kFill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
+    const double units = ((double)a.T * a.G / (16 * NB) + a.B) * a.H, quant = W * kStep;
+    const double want = units * (a.keys / quant + 1 + kStart) / kLeast<W> + 1;
+    int* counters = static_cast<int*>(ws);
+    const unsigned grid = ((want < kFill ? (unsigned)want : kFill) + kXcds - 1) / kXcds * kXcds;
+    hipLaunchKernelGGL((attend8_split_kernel<DT, D, W, NB>), dim3(grid), dim3(64 * W),
+                       (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)), stream, a, reinterpret_cast<float*>(counters + kCounters), counters);
+    return hipGetLastError();
+  }
+  static void name(char* to, size_t n) { std::snprintf(to, n, "attend8_split_kernel<%d, %d, %d, %d>", DT, D, W, NB); }
+};
+
+template <int D>
+struct Rows {
+  static hipError_t launch(const AttendArgs& a, void* ws, hipStream_t stream) { return launch_attend_rows(a, D, ws, stream); }
+  static void name(char* to, size_t n) { std::snprintf(to, n, "attend8_rows_kernel<%d, 2>", D); }
+};
+
+// f of the kernel for these sizes.
+template <int DT, int D, int NB, typename F>
+auto with_split(const AttendArgs& a, F f) {
+  constexpr int LARGE = kLarge<DT, D, NB>;
+  return large_workgroups<NB, LARGE>(a) ? f(Split<DT, D, LARGE, NB>()) : f(Split<DT, D, 4, NB>());
+}
+template <typename F>
+auto with_kernel(const AttendArgs& a, int dtype, int d, F f) {
+  if (by_rows(a, dtype, d)) return d == 64 ? f(Rows<64>()) : f(Rows<128>());
+  if (two_tiles(a, dtype)) return d == 64 ? with_split<0, 64, 2>(a, f) : with_split<0, 128, 2>(a, f);
+  if (dtype == 0) return d == 64 ? with_split<0, 64, 1>(a, f) : with_split<0, 128, 1>(a, f);
+  return d == 64 ? with_split<1, 64, 1>(a, f) : with_split<1, 128, 1>(a, f);
 }
 
-template <int DT, int D, int NB>
-static hipError_t launch_split(const AttendArgs& a, void* ws, hipStream_t stream) {
-  constexpr int LARGE = kLarge<DT, D, NB>;
-  return large_workgroups<NB, LARGE>(a) ? launch_split<DT, D, LARGE, NB>(a, ws, stream)
-                                        : launch_split<DT, D, 4, NB>(a, ws, stream);
-}
+}  // namespace
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
-  if (by_rows(a, dtype, d)) return launch_attend_rows(a, d, ws, stream);
-  if (two_tiles(a, dtype)) return d == 64 ? launch_split<0, 64, 2>(a, ws, stream) : launch_split<0, 128, 2>(a, ws, stream);
-  if (dtype == 0) return d == 64 ? launch_split<0, 64, 1>(a, ws, stream) : launch_split<0, 128, 1>(a, ws, stream);
-  return d == 64 ? launch_split<1, 64, 1>(a, ws, stream) : launch_split<1, 128, 1>(a, ws, stream);
+  return with_kernel(a, dtype, d, [&](auto k) { return k.launch(a, ws, stream); });
+}
+
+const char* attend_kernel_name(const AttendArgs& a, int dtype, int d) {
+  return with_kernel(a, dtype, d, [](auto k) -> const char* {
+    struct Name {
+      char text[48];
+      Name() { decltype(k)::name(text, sizeof(text)); }
+    };
+    static const Name name;
+    return name.text;
+  });
 }
 
 }  // namespace kvx

@@ -49,6 +49,8 @@ struct AttendArgs {
   int64_t keys;             // most a request has, as far as the host knows: for the choice of kernel
 };
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream);
+// The kernel it takes, as a trace shows it; a static string.
+const char* attend_kernel_name(const AttendArgs& a, int dtype, int d);
 size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);
 // Its kernel for many query rows a request (bf16).
 hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream);

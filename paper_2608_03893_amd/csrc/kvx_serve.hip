@@ -227,6 +227,29 @@ static kvx_status check_attend(const kvx_attend_dims* dims, kvx_dtype dtype) {
   return KVX_OK;
 }
 
+// The sizes that a launch goes by.
+static kvx::AttendArgs attend_sizes(const kvx_attend_dims& m, const kvx_pool& pool, int log2p) {
+  kvx::AttendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.B = m.B;
+  a.H = m.H;
+  a.G = m.G;
+  a.T = m.T;
+  a.M = pool.max_pages;
+  a.N = pool.num_pages;
+  a.log2p = log2p;
+  a.keys = (int64_t)a.M << log2p;
+  if (m.longest > 0 && m.longest < a.keys) a.keys = m.longest;
+  return a;
+}
+
+const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype) {
+  int log2p;
+  if (check_pool(pool, true, &log2p) != KVX_OK || check_attend(dims, dtype) != KVX_OK || dims->B == 0 || dims->T == 0)
+    return nullptr;
+  return kvx::attend_kernel_name(attend_sizes(*dims, *pool, log2p), dtype == KVX_BF16 ? 0 : 1, dims->d);
+}
+
 size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype) {
   if (check_attend(dims, dtype) != KVX_OK || dims->B == 0 || dims->T == 0) return 0;
   return kvx::attend_ws_bytes(dims->B, dims->G, dims->T, dims->d, dtype == KVX_BF16 ? 0 : 1);
@@ -274,8 +297,7 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
       return set_error(KVX_ERR_WORKSPACE, "workspace is not 256-byte aligned");
   }
   if ((st = check_alias(outs, 3, in, 6)) != KVX_OK) return st;
-  kvx::AttendArgs a;
-  std::memset(&a, 0, sizeof(a));
+  kvx::AttendArgs a = attend_sizes(m, *pool, log2p);
   a.q = q;
   a.q_stride[0] = q_strides[0];
   a.q_stride[1] = q_strides[1];
@@ -287,15 +309,6 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
   a.out = out;
   a.lse = lse;
   a.scale_log2 = scale * 1.44269504088896340736f;
-  a.B = m.B;
-  a.H = m.H;
-  a.G = m.G;
-  a.T = m.T;
-  a.M = pool->max_pages;
-  a.N = pool->num_pages;
-  a.log2p = log2p;
-  a.keys = (int64_t)a.M << log2p;
-  if (m.longest > 0 && m.longest < a.keys) a.keys = m.longest;
   const hipError_t e = kvx::launch_attend(a, dt, m.d, workspace, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
   return ok();

@@ -30,7 +30,7 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "fit_workspace_bytes", "fit_cache", "probe_workspace_bytes", "probe_r2",
            "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
            "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
-           "attend_workspace_bytes", "attend_workspace", "attend_cache8"]
+           "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -180,6 +180,8 @@ def load():
     L.kvx_attend_workspace_bytes.restype = SZ
     L.kvx_attend_cache8.argtypes = [AP, PP, I32, P, P, P, P, P, P, P, F32, P, P, P, SZ, P]
     L.kvx_attend_cache8.restype = I32
+    L.kvx_attend_kernel_name.argtypes = [AP, PP, I32]
+    L.kvx_attend_kernel_name.restype = ctypes.c_char_p
     L.kvx_last_error.argtypes = []
     L.kvx_last_error.restype = ctypes.c_char_p
     L.kvx_version.argtypes = []
@@ -683,6 +685,16 @@ def attend_workspace_bytes(dims: AttendDims, dtype: str = "bf16") -> int:
     if dtype not in ("bf16", "f32"):
         raise ValueError("dtype must be 'bf16' or 'f32'")
     return int(load().kvx_attend_workspace_bytes(ctypes.byref(dims), 0 if dtype == "bf16" else 1))
+
+
+def attend_kernel_name(dims: AttendDims, pool: Pool, dtype: str = "bf16") -> str:
+    """Kernel the library would launch for these sizes, as a trace shows it."""
+    if dtype not in ("bf16", "f32"):
+        raise ValueError("dtype must be 'bf16' or 'f32'")
+    r = load().kvx_attend_kernel_name(ctypes.byref(dims), ctypes.byref(pool), 0 if dtype == "bf16" else 1)
+    if r is None:
+        raise ValueError("invalid sizes, or a call without rows")
+    return r.decode()
 
 
 def attend_workspace(q, pool, block_tables, stream=None):
