@@ -1,5 +1,5 @@
 """Every attention kernel over the 8-bit pool, by the name that the library gives, on what it
-can go wrong at: NaN codes, missing pages, scales of every kind, units
+can go wrong at: NaN codes, missing pages, lengths past the table, scales of every kind, units
 over several workgroups and several units a workgroup.
 
 Bounds, element by element, with A, S, u as in test_gpu_attend8 and n the most keys that a
@@ -102,6 +102,18 @@ def test_ragged_requests(gpu_kvx, kernel):
     c["lens"][::3] = 0                       # and requests without keys
     want, empty = _check(gpu_kvx, kernel, c, "without keys")
     assert empty.any() and not empty.all()
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_lengths_past_the_table(gpu_kvx, kernel):
+    """Cut to what the table holds, all of it live pages; negative ones are none."""
+    rng = np.random.default_rng(901)
+    size, _, _ = KERNELS[kernel]
+    B, M = SIZES[size][0], SIZES[size][4]
+    c = _sized(rng, kernel, lens=[M * P] * B)
+    c["lens"] = np.array([[M * P + 1, 2 ** 31 - 1, -7, M * P, -2 ** 31, 2 ** 31 - P, 5][b % 7] for b in range(B)])
+    c["cu"][-1] = 2 ** 31 - 1                # rows past the last one
+    _check(gpu_kvx, kernel, c, "past the table")
 
 
 @pytest.mark.parametrize("kernel", KERNELS)
