@@ -1,8 +1,11 @@
 """Host-side bounds of the serving entry points that test_abi_serve does not reach (no GPU
 needed).  Every rejected call carries a second defect that is checked last, as there."""
 
+import pytest
+
+from paper_2608_03893_amd import kvx
 from tests.test_abi_host import L  # noqa: F401  (the library fixture)
-from tests.test_abi_serve import Plan, Store, _expect
+from tests.test_abi_serve import Attend, Plan, Store, _expect
 
 
 def test_rows_of_a_call(L):
@@ -12,3 +15,41 @@ def test_rows_of_a_call(L):
         _expect(L, 5, Store, T=T, **{**near, "scales": near["slots"]})
         _expect(L, 5, Plan, T=T)
     _expect(L, 6, Store, T=1 << 30, **{**near, "scales": near["slots"]})   # comes to the last check
+
+
+# (B, T, dtype): below 96 query rows a request and KV head, at it, and fp32 queries
+@pytest.mark.parametrize("B,T,dtype", [(3, 71, 0), (3, 72, 0), (3, 72, 1), (1, 1, 0), (4096, 1 << 17, 0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_workspace(L, B, T, dtype, d):
+    dims = kvx.AttendDims(B, 2, 4, T, d, 0)
+    need = kvx.attend_workspace_bytes(dims, "f32" if dtype else "bf16")
+    assert need > kvx.ATTEND_COUNTER_BYTES
+    call = dict(dims=dims, dtype=dtype, qs=(8 * d, d))
+    _expect(L, 7, Attend, **call, ws=None, wsb=need)
+    _expect(L, 7, Attend, **call, wsb=need - 1)
+    _expect(L, 7, Attend, **call, wsb=0)
+    at = 1 << 40
+    for off in (16, 128):
+        _expect(L, 7, Attend, **call, ws=at + off, wsb=need)
+    _expect(L, 6, Attend, **call, ws=at, wsb=need)                # comes to the last check
+    base = Attend()
+    for name in ("q", "codes", "scales", "tables", "lens", "cu", "out", "lse"):
+        for ws in (getattr(base, name), getattr(base, name) - need // 256 * 256 + 256):   # its last bytes
+            if ws > 0:
+                assert Attend(**call, ws=ws, wsb=1 << 40).run(L) == 6, (name, L.kvx_last_error())
+
+
+def test_a_workspace_of_few_rows_is_too_small_for_chunks(L):
+    """The bytes change where the kernel by rows may be chosen, and never fall as rows grow."""
+    for d in (64, 128):
+        few, many = (kvx.attend_workspace_bytes(kvx.AttendDims(3, 2, 4, T, d, 0)) for T in (71, 72))
+        assert few < many
+        _expect(L, 7, Attend, dims=kvx.AttendDims(3, 2, 4, 72, d, 0), qs=(8 * d, d), wsb=few)
+        assert kvx.attend_workspace_bytes(kvx.AttendDims(3, 2, 4, 1 << 20, d, 0)) == many
+
+
+def test_attention_bound_of_the_longest(L):
+    for longest in (-1, -2 ** 31):
+        dims = kvx.AttendDims(3, 2, 4, 10, 128, longest)
+        _expect(L, 2, Attend, dims=dims)
+        assert L.kvx_attend_workspace_bytes(dims, 0) == 0
