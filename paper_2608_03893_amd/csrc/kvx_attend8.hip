@@ -594,11 +594,11 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) at
 
 // By rows (bf16 only): blocks of 256 rows share the widened codes.  Pays from 96 rows a
 // request on where blocks are enough for the CUs or the work is, else its joins cost more.
-//   d = 128, split / by rows    B = 64, 64 rows, 1000 keys 58 / 58    96 rows 80 / 61
-//     B = 32, 128 rows, 300 keys 27 / 19     B = 16, 160 rows, 5000 keys 131 / 93
-//     B = 8,  256 rows, 5000 keys 77 / 84, 16000 keys 211 / 188
-//     B = 1,  2048 rows, 2178 keys 37 / 63, 16000 keys 198 / 167
-//   d = 64   B = 64, 64 rows, 1000 keys 35 / 46    128 rows 59 / 47
+//   d = 128, split / by rows    B = 64, 64 rows, 1000 keys 57 / 77    96 rows 79 / 78
+//     B = 32, 128 rows, 300 keys 27 / 21     B = 16, 160 rows, 5000 keys 152 / 128
+//     B = 8,  256 rows, 5000 keys 88 / 98, 16000 keys 262 / 224
+//     B = 1,  2048 rows, 2178 keys 39 / 65, 16000 keys 226 / 198
+//   d = 64   B = 64, 64 rows, 1000 keys 38 / 55    128 rows 61 / 56
 bool may_go_by_rows(int B, int G, int T, int dtype) { return dtype == 0 && (int64_t)T * G >= (int64_t)B * 96; }
 bool by_rows(const AttendArgs& a, int dtype, int d) {
   const int64_t rows = (int64_t)a.T * a.G, units = (rows / 256 > a.B ? rows / 256 : a.B) * a.H;
@@ -608,9 +608,9 @@ bool by_rows(const AttendArgs& a, int dtype, int d) {
 
 // Blocks of 32 rows (bf16 only), whose codes are loaded and widened once for two row tiles,
 // where a request brings more than one tile and the blocks' keys come to 512 a CU:
-//   d = 128, 16 / 32 rows a block    B = 64, 32 rows, 1000 keys 47 / 36, 5000 keys 229 / 131
-//     B = 8, 128 rows, 5000 keys 70 / 45     B = 2, 24 rows, 1000 keys 14 / 16
-//   d = 64   B = 32, 32 rows, 5000 keys 50 / 40
+//   d = 128, 16 / 32 rows a block    B = 64, 32 rows, 1000 keys 48 / 34, 5000 keys 246 / 128
+//     B = 8, 128 rows, 5000 keys 82 / 51     B = 2, 24 rows, 1000 keys 13 / 16
+//   d = 64   B = 32, 32 rows, 5000 keys 62 / 41
 bool two_tiles(const AttendArgs& a, int dtype) {
   const int64_t rows = (int64_t)a.T * a.G, blocks = rows / 32 > a.B ? rows / 32 : a.B;
   return dtype == 0 && rows > 16 * (int64_t)a.B && (double)blocks * a.H * a.keys >= 256 * 512;
@@ -618,23 +618,26 @@ bool two_tiles(const AttendArgs& a, int dtype) {
 
 // One large workgroup a CU instead of several of four waves: a unit then has fewer partial
 // sums or none.
-//   Blocks of 32 rows: fewer than two units a CU (32 requests of 24 rows and 2178 keys 44 ->
-//   35, 64 of 1000 33 against 38) of 1024 keys and more (a prompt of 195 tokens 17 against 19).
+//   Blocks of 32 rows: fewer than two units a CU of 1024 keys and more (32 requests of 24 rows
+//   and 2178 keys 44 -> 34, d = 64 33 -> 23; but 64 of 1000 32 against 37, 1560 rows of one over
+//   1000 23 against 28).
 //   Blocks of 16: where the units' keys come to 256 a CU (a decoding step of 32 requests of
-//   2178 keys 43 -> 35, 16 of 1000 20 -> 17, 4 contexts up to 131070 97 -> 91), but not
-//   - for requests of more than 32 rows (a mixed batch of 8: 26 against 18);
+//   2178 keys 42 -> 32, 16 of 1000 20 -> 15, 4 contexts up to 131070 101 -> 95), but not
 //   - for few units of one to three rows, whose sums join fast, until their keys come to
-//     2048 a CU (G = 1, 16000 keys 17 against 20; two heads, 16 contexts up to 24900 23 -> 20);
-//   - for many short units, where starts and ends of small workgroups overlap: 256 requests
-//     of 300 keys 43 against 59, of 1000 113 against 117, of 2178 231 -> 220; with eight
-//     waves (fp32, d = 128) for many units of any length, 115 against 121.
+//     2048 a CU (G = 1, 16000 keys 18 against 20);
+//   - for two units a CU and more of requests of more than 32 rows (fp32: 8 requests of 128 rows
+//     and 1000 keys 23 against 27, 2048 rows of one over 10240, d = 64, 141 against 157; with
+//     fewer units 8 of 64 rows and 1000 keys 22 -> 17, 512 rows over 304 12.5 -> 10.1), or of
+//     few keys, where starts and ends of small workgroups overlap (256 requests of 300 keys 45
+//     against 66, of 1000 111 against 118, of 2178 233 -> 225), or with eight waves (fp32,
+//     d = 128: 256 requests of 1000 keys 113 against 130).
 template <int NB, int LARGE>
 bool large_workgroups(const AttendArgs& a) {
   const int64_t rows = (int64_t)a.T * a.G, B = a.B, blocks = rows / (16 * NB) > B ? rows / (16 * NB) : B;
   const int64_t units = blocks * a.H, keys = a.keys;
   if (NB == 2) return units < 512 && keys >= 1024;
   const double least = units < 64 && rows < 4 * B ? 256 * 2048 : 256 * 256;
-  return rows <= 32 * B && (double)units * keys >= least && (units < 512 || (LARGE >= 12 && keys > 1024));
+  return (double)units * keys >= least && (units < 512 || (rows <= 32 * B && LARGE >= 12 && keys > 1024));
 }
 
 }  // namespace

@@ -44,7 +44,10 @@ SPLIT, ROWS = "attend8_split_kernel<%d, %d, %d, %d>", "attend8_rows_kernel<%d, 2
     (dict(B=64, rows=8, keys=1040), SPLIT % (0, 128, 12, 1)),
     (dict(B=64, rows=8, keys=1040, d=64), SPLIT % (0, 64, 12, 1)),
     (dict(B=8, rows=32, keys=1024, dtype="f32"), SPLIT % (1, 128, 8, 1)),
-    (dict(B=8, rows=40, keys=1024, dtype="f32"), SPLIT % (1, 128, 4, 1)),
+    (dict(B=8, rows=120, keys=1024, dtype="f32"), SPLIT % (1, 128, 8, 1)),
+    (dict(B=8, rows=128, keys=4096, dtype="f32"), SPLIT % (1, 128, 4, 1)),         # 512 units
+    (dict(B=8, rows=128, keys=4096, d=64, dtype="f32"), SPLIT % (1, 64, 4, 1)),
+    (dict(B=2, rows=64, keys=1024), SPLIT % (0, 128, 12, 1)),       # too few keys for 32 rows a block
     (dict(B=64, rows=8, keys=4096, dtype="f32"), SPLIT % (1, 128, 4, 1)),
     (dict(B=64, rows=8, keys=4096, d=64, dtype="f32"), SPLIT % (1, 64, 12, 1)),
     # a stated bound counts where it is below the tables' length
