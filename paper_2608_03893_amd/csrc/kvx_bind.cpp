@@ -33,7 +33,7 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
 }
 
 int32_t size32(int64_t n) {
-  TORCH_CHECK_VALUE(n <= INT_MAX, "a size passes 2^31");
+  TORCH_CHECK_VALUE(n >= INT_MIN && n <= INT_MAX, "a size of ", n, " does not fit 32 bits");
   return (int32_t)n;
 }
 
@@ -136,6 +136,7 @@ PyObject* plan_pages(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (PyErr_Occurred()) throw python_error();
   const int64_t B = tables.size(0), M = tables.size(1), N = ring.size(0);
   const kvx_pool pool{size32(N), size32(page_size), size32(M)};
+  const int32_t rows32 = size32(T);
   const Place place{lens.device()};
   const int32_t *lens_at = int32_at(place, lens, "lens", {B}), *add_at = int32_at(place, add, "add", {B});
   int32_t *tables_at = int32_at(place, tables, "block_tables", {B, M}), *ring_at = int32_at(place, ring, "free_ring", {N});
@@ -167,7 +168,7 @@ PyObject* plan_pages(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Py_INCREF(result);
   }
   try {
-    call(place, plan_pages_entry, &pool, size32(B), size32(T), lens_at, add_at, tables_at, ring_at, free_at, outs[0], outs[1],
+    call(place, plan_pages_entry, &pool, size32(B), rows32, lens_at, add_at, tables_at, ring_at, free_at, outs[0], outs[1],
          outs[2], outs[3], outs[4], stream_of(args[8], lens));
   } catch (...) {
     Py_DECREF(result);

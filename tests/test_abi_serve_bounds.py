@@ -2,6 +2,7 @@
 needed).  Every rejected call carries a second defect that is checked last, as there."""
 
 import pytest
+import torch
 
 from paper_2608_03893_amd import kvx
 from tests.test_abi_host import L  # noqa: F401  (the library fixture)
@@ -53,3 +54,15 @@ def test_attention_bound_of_the_longest(L):
         dims = kvx.AttendDims(3, 2, 4, 10, 128, longest)
         _expect(L, 2, Attend, dims=dims)
         assert L.kvx_attend_workspace_bytes(dims, 0) == 0
+
+
+def test_binding_refuses_sizes_outside_32_bits():
+    """Neither cut to 32 bits nor allocated for first."""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    for T, page in ((4, 2 ** 32 + 16), (4, -2 ** 32 + 16), (2 ** 32 + 4, 16), (2 ** 31, 16), (-2 ** 32 + 4, 16)):
+        with pytest.raises(ValueError, match="32 bits"):
+            kvx.plan_pages(i(3), i(3), i(3, 2), i(9), i(2), T, page)
+    q, pool = torch.zeros((5, 6, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 64, 64), dtype=torch.float8_e4m3fn)
+    for longest in (2 ** 31, -2 ** 32 + 5):
+        with pytest.raises(ValueError, match="32 bits"):
+            kvx.attend_cache8(q, pool, torch.ones((2, 2, 4)), i(2, 4), i(2), i(3), longest=longest)
