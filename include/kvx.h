@@ -479,7 +479,9 @@ typedef struct kvx_pool {
  * max_pages, its rows would pass T, or the free pages run out (requests are served
  * in order, and behind one that finds too few none gets any; the pages of
  * requests that end in this call are free from the next call on): its length
- * stays, its rows' slots are -1, and it takes no page.
+ * stays, its rows' slots are -1, and it takes no page.  Its rows still count in
+ * cu_out, though the pool never holds their tokens: what attention gives for rows
+ * whose slot is -1 means nothing.
  *   lens, add      int32 [B]
  *   block_tables   int32 [B, max_pages], updated: page ids of each request, in
  *                  order of position; only entries of newly taken pages are
@@ -560,13 +562,14 @@ size_t kvx_attend_workspace_bytes(const kvx_attend_dims* dims, kvx_dtype dtype);
  *   workspace      >= kvx_attend_workspace_bytes, 256-byte aligned; its first
  *                  KVX_ATTEND_COUNTER_BYTES are zero before its first use (counters,
  *                  which every call leaves at zero; the rest may hold anything);
- *                  calls of any sizes may follow one another in it
+ *                  calls of any sizes may follow one another in it on a stream
  * Scores, softmax statistics and sums are held in fp32.  The probabilities (times
  * the page's value scale) enter their product with the values with 16 bits for
  * bf16 queries, so that the output's own rounding is the only one that counts, and
- * with 24 for fp32 queries.  Codes enter exactly.  A NaN code, and a value scale
- * that is NaN or infinite, make NaN in the rows that see a key of theirs, and leave
- * the other rows as they are. */
+ * with 24 for fp32 queries.  Codes enter exactly.  Sums are divided last, over
+ * probabilities of up to 2^8: the largest value times the keys has to stay below
+ * 2^119.  A NaN code, and a value scale that is NaN or infinite, make NaN in the rows
+ * that see a key of theirs, and leave the other rows as they are. */
 kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype,
                              const void* q, const int64_t* q_strides, const uint8_t* codes,
                              const float* scales, const int32_t* block_tables,

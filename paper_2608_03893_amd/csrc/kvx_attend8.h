@@ -56,7 +56,7 @@ __device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
 // (relative error 0.0018 for 0.00167 over 64 ragged requests, 0.0021 for 0.00166 in a chunk of
 // 2048 x 10240; with two 0.0002 to 0.0016 of them are not).  The second term costs 1% where the
 // bytes bound the time (59.3 us for 58.7, mixed batch 22.6 for 21.8) and a third where the
-// products do (815 us for 618).
+// products do (818 us for 618).
 template <int DT>
 constexpr int kTerms = DT == 0 ? 2 : 3;
 

@@ -20,7 +20,7 @@
 // from partial sums in order of the keys, so results do not depend on timing.
 //
 // Measured, d = 128, G = 8, 8 KV heads, 16-token pages that no cache holds: 32 requests of
-// 5000 keys 64 us (5.1 TB/s), 16 of 2178 26 us (2.7), 1 of 5000 13.6 us, 1 of 300 8.3 us:
+// 5000 keys 64 us (5.1 TB/s), 16 of 2178 24 us (3.0), 1 of 5000 14.1 us, 1 of 300 8.7 us:
 // a launch, the lengths, pages, keys and joins, each of which waits for the one before, take
 // 8 to 12 us, and the bytes come on top.
 #include "kvx_attend8.h"

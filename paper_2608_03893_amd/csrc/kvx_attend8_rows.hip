@@ -11,10 +11,10 @@
 // there, and else to the probabilities.
 //
 // Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them:
-// 2048 new tokens of 64 heads over 10240 keys, d = 128, 815 us: 760 TFLOP/s, and 1140 with the
+// 2048 new tokens of 64 heads over 10240 keys, d = 128, 820 us: 755 TFLOP/s, and 1130 with the
 // products of the probabilities' second term, where a large product of the library reaches
-// 1230.  With one term, to form a step's scores beside the exponentials of the step before took
-// as long (a quarter more products of keys, and 8% more time).
+// 1230 (another card: 920 us).  With one term, to form a step's scores beside the exponentials of
+// the step before took 8% longer.
 //
 // One workgroup a CU; each takes an equal share of the weight of all (request, head, block
 // of rows), a block's weight being the keys that its last row sees.  Neighbouring
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_rows_kernel(AttendArgs a,
 #pragma unroll 1
       for (int s = 0; s < kSteps && key <= lim_hi; ++s, key += kStep) {
         // A SIMD's two waves take turns at going first, two steps each: left alone, one always
-        // does, and waits at the barrier for a third of the time (631 -> 615 us).
+        // does, and waits at the barrier for a third of the time (834 -> 820 us).
         if ((s >> 1 ^ wave >> 2) & 1) __builtin_amdgcn_s_setprio(1);
         else __builtin_amdgcn_s_setprio(0);
         const float sc[2] = {ksc[buf][s][0], ksc[buf][s][1]};

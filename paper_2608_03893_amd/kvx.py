@@ -712,6 +712,7 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
                   workspace=None, stream=None, longest=0):
     """Causal attention of the newest tokens over one layer of the 8-bit pool
     (enqueued on the stream); returns out [T, H*G, d], with_lse also lse [T, H*G].
+    For inference: results carry no gradient, whether or not q requires one.
 
     q [T, H*G, d] bf16 or fp32 (d dense); pool [2, H, num_slots, d], scales
     [2, H, num_pages]; block_tables [B, max_pages], lens [B] (tokens in the pool,
