@@ -31,7 +31,8 @@
  *     Repeated indices are allowed.  The table is read during the call and
  *     may be freed when the call returns.
  *   - Calls are asynchronous: work is enqueued on `stream` (a hipStream_t;
- *     NULL is the default stream) and the call returns without waiting.
+ *     NULL is the current device's default stream, and that device then has
+ *     to be the operands') and the call returns without waiting.
  *   - Every argument is validated on the host before anything is enqueued.
  *     On any status other than KVX_OK nothing was enqueued and the target
  *     is untouched; kvx_last_error() describes the failure.
