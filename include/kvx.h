@@ -584,6 +584,28 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
  * static string, NULL for invalid arguments and for calls that launch nothing. */
 const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype);
 
+/* RMS norm and position rotation of a step's query and key heads, as the target
+ * model's layers do between their projections and the cache (kvx_store_cache8)
+ * or the attention.  For row t, head h and x = q[t, h] (k[t, h] alike):
+ *   y = R(positions[t]) (x / sqrt(mean(x^2) + eps) * q_weight)
+ * with the rotation R of `rope` (see kvx_rope); without weights (NULL) the operand
+ * is rotated only.  Formed in fp32 from sines and cosines of angles in fp64, and
+ * rounded once, to the outputs.
+ *   Hq, Hk       query heads (>= 1) and key heads (0: no keys, k and what belongs
+ *                to it are not looked at); their sum at most 65535
+ *   q, k         bf16 or fp32; (t, h, c) at t * strides[0] + h * strides[1] + c
+ *                (HOST int64 [2], in elements, not negative, multiples of 16 bytes)
+ *   q_weight, k_weight   [d] in the same type, or NULL
+ *   eps          finite, not negative
+ *   positions    int32 [T]
+ *   q_out, k_out [T, Hq, d], [T, Hk, d]; each may be its own input where that is
+ *                dense, and may overlap nothing else
+ * Squares that pass the range of fp32 are summed in fp64. */
+kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int32_t d, const void* q,
+                         const int64_t* q_strides, const void* k, const int64_t* k_strides,
+                         const void* q_weight, const void* k_weight, float eps, const kvx_rope* rope,
+                         const int32_t* positions, void* q_out, void* k_out, void* stream);
+
 /* Text for the last non-OK status returned on the calling thread ("" if
  * none).  The pointer stays valid until the next kvx call on that thread. */
 const char* kvx_last_error(void);

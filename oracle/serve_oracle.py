@@ -154,3 +154,22 @@ def attend_cache8(q, codes, scales, tables, lens, cu, scale):
                     size_v[t, x] = p @ np.abs(V[see])
                     size_s[t, x] = abs(scale) * (np.abs(K[see]) @ np.abs(q[t, x])).max()
     return out, lse, size_v, size_s
+
+
+def norm_rope(x, weight, eps, positions, rope):
+    """x [T, heads, d] float64: every head's RMS norm times weight (None: no norm), rotated.
+    Returns the result and, for error bounds, the size of each plane it came from."""
+    from oracle.kvx_oracle import rope_rotate
+    x = np.asarray(x, np.float64)
+    if weight is not None:
+        with np.errstate(all="ignore"):
+            x = x / np.sqrt((x * x).mean(2, keepdims=True) + eps) * np.asarray(weight, np.float64)
+    size = np.empty_like(x)
+    first, second = _rope_planes(x.shape[2], rope)
+    size[..., first] = size[..., second] = np.hypot(x[..., first], x[..., second])
+    return rope_rotate(x.transpose(1, 0, 2), positions, rope).transpose(1, 0, 2), size
+
+
+def _rope_planes(d, rope):
+    j = np.arange(d // 2)
+    return (j, j + d // 2) if int(rope.get("style", 0)) == 0 else (2 * j, 2 * j + 1)

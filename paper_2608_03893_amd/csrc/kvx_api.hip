@@ -6,6 +6,7 @@
 #include "kvx.h"
 #include "kvx_fitplan.h"
 #include "kvx_internal.h"
+#include "kvx_serve.h"
 #include "kvx_wplan.h"
 
 #include <cmath>
@@ -913,6 +914,8 @@ kvx_status set_error(kvx_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
+kvx_status check_rope_params(const kvx_rope* r, const char* which) { return check_rope(r, which); }
+void rope_frequencies(const kvx_rope& r, int d, InvFreq& out) { inv_freq(r, d, out); }
 }  // namespace kvx
 
 extern "C" {

@@ -23,6 +23,7 @@ decltype(&kvx_plan_pages) plan_pages_entry = nullptr;
 decltype(&kvx_store_cache8) store_cache8_entry = nullptr;
 decltype(&kvx_attend_cache8) attend_cache8_entry = nullptr;
 decltype(&kvx_attend_workspace_bytes) attend_workspace_bytes_entry = nullptr;
+decltype(&kvx_norm_rope) norm_rope_entry = nullptr;
 PyObject* check_status = nullptr;    // raises for a status that is not KVX_OK
 PyObject* plan_type = nullptr;       // the tuple plan_pages returns
 PyObject* current_stream = nullptr;  // raw handle of a device's current stream
@@ -259,28 +260,94 @@ PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of kvx_plan_pages, kvx_store_cache8, kvx_attend_cache8 and
-//      kvx_attend_workspace_bytes, check_status, plan_type, current_stream)
+// norm_rope(q, k or None, q_weight or None, k_weight or None, address of a kvx_rope, positions, eps,
+//           (q_out, k_out or None) or None, stream or None)
+PyObject* norm_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  arguments(nargs, 9);
+  const bool keys = args[1] != Py_None;
+  const at::Tensor &q = tensor(args[0], "q"), &k = keys ? tensor(args[1], "k") : q;
+  const at::Tensor& positions = tensor(args[5], "positions");
+  TORCH_CHECK_VALUE(q.dim() == 3 && k.dim() == 3 && k.size(0) == q.size(0) && k.size(2) == q.size(2) &&
+                        k.scalar_type() == q.scalar_type(),
+                    "q must be [T, H*G, d] and k [T, H, d], of one dtype");
+  TORCH_CHECK_VALUE(k.size(1) >= 1, "k has no heads");
+  const int64_t T = q.size(0), d = q.size(2);
+  const kvx_dtype dtype = dtype_of(q);
+  const Place place{q.device()};
+  const void *x[2] = {rows_address(place, q, "q"), keys ? rows_address(place, k, "k") : nullptr}, *weight[2] = {nullptr, nullptr};
+  const int64_t qs[2] = {q.stride(0), q.stride(1)}, ks[2] = {k.stride(0), k.stride(1)};
+  static const char* const names[2] = {"q_weight", "k_weight"};
+  for (int i = 0; i < 2; ++i) {
+    if (args[2 + i] == Py_None) continue;
+    TORCH_CHECK_VALUE(i == 0 || keys, "k_weight without k");
+    const at::Tensor& w = tensor(args[2 + i], names[i]);
+    TORCH_CHECK_VALUE(w.sizes() == at::IntArrayRef{d} && w.scalar_type() == q.scalar_type(), names[i],
+                      " must be [d] with q's dtype");
+    weight[i] = address(place, w, names[i]);
+  }
+  const kvx_rope* rope = static_cast<const kvx_rope*>(PyLong_AsVoidPtr(args[4]));
+  const double eps = PyFloat_AsDouble(args[6]);
+  if (PyErr_Occurred()) throw python_error();
+  const int32_t* positions_at = int32_at(place, positions, "positions", {T});
+  at::Tensor out[2];
+  if (args[7] == Py_None) {
+    out[0] = at::empty(q.sizes(), q.options());
+    if (keys) out[1] = at::empty(k.sizes(), k.options());
+  } else {
+    TORCH_CHECK_TYPE(PyTuple_Check(args[7]) && PyTuple_GET_SIZE(args[7]) == 2, "out must be a pair (q, k)");
+    for (int i = 0; i <= (keys ? 1 : 0); ++i) {
+      out[i] = tensor(PyTuple_GET_ITEM(args[7], i), i == 0 ? "out[0]" : "out[1]");
+      const at::Tensor& like = i == 0 ? q : k;
+      TORCH_CHECK_VALUE(out[i].sizes() == like.sizes() && out[i].scalar_type() == like.scalar_type(),
+                        "out must have the shapes and dtype of q and k");
+    }
+  }
+  call(place, norm_rope_entry, dtype, size32(T), size32(q.size(1)), keys ? size32(k.size(1)) : 0, size32(d), x[0], qs, x[1],
+       ks, weight[0], weight[1], (float)eps, rope, positions_at, address(place, out[0], "out[0]"),
+       keys ? address(place, out[1], "out[1]") : nullptr, stream_of(args[8], q));
+  if (args[7] != Py_None) {
+    Py_INCREF(args[7]);
+    return args[7];
+  }
+  PyObject* pair = PyTuple_New(2);
+  if (pair == nullptr) throw python_error();
+  PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(std::move(out[0])));
+  if (!keys) Py_INCREF(Py_None);
+  PyTuple_SET_ITEM(pair, 1, keys ? THPVariable_Wrap(std::move(out[1])) : Py_None);
+  return pair;
+  END_HANDLE_TH_ERRORS
+}
+
+template <typename F>
+bool entry(PyObject* args, Py_ssize_t i, F* to) {
+  void* p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
+  if (PyErr_Occurred()) return false;
+  *to = reinterpret_cast<F>(p);
+  return true;
+}
+
+// bind(check_status, plan_type, current_stream, addresses of kvx_plan_pages, kvx_store_cache8,
+//      kvx_attend_cache8, kvx_attend_workspace_bytes, kvx_norm_rope)
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *plan, *store, *attend, *bytes, *check, *type, *stream;
-  if (!PyArg_ParseTuple(args, "OOOOOO!O", &plan, &store, &attend, &bytes, &check, &PyType_Type, &type, &stream))
+  if (PyTuple_GET_SIZE(args) != 8) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 8 arguments");
     return nullptr;
-  void *p = PyLong_AsVoidPtr(plan), *s = PyLong_AsVoidPtr(store), *a = PyLong_AsVoidPtr(attend), *w = PyLong_AsVoidPtr(bytes);
-  if (PyErr_Occurred()) return nullptr;
-  if (!PyType_IsSubtype(reinterpret_cast<PyTypeObject*>(type), &PyTuple_Type)) {
+  }
+  PyObject* type = PyTuple_GET_ITEM(args, 1);
+  if (!PyType_Check(type) || !PyType_IsSubtype(reinterpret_cast<PyTypeObject*>(type), &PyTuple_Type)) {
     PyErr_SetString(PyExc_TypeError, "plan_type must be a tuple type");
     return nullptr;
   }
-  Py_INCREF(check);
-  Py_INCREF(type);
-  Py_INCREF(stream);
-  check_status = check;
+  if (!entry(args, 3, &plan_pages_entry) || !entry(args, 4, &store_cache8_entry) || !entry(args, 5, &attend_cache8_entry) ||
+      !entry(args, 6, &attend_workspace_bytes_entry) || !entry(args, 7, &norm_rope_entry))
+    return nullptr;
+  check_status = PyTuple_GET_ITEM(args, 0);
   plan_type = type;
-  current_stream = stream;
-  plan_pages_entry = reinterpret_cast<decltype(plan_pages_entry)>(p);
-  store_cache8_entry = reinterpret_cast<decltype(store_cache8_entry)>(s);
-  attend_cache8_entry = reinterpret_cast<decltype(attend_cache8_entry)>(a);
-  attend_workspace_bytes_entry = reinterpret_cast<decltype(attend_workspace_bytes_entry)>(w);
+  current_stream = PyTuple_GET_ITEM(args, 2);
+  Py_INCREF(check_status);
+  Py_INCREF(plan_type);
+  Py_INCREF(current_stream);
   Py_RETURN_NONE;
 }
 
@@ -289,6 +356,7 @@ PyMethodDef methods[] = {
     {"plan_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(plan_pages)), METH_FASTCALL, nullptr},
     {"store_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(store_cache8)), METH_FASTCALL, nullptr},
     {"attend_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend_cache8)), METH_FASTCALL, nullptr},
+    {"norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm_rope)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvx_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,6 +1,6 @@
 // Internal interface of the serving operators: host checks (kvx_serve.hip), page
-// plan (kvx_pages.hip), 8-bit store (kvx_store8.hip) and attention over the 8-bit
-// pool (kvx_attend8.hip).
+// plan (kvx_pages.hip), 8-bit store (kvx_store8.hip), attention over the 8-bit
+// pool (kvx_attend8.hip), norm and rotation (kvx_normrope.hip).
 #pragma once
 
 #include "kvx_internal.h"
@@ -55,5 +55,22 @@ size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);
 // Its kernel for many query rows a request (bf16).
 hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream);
 size_t attend_rows_ws_bytes(int d);
+
+struct NormRopeArgs {
+  const void* x[2];         // queries, keys
+  int64_t stride[2][2];     // elements: row, head
+  const void* weight[2];    // [d] or nullptr: no norm
+  void* out[2];             // [T, heads, d]
+  const int32_t* positions; // [T]
+  InvFreq turns;            // of each plane a position, 1 / (2 pi) times its frequency
+  float eps;
+  int32_t T, heads[2];
+  int32_t groups, chunks;   // head groups of a wave, waves of a token
+};
+hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, int d, int style, hipStream_t stream);
+
+// RoPE parameters: the map's checks and frequencies (kvx_api.hip).
+kvx_status check_rope_params(const kvx_rope* r, const char* which);
+void rope_frequencies(const kvx_rope& r, int d, InvFreq& out);
 
 }  // namespace kvx

@@ -1,5 +1,5 @@
 // Host side of the serving entry points of include/kvx.h (page plan, 8-bit store,
-// attention over the 8-bit pool): argument checks and launches.  Every check runs
+// attention over the 8-bit pool, norm and rotation): argument checks and launches.  Every check runs
 // before the first HIP call, so a rejected call enqueues nothing.
 #include "kvx_serve.h"
 
@@ -311,6 +311,72 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
   a.scale_log2 = scale * 1.44269504088896340736f;
   const hipError_t e = kvx::launch_attend(a, dt, m.d, workspace, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
+  return ok();
+}
+
+kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int32_t d, const void* q,
+                         const int64_t* q_strides, const void* k, const int64_t* k_strides,
+                         const void* q_weight, const void* k_weight, float eps, const kvx_rope* rope,
+                         const int32_t* positions, void* q_out, void* k_out, void* stream) {
+  kvx_status st = check_dtype(dtype);
+  if (st != KVX_OK) return st;
+  if ((st = check_d(d)) != KVX_OK) return st;
+  if (T < 0 || Hq < 1 || Hk < 0)
+    return set_error(KVX_ERR_SHAPE, "T=%d Hq=%d Hk=%d out of range (T, Hk >= 0, Hq >= 1)", T, Hq, Hk);
+  if ((st = check_rows(T)) != KVX_OK) return st;
+  if ((int64_t)Hq + Hk > 65535)
+    return set_error(KVX_ERR_UNSUPPORTED, "Hq+Hk=%lld exceeds 65535 heads", (long long)Hq + Hk);
+  if (!std::isfinite(eps) || eps < 0) return set_error(KVX_ERR_SHAPE, "eps must be finite and not negative");
+  if ((st = kvx::check_rope_params(rope, "target")) != KVX_OK) return st;
+  if (T == 0) return ok();
+  const int es = dtype == KVX_BF16 ? 2 : 4;
+  const int32_t heads[2] = {Hq, Hk};
+  const void* x[2] = {q, k};
+  const int64_t* strides[2] = {q_strides, k_strides};
+  const char* names[2] = {"q", "k"};
+  uint64_t bytes[2] = {0, 0};
+  const int operands = Hk > 0 ? 2 : 1;
+  for (int i = 0; i < operands; ++i) {
+    const int32_t n[2] = {T, heads[i]};
+    if ((st = check_strides(names[i], strides[i], n, 2, es, d, &bytes[i])) != KVX_OK) return st;
+  }
+  const uint64_t wb = (uint64_t)d * es;
+  const Span in[] = {{q, bytes[0], "q"},       {k, bytes[1], "k"}, {q_weight, wb, "q_weight"},
+                     {k_weight, operands > 1 ? wb : 0, "k_weight"}, {positions, (uint64_t)T * 4, "positions"}};
+  const Span out[] = {{q_out, (uint64_t)T * Hq * d * es, "q_out"}, {k_out, (uint64_t)T * Hk * d * es, "k_out"}};
+  if ((st = check_pointers(in, operands, 16)) != KVX_OK) return st;
+  for (int i = 0; i < operands; ++i)
+    if (in[2 + i].p != nullptr && (st = check_pointers(in + 2 + i, 1, 16)) != KVX_OK) return st;
+  if ((st = check_pointers(in + 4, 1, 4)) != KVX_OK) return st;
+  if ((st = check_pointers(out, operands, 16)) != KVX_OK) return st;
+  // an output may be its own dense input: every element is read before it is written, by its lane
+  Span others[5];
+  for (int i = 0; i < operands; ++i) {
+    const bool in_place = out[i].p == x[i] && (heads[i] == 1 || strides[i][1] == d) &&
+                          (T == 1 || strides[i][0] == (int64_t)heads[i] * d);
+    for (int j = 0; j < 5; ++j) others[j] = in[j];
+    if (in_place) others[i].bytes = 0;
+    if ((st = check_alias(out + i, 1, others, 5)) != KVX_OK) return st;
+  }
+  if ((st = check_alias(out, operands, nullptr, 0)) != KVX_OK) return st;
+  kvx::NormRopeArgs a;
+  std::memset(&a, 0, sizeof(a));
+  for (int i = 0; i < operands; ++i) {
+    a.x[i] = x[i];
+    a.stride[i][0] = strides[i][0];
+    a.stride[i][1] = strides[i][1];
+    a.weight[i] = in[2 + i].p;
+    a.out[i] = i == 0 ? q_out : k_out;
+    a.heads[i] = heads[i];
+  }
+  a.positions = positions;
+  a.eps = eps;
+  a.T = T;
+  kvx::rope_frequencies(*rope, d, a.turns);
+  for (int j = 0; j < d / 2; ++j) a.turns.w[j] *= 0.15915494309189533576888376337251;   // 1 / (2 pi)
+  const hipError_t e = kvx::launch_norm_rope(a, dtype == KVX_BF16 ? 0 : 1, d, rope->style,
+                                             reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return set_error(KVX_ERR_HIP, "norm and rotation launch: %s", hipGetErrorString(e));
   return ok();
 }
 

@@ -9,7 +9,7 @@ built, ``load()`` raises.
 
 Entry points mirror include/kvx.h: ``workspace_bytes``, ``rope_prepare``,
 ``map_cache``, ``map_layer``, ``map_cache_slots``; and for serving from the
-mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``.
+mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``, ``norm_rope``.
 """
 
 from __future__ import annotations
@@ -30,7 +30,8 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "fit_workspace_bytes", "fit_cache", "probe_workspace_bytes", "probe_r2",
            "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
            "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
-           "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8"]
+           "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8",
+           "norm_rope"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -182,6 +183,8 @@ def load():
     L.kvx_attend_cache8.restype = I32
     L.kvx_attend_kernel_name.argtypes = [AP, PP, I32]
     L.kvx_attend_kernel_name.restype = ctypes.c_char_p
+    L.kvx_norm_rope.argtypes = [I32, I32, I32, I32, I32, P, P, P, P, P, P, F32, RP, P, P, P, P]
+    L.kvx_norm_rope.restype = I32
     L.kvx_last_error.argtypes = []
     L.kvx_last_error.restype = ctypes.c_char_p
     L.kvx_version.argtypes = []
@@ -640,8 +643,8 @@ def _native():
             raise KvxNotBuilt(f"{bind_path()}: {e}; run python -m paper_2608_03893_amd.build") from e
         entry = [ctypes.cast(f, ctypes.c_void_p).value
                  for f in (lib.kvx_plan_pages, lib.kvx_store_cache8, lib.kvx_attend_cache8,
-                           lib.kvx_attend_workspace_bytes)]
-        _kvx_bind.bind(*entry, _check, PagePlan, torch._C._cuda_getCurrentRawStream)
+                           lib.kvx_attend_workspace_bytes, lib.kvx_norm_rope)]
+        _kvx_bind.bind(_check, PagePlan, torch._C._cuda_getCurrentRawStream, *entry)
         _BIND = _kvx_bind
     return _BIND
 
@@ -726,3 +729,20 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     with torch.cuda.stream(stream):
         return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, stream.cuda_stream,
                  longest)
+
+
+def norm_rope(q, k, q_weight, k_weight, rope, positions, eps=1e-6, out=None, stream=None):
+    """RMS norm and position rotation of query and key heads in one pass (enqueued on the
+    stream); returns (q, k) normed and rotated, dense, as store_cache8 (k transposed to
+    [1, H, T, d]) and attend_cache8 take them.  For inference: no gradient.
+
+    q [T, H*G, d], k [T, H, d] or None, bf16 or fp32, d dense, other strides of 16 bytes (parts
+    of a projection's rows are taken as they are); q_weight, k_weight [d] in the same type, or
+    None: rotated only; rope: the model's Rope or dict (see make_rope); positions int32 [T];
+    out: the pair to write to, which may be (q, k) itself where these are dense."""
+    f, rope = (_BIND or _native()).norm_rope, make_rope(rope)
+    at = ctypes.addressof(rope)
+    if stream is None:
+        return f(q, k, q_weight, k_weight, at, positions, eps, out, None)
+    with torch.cuda.stream(stream):
+        return f(q, k, q_weight, k_weight, at, positions, eps, out, stream.cuda_stream)
