@@ -606,6 +606,38 @@ kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int
                          const void* q_weight, const void* k_weight, float eps, const kvx_rope* rope,
                          const int32_t* positions, void* q_out, void* k_out, void* stream);
 
+/* Next tokens drawn from B rows of V logits, each with settings of its own.  The
+ * tokens of a row are ordered by falling logit, equal ones by rising index; then
+ *   top_k    keeps the first top_k tokens            (<= 0 or >= V: all)
+ *   top_p    of these the first whose probabilities, softmax(logits / temperature)
+ *            over them, reach top_p                  (>= 1 or NaN: all)
+ *   min_p    of these the ones of at least min_p times the best one's probability
+ *                                                    (<= 0 or NaN: all)
+ * and at least the best one stays.  The token drawn is the first, in order of the
+ * vocabulary, at which the sum of the kept probabilities exceeds u times their
+ * total.  A temperature of 0 (or less, or NaN) takes the best token, whatever the
+ * rest says.  Logits of -inf and NaN are never drawn; a row that has no others
+ * gives token -1 and logprob -inf; +inf leaves only its like.  Probabilities are
+ * formed in 64 bits and summed as whole numbers, multiples of 2^-43 of the best
+ * one, so a result does not depend on the order of sums; tokens below 2^-44 of
+ * the best one's are never drawn.
+ *   logits       bf16 or fp32, row b at b * stride (elements, not negative)
+ *   u            fp32 [B], uniform in [0, 1) (0 below it or NaN, 1 above)
+ *   temperature, top_p, min_p   fp32 [B] or NULL (1, all, all)
+ *   top_k        int32 [B] or NULL (all)
+ *   tokens       int32 [B]
+ *   logprob      fp32 [B] or NULL: ln of the probability with which the token was
+ *                drawn, among the kept ones (0 where the temperature is 0)
+ *   workspace    >= kvx_sample_workspace_bytes, 256-byte aligned; may hold
+ *                anything; calls on one stream may share it */
+#define KVX_MAX_DRAWS 65535
+#define KVX_MAX_VOCABULARY 1048576
+size_t kvx_sample_workspace_bytes(kvx_dtype dtype, int32_t B, int32_t V);
+kvx_status kvx_sample_tokens(kvx_dtype dtype, int32_t B, int32_t V, const void* logits, int64_t stride,
+                             const float* u, const float* temperature, const int32_t* top_k,
+                             const float* top_p, const float* min_p, int32_t* tokens, float* logprob,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text for the last non-OK status returned on the calling thread ("" if
  * none).  The pointer stays valid until the next kvx call on that thread. */
 const char* kvx_last_error(void);

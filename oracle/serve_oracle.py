@@ -173,3 +173,37 @@ def norm_rope(x, weight, eps, positions, rope):
 def _rope_planes(d, rope):
     j = np.arange(d // 2)
     return (j, j + d // 2) if int(rope.get("style", 0)) == 0 else (2 * j, 2 * j + 1)
+
+
+def sample_token(row, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The token drawn from one row of logits (float64), ln of its probability among the kept
+    ones, and how near the draw came to another answer: the least distance, over the total
+    weight, of a border (the draw's, top-p's, min-p's over the best weight) from its number."""
+    x = np.where(np.isnan(row), -np.inf, np.asarray(row, np.float64))
+    best = int(np.argmax(x))
+    if x[best] == -np.inf:
+        return -1, -np.inf, np.inf
+    if not temperature > 0:
+        return best, 0.0, np.inf
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.where(x == x[best], 1.0, np.exp((x - x[best]) / temperature))
+    w[(x == -np.inf) | ((x < x[best]) & (x[best] == np.inf))] = 0.0
+    order = np.lexsort((np.arange(len(x)), -x))
+    near = np.inf
+    if 0 < top_k < len(x):
+        order = order[:top_k]
+    if top_p < 1:
+        cum = np.cumsum(w[order])
+        t = max(float(top_p), 0.0) * cum[-1]
+        near = min(near, np.abs(cum - t).min() / cum[-1])
+        order = order[:int(np.searchsorted(cum, t)) + 1]
+    if min_p > 0:
+        floor = min(float(min_p), 1.0)
+        near = min(near, np.abs(np.where(w[order] == 1.0, 2.0, w[order]) - floor).min())
+        order = order[w[order] >= floor]
+    kept = np.sort(order)
+    cum = np.cumsum(w[kept])
+    t = min(max(float(u), 0.0), 1.0) * cum[-1]
+    near = min(near, np.abs(cum[:-1] - t).min(initial=np.inf) / cum[-1])
+    n = min(int(np.searchsorted(cum, t, side="right")), int(np.flatnonzero(w[kept]).max()))
+    return int(kept[n]), float(np.log(w[kept[n]] / cum[-1])), near

@@ -24,6 +24,8 @@ decltype(&kvx_store_cache8) store_cache8_entry = nullptr;
 decltype(&kvx_attend_cache8) attend_cache8_entry = nullptr;
 decltype(&kvx_attend_workspace_bytes) attend_workspace_bytes_entry = nullptr;
 decltype(&kvx_norm_rope) norm_rope_entry = nullptr;
+decltype(&kvx_sample_workspace_bytes) sample_workspace_bytes_entry = nullptr;
+decltype(&kvx_sample_tokens) sample_tokens_entry = nullptr;
 PyObject* check_status = nullptr;    // raises for a status that is not KVX_OK
 PyObject* plan_type = nullptr;       // the tuple plan_pages returns
 PyObject* current_stream = nullptr;  // raw handle of a device's current stream
@@ -319,6 +321,57 @@ PyObject* norm_rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// sample_tokens(logits, u, temperature, top_k, top_p, min_p (or None), out or None, with_logprob,
+//               workspace or None, stream or None)
+PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  arguments(nargs, 10);
+  const at::Tensor& logits = tensor(args[0], "logits");
+  TORCH_CHECK_VALUE(logits.dim() == 2, "logits must be [B, V]");
+  const int64_t B = logits.size(0), V = logits.size(1);
+  const kvx_dtype dtype = dtype_of(logits);
+  const Place place{logits.device()};
+  const void* logits_at = rows_address(place, logits, "logits");
+  auto floats = [&](PyObject* o, const char* name) -> const float* {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, name);
+    TORCH_CHECK_VALUE(t.scalar_type() == at::kFloat && t.sizes() == at::IntArrayRef{B}, name, " must be float32 [B]");
+    return static_cast<const float*>(address(place, t, name));
+  };
+  TORCH_CHECK_TYPE(THPVariable_Check(args[1]), "u must be a tensor");
+  const float *u_at = floats(args[1], "u"), *temperature = floats(args[2], "temperature");
+  const int32_t* top_k = args[3] == Py_None ? nullptr : int32_at(place, tensor(args[3], "top_k"), "top_k", {B});
+  const float *top_p = floats(args[4], "top_p"), *min_p = floats(args[5], "min_p");
+  const int with_logprob = PyObject_IsTrue(args[7]);
+  if (PyErr_Occurred()) throw python_error();
+  const int32_t B32 = size32(B), V32 = size32(V);
+  at::Tensor out, logprob, workspace;
+  if (args[8] == Py_None) {
+    const int64_t need = (int64_t)sample_workspace_bytes_entry(dtype, B32, V32);
+    if (need > 0) workspace = at::empty({need}, logits.options().dtype(at::kByte));
+  } else {
+    workspace = tensor(args[8], "workspace");
+  }
+  if (args[6] == Py_None) out = at::empty({B}, logits.options().dtype(at::kInt));
+  else out = tensor(args[6], "out");
+  int32_t* tokens = int32_at(place, out, "out", {B});
+  if (with_logprob) logprob = at::empty({B}, logits.options().dtype(at::kFloat));
+  call(place, sample_tokens_entry, dtype, B32, V32, logits_at, logits.stride(0), u_at, temperature, top_k, top_p, min_p, tokens,
+       with_logprob ? static_cast<float*>(logprob.data_ptr()) : nullptr,
+       workspace.defined() ? address(place, workspace, "workspace") : nullptr,
+       workspace.defined() ? (size_t)workspace.nbytes() : (size_t)0, stream_of(args[9], logits));
+  PyObject* result = args[6];
+  if (result == Py_None) result = THPVariable_Wrap(std::move(out));
+  else Py_INCREF(result);
+  if (!with_logprob || result == nullptr) return result;
+  PyObject* second = THPVariable_Wrap(std::move(logprob));
+  PyObject* both = second == nullptr ? nullptr : PyTuple_Pack(2, result, second);
+  Py_DECREF(result);
+  Py_XDECREF(second);
+  return both;
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 bool entry(PyObject* args, Py_ssize_t i, F* to) {
   void* p = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
@@ -328,10 +381,11 @@ bool entry(PyObject* args, Py_ssize_t i, F* to) {
 }
 
 // bind(check_status, plan_type, current_stream, addresses of kvx_plan_pages, kvx_store_cache8,
-//      kvx_attend_cache8, kvx_attend_workspace_bytes, kvx_norm_rope)
+//      kvx_attend_cache8, kvx_attend_workspace_bytes, kvx_norm_rope, kvx_sample_workspace_bytes,
+//      kvx_sample_tokens)
 PyObject* bind(PyObject*, PyObject* args) {
-  if (PyTuple_GET_SIZE(args) != 8) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 8 arguments");
+  if (PyTuple_GET_SIZE(args) != 10) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 10 arguments");
     return nullptr;
   }
   PyObject* type = PyTuple_GET_ITEM(args, 1);
@@ -340,7 +394,8 @@ PyObject* bind(PyObject*, PyObject* args) {
     return nullptr;
   }
   if (!entry(args, 3, &plan_pages_entry) || !entry(args, 4, &store_cache8_entry) || !entry(args, 5, &attend_cache8_entry) ||
-      !entry(args, 6, &attend_workspace_bytes_entry) || !entry(args, 7, &norm_rope_entry))
+      !entry(args, 6, &attend_workspace_bytes_entry) || !entry(args, 7, &norm_rope_entry) ||
+      !entry(args, 8, &sample_workspace_bytes_entry) || !entry(args, 9, &sample_tokens_entry))
     return nullptr;
   check_status = PyTuple_GET_ITEM(args, 0);
   plan_type = type;
@@ -356,6 +411,7 @@ PyMethodDef methods[] = {
     {"plan_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(plan_pages)), METH_FASTCALL, nullptr},
     {"store_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(store_cache8)), METH_FASTCALL, nullptr},
     {"attend_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend_cache8)), METH_FASTCALL, nullptr},
+    {"sample_tokens", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sample_tokens)), METH_FASTCALL, nullptr},
     {"norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm_rope)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvx_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

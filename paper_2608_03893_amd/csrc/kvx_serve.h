@@ -1,6 +1,7 @@
 // Internal interface of the serving operators: host checks (kvx_serve.hip), page
 // plan (kvx_pages.hip), 8-bit store (kvx_store8.hip), attention over the 8-bit
-// pool (kvx_attend8.hip), norm and rotation (kvx_normrope.hip).
+// pool (kvx_attend8.hip), norm and rotation (kvx_normrope.hip),
+// token sampling (kvx_sample.hip).
 #pragma once
 
 #include "kvx_internal.h"
@@ -68,6 +69,19 @@ struct NormRopeArgs {
   int32_t groups, chunks;   // head groups of a wave, waves of a token
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, int d, int style, hipStream_t stream);
+
+struct SampleArgs {
+  const void* logits;
+  int64_t stride;           // elements between rows
+  const float* u;           // [B]
+  const float *temperature, *top_p, *min_p;   // [B] or nullptr: off
+  const int32_t* top_k;     // [B] or nullptr
+  int32_t* tokens;          // [B]
+  float* logprob;           // [B] or nullptr
+  int32_t B, V;
+};
+hipError_t launch_sample(const SampleArgs& a, int dtype, void* ws, hipStream_t stream);
+size_t sample_ws_bytes(int B, int V, int dtype);
 
 // RoPE parameters: the map's checks and frequencies (kvx_api.hip).
 kvx_status check_rope_params(const kvx_rope* r, const char* which);

@@ -1,5 +1,6 @@
 // Host side of the serving entry points of include/kvx.h (page plan, 8-bit store,
-// attention over the 8-bit pool, norm and rotation): argument checks and launches.  Every check runs
+// attention over the 8-bit pool, norm and rotation, token sampling): argument checks and
+// launches.  Every check runs
 // before the first HIP call, so a rejected call enqueues nothing.
 #include "kvx_serve.h"
 
@@ -109,6 +110,17 @@ kvx_status check_pointers(const Span* s, int n, uintptr_t align) {
     if (!aligned(s[i].p, align))
       return set_error(KVX_ERR_UNSUPPORTED, "%s is not %d-byte aligned", s[i].name, (int)align);
   }
+  return KVX_OK;
+}
+
+kvx_status check_workspace(const void* workspace, size_t bytes, uint64_t need) {
+  if (need == 0) return KVX_OK;
+  if (workspace == nullptr)
+    return set_error(KVX_ERR_WORKSPACE, "workspace is NULL (%llu bytes needed)", (unsigned long long)need);
+  if (bytes < need)
+    return set_error(KVX_ERR_WORKSPACE, "workspace has %llu bytes, %llu needed", (unsigned long long)bytes,
+                     (unsigned long long)need);
+  if (!aligned(workspace, 256)) return set_error(KVX_ERR_WORKSPACE, "workspace is not 256-byte aligned");
   return KVX_OK;
 }
 
@@ -286,16 +298,7 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
   if ((st = check_pointers(in + 2, 4, 4)) != KVX_OK) return st;
   if ((st = check_pointers(outs, 1, 16)) != KVX_OK) return st;
   if (lse != nullptr && (st = check_pointers(outs + 1, 1, 4)) != KVX_OK) return st;
-  if (need > 0) {
-    if (workspace == nullptr)
-      return set_error(KVX_ERR_WORKSPACE, "workspace is NULL (%llu bytes needed)",
-                       (unsigned long long)need);
-    if (workspace_bytes < need)
-      return set_error(KVX_ERR_WORKSPACE, "workspace has %llu bytes, %llu needed",
-                       (unsigned long long)workspace_bytes, (unsigned long long)need);
-    if (!aligned(workspace, 256))
-      return set_error(KVX_ERR_WORKSPACE, "workspace is not 256-byte aligned");
-  }
+  if ((st = check_workspace(workspace, workspace_bytes, need)) != KVX_OK) return st;
   if ((st = check_alias(outs, 3, in, 6)) != KVX_OK) return st;
   kvx::AttendArgs a = attend_sizes(m, *pool, log2p);
   a.q = q;
@@ -377,6 +380,62 @@ kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int
   const hipError_t e = kvx::launch_norm_rope(a, dtype == KVX_BF16 ? 0 : 1, d, rope->style,
                                              reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "norm and rotation launch: %s", hipGetErrorString(e));
+  return ok();
+}
+
+static kvx_status check_sample(kvx_dtype dtype, int32_t B, int32_t V) {
+  kvx_status st = check_dtype(dtype);
+  if (st != KVX_OK) return st;
+  if (B < 0 || V < 1) return set_error(KVX_ERR_SHAPE, "B=%d V=%d out of range (B >= 0, V >= 1)", B, V);
+  if (B > KVX_MAX_DRAWS || V > KVX_MAX_VOCABULARY)
+    return set_error(KVX_ERR_UNSUPPORTED, "B=%d exceeds %d rows or V=%d exceeds %d tokens", B, KVX_MAX_DRAWS, V,
+                     KVX_MAX_VOCABULARY);
+  return KVX_OK;
+}
+
+size_t kvx_sample_workspace_bytes(kvx_dtype dtype, int32_t B, int32_t V) {
+  if (check_sample(dtype, B, V) != KVX_OK || B == 0) return 0;
+  return kvx::sample_ws_bytes(B, V, dtype == KVX_BF16 ? 0 : 1);
+}
+
+kvx_status kvx_sample_tokens(kvx_dtype dtype, int32_t B, int32_t V, const void* logits, int64_t stride,
+                             const float* u, const float* temperature, const int32_t* top_k,
+                             const float* top_p, const float* min_p, int32_t* tokens, float* logprob,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  kvx_status st = check_sample(dtype, B, V);
+  if (st != KVX_OK) return st;
+  const int dt = dtype == KVX_BF16 ? 0 : 1, es = dt == 0 ? 2 : 4;
+  if (B > 1 && stride < 0) return set_error(KVX_ERR_SHAPE, "logits stride %lld is negative", (long long)stride);
+  const unsigned __int128 bytes = ((unsigned __int128)(B > 1 ? B - 1 : 0) * (uint64_t)(B > 1 ? stride : 0) + (uint32_t)V) * es;
+  if (bytes >= (uint64_t)1 << 60) return set_error(KVX_ERR_SHAPE, "logits stride reaches too far");
+  if (B == 0) return ok();
+  const uint64_t b4 = (uint64_t)B * 4, need = kvx::sample_ws_bytes(B, V, dt);
+  const Span in[] = {{logits, (uint64_t)bytes, "logits"}, {u, b4, "u"},          {temperature, b4, "temperature"},
+                     {top_k, b4, "top_k"},               {top_p, b4, "top_p"}, {min_p, b4, "min_p"}};
+  const Span out[] = {{tokens, b4, "tokens"}, {logprob, b4, "logprob"}, {workspace, need, "workspace"}};
+  if ((st = check_pointers(in, 1, es)) != KVX_OK) return st;
+  if ((st = check_pointers(in + 1, 1, 4)) != KVX_OK) return st;
+  for (int i = 2; i < 6; ++i)
+    if (in[i].p != nullptr && (st = check_pointers(in + i, 1, 4)) != KVX_OK) return st;
+  if ((st = check_pointers(out, 1, 4)) != KVX_OK) return st;
+  if (logprob != nullptr && (st = check_pointers(out + 1, 1, 4)) != KVX_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, need)) != KVX_OK) return st;
+  if ((st = check_alias(out, 3, in, 6)) != KVX_OK) return st;
+  kvx::SampleArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.logits = logits;
+  a.stride = stride;
+  a.u = u;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.tokens = tokens;
+  a.logprob = logprob;
+  a.B = B;
+  a.V = V;
+  const hipError_t e = kvx::launch_sample(a, dt, workspace, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return set_error(KVX_ERR_HIP, "token sampling launch: %s", hipGetErrorString(e));
   return ok();
 }
 

@@ -9,7 +9,8 @@ built, ``load()`` raises.
 
 Entry points mirror include/kvx.h: ``workspace_bytes``, ``rope_prepare``,
 ``map_cache``, ``map_layer``, ``map_cache_slots``; and for serving from the
-mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``, ``norm_rope``.
+mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``, ``norm_rope``,
+``sample_tokens``.
 """
 
 from __future__ import annotations
@@ -31,7 +32,7 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
            "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
            "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8",
-           "norm_rope"]
+           "norm_rope", "sample_workspace", "sample_tokens"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -185,6 +186,10 @@ def load():
     L.kvx_attend_kernel_name.restype = ctypes.c_char_p
     L.kvx_norm_rope.argtypes = [I32, I32, I32, I32, I32, P, P, P, P, P, P, F32, RP, P, P, P, P]
     L.kvx_norm_rope.restype = I32
+    L.kvx_sample_workspace_bytes.argtypes = [I32, I32, I32]
+    L.kvx_sample_workspace_bytes.restype = SZ
+    L.kvx_sample_tokens.argtypes = [I32, I32, I32, P, I64, P, P, P, P, P, P, P, P, SZ, P]
+    L.kvx_sample_tokens.restype = I32
     L.kvx_last_error.argtypes = []
     L.kvx_last_error.restype = ctypes.c_char_p
     L.kvx_version.argtypes = []
@@ -643,7 +648,8 @@ def _native():
             raise KvxNotBuilt(f"{bind_path()}: {e}; run python -m paper_2608_03893_amd.build") from e
         entry = [ctypes.cast(f, ctypes.c_void_p).value
                  for f in (lib.kvx_plan_pages, lib.kvx_store_cache8, lib.kvx_attend_cache8,
-                           lib.kvx_attend_workspace_bytes, lib.kvx_norm_rope)]
+                           lib.kvx_attend_workspace_bytes, lib.kvx_norm_rope,
+                           lib.kvx_sample_workspace_bytes, lib.kvx_sample_tokens)]
         _kvx_bind.bind(_check, PagePlan, torch._C._cuda_getCurrentRawStream, *entry)
         _BIND = _kvx_bind
     return _BIND
@@ -746,3 +752,29 @@ def norm_rope(q, k, q_weight, k_weight, rope, positions, eps=1e-6, out=None, str
         return f(q, k, q_weight, k_weight, at, positions, eps, out, None)
     with torch.cuda.stream(stream):
         return f(q, k, q_weight, k_weight, at, positions, eps, out, stream.cuda_stream)
+
+
+def sample_workspace(logits, stream=None):
+    """A workspace for sample_tokens calls of these logits' shape, to be kept between them."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [B, V]")
+    need = int(load().kvx_sample_workspace_bytes(_dtype_code(logits), *logits.shape))
+    return _scratch(need, logits.device, stream)
+
+
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+                  with_logprob=False, workspace=None, stream=None):
+    """Next tokens int32 [B] drawn from logits [B, V] (enqueued on the stream); with_logprob
+    also the logarithms fp32 [B] of the probabilities with which they were drawn.
+
+    logits bf16 or fp32, dense rows; u fp32 [B]: a uniform random number for each row;
+    temperature, top_p, min_p fp32 [B], top_k int32 [B] or None: off.  Tokens ordered by
+    falling logit, equal ones by index: the first top_k, of these the first whose
+    probabilities reach top_p, of these those of at least min_p of the best one's.  Drawn by
+    u in order of the vocabulary; temperature 0: the best one.  -1 where no logit is finite
+    (masked rows); see include/kvx.h for the rest."""
+    f = (_BIND or _native()).sample_tokens
+    if stream is None:
+        return f(logits, u, temperature, top_k, top_p, min_p, out, with_logprob, workspace, None)
+    with torch.cuda.stream(stream):
+        return f(logits, u, temperature, top_k, top_p, min_p, out, with_logprob, workspace, stream.cuda_stream)
