@@ -584,6 +584,35 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
  * static string, NULL for invalid arguments and for calls that launch nothing. */
 const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype);
 
+/* Attention of requests that share prefixes, each prefix read and multiplied once for
+ * all rows that see it (a common context handed over once, and many continuations).
+ * Prefix s has prefix_lens[s] tokens in the pages prefix_tables[s]; requests
+ * prefix_cu[s] .. prefix_cu[s + 1] - 1 share it, and those before prefix_cu[0] and from
+ * prefix_cu[S] on have none.  A request's keys are its prefix's, all of which every row
+ * of it sees, and behind them its own, for which block_tables, lens, cu and the rest
+ * are as in kvx_attend_cache8: row i of n sees own keys 0 .. lens[b] - n + i.  lens
+ * and block_tables count and list own tokens only (so kvx_plan_pages hands out and
+ * takes back own pages alone; a token's position is its prefix's length more than
+ * the plan's), and own tokens begin on a page of their own.
+ *   prefix          S, the entries of a row of prefix_tables, and the most keys of
+ *                   a prefix (0: as many as its row holds; see kvx_attend_dims)
+ *   prefix_tables   int32 [S, prefix->max_pages]; entries out of range: unseen keys
+ *   prefix_lens     int32 [S], at most prefix->max_pages * page_size
+ *   prefix_cu       int32 [S + 1], rising, at most B
+ *   workspace       >= kvx_prefix_workspace_bytes, else as in kvx_attend_cache8
+ * dims, pool: the requests' (pool->max_pages: entries of a row of block_tables).
+ * S == 0 is kvx_attend_cache8.  The two parts of a row are joined in fp32. */
+typedef struct kvx_prefix_dims {
+  int32_t S, max_pages, longest;
+} kvx_prefix_dims;
+size_t kvx_prefix_workspace_bytes(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, kvx_dtype dtype);
+kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, const kvx_pool* pool,
+                              kvx_dtype dtype, const void* q, const int64_t* q_strides, const uint8_t* codes,
+                              const float* scales, const int32_t* prefix_tables, const int32_t* prefix_lens,
+                              const int32_t* prefix_cu, const int32_t* block_tables, const int32_t* lens,
+                              const int32_t* cu, float scale, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 /* RMS norm and position rotation of a step's query and key heads, as the target
  * model's layers do between their projections and the cache (kvx_store_cache8)
  * or the attention.  For row t, head h and x = q[t, h] (k[t, h] alike):

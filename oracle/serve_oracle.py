@@ -207,3 +207,49 @@ def sample_token(row, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     near = min(near, np.abs(cum[:-1] - t).min(initial=np.inf) / cum[-1])
     n = min(int(np.searchsorted(cum, t, side="right")), int(np.flatnonzero(w[kept]).max()))
     return int(kept[n]), float(np.log(w[kept[n]] / cum[-1])), near
+
+
+def attend_prefix8(q, codes, scales, prefix_tables, prefix_lens, prefix_cu, tables, lens, cu, scale):
+    """attend_cache8 where requests prefix_cu[s] .. prefix_cu[s + 1] - 1 have the keys of prefix s
+    before their own; every row sees all of these."""
+    T, heads, d = q.shape
+    H, S, N = codes.shape[1], codes.shape[2], scales.shape[2]
+    G, P, B = heads // H, S // N, tables.shape[0]
+    out = np.full(q.shape, np.nan)
+    lse = np.full((T, heads), np.nan)
+    size_v, size_s = np.zeros(q.shape), np.zeros((T, heads))
+
+    def keys(table, n):
+        n = min(max(int(n), 0), len(table) * P)
+        page = np.repeat(table[:-(-n // P)].astype(np.int64), P)[:n]
+        real = (page >= 0) & (page < N)
+        return real, np.where(real, page, 0) * P + np.arange(n) % P
+
+    for b in range(B):
+        a, e = min(max(int(cu[b]), 0), T), min(int(cu[b + 1]), T)
+        mine = [s for s in range(len(prefix_lens)) if prefix_cu[s] <= b < prefix_cu[s + 1]]
+        real, slot = keys(tables[b], lens[b])
+        first = 0
+        if mine:
+            real_p, slot_p = keys(prefix_tables[mine[0]], prefix_lens[mine[0]])
+            first = len(slot_p)
+            real, slot = np.concatenate([real_p, real]), np.concatenate([slot_p, slot])
+        for h in range(H):
+            K = E4M3[codes[0, h, slot]] * scales[0, h, slot // P, None]
+            V = E4M3[codes[1, h, slot]] * scales[1, h, slot // P, None]
+            for t in range(a, e):
+                own = max(len(slot) - first - (e - t) + 1, 0)
+                see = np.flatnonzero(real[:first + own])
+                for x in range(h * G, (h + 1) * G):
+                    if len(see) == 0:
+                        out[t, x], lse[t, x] = 0.0, -np.inf
+                        continue
+                    s = scale * (K[see] @ q[t, x])
+                    top = s.max()
+                    p = np.exp(s - top)
+                    lse[t, x] = top + np.log(p.sum())
+                    p /= p.sum()
+                    out[t, x] = p @ V[see]
+                    size_v[t, x] = p @ np.abs(V[see])
+                    size_s[t, x] = abs(scale) * (np.abs(K[see]) @ np.abs(q[t, x])).max()
+    return out, lse, size_v, size_s

@@ -122,9 +122,50 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return a / b;
 }
 
+// Last key that the rows of a request's new token `token` see.
+__device__ __forceinline__ int last_key(const AttendArgs&, const Request& r, int token) { return r.len - r.tokens + token; }
+
+// What becomes of a unit's sums (request b's): of row `to` the reference `top` of its exponents,
+// their sum `den`, and the weighted values.
+struct Finish {
+  // Four channels from jc on.
+  template <int DT, int D>
+  __device__ __forceinline__ void row(const AttendArgs& a, int64_t to, int jc, float top, float den, f32x4_t sum) const {
+    const f32x4_t y = sum * (den == 0.0f ? 0.0f : 1.0f / den);    // no key: 0
+    if (DT == 0)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to * D + jc) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+    else
+      *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + to * D + jc) = y;
+    if (a.lse != nullptr && jc == 0)
+      a.lse[to] = den == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+  }
+  // bf16, channels (4 g4 + i) C + c, C = D / 16, of one of four lanes.
+  template <int D>
+  __device__ __forceinline__ void tile(const AttendArgs& a, int64_t to, int g4, float m, float l, const f32x4_t* o) const {
+    constexpr int C = D / 16;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;    // no key: 0
+    u32x4_t* y = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) + to * D + 4 * C * g4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (C == 8) {
+        u32x4_t w;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = pack2(o[(2 * c) % C][i] * f, o[(2 * c + 1) % C][i] * f);
+        y[i] = w;
+      } else if (i % 2 == 0) {
+        y[i / 2] = (u32x4_t){pack2(o[0][i] * f, o[1][i] * f), pack2(o[2][i] * f, o[3][i] * f),
+                             pack2(o[0][i + 1] * f, o[1][i + 1] * f), pack2(o[2][i + 1] * f, o[3][i + 1] * f)};
+      }
+    }
+    if (a.lse != nullptr && g4 == 0)
+      a.lse[to] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+  }
+};
+__device__ __forceinline__ Finish finisher(const AttendArgs&, int) { return Finish(); }
+
 // pre[b] = sum of weight(request, number) over requests 0 .. b, by a workgroup of THREADS; part: an entry per wave.
-template <int THREADS, typename W>
-__device__ __forceinline__ void prefix_requests(const AttendArgs& a, int64_t* pre, int64_t* part, W weight) {
+template <int THREADS, typename A, typename W>
+__device__ __forceinline__ void prefix_requests(const A& a, int64_t* pre, int64_t* part, W weight) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int chunk = (a.B + THREADS - 1) / THREADS;
   const int b0 = tid * chunk < a.B ? tid * chunk : a.B, b1 = b0 + chunk < a.B ? b0 + chunk : a.B;

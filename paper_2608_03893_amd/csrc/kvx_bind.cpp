@@ -26,6 +26,8 @@ decltype(&kvx_attend_workspace_bytes) attend_workspace_bytes_entry = nullptr;
 decltype(&kvx_norm_rope) norm_rope_entry = nullptr;
 decltype(&kvx_sample_workspace_bytes) sample_workspace_bytes_entry = nullptr;
 decltype(&kvx_sample_tokens) sample_tokens_entry = nullptr;
+decltype(&kvx_prefix_workspace_bytes) prefix_workspace_bytes_entry = nullptr;
+decltype(&kvx_attend_prefix8) attend_prefix8_entry = nullptr;
 PyObject* check_status = nullptr;    // raises for a status that is not KVX_OK
 PyObject* plan_type = nullptr;       // the tuple plan_pages returns
 PyObject* current_stream = nullptr;  // raw handle of a device's current stream
@@ -206,59 +208,111 @@ PyObject* store_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// What both attention calls have: operands, sizes, outputs.
+struct Attention {
+  const at::Tensor &q, &codes, &scales, &tables;
+  const int64_t T, heads, d, H, B, M;
+  const kvx_pool pool;
+  const kvx_attend_dims dims;
+  const kvx_dtype dtype;
+  const Place place;
+  const void* q_at;
+  const int64_t strides[2];
+  const uint8_t* codes_at;
+  const float* scales_at;
+  const int32_t *tables_at, *lens_at, *cu_at;
+  float scale;
+  int with_lse;
+  at::Tensor out, lse;
+
+  static const at::Tensor& shaped(const at::Tensor& q, const at::Tensor& codes, const at::Tensor& tables) {
+    TORCH_CHECK_VALUE(q.dim() == 3 && codes.dim() == 4 && tables.dim() == 2,
+                      "q must be [T, H*G, d], pool [2, H, num_slots, d], block_tables [B, max_pages]");
+    TORCH_CHECK_VALUE(codes.size(1) >= 1 && q.size(1) % codes.size(1) == 0 && codes.size(3) == q.size(2), q.size(1),
+                      " query heads of ", q.size(2), " channels on a pool of ", codes.size(1), " heads of ", codes.size(3));
+    return q;
+  }
+  Attention(PyObject* q_, PyObject* codes_, PyObject* scales_, PyObject* tables_, PyObject* lens, PyObject* cu,
+            PyObject* scale_, PyObject* lse_, PyObject* longest)
+      : q(shaped(tensor(q_, "q"), tensor(codes_, "pool"), tensor(tables_, "block_tables"))), codes(tensor(codes_, "pool")),
+        scales(tensor(scales_, "scales")), tables(tensor(tables_, "block_tables")), T(q.size(0)), heads(q.size(1)),
+        d(q.size(2)), H(codes.size(1)), B(tables.size(0)), M(tables.size(1)), pool(pool_of(codes, scales, {2, H}, size32(M))),
+        dims{size32(B), size32(H), size32(heads / H), size32(T), size32(d), size32(PyLong_AsLongLong(longest))},
+        dtype(dtype_of(q)), place{q.device()}, q_at(rows_address(place, q, "q")), strides{q.stride(0), q.stride(1)},
+        codes_at(static_cast<const uint8_t*>(address(place, codes, "pool"))),
+        scales_at(static_cast<const float*>(address(place, scales, "scales"))),
+        tables_at(int32_at(place, tables, "block_tables", {B, M})), lens_at(int32_at(place, tensor(lens, "lens"), "lens", {B})),
+        cu_at(int32_at(place, tensor(cu, "cu"), "cu", {B + 1})),
+        scale((float)(scale_ == Py_None ? 1.0 / std::sqrt((double)d) : PyFloat_AsDouble(scale_))),
+        with_lse(PyObject_IsTrue(lse_)) {
+    if (PyErr_Occurred()) throw python_error();
+  }
+  // The workspace given, or one of `need` bytes whose counters are cleared.
+  at::Tensor workspace(PyObject* given, size_t need) const {
+    if (given != Py_None) return tensor(given, "workspace");
+    const at::Tensor w = at::empty({need > 0 ? (int64_t)need : 1}, q.options().dtype(at::kByte));
+    if (need > 0) w.narrow(0, 0, KVX_ATTEND_COUNTER_BYTES).zero_();
+    return w;
+  }
+  void outputs(PyObject* given) {
+    if (given == Py_None) {
+      out = at::empty(q.sizes(), q.options());
+    } else {
+      out = tensor(given, "out");
+      TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out must have q's shape and dtype");
+    }
+    if (with_lse) lse = at::empty({T, heads}, q.options().dtype(at::kFloat));
+  }
+  float* lse_at() const { return with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr; }
+  PyObject* result(PyObject* given) {
+    PyObject* first = given;
+    if (given == Py_None) first = THPVariable_Wrap(std::move(out));
+    else Py_INCREF(given);
+    if (!with_lse || first == nullptr) return first;
+    PyObject* second = THPVariable_Wrap(std::move(lse));
+    PyObject* both = second == nullptr ? nullptr : PyTuple_Pack(2, first, second);
+    Py_DECREF(first);
+    Py_XDECREF(second);
+    return both;
+  }
+};
+
 // attend_cache8(q, pool, scales, block_tables, lens, cu, scale or None, out or None, with_lse,
 //               workspace or None, stream or None, longest)
 PyObject* attend_cache8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   arguments(nargs, 12);
-  const at::Tensor &q = tensor(args[0], "q"), &codes = tensor(args[1], "pool"), &scales = tensor(args[2], "scales");
-  const at::Tensor &tables = tensor(args[3], "block_tables"), &lens = tensor(args[4], "lens"), &cu = tensor(args[5], "cu");
-  TORCH_CHECK_VALUE(q.dim() == 3 && codes.dim() == 4 && tables.dim() == 2,
-                    "q must be [T, H*G, d], pool [2, H, num_slots, d], block_tables [B, max_pages]");
-  const int64_t T = q.size(0), heads = q.size(1), d = q.size(2), H = codes.size(1), B = tables.size(0), M = tables.size(1);
-  TORCH_CHECK_VALUE(H >= 1 && heads % H == 0 && codes.size(3) == d, heads, " query heads of ", d,
-                    " channels on a pool of ", H, " heads of ", codes.size(3));
-  const kvx_pool pool = pool_of(codes, scales, {2, H}, size32(M));
-  const kvx_attend_dims dims{size32(B), size32(H), size32(heads / H), size32(T), size32(d),
-                             size32(PyLong_AsLongLong(args[11]))};
-  const kvx_dtype dtype = dtype_of(q);
-  const Place place{q.device()};
-  const void* q_at = rows_address(place, q, "q");
-  const int64_t strides[2] = {q.stride(0), q.stride(1)};
-  const uint8_t* codes_at = static_cast<const uint8_t*>(address(place, codes, "pool"));
-  const float* scales_at = static_cast<const float*>(address(place, scales, "scales"));
-  const int32_t *tables_at = int32_at(place, tables, "block_tables", {B, M}), *lens_at = int32_at(place, lens, "lens", {B});
-  const int32_t* cu_at = int32_at(place, cu, "cu", {B + 1});
-  const double scale = args[6] == Py_None ? 1.0 / std::sqrt((double)d) : PyFloat_AsDouble(args[6]);
-  const int with_lse = PyObject_IsTrue(args[8]);
+  Attention x(args[0], args[1], args[2], args[3], args[4], args[5], args[6], args[8], args[11]);
+  const at::Tensor workspace = x.workspace(args[9], args[9] == Py_None ? attend_workspace_bytes_entry(&x.dims, x.dtype) : 0);
+  x.outputs(args[7]);
+  call(x.place, attend_cache8_entry, &x.dims, &x.pool, x.dtype, x.q_at, x.strides, x.codes_at, x.scales_at, x.tables_at,
+       x.lens_at, x.cu_at, x.scale, address(x.place, x.out, "out"), x.lse_at(), address(x.place, workspace, "workspace"),
+       (size_t)workspace.numel(), stream_of(args[10], x.q));
+  return x.result(args[7]);
+  END_HANDLE_TH_ERRORS
+}
+
+// attend_prefix8(q, pool, scales, prefix_tables, prefix_lens, prefix_cu, block_tables, lens, cu, scale or
+//                None, out or None, with_lse, workspace or None, stream or None, longest, longest_prefix)
+PyObject* attend_prefix8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  arguments(nargs, 16);
+  Attention x(args[0], args[1], args[2], args[6], args[7], args[8], args[9], args[11], args[14]);
+  const at::Tensor& tables = tensor(args[3], "prefix_tables");
+  TORCH_CHECK_VALUE(tables.dim() == 2, "prefix_tables must be [S, max_pages]");
+  const int64_t S = tables.size(0), M = tables.size(1), longest = PyLong_AsLongLong(args[15]);
   if (PyErr_Occurred()) throw python_error();
-  at::Tensor out, lse, workspace;
-  if (args[9] == Py_None) {
-    const int64_t need = (int64_t)attend_workspace_bytes_entry(&dims, dtype);
-    workspace = at::empty({need > 0 ? need : 1}, q.options().dtype(at::kByte));
-    if (need > 0) workspace.narrow(0, 0, KVX_ATTEND_COUNTER_BYTES).zero_();
-  } else {
-    workspace = tensor(args[9], "workspace");
-  }
-  if (args[7] == Py_None) {
-    out = at::empty(q.sizes(), q.options());
-  } else {
-    out = tensor(args[7], "out");
-    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out must have q's shape and dtype");
-  }
-  if (with_lse) lse = at::empty({T, heads}, q.options().dtype(at::kFloat));
-  call(place, attend_cache8_entry, &dims, &pool, dtype, q_at, strides, codes_at, scales_at, tables_at, lens_at, cu_at,
-       (float)scale, address(place, out, "out"), with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
-       address(place, workspace, "workspace"), (size_t)workspace.numel(), stream_of(args[10], q));
-  PyObject* result = args[7];
-  if (result == Py_None) result = THPVariable_Wrap(std::move(out));
-  else Py_INCREF(result);
-  if (!with_lse || result == nullptr) return result;
-  PyObject* second = THPVariable_Wrap(std::move(lse));
-  PyObject* both = second == nullptr ? nullptr : PyTuple_Pack(2, result, second);
-  Py_DECREF(result);
-  Py_XDECREF(second);
-  return both;
+  const kvx_prefix_dims prefix{size32(S), size32(M), size32(longest)};
+  const int32_t *tables_at = int32_at(x.place, tables, "prefix_tables", {S, M}),
+                *lens_at = int32_at(x.place, tensor(args[4], "prefix_lens"), "prefix_lens", {S}),
+                *cu_at = int32_at(x.place, tensor(args[5], "prefix_cu"), "prefix_cu", {S + 1});
+  const at::Tensor workspace =
+      x.workspace(args[12], args[12] == Py_None ? prefix_workspace_bytes_entry(&x.dims, &prefix, x.dtype) : 0);
+  x.outputs(args[10]);
+  call(x.place, attend_prefix8_entry, &x.dims, &prefix, &x.pool, x.dtype, x.q_at, x.strides, x.codes_at, x.scales_at, tables_at,
+       lens_at, cu_at, x.tables_at, x.lens_at, x.cu_at, x.scale, address(x.place, x.out, "out"), x.lse_at(),
+       address(x.place, workspace, "workspace"), (size_t)workspace.numel(), stream_of(args[13], x.q));
+  return x.result(args[10]);
   END_HANDLE_TH_ERRORS
 }
 
@@ -382,10 +436,10 @@ bool entry(PyObject* args, Py_ssize_t i, F* to) {
 
 // bind(check_status, plan_type, current_stream, addresses of kvx_plan_pages, kvx_store_cache8,
 //      kvx_attend_cache8, kvx_attend_workspace_bytes, kvx_norm_rope, kvx_sample_workspace_bytes,
-//      kvx_sample_tokens)
+//      kvx_sample_tokens, kvx_prefix_workspace_bytes, kvx_attend_prefix8)
 PyObject* bind(PyObject*, PyObject* args) {
-  if (PyTuple_GET_SIZE(args) != 10) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 10 arguments");
+  if (PyTuple_GET_SIZE(args) != 12) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 12 arguments");
     return nullptr;
   }
   PyObject* type = PyTuple_GET_ITEM(args, 1);
@@ -395,7 +449,8 @@ PyObject* bind(PyObject*, PyObject* args) {
   }
   if (!entry(args, 3, &plan_pages_entry) || !entry(args, 4, &store_cache8_entry) || !entry(args, 5, &attend_cache8_entry) ||
       !entry(args, 6, &attend_workspace_bytes_entry) || !entry(args, 7, &norm_rope_entry) ||
-      !entry(args, 8, &sample_workspace_bytes_entry) || !entry(args, 9, &sample_tokens_entry))
+      !entry(args, 8, &sample_workspace_bytes_entry) || !entry(args, 9, &sample_tokens_entry) ||
+      !entry(args, 10, &prefix_workspace_bytes_entry) || !entry(args, 11, &attend_prefix8_entry))
     return nullptr;
   check_status = PyTuple_GET_ITEM(args, 0);
   plan_type = type;
@@ -411,6 +466,7 @@ PyMethodDef methods[] = {
     {"plan_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(plan_pages)), METH_FASTCALL, nullptr},
     {"store_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(store_cache8)), METH_FASTCALL, nullptr},
     {"attend_cache8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend_cache8)), METH_FASTCALL, nullptr},
+    {"attend_prefix8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend_prefix8)), METH_FASTCALL, nullptr},
     {"sample_tokens", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sample_tokens)), METH_FASTCALL, nullptr},
     {"norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm_rope)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

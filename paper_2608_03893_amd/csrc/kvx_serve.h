@@ -1,6 +1,6 @@
 // Internal interface of the serving operators: host checks (kvx_serve.hip), page
 // plan (kvx_pages.hip), 8-bit store (kvx_store8.hip), attention over the 8-bit
-// pool (kvx_attend8.hip), norm and rotation (kvx_normrope.hip),
+// pool (kvx_attend8.hip) and over shared prefixes (kvx_prefix8_*.hip), norm and rotation (kvx_normrope.hip),
 // token sampling (kvx_sample.hip).
 #pragma once
 
@@ -36,6 +36,7 @@ struct StoreArgs {
 hipError_t launch_store(const StoreArgs& a, int dtype, int d, hipStream_t stream);
 
 struct AttendArgs {
+  static constexpr bool kCausal = true;
   const void* q;
   int64_t q_stride[2];      // elements: row, query head
   const uint8_t* codes;     // [2, H, N << log2p, d]
@@ -56,6 +57,19 @@ size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);
 // Its kernel for many query rows a request (bf16).
 hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream);
 size_t attend_rows_ws_bytes(int d);
+
+// Attention over prefixes that requests share (kvx_prefix8_*.hip), in two launches: the common
+// part's B, tables, lens, M and keys are the prefixes', the own part's the requests'.
+struct PrefixArgs : AttendArgs {
+  const int32_t* shares;    // [prefixes + 1] requests of each prefix
+  float* sums;              // [T, H * G, d] the common part's weighted values
+  float* stats;             // [T, H * G, 2] reference and sum of its exponentials
+  int32_t prefixes, requests;
+};
+hipError_t launch_prefix_common(const PrefixArgs& a, int dtype, int d, void* ws, hipStream_t stream);
+hipError_t launch_prefix_own(const PrefixArgs& a, int dtype, int d, void* ws, hipStream_t stream);
+hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream);
+hipError_t launch_prefix_own_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream);
 
 struct NormRopeArgs {
   const void* x[2];         // queries, keys

@@ -383,6 +383,110 @@ kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int
   return ok();
 }
 
+static kvx_status check_prefix(const kvx_prefix_dims* p) {
+  if (p == nullptr) return set_error(KVX_ERR_NULL, "prefix is NULL");
+  if (p->S < 0 || p->max_pages < 1 || p->longest < 0)
+    return set_error(KVX_ERR_SHAPE, "prefix out of range: S=%d max_pages=%d longest=%d", p->S, p->max_pages, p->longest);
+  if (p->S > KVX_MAX_REQUESTS)
+    return set_error(KVX_ERR_UNSUPPORTED, "S=%d exceeds %d prefixes", p->S, KVX_MAX_REQUESTS);
+  return KVX_OK;
+}
+
+// The workspace: counters and partial sums of either part, the common part's sums and statistics.
+struct PrefixSpace {
+  uint64_t sums, stats, bytes;
+};
+static PrefixSpace prefix_space(const kvx_attend_dims& m, int32_t S, int dt) {
+  const uint64_t own = kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt);
+  const uint64_t common = S > 0 ? kvx::attend_ws_bytes(S, m.G, m.T, m.d, dt) : 0;
+  const uint64_t rows = S > 0 ? (uint64_t)m.T * m.H * m.G : 0;
+  PrefixSpace s;
+  s.sums = ((own > common ? own : common) + 255) / 256 * 256;
+  s.stats = s.sums + (rows * m.d * 4 + 255) / 256 * 256;
+  s.bytes = s.stats + rows * 8;
+  return s;
+}
+
+size_t kvx_prefix_workspace_bytes(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, kvx_dtype dtype) {
+  if (check_attend(dims, dtype) != KVX_OK || check_prefix(prefix) != KVX_OK || dims->B == 0 || dims->T == 0) return 0;
+  return prefix_space(*dims, prefix->S, dtype == KVX_BF16 ? 0 : 1).bytes;
+}
+
+kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, const kvx_pool* pool,
+                              kvx_dtype dtype, const void* q, const int64_t* q_strides, const uint8_t* codes,
+                              const float* scales, const int32_t* prefix_tables, const int32_t* prefix_lens,
+                              const int32_t* prefix_cu, const int32_t* block_tables, const int32_t* lens,
+                              const int32_t* cu, float scale, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  int log2p;
+  kvx_status st = check_pool(pool, true, &log2p);
+  if (st != KVX_OK) return st;
+  if ((st = check_attend(dims, dtype)) != KVX_OK) return st;
+  if ((st = check_prefix(prefix)) != KVX_OK) return st;
+  const kvx_attend_dims& m = *dims;
+  if (!std::isfinite(scale)) return set_error(KVX_ERR_SHAPE, "scale must be finite");
+  if (m.B == 0 || m.T == 0) return ok();
+  const int dt = dtype == KVX_BF16 ? 0 : 1, es = dt == 0 ? 2 : 4;
+  const int32_t n[2] = {m.T, m.H * m.G}, S = prefix->S;
+  uint64_t qb;
+  if ((st = check_strides("q", q_strides, n, 2, es, m.d, &qb)) != KVX_OK) return st;
+  const uint64_t pages = (uint64_t)2 * m.H * pool->num_pages, b4 = (uint64_t)m.B * 4, s4 = (uint64_t)S * 4;
+  const uint64_t rows = (uint64_t)m.T * m.H * m.G;
+  const PrefixSpace space = prefix_space(m, S, dt);
+  const Span in[] = {{q, qb, "q"},
+                     {codes, pages * pool->page_size * m.d, "codes"},
+                     {scales, pages * 4, "scales"},
+                     {block_tables, b4 * pool->max_pages, "block_tables"},
+                     {lens, b4, "lens"},
+                     {cu, b4 + 4, "cu"},
+                     {prefix_tables, s4 * prefix->max_pages, "prefix_tables"},
+                     {prefix_lens, s4, "prefix_lens"},
+                     {prefix_cu, S > 0 ? s4 + 4 : 0, "prefix_cu"}};
+  const Span outs[] = {{out, rows * m.d * es, "out"}, {lse, rows * 4, "lse"}, {workspace, space.bytes, "workspace"}};
+  if ((st = check_pointers(in, 2, 16)) != KVX_OK) return st;
+  if ((st = check_pointers(in + 2, S > 0 ? 7 : 4, 4)) != KVX_OK) return st;
+  if ((st = check_pointers(outs, 1, 16)) != KVX_OK) return st;
+  if (lse != nullptr && (st = check_pointers(outs + 1, 1, 4)) != KVX_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, space.bytes)) != KVX_OK) return st;
+  if ((st = check_alias(outs, 3, in, 9)) != KVX_OK) return st;
+  kvx::PrefixArgs a;
+  std::memset(&a, 0, sizeof(a));
+  static_cast<kvx::AttendArgs&>(a) = attend_sizes(m, *pool, log2p);
+  a.q = q;
+  a.q_stride[0] = q_strides[0];
+  a.q_stride[1] = q_strides[1];
+  a.codes = codes;
+  a.scales = scales;
+  a.tables = block_tables;
+  a.lens = lens;
+  a.cu = cu;
+  a.out = out;
+  a.lse = lse;
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  hipStream_t on = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (S == 0) {
+    e = kvx::launch_attend(a, dt, m.d, workspace, on);
+  } else {
+    a.shares = prefix_cu;
+    a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.sums);
+    a.stats = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.stats);
+    a.prefixes = S;
+    a.requests = m.B;
+    kvx::PrefixArgs c = a;
+    c.B = S;
+    c.tables = prefix_tables;
+    c.lens = prefix_lens;
+    c.M = prefix->max_pages;
+    c.keys = (int64_t)c.M << log2p;
+    if (prefix->longest > 0 && prefix->longest < c.keys) c.keys = prefix->longest;
+    e = kvx::launch_prefix_common(c, dt, m.d, workspace, on);
+    if (e == hipSuccess) e = kvx::launch_prefix_own(a, dt, m.d, workspace, on);
+  }
+  if (e != hipSuccess) return set_error(KVX_ERR_HIP, "prefix attention launch: %s", hipGetErrorString(e));
+  return ok();
+}
+
 static kvx_status check_sample(kvx_dtype dtype, int32_t B, int32_t V) {
   kvx_status st = check_dtype(dtype);
   if (st != KVX_OK) return st;

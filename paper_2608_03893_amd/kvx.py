@@ -9,7 +9,7 @@ built, ``load()`` raises.
 
 Entry points mirror include/kvx.h: ``workspace_bytes``, ``rope_prepare``,
 ``map_cache``, ``map_layer``, ``map_cache_slots``; and for serving from the
-mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``, ``norm_rope``,
+mapped cache ``plan_pages``, ``store_cache8``, ``attend_cache8``, ``attend_prefix8``, ``norm_rope``,
 ``sample_tokens``.
 """
 
@@ -32,7 +32,7 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
            "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
            "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8",
-           "norm_rope", "sample_workspace", "sample_tokens"]
+           "PrefixDims", "prefix_workspace_bytes", "prefix_workspace", "attend_prefix8", "norm_rope", "sample_workspace", "sample_tokens"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -89,6 +89,11 @@ class AttendDims(ctypes.Structure):
     """kvx_attend_dims: sizes of an attention call over the 8-bit pool."""
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("G", ctypes.c_int32),
                 ("T", ctypes.c_int32), ("d", ctypes.c_int32), ("longest", ctypes.c_int32)]
+
+
+class PrefixDims(ctypes.Structure):
+    """kvx_prefix_dims: shared prefixes of an attention call."""
+    _fields_ = [("S", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("longest", ctypes.c_int32)]
 
 
 class Rope(ctypes.Structure):
@@ -186,6 +191,11 @@ def load():
     L.kvx_attend_kernel_name.restype = ctypes.c_char_p
     L.kvx_norm_rope.argtypes = [I32, I32, I32, I32, I32, P, P, P, P, P, P, F32, RP, P, P, P, P]
     L.kvx_norm_rope.restype = I32
+    XDP = ctypes.POINTER(PrefixDims)
+    L.kvx_prefix_workspace_bytes.argtypes = [AP, XDP, I32]
+    L.kvx_prefix_workspace_bytes.restype = SZ
+    L.kvx_attend_prefix8.argtypes = [AP, XDP, PP, I32, P, P, P, P, P, P, P, P, P, P, F32, P, P, P, SZ, P]
+    L.kvx_attend_prefix8.restype = I32
     L.kvx_sample_workspace_bytes.argtypes = [I32, I32, I32]
     L.kvx_sample_workspace_bytes.restype = SZ
     L.kvx_sample_tokens.argtypes = [I32, I32, I32, P, I64, P, P, P, P, P, P, P, P, SZ, P]
@@ -649,7 +659,8 @@ def _native():
         entry = [ctypes.cast(f, ctypes.c_void_p).value
                  for f in (lib.kvx_plan_pages, lib.kvx_store_cache8, lib.kvx_attend_cache8,
                            lib.kvx_attend_workspace_bytes, lib.kvx_norm_rope,
-                           lib.kvx_sample_workspace_bytes, lib.kvx_sample_tokens)]
+                           lib.kvx_sample_workspace_bytes, lib.kvx_sample_tokens,
+                           lib.kvx_prefix_workspace_bytes, lib.kvx_attend_prefix8)]
         _kvx_bind.bind(_check, PagePlan, torch._C._cuda_getCurrentRawStream, *entry)
         _BIND = _kvx_bind
     return _BIND
@@ -735,6 +746,46 @@ def attend_cache8(q, pool, scales, block_tables, lens, cu, scale=None, out=None,
     with torch.cuda.stream(stream):
         return f(q, pool, scales, block_tables, lens, cu, scale, out, with_lse, workspace, stream.cuda_stream,
                  longest)
+
+
+def prefix_workspace_bytes(dims: AttendDims, prefix: PrefixDims, dtype: str = "bf16") -> int:
+    if dtype not in ("bf16", "f32"):
+        raise ValueError("dtype must be 'bf16' or 'f32'")
+    return int(load().kvx_prefix_workspace_bytes(ctypes.byref(dims), ctypes.byref(prefix), 0 if dtype == "bf16" else 1))
+
+
+def prefix_workspace(q, pool, prefix_tables, block_tables, stream=None):
+    """A workspace for attend_prefix8 calls of these shapes, to be kept between them (its
+    counters cleared, as the first use needs)."""
+    if prefix_tables.dim() != 2:
+        raise ValueError("prefix_tables must be [S, max_pages]")
+    prefix = PrefixDims(prefix_tables.shape[0], prefix_tables.shape[1], 0)
+    need = int(load().kvx_prefix_workspace_bytes(ctypes.byref(_attend_dims(q, pool, block_tables)),
+                                                 ctypes.byref(prefix), _dtype_code(q)))
+    with torch.cuda.stream(_torch_stream(stream, q.device)):
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace[:ATTEND_COUNTER_BYTES].zero_()
+        return workspace
+
+
+def attend_prefix8(q, pool, scales, prefix_tables, prefix_lens, prefix_cu, block_tables, lens, cu, scale=None,
+                   out=None, with_lse=False, workspace=None, stream=None, longest=0, longest_prefix=0):
+    """attend_cache8 for requests that share prefixes, each of which is read once for all of them
+    (enqueued on the stream); returns out [T, H*G, d], with_lse also lse [T, H*G].  For inference.
+
+    Prefix s: prefix_lens[s] tokens in the pages prefix_tables[s] of the same pool, shared by
+    requests prefix_cu[s] .. prefix_cu[s + 1] - 1 (int32 [S, pages], [S], [S + 1]).  block_tables,
+    lens and cu are the requests' own, as in attend_cache8: a request's keys are its prefix's,
+    which all its rows see, and behind them its own.  Requests outside prefix_cu have no prefix.
+    longest, longest_prefix: bounds of own keys and of a prefix, if the host knows them;
+    workspace: a prefix_workspace that calls on one stream share, else one is made."""
+    f = (_BIND or _native()).attend_prefix8
+    if stream is None:
+        return f(q, pool, scales, prefix_tables, prefix_lens, prefix_cu, block_tables, lens, cu, scale, out, with_lse,
+                 workspace, None, longest, longest_prefix)
+    with torch.cuda.stream(stream):
+        return f(q, pool, scales, prefix_tables, prefix_lens, prefix_cu, block_tables, lens, cu, scale, out, with_lse,
+                 workspace, stream.cuda_stream, longest, longest_prefix)
 
 
 def norm_rope(q, k, q_weight, k_weight, rope, positions, eps=1e-6, out=None, stream=None):
