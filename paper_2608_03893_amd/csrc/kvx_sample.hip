@@ -10,25 +10,35 @@
 // that sums are the same in whatever order they are formed.  Tokens below 2^-44 of the best
 // one's weight have none.
 //
-// A workgroup takes a row.  Pass 1 finds the largest logit, and a bound that at least k logits
-// reach: the least, over the waves, of the m-th largest maximum of a lane's logits.  Pass 2
-// gathers the logits from that bound on into LDS, where they are sorted and cut.  Without top-k
-// the bound is a guess, and pass 2 sums all weights to see whether the list holds enough of
-// them.  Where the list is too short or too long, the cut is found by histograms of 2048 bins
-// over the weights' range, and the draw takes sums over the whole row.
+// A row is cut into strips, one a wave, and goes through three launches; in each the workgroup
+// that comes last at a row's counter goes on with what all have found.
+//   1  every strip's largest logit, and how far up its lanes' maxima reach
+//   2  by the row's settings:
+//        no top-k or top-p   the strips' sums of weights; last: the draw
+//        a small top-k       the logits from a bound on that at least k reach (from the lanes'
+//                            maxima: few more than k) as a list; last: sorted, cut, drawn from
+//        else                a histogram of counts and weights over the weights' range; last: the
+//                            bins that the cuts lie in
+//   3  rows of the last kind: the strips' sums of weights above these bins, the tokens in them as
+//      a list; last: sorted, the cut, the draw
+// Where a list would not fit LDS (thousands of equal logits at a cut) one workgroup narrows the
+// bins down over the whole row instead.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
 
 namespace kvx {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kList = 4096;                // most tokens sorted in LDS
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kList = 2048;                // most tokens sorted in LDS
+constexpr int kShort = 1024;               // and in the second launch, where more workgroups share it
 constexpr int kBins = 2048;
+constexpr int kStrips = 256;               // most strips of a row
+constexpr int kReach = 6;                  // a strip's lanes' maxima number 1, 2, 4, .. 32 by size
 constexpr int kFraction = 43;              // bits of a weight behind the point
 constexpr double kOne = 8796093022208.0;   // 2^43: the best token's weight
 constexpr float kRange = 30.5f;            // 44 ln 2: what a weight of 2^-44 is below the best, over T
-static_assert(kList % kThreads == 0, "a thread's entries of the list");
+static_assert(kList % kThreads == 0 && kShort % kThreads == 0, "a thread's entries of the list");
 
 template <int DT>
 struct Logits;
@@ -109,6 +119,7 @@ struct Setting {
   uint64_t least;       // weight that min-p asks for
   int32_t k;            // 0: all
   double p;             // 2: all
+  double u;
 };
 
 template <int DT>
@@ -149,6 +160,41 @@ struct Row {
       }
     }
   }
+  // Strip n of `strips`: its vectors, and its logits, those outside whole vectors with the first
+  // and the last strip.
+  struct Strip {
+    int32_t v0, v1, lo, hi;
+  };
+  __device__ __forceinline__ int per(int strips) const { return ((vecs + strips - 1) / strips + 63) / 64 * 64; }
+  __device__ __forceinline__ Strip strip(int n, int strips) const {
+    const int64_t first = (int64_t)n * per(strips);
+    Strip s;
+    s.v0 = first < vecs ? (int32_t)first : vecs;
+    s.v1 = first + per(strips) < vecs ? (int32_t)first + per(strips) : vecs;
+    s.lo = n == 0 ? 0 : head + s.v0 * LG::N;
+    s.hi = n == strips - 1 ? V : head + s.v1 * LG::N;
+    return s;
+  }
+  __device__ __forceinline__ int strip_of(int32_t i, int strips) const {
+    const int32_t v = (i - head) / LG::N;
+    return i < head ? 0 : v < vecs ? v / per(strips) : strips - 1;
+  }
+  // f as in vectors, for all logits of a strip by a wave.
+  template <bool BACK, int FLIGHT, typename F>
+  __device__ __forceinline__ void of_strip(int n, int strips, F f) const {
+    const int lane = threadIdx.x & 63;
+    const Strip s = strip(n, strips);
+    if (s.v0 < s.v1) vectors<BACK, FLIGHT>(s.v0, s.v1, lane, 64, f);
+    if (n == 0 || n == strips - 1) {
+      int32_t i = lane < 2 * LG::N ? loose(lane) : -1;
+      if (i >= 0 && !(i < head ? n == 0 : n == strips - 1)) i = -1;
+      float y[LG::N];
+#pragma unroll
+      for (int e = 0; e < LG::N; ++e) y[e] = -INFINITY;
+      if (i >= 0) y[0] = at(i);
+      f(y, i);
+    }
+  }
   // logits outside whole vectors: thread i < 2 N has one
   __device__ __forceinline__ int32_t loose(int i) const {
     if (i < head) return i;
@@ -170,24 +216,27 @@ struct Row {
   }
 };
 
-struct Shared {
+template <int LIST>
+struct SharedOf {
   union {
     struct {
       uint64_t weight[kBins];
       uint32_t count[kBins];
     } bin;
     struct {
-      uint64_t entry[kList];       // ~key, index: rises in the order of the tokens
-      uint64_t weight[kList];
+      uint64_t entry[LIST];        // ~key, index: rises in the order of the tokens
+      uint64_t weight[LIST];
     } list;
   };
   uint64_t part[kWaves];
-  float fpart[kWaves];
-  uint32_t count, lowest, highest, slot;
   uint64_t found[4];
+  uint64_t strip[kStrips];
+  uint32_t count, lowest, highest, slot;
+  int last;
 };
 
-__device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared& s) {
+template <typename SH>
+__device__ __forceinline__ uint64_t block_sum(uint64_t v, SH& s) {
   v = wave_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) s.part[threadIdx.x >> 6] = v;
@@ -198,7 +247,8 @@ __device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared& s) {
   return v;
 }
 // Sum over the threads up to this one.
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, Shared& s) {
+template <typename SH>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, SH& s) {
   const int wave = threadIdx.x >> 6;
   v = wave_scan(v, threadIdx.x & 63);
   __syncthreads();
@@ -228,39 +278,87 @@ __device__ __forceinline__ void sort_entries(uint64_t* e, int n) {
   __syncthreads();
 }
 
-template <int DT>
+// A row in the workspace.
+struct State {
+  uint32_t listed;            // entries of the list
+  int arrived[2];             // workgroups, in launches 2 and 3
+  int mode;                   // what launch 3 does
+  int32_t above, upto, at_k;  // bins: sums up to `above`, listed above .. upto and at_k (-1: none)
+  uint32_t before_k;          // tokens in bins before at_k
+  uint64_t weight_k;          // weights before at_k, before `above`, of all
+  uint64_t weight_above, total;
+};
+enum { kDone = 0, kCut = 1, kNarrow = 2 };
+struct Space {
+  State state;
+  float top[kStrips];
+  uint32_t first[kStrips];               // index of the first largest (greedy rows)
+  float reach[kStrips * kReach];
+  uint64_t sum[kStrips];
+  uint64_t entry[kList];
+  uint64_t weight[kBins];
+  uint32_t count[kBins];
+};
+
+template <typename T>
+__device__ __forceinline__ void put(T* to, T v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ __forceinline__ T get(const T* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// True in the workgroup that comes last of `count`; what all have put is there then.
+template <typename SH>
+__device__ __forceinline__ bool come_last(int* counter, int count, SH& s) {
+  if (count == 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    return true;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    s.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+  __syncthreads();
+  return s.last != 0;
+}
+
+
+template <int DT, int LIST>
 struct Sampler {
   const Row<DT> row;
-  Shared& s;
+  SharedOf<LIST>& s;
   Setting set;
   static constexpr int N = Logits<DT>::N;
 
   __device__ __forceinline__ uint64_t weight(float x) const { return weight_of(x, set.top, set.by); }
 
-  // Gathers the tokens that `take` accepts, as entries; returns their number, which may exceed
-  // the list (which then holds some of them).  more(x): whatever else a pass does.
-  template <int FLIGHT, typename F, typename M>
-  __device__ __forceinline__ int gather(F take, M more) {
+  // Entries of the tokens that `take` accepts among y, to places that `reserve` gives out
+  // (called by one lane with their number) below `most`.
+  template <typename F, typename R>
+  __device__ __forceinline__ void append(const float* y, int32_t first, uint64_t* to, uint32_t most, F take, R reserve) const {
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) some |= take(y[e]);
+    if (!__any(some)) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const bool mine = take(y[e]);
+      const uint64_t who = __ballot(mine);
+      if (who == 0) continue;
+      uint32_t at = 0;
+      const int lane = threadIdx.x & 63, one = __builtin_ctzll(who);
+      if (lane == one) at = reserve((uint32_t)__popcll(who));
+      at = (uint32_t)__shfl((int)at, one, 64) + (uint32_t)__popcll(who & ((1ull << lane) - 1));
+      if (mine && at < most) put(to + at, (uint64_t)~key_of(y[e]) << 32 | (uint32_t)(first + e));
+    }
+  }
+  // The row's tokens that `take` accepts, as entries; their number.
+  template <typename F>
+  __device__ __forceinline__ int gather(F take) {
     __syncthreads();
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
-    row.template all<true, FLIGHT>([&](const float* y, int32_t first) {
-      more(y);
-      bool some = false;
-#pragma unroll
-      for (int e = 0; e < N; ++e) some |= take(y[e]);
-      if (!__any(some)) return;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const bool mine = take(y[e]);
-        const uint64_t who = __ballot(mine);
-        if (who == 0) continue;
-        uint32_t at = 0;
-        const int lane = threadIdx.x & 63;
-        if (lane == __builtin_ctzll(who)) at = atomicAdd(&s.count, (uint32_t)__popcll(who));
-        at = (uint32_t)__shfl((int)at, __builtin_ctzll(who), 64) + (uint32_t)__popcll(who & ((1ull << lane) - 1));
-        if (mine && at < kList) s.list.entry[at] = (uint64_t)~key_of(y[e]) << 32 | (uint32_t)(first + e);
-      }
+    row.template all<true, 2>([&](const float* y, int32_t first) {
+      append(y, first, s.list.entry, LIST, take, [&](uint32_t n) { return atomicAdd(&s.count, n); });
     });
     __syncthreads();
     return (int)s.count;
@@ -268,7 +366,7 @@ struct Sampler {
 
   // Entries in order and their weights; a thread gets the sums up to each of its entries
   // (kList / kThreads neighbouring ones).
-  static constexpr int kMine = kList / kThreads;
+  static constexpr int kMine = LIST / kThreads;
   __device__ __forceinline__ void order(int n, uint64_t* sums) {
     sort_entries(s.list.entry, n);
     uint64_t mine = 0;
@@ -310,7 +408,7 @@ struct Sampler {
     return t < total ? t : total - 1;
   }
 
-  __device__ __forceinline__ void put(const SampleArgs& a, int b, int32_t token, float x, uint64_t total) {
+  __device__ __forceinline__ void put_token(const SampleArgs& a, int b, int32_t token, float x, uint64_t total) {
     a.tokens[b] = token;
     if (a.logprob != nullptr) {
       const double y = x == set.top ? 0.0 : ((double)x - (double)set.top) * set.by;
@@ -344,7 +442,7 @@ struct Sampler {
     for (int i = 0; i < kMine; ++i) {
       if (sum <= t && t < sum + w[i]) {
         const int32_t token = (int32_t)(s.list.entry[threadIdx.x * kMine + i] >> 32);
-        put(a, b, token, row.at(token), total);
+        put_token(a, b, token, row.at(token), total);
       }
       sum += w[i];
     }
@@ -377,46 +475,84 @@ struct Sampler {
     return (int32_t)s.slot;
   }
 
-  // Sums of f over the whole row, each wave's part of it in order of the vocabulary; then the
-  // draw from them.
+  // The draw from the strips' sums (in s.strip) of f.
   template <typename F>
-  __device__ __forceinline__ void draw_row(const SampleArgs& a, int b, double u, F f) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int per = ((row.vecs + kWaves - 1) / kWaves + 63) / 64 * 64;
-    const int v0 = wave * per < row.vecs ? wave * per : row.vecs, v1 = v0 + per < row.vecs ? v0 + per : row.vecs;
-    // its logits: whole vectors, the loose ones at both ends with the first and the last wave
-    const int32_t lo = wave == 0 ? 0 : row.head + v0 * N, hi = wave == kWaves - 1 ? row.V : row.head + v1 * N;
-    uint64_t sum = 0;
-    if (v0 < v1)
-      row.template vectors<true, 1>(v0, v1, lane, 64, [&](const float* y, int32_t first) {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (y[e] != -INFINITY) sum += f(y[e], first + e);
-      });
-    if (wave == 0 || wave == kWaves - 1) {
-      const int32_t i = lane < 2 * N ? row.loose(lane) : -1;
-      if (i >= 0 && (wave == 0) == (i < row.head)) sum += f(row.at(i), i);
-    }
-    sum = wave_sum(sum);
+  __device__ __forceinline__ void draw_strips(const SampleArgs& a, int b, int strips, double u, F f) {
+    const uint64_t v = (int)threadIdx.x < strips ? s.strip[threadIdx.x] : 0, upto = block_scan(v, s);
     __syncthreads();
-    if (lane == 0) s.part[wave] = sum;
+    if (threadIdx.x == kThreads - 1) s.found[0] = upto;
     __syncthreads();
-    uint64_t total = 0;
-    for (int w = 0; w < kWaves; ++w) total += s.part[w];
-    uint64_t t = behind(u, total);
-    int w = 0;
-    while (w < kWaves - 1 && t >= s.part[w]) t -= s.part[w++];
-    __syncthreads();
-    if (wave == w && lane == 0) {
-      s.found[1] = (uint64_t)lo;
-      s.found[2] = (uint64_t)hi;
+    const uint64_t total = s.found[0], t = behind(u, total);
+    if (v > 0 && upto - v <= t && t < upto) {
+      s.slot = threadIdx.x;
+      s.found[1] = t - (upto - v);
     }
     __syncthreads();
-    const int32_t token = locate((int32_t)s.found[1], (int32_t)s.found[2], t, f);
-    if (threadIdx.x == 0) put(a, b, token, row.at(token), total);
+    const typename Row<DT>::Strip where = row.strip((int)s.slot, strips);
+    const int32_t token = locate(where.lo, where.hi, s.found[1], f);
+    if (threadIdx.x == 0) put_token(a, b, token, row.at(token), total);
   }
 
   // ---- the cut by histograms ----
+
+  // What launch 3 has to look at, from the histogram of the row, which becomes sums up to each bin.
+  __device__ __forceinline__ int first_bin(bool by_count, uint64_t target) {
+    constexpr int M = kBins / kThreads;
+    uint64_t below = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int j = threadIdx.x * M + i;
+      below += (by_count ? (uint64_t)s.bin.count[j] : s.bin.weight[j]) < target;
+    }
+    return (int)block_sum(below, s);      // kBins: no bin reaches it
+  }
+  __device__ __forceinline__ void plan(State& to) {
+    constexpr int M = kBins / kThreads;
+    uint64_t c = 0, w = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      c += s.bin.count[threadIdx.x * M + i];
+      w += s.bin.weight[threadIdx.x * M + i];
+    }
+    uint64_t c0 = block_scan(c, s) - c, w0 = block_scan(w, s) - w;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      c0 += s.bin.count[threadIdx.x * M + i];
+      w0 += s.bin.weight[threadIdx.x * M + i];
+      s.bin.count[threadIdx.x * M + i] = (uint32_t)c0;
+      s.bin.weight[threadIdx.x * M + i] = w0;
+    }
+    __syncthreads();
+    auto count = [&](int i) { return i < 0 ? 0u : s.bin.count[i]; };
+    auto weight_to = [&](int i) { return i < 0 ? (uint64_t)0 : s.bin.weight[i]; };
+    const bool by_k = set.k > 0 && (uint32_t)set.k < count(kBins - 1), by_p = set.p <= 1.0;
+    State st;
+    st.at_k = by_k ? first_bin(true, (uint64_t)set.k) : -1;
+    st.before_k = by_k ? count(st.at_k - 1) : 0;
+    st.weight_k = by_k ? weight_to(st.at_k - 1) : 0;
+    st.total = weight_to(kBins - 1);
+    if (by_p) {       // for the least and the largest weight that top-k may leave
+      const uint64_t least = by_k ? st.weight_k : st.total, most = by_k ? weight_to(st.at_k) : st.total;
+      st.above = least > 0 ? first_bin(false, up_to(set.p, least)) : 0;
+      st.upto = first_bin(false, up_to(set.p, most));
+    } else {
+      st.above = by_k ? st.at_k : kBins;       // else nothing is cut
+      st.upto = by_k ? st.at_k : -1;
+    }
+    st.weight_above = weight_to(st.above - 1);
+    uint32_t listed = st.upto >= st.above ? count(st.upto) - count(st.above - 1) : 0;
+    if (by_k && st.at_k > st.upto) listed += count(st.at_k) - count(st.at_k - 1);
+    if (threadIdx.x == 0) {
+      to.above = st.above;
+      to.upto = st.upto;
+      to.at_k = st.at_k;
+      to.before_k = st.before_k;
+      to.weight_k = st.weight_k;
+      to.weight_above = st.weight_above;
+      to.total = st.total;
+      to.mode = listed <= kList ? kCut : kNarrow;
+    }
+  }
 
   // A range of logits: those of one bin over the weights' range, or of keys lo .. hi.
   struct Range {
@@ -507,7 +643,7 @@ struct Sampler {
     histogram(r, true, 0);
     r.bin = find_bin(before, by_count, target, &own);
     if (r.bin < 0) return {-INFINITY, 0, 0, true};
-    while (own > kList) {
+    while (own > LIST) {
       // the keys that there are
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -553,7 +689,7 @@ struct Sampler {
       r.hi = top;
     }
     const Range range = r;
-    const int n = gather<2>([&](float x) { return x != -INFINITY && in(range, x); }, [](const float*) {});
+    const int n = gather([&](float x) { return x != -INFINITY && in(range, x); });
     uint64_t sums[kMine];
     order(n, sums);
     const int at = by_count ? (int)(target - before.count) - 1 : reach(n, sums, target - before.weight);
@@ -563,54 +699,8 @@ struct Sampler {
   }
 };
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
-  using LG = Logits<DT>;
-  constexpr int N = LG::N;
-  __shared__ Shared s;
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Row<DT> row(static_cast<const typename LG::T*>(a.logits) + b * a.stride, a.V);
-  const float temperature = a.temperature == nullptr ? 1.0f : a.temperature[b];
-  const bool greedy = !(temperature > 0.0f);
-
-  // pass 1: the largest logit
-  float most = -INFINITY;
-  row.template all<false, 4>([&](const float* y, int32_t) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) most = fmaxf(most, y[e]);
-  });
-  float top = most;
-#pragma unroll
-  for (int n = 32; n; n >>= 1) top = fmaxf(top, __shfl_xor(top, n, 64));
-  if (lane == 0) s.fpart[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s.fpart[w]);
-  if (top == -INFINITY) {      // nothing is allowed
-    if (threadIdx.x == 0) {
-      a.tokens[b] = -1;
-      if (a.logprob != nullptr) a.logprob[b] = -INFINITY;
-    }
-    return;
-  }
-  if (greedy) {
-    if (threadIdx.x == 0) s.lowest = ~0u;
-    __syncthreads();
-    uint32_t first = ~0u;
-    row.template all<true, 2>([&](const float* y, int32_t at) {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (y[e] == top && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
-    });
-    if (first != ~0u) atomicMin(&s.lowest, first);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      a.tokens[b] = (int32_t)s.lowest;
-      if (a.logprob != nullptr) a.logprob[b] = 0.0f;
-    }
-    return;
-  }
-
+// Settings of row b once its largest logit is known.
+__device__ __forceinline__ Setting setting(const SampleArgs& a, int b, float top, float temperature) {
   Setting set;
   set.top = top;
   set.by = 1.4426950408889634 / (double)temperature;
@@ -621,102 +711,398 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
   set.p = p < 1.0f ? (double)p : 2.0;
   const float min_p = a.min_p == nullptr ? 0.0f : a.min_p[b];
   set.least = min_p > 0.0f ? (uint64_t)ceil((min_p < 1.0f ? (double)min_p : 1.0) * kOne) : 1;
-  float r = a.u[b];
-  const double u = r > 0.0f ? (r < 1.0f ? (double)r : 1.0) : 0.0;
-  const bool by_p = set.p <= 1.0;
-  Sampler<DT> z{row, s, set};
+  const float u = a.u[b];
+  set.u = u > 0.0f ? (u < 1.0f ? (double)u : 1.0) : 0.0;
+  return set;
+}
+__device__ __forceinline__ float temperature_of(const SampleArgs& a, int b) {
+  return a.temperature == nullptr ? 1.0f : a.temperature[b];
+}
+// Which way a row goes through launch 2.
+enum { kPlain, kByList, kByBins };
+__device__ __forceinline__ int way_of(const Setting& set, int strips) {
+  if (set.k == 0) return set.p > 1.0 ? kPlain : kByBins;
+  return set.k <= (1 << (kReach - 1)) * strips ? kByList : kByBins;
+}
 
-  if (set.k == 0 && !by_p) {
-    z.draw_row(a, b, u, [&](float x, int32_t) -> uint64_t {
-      const uint64_t w = z.weight(x);
-      return w >= set.least ? w : 0;
+template <int DT>
+__device__ __forceinline__ Row<DT> row_of(const SampleArgs& a, int b) {
+  return Row<DT>(static_cast<const typename Logits<DT>::T*>(a.logits) + b * a.stride, a.V);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) sample_top_kernel(SampleArgs a, Space* spaces, int chunks) {
+  constexpr int N = Logits<DT>::N;
+  const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
+  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
+  const Row<DT> row = row_of<DT>(a, b);
+  Space& space = spaces[b];
+  const float temperature = temperature_of(a, b);
+  if (chunk == 0 && threadIdx.x == 0) {
+    space.state.listed = 0;
+    space.state.arrived[0] = space.state.arrived[1] = 0;
+    space.state.mode = kDone;
+  }
+  if (!(temperature > 0.0f)) {
+    float most = -INFINITY;
+    uint32_t first = ~0u;
+    row.template of_strip<false, 4>(n, strips, [&](const float* y, int32_t at) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (y[e] > most || (y[e] == most && (uint32_t)(at + e) < first)) {
+          most = y[e];
+          first = (uint32_t)(at + e);
+        }
     });
+#pragma unroll
+    for (int i = 32; i; i >>= 1) {
+      const float m = __shfl_xor(most, i, 64);
+      const uint32_t f = (uint32_t)__shfl_xor((int)first, i, 64);
+      if (m > most || (m == most && f < first)) {
+        most = m;
+        first = f;
+      }
+    }
+    if (lane == 0) {
+      space.top[n] = most;
+      space.first[n] = first;
+    }
     return;
   }
-  uint64_t sum = 0;
-  auto add = [&](const float* y) {
+  const Setting set = setting(a, b, 0.0f, temperature);
+  const int way = way_of(set, strips);
+  if (way == kByBins && chunks > 1)
+    for (int i = chunk * kThreads + (int)threadIdx.x; i < kBins; i += chunks * kThreads) {
+      space.weight[i] = 0;
+      space.count[i] = 0;
+    }
+  float most = -INFINITY;
+  row.template of_strip<false, 4>(n, strips, [&](const float* y, int32_t) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : z.weight(y[e]);
-  };
-  if (set.k <= 512) {
-    // the m-th largest of a wave's lanes, the least of which at least k logits reach
-    const int m = set.k > 0 ? (set.k + kWaves - 1) / kWaves : 16;
-    float v = most;
+    for (int e = 0; e < N; ++e) most = fmaxf(most, y[e]);
+  });
+  if (way == kByList) {      // the lanes' maxima in falling order
 #pragma unroll
     for (int size = 2; size <= 64; size <<= 1)
 #pragma unroll
       for (int j = size >> 1; j; j >>= 1) {
-        const float o = __shfl_xor(v, j, 64);
+        const float o = __shfl_xor(most, j, 64);
         const bool larger = ((lane & j) == 0) == ((lane & size) == 0);
-        v = larger ? fmaxf(v, o) : fminf(v, o);
+        most = larger ? fmaxf(most, o) : fminf(most, o);
       }
-    v = __shfl(v, m - 1, 64);
-    __syncthreads();
-    if (lane == 0) s.fpart[wave] = v;
-    __syncthreads();
-    float bound = s.fpart[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) bound = fminf(bound, s.fpart[w]);
-    const bool sums = set.k == 0;
-    auto take = [&](float x) { return x >= bound && x != -INFINITY; };
-    const int n = sums ? z.template gather<1>(take, add) : z.template gather<4>(take, [](const float*) {});
-    if (n <= kList) {
-      if (sums) sum = block_sum(sum, s);
-      uint64_t upto[Sampler<DT>::kMine];
-      z.order(n, upto);
-      int keep = set.k > 0 && set.k < n ? set.k : n;
-      bool enough = true;
-      if (by_p) {
-        const uint64_t total = sums ? sum : z.sum_at(upto, keep - 1);
-        const int at = z.reach(n, upto, z.up_to(set.p, total));
-        enough = at < n;
-        keep = at + 1 < keep ? at + 1 : keep;
-      }
-      if (enough) {
-        uint64_t strong = 0;      // entries that min-p lets through come first
+    for (int r = 0; r < kReach; ++r)
+      if (lane == (1 << r) - 1) space.reach[n * kReach + r] = most;
+  } else {
 #pragma unroll
-        for (int i = 0; i < Sampler<DT>::kMine; ++i) {
-          const int at = threadIdx.x * Sampler<DT>::kMine + i;
-          strong += at < n && s.list.weight[at] >= set.least;
-        }
-        const int most_p = (int)block_sum(strong, s);
-        keep = most_p < keep ? most_p : keep;
-        z.draw_list(a, b, keep, z.sum_at(upto, keep - 1), u);
-        return;
-      }
-    }
+    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i, 64));
   }
-  typename Sampler<DT>::Cut cut = {-INFINITY, 0, 0, true};
-  for (int stage = set.k > 0 ? 0 : 1; stage < (by_p ? 2 : 1); ++stage) {      // top-k, top-p
-    uint64_t target = (uint64_t)set.k;
-    if (stage == 1) {
-      uint64_t total = cut.weight;
-      if (cut.all) {
-        sum = 0;
-        row.template all<true, 1>([&](const float* y, int32_t) { add(y); });
-        total = block_sum(sum, s);
-      }
-      target = z.up_to(set.p, total);
+  if (lane == 0) space.top[n] = most;
+}
+
+// A logit that at least k of the row reach, and hardly more: the largest number, to 11 bits, that
+// the maxima of enough lanes do.  By one wave.
+__device__ __forceinline__ float bound_of(const Space& space, int strips, int k) {
+  constexpr int M = kStrips / 64;
+  const int lane = threadIdx.x & 63;
+  float v[M][kReach];
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int r = 0; r < kReach; ++r) v[i][r] = lane + 64 * i < strips ? space.reach[(lane + 64 * i) * kReach + r] : -INFINITY;
+  uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);    // enough reach lo
+  auto enough = [&](uint32_t key) {
+    const float x = of_key(key);
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      if (64 * i >= strips) break;
+#pragma unroll
+      for (int r = 0; r < kReach; ++r) count += __popcll(__ballot(v[i][r] >= x)) * (r == 0 ? 1 : 1 << (r - 1));
     }
-    cut = z.find_cut(stage == 0, target);
+    return count >= k;
+  };
+#pragma unroll 1
+  for (int step = 0; step < 20; ++step) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (enough(mid)) lo = mid;
+    else hi = mid;
   }
-  z.draw_row(a, b, u, [&](float x, int32_t i) -> uint64_t {
+  return of_key(lo);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a, Space* spaces, int chunks) {
+  constexpr int N = Logits<DT>::N;
+  using SH = SharedOf<kShort>;
+  using Z = Sampler<DT, kShort>;
+  __shared__ SH s;
+  // the rows that were read last first: what of them is still in the caches
+  const int at = blockIdx.x / chunks, b = a.B - 1 - at, chunk = blockIdx.x - at * chunks;
+  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
+  Space& space = spaces[b];
+  const float temperature = temperature_of(a, b);
+  float top = -INFINITY;
+  for (int i = lane; i < strips; i += 64) top = fmaxf(top, space.top[i]);
+#pragma unroll
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
+  const bool none = top == -INFINITY;
+  if (none || !(temperature > 0.0f)) {      // nothing is allowed, or the best token is asked for
+    if (chunk != 0 || threadIdx.x >= 64) return;
+    uint32_t first = ~0u;
+    for (int i = lane; !none && i < strips; i += 64)
+      if (space.top[i] == top && space.first[i] < first) first = space.first[i];
+#pragma unroll
+    for (int i = 32; i; i >>= 1) {
+      const uint32_t f = (uint32_t)__shfl_xor((int)first, i, 64);
+      first = f < first ? f : first;
+    }
+    if (lane == 0) {
+      a.tokens[b] = none ? -1 : (int32_t)first;
+      if (a.logprob != nullptr) a.logprob[b] = none ? -INFINITY : 0.0f;
+    }
+    return;
+  }
+  Z z{row_of<DT>(a, b), s, setting(a, b, top, temperature)};
+  const Setting& set = z.set;
+  const int way = way_of(set, strips);
+
+  if (way == kPlain) {
+    auto weight = [&](float x, int32_t) -> uint64_t {
+      const uint64_t w = z.weight(x);
+      return w >= set.least ? w : 0;
+    };
+    uint64_t sum = 0;
+    z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t i) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : weight(y[e], i);
+    });
+    sum = wave_sum(sum);
+    if (lane == 0) put(&space.sum[n], sum);
+    if (!come_last(&space.state.arrived[0], chunks, s)) return;
+    if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
+    __syncthreads();
+    z.draw_strips(a, b, strips, set.u, weight);
+    return;
+  }
+
+  if (way == kByList) {
+    if (threadIdx.x < 64) {
+      const float x = bound_of(space, strips, set.k);
+      if (lane == 0) s.found[0] = __float_as_uint(x);
+    }
+    __syncthreads();
+    const float bound = __uint_as_float((uint32_t)s.found[0]);
+    z.row.template of_strip<true, 4>(n, strips, [&](const float* y, int32_t first) {
+      z.append(y, first, space.entry, kShort, [&](float x) { return x >= bound && x != -INFINITY; },
+               [&](uint32_t m) {
+                 return __hip_atomic_fetch_add(&space.state.listed, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+               });
+    });
+    if (!come_last(&space.state.arrived[0], chunks, s)) return;
+    const int listed = (int)get(&space.state.listed);
+    if (listed > kShort) {
+      if (threadIdx.x == 0) space.state.mode = kNarrow;
+      return;
+    }
+    for (int i = threadIdx.x; i < listed; i += kThreads) s.list.entry[i] = get(&space.entry[i]);
+    __syncthreads();
+    uint64_t upto[Z::kMine];
+    z.order(listed, upto);
+    int keep = set.k < listed ? set.k : listed;
+    if (set.p <= 1.0) {
+      const int reached = z.reach(listed, upto, z.up_to(set.p, z.sum_at(upto, keep - 1))) + 1;
+      keep = reached < keep ? reached : keep;
+    }
+    uint64_t strong = 0;      // entries that min-p lets through come first
+#pragma unroll
+    for (int i = 0; i < Z::kMine; ++i) {
+      const int j = threadIdx.x * Z::kMine + i;
+      strong += j < listed && s.list.weight[j] >= set.least;
+    }
+    const int allowed = (int)block_sum(strong, s);
+    keep = allowed < keep ? allowed : keep;
+    z.draw_list(a, b, keep, z.sum_at(upto, keep - 1), set.u);
+    return;
+  }
+
+  // a histogram of the strips of this workgroup, then of all
+  for (int i = threadIdx.x; i < kBins; i += kThreads) {
+    s.bin.weight[i] = 0;
+    s.bin.count[i] = 0;
+  }
+  __syncthreads();
+  z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int i = y[e] == -INFINITY ? kBins : z.bin_of(y[e]);
+      if (i >= kBins) continue;
+      atomicAdd(&s.bin.count[i], 1u);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin.weight[i]), (unsigned long long)z.weight(y[e]));
+    }
+  });
+  __syncthreads();
+  if (chunks > 1) {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      if (s.bin.count[i] == 0) continue;
+      __hip_atomic_fetch_add(&space.count[i], s.bin.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_fetch_add(&space.weight[i], s.bin.weight[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (!come_last(&space.state.arrived[0], chunks, s)) return;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      s.bin.weight[i] = get(&space.weight[i]);
+      s.bin.count[i] = get(&space.count[i]);
+    }
+    __syncthreads();
+  }
+  z.plan(space.state);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Space* spaces, int chunks) {
+  using SH = SharedOf<kList>;
+  using Z = Sampler<DT, kList>;
+  constexpr int N = Logits<DT>::N;
+  __shared__ SH s;
+  const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
+  Space& space = spaces[b];
+  const int mode = space.state.mode;
+  if (mode == kDone || (mode == kNarrow && chunk != 0)) return;
+  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
+  float top = -INFINITY;
+  for (int i = lane; i < strips; i += 64) top = fmaxf(top, space.top[i]);
+#pragma unroll
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
+  Z z{row_of<DT>(a, b), s, setting(a, b, top, temperature_of(a, b))};
+  const Setting& set = z.set;
+  typename Z::Cut cut = {-INFINITY, 0, 0, true};
+  auto kept = [&](float x, int32_t i) -> uint64_t {
     if (!(x > cut.x || (x == cut.x && (cut.all || i <= cut.index)))) return 0;
     const uint64_t w = z.weight(x);
     return w >= set.least ? w : 0;
+  };
+  uint64_t sum = 0;
+
+  if (mode == kNarrow) {
+    for (int stage = set.k > 0 ? 0 : 1; stage < (set.p <= 1.0 ? 2 : 1); ++stage) {      // top-k, top-p
+      uint64_t target = (uint64_t)set.k;
+      if (stage == 1) {
+        uint64_t total = cut.weight;
+        if (cut.all) {
+          sum = 0;
+          z.row.template all<true, 1>([&](const float* y, int32_t) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : z.weight(y[e]);
+          });
+          total = block_sum(sum, s);
+        }
+        target = z.up_to(set.p, total);
+      }
+      cut = z.find_cut(stage == 0, target);
+    }
+    for (int m = threadIdx.x >> 6; m < strips; m += kWaves) {
+      sum = 0;
+      z.row.template of_strip<true, 1>(m, strips, [&](const float* y, int32_t first) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (y[e] != -INFINITY) sum += kept(y[e], first + e);
+      });
+      sum = wave_sum(sum);
+      if (lane == 0) s.strip[m] = sum;
+    }
+    __syncthreads();
+    z.draw_strips(a, b, strips, set.u, kept);
+    return;
+  }
+
+  const State st = space.state;
+  z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t first) {
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) some |= y[e] != -INFINITY && z.bin_of(y[e]) < st.above;
+    if (__any(some)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (y[e] != -INFINITY && z.bin_of(y[e]) < st.above) sum += kept(y[e], first + e);
+    }
+    z.append(y, first, space.entry, kList,
+             [&](float x) {
+               const int i = z.bin_of(x);
+               return x != -INFINITY && i < kBins && ((i >= st.above && i <= st.upto) || i == st.at_k);
+             },
+             [&](uint32_t m) {
+               return __hip_atomic_fetch_add(&space.state.listed, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+             });
   });
+  sum = wave_sum(sum);
+  if (lane == 0) put(&space.sum[n], sum);
+  if (!come_last(&space.state.arrived[1], chunks, s)) return;
+  const int listed = (int)get(&space.state.listed);
+  for (int i = threadIdx.x; i < listed; i += kThreads) s.list.entry[i] = get(&space.entry[i]);
+  if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
+  __syncthreads();
+  if (listed > 0) {
+    uint64_t upto[Z::kMine];
+    z.order(listed, upto);
+    int keep = listed;
+    uint64_t total = st.total;
+    if (st.at_k >= 0) {       // tokens of bin at_k come last
+      uint64_t before = 0;
+#pragma unroll
+      for (int i = 0; i < Z::kMine; ++i) {
+        const int j = threadIdx.x * Z::kMine + i;
+        before += j < listed && z.bin_of(of_key(~(uint32_t)(s.list.entry[j] >> 32))) < st.at_k;
+      }
+      const int ahead = (int)block_sum(before, s);
+      keep = ahead + (int)((uint32_t)set.k - st.before_k);
+      const uint64_t whole = z.sum_at(upto, keep - 1);
+      total = st.weight_k + whole - (ahead > 0 ? z.sum_at(upto, ahead - 1) : 0);
+    }
+    if (set.p <= 1.0) {
+      const uint64_t t = z.up_to(set.p, total);
+      const int reached = z.reach(listed, upto, t > st.weight_above ? t - st.weight_above : 1) + 1;
+      keep = reached < keep ? reached : keep;
+    }
+    const uint64_t e = s.list.entry[keep - 1];
+    cut = {of_key(~(uint32_t)(e >> 32)), (int32_t)(uint32_t)e, 0, false};
+    for (int i = threadIdx.x; i < keep; i += kThreads) {
+      const uint64_t w = s.list.weight[i];
+      if (w >= set.least)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.strip[z.row.strip_of((int32_t)(uint32_t)s.list.entry[i], strips)]),
+                  (unsigned long long)w);
+    }
+    __syncthreads();
+  }
+  z.draw_strips(a, b, strips, set.u, kept);
+}
+
+// Workgroups of a row: as many as fill the chip, of two vectors a lane at least.
+constexpr int kFill = 2048;
+template <int DT>
+int chunks_of(int B, int V) {
+  const int most = (V / Logits<DT>::N + 2 * kThreads - 1) / (2 * kThreads);
+  int n = kFill / B;
+  n = n < most ? n : most;
+  return n < 1 ? 1 : n < kStrips / kWaves ? n : kStrips / kWaves;
+}
+
+template <int DT>
+hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
+  Space* spaces = static_cast<Space*>(ws);
+  const int chunks = chunks_of<DT>(a.B, a.V);
+  const dim3 grid((unsigned)(a.B * chunks)), block(kThreads);
+  hipLaunchKernelGGL((sample_top_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
+  hipLaunchKernelGGL((sample_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
+  hipLaunchKernelGGL((sample_cut_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, void* ws, hipStream_t stream) {
-  if (dtype == 0)
-    hipLaunchKernelGGL((sample_kernel<0>), dim3(a.B), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((sample_kernel<1>), dim3(a.B), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  return dtype == 0 ? launch<0>(a, ws, stream) : launch<1>(a, ws, stream);
 }
 
-size_t sample_ws_bytes(int B, int V, int dtype) { return 0; }
+size_t sample_ws_bytes(int B) { return (size_t)B * sizeof(Space); }
 
 }  // namespace kvx

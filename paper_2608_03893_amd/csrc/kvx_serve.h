@@ -95,7 +95,7 @@ struct SampleArgs {
   int32_t B, V;
 };
 hipError_t launch_sample(const SampleArgs& a, int dtype, void* ws, hipStream_t stream);
-size_t sample_ws_bytes(int B, int V, int dtype);
+size_t sample_ws_bytes(int B);
 
 // RoPE parameters: the map's checks and frequencies (kvx_api.hip).
 kvx_status check_rope_params(const kvx_rope* r, const char* which);

@@ -499,7 +499,7 @@ static kvx_status check_sample(kvx_dtype dtype, int32_t B, int32_t V) {
 
 size_t kvx_sample_workspace_bytes(kvx_dtype dtype, int32_t B, int32_t V) {
   if (check_sample(dtype, B, V) != KVX_OK || B == 0) return 0;
-  return kvx::sample_ws_bytes(B, V, dtype == KVX_BF16 ? 0 : 1);
+  return kvx::sample_ws_bytes(B);
 }
 
 kvx_status kvx_sample_tokens(kvx_dtype dtype, int32_t B, int32_t V, const void* logits, int64_t stride,
@@ -513,7 +513,7 @@ kvx_status kvx_sample_tokens(kvx_dtype dtype, int32_t B, int32_t V, const void* 
   const unsigned __int128 bytes = ((unsigned __int128)(B > 1 ? B - 1 : 0) * (uint64_t)(B > 1 ? stride : 0) + (uint32_t)V) * es;
   if (bytes >= (uint64_t)1 << 60) return set_error(KVX_ERR_SHAPE, "logits stride reaches too far");
   if (B == 0) return ok();
-  const uint64_t b4 = (uint64_t)B * 4, need = kvx::sample_ws_bytes(B, V, dt);
+  const uint64_t b4 = (uint64_t)B * 4, need = kvx::sample_ws_bytes(B);
   const Span in[] = {{logits, (uint64_t)bytes, "logits"}, {u, b4, "u"},          {temperature, b4, "temperature"},
                      {top_k, b4, "top_k"},               {top_p, b4, "top_p"}, {min_p, b4, "min_p"}};
   const Span out[] = {{tokens, b4, "tokens"}, {logprob, b4, "logprob"}, {workspace, need, "workspace"}};

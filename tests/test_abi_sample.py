@@ -46,11 +46,22 @@ def test_operands(L):
     _expect(L, 6, Sample, dtype=0, logits=20 * A + 2)    # bf16 rows begin anywhere
 
 
-@pytest.mark.parametrize("out", ["tokens", "logprob"])
+@pytest.mark.parametrize("dtype,B,V", [(0, 1, 1), (1, 8, 1000), (0, 512, 1 << 20), (1, 65535, 7)])
+def test_workspace(L, dtype, B, V):
+    need = L.kvx_sample_workspace_bytes(dtype, B, V)
+    call = dict(dtype=dtype, B=B, V=V, stride=V, logits=100 * A, ws=2000 * A)
+    assert need > 0
+    _expect(L, 7, Sample, **{**call, "ws": None}, wsb=need)
+    _expect(L, 7, Sample, **call, wsb=need - 1)
+    _expect(L, 7, Sample, **{**call, "ws": 2000 * A + 64}, wsb=need)
+    _expect(L, 6, Sample, **call, wsb=need)
+
+
+@pytest.mark.parametrize("out", ["tokens", "logprob", "ws"])
 @pytest.mark.parametrize("name", ["logits", "u", "temperature", "top_k", "top_p", "min_p"])
 def test_outputs_overlap_nothing(L, out, name):
     assert Sample(**{out: getattr(Sample(), name)}).run(L) == 6
-    assert Sample(**{name: getattr(Sample(), out) - 28}).run(L) == 6 or name == "logits"
+    assert Sample(**{name: getattr(Sample(), out) - 28}).run(L) == 6
 
 
 def test_empty_calls_launch_nothing(L):

@@ -227,3 +227,7 @@ def test_what_the_binding_refuses(gpu_kvx):
         f(x, u, out=i.long())
     with pytest.raises(gpu_kvx.KvxError, match="overlaps"):
         f(x, u, None, i, out=i)
+    ws = gpu_kvx.sample_workspace(x)
+    for bad in (ws[:-1], ws[:0], ws[128:]):
+        with pytest.raises(gpu_kvx.KvxError, match="workspace"):
+            f(x, u, workspace=bad)
