@@ -657,8 +657,13 @@ kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int
  *   tokens       int32 [B]
  *   logprob      fp32 [B] or NULL: ln of the probability with which the token was
  *                drawn, among the kept ones (0 where the temperature is 0)
- *   workspace    >= kvx_sample_workspace_bytes, 256-byte aligned; may hold
- *                anything; calls on one stream may share it */
+ *   workspace    >= kvx_sample_workspace_bytes, 256-byte aligned.  A row has
+ *                kvx_sample_workspace_bytes(dtype, 1, V) bytes of it, the first
+ *                KVX_SAMPLE_COUNTER_BYTES of which are zero before the first use
+ *                (counters, which every call leaves at zero; the rest may hold
+ *                anything); calls of any sizes may follow one another in it on a
+ *                stream */
+#define KVX_SAMPLE_COUNTER_BYTES 16
 #define KVX_MAX_DRAWS 65535
 #define KVX_MAX_VOCABULARY 1048576
 size_t kvx_sample_workspace_bytes(kvx_dtype dtype, int32_t B, int32_t V);

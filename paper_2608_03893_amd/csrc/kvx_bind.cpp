@@ -402,7 +402,10 @@ PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   at::Tensor out, logprob, workspace;
   if (args[8] == Py_None) {
     const int64_t need = (int64_t)sample_workspace_bytes_entry(dtype, B32, V32);
-    if (need > 0) workspace = at::empty({need}, logits.options().dtype(at::kByte));
+    if (need > 0) {
+      workspace = at::empty({need}, logits.options().dtype(at::kByte));
+      workspace.view({B, -1}).narrow(1, 0, KVX_SAMPLE_COUNTER_BYTES).zero_();
+    }
   } else {
     workspace = tensor(args[8], "workspace");
   }

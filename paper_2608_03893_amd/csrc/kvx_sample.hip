@@ -10,19 +10,19 @@
 // that sums are the same in whatever order they are formed.  Tokens below 2^-44 of the best
 // one's weight have none.
 //
-// A row is cut into strips, one a wave, and goes through three launches; in each the workgroup
-// that comes last at a row's counter goes on with what all have found.
-//   1  every strip's largest logit, and how far up its lanes' maxima reach
-//   2  by the row's settings:
-//        no top-k or top-p   the strips' sums of weights; last: the draw
-//        a small top-k       the logits from a bound on that at least k reach (from the lanes'
-//                            maxima: few more than k) as a list; last: sorted, cut, drawn from
-//        else                a histogram of counts and weights over the weights' range; last: the
-//                            bins that the cuts lie in
-//   3  rows of the last kind: the strips' sums of weights above these bins, the tokens in them as
-//      a list; last: sorted, the cut, the draw
-// Where a list would not fit LDS (thousands of equal logits at a cut) one workgroup narrows the
-// bins down over the whole row instead.
+// A row is cut into chunks, one a workgroup, and into strips, one or several a wave, and goes
+// through up to three launches; in each the workgroup that comes last at a row's counter goes on
+// with what all have found.
+//   1  The largest logits; the answer for greedy rows.  For a small top-k also the answer: a
+//      workgroup takes a list of the logits from a bound on that k of its own reach, which the
+//      maxima of its lanes say, anew whenever four times as much has been seen (so that a list
+//      holds few times k); last, the lists' tokens above the row's own such bound, the cut, the draw.
+//   2  Rows without top-k and top-p: the strips' sums of weights; last: the draw.  Others: a
+//      histogram of counts and weights over the weights' range; last: the bins that the cuts lie in.
+//   3  Rows of the last kind: the strips' sums of weights above these bins, the tokens in them as
+//      a list; last: the cut, the draw.
+// Where a list would not fit (thousands of equal logits at a cut) the row goes the next way, and at
+// last one workgroup narrows the bins down over the whole row.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
 
@@ -30,11 +30,14 @@ namespace kvx {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kList = 2048;                // most tokens sorted in LDS
-constexpr int kShort = 1024;               // and in the second launch, where more workgroups share it
+constexpr int kList = 2048;                // most tokens of a list in LDS
+constexpr int kShort = 2048;               // and in the first launch
+constexpr int kLong = 6144;                // and of all workgroups of a row together
+constexpr int kFew = 256;                  // most tokens that are ranked by counting
 constexpr int kBins = 2048;
-constexpr int kStrips = 256;               // most strips of a row
-constexpr int kReach = 6;                  // a strip's lanes' maxima number 1, 2, 4, .. 32 by size
+constexpr int kStrips = 256;               // most strips of a row, and waves
+constexpr int kHeld = 4;                   // vectors of a lane that the first bound is from
+constexpr int kFinal = 4;                  // logits of a thread in the last step of a draw
 constexpr int kFraction = 43;              // bits of a weight behind the point
 constexpr double kOne = 8796093022208.0;   // 2^43: the best token's weight
 constexpr float kRange = 30.5f;            // 44 ln 2: what a weight of 2^-44 is below the best, over T
@@ -128,7 +131,8 @@ struct Row {
   using T = typename LG::T;
   const T* x;
   int32_t V, head, vecs;      // logits before the first 16-byte boundary, whole vectors behind it
-  __device__ __forceinline__ Row(const T* from, int32_t v) : x(from), V(v) {
+  int32_t per;                // vectors of a strip
+  __device__ __forceinline__ Row(const T* from, int32_t v, int32_t p) : x(from), V(v), per(p) {
     head = (int32_t)(-(reinterpret_cast<uintptr_t>(from) / sizeof(T)) & (LG::N - 1));
     head = head < V ? head : V;
     vecs = (V - head) / LG::N;
@@ -141,22 +145,28 @@ struct Row {
   __device__ __forceinline__ void vectors(int v0, int v1, int me, int n, F f) const {
     const u32x4_t* from = reinterpret_cast<const u32x4_t*>(x + head);
     const int steps = (v1 - v0 + n - 1) / n;
+    u32x4_t q[FLIGHT];
+    auto vector = [&](int s) {      // -1: none
+      const int v = v0 + (BACK ? steps - 1 - s : s) * n + me;
+      return s < steps && v < v1 ? v : -1;
+    };
+    auto load = [&](int s) {
+      const int v = vector(s);
+      return from[v < 0 ? v0 : v];
+    };
+#pragma unroll
+    for (int i = 0; i < FLIGHT; ++i) q[i] = load(i);
     for (int s = 0; s < steps; s += FLIGHT) {
-      u32x4_t q[FLIGHT];
-      int v[FLIGHT];
 #pragma unroll
       for (int i = 0; i < FLIGHT; ++i) {
-        v[i] = v0 + (BACK ? steps - 1 - s - i : s + i) * n + me;
-        if (s + i >= steps || v[i] >= v1) v[i] = -1;
-        q[i] = from[v[i] < 0 ? v0 : v[i]];
-      }
-#pragma unroll
-      for (int i = 0; i < FLIGHT; ++i) {
+        if (s + i >= steps) break;
+        const int v = vector(s + i);
         float y[LG::N];
         LG::get(q[i], y);
+        q[i] = load(s + i + FLIGHT);
 #pragma unroll
-        for (int e = 0; e < LG::N; ++e) y[e] = v[i] < 0 ? -INFINITY : clean(y[e]);
-        f(y, head + v[i] * LG::N);
+        for (int e = 0; e < LG::N; ++e) y[e] = v < 0 ? -INFINITY : clean(y[e]);
+        f(y, head + v * LG::N);
       }
     }
   }
@@ -165,19 +175,18 @@ struct Row {
   struct Strip {
     int32_t v0, v1, lo, hi;
   };
-  __device__ __forceinline__ int per(int strips) const { return ((vecs + strips - 1) / strips + 63) / 64 * 64; }
   __device__ __forceinline__ Strip strip(int n, int strips) const {
-    const int64_t first = (int64_t)n * per(strips);
+    const int32_t first = n * per;
     Strip s;
-    s.v0 = first < vecs ? (int32_t)first : vecs;
-    s.v1 = first + per(strips) < vecs ? (int32_t)first + per(strips) : vecs;
+    s.v0 = first < vecs ? first : vecs;
+    s.v1 = first + per < vecs ? first + per : vecs;
     s.lo = n == 0 ? 0 : head + s.v0 * LG::N;
     s.hi = n == strips - 1 ? V : head + s.v1 * LG::N;
     return s;
   }
   __device__ __forceinline__ int strip_of(int32_t i, int strips) const {
     const int32_t v = (i - head) / LG::N;
-    return i < head ? 0 : v < vecs ? v / per(strips) : strips - 1;
+    return i < head ? 0 : v < vecs ? v / per : strips - 1;
   }
   // f as in vectors, for all logits of a strip by a wave.
   template <bool BACK, int FLIGHT, typename F>
@@ -217,22 +226,37 @@ struct Row {
 };
 
 template <int LIST>
-struct SharedOf {
-  union {
-    struct {
-      uint64_t weight[kBins];
-      uint32_t count[kBins];
-    } bin;
-    struct {
-      uint64_t entry[LIST];        // ~key, index: rises in the order of the tokens
-      uint64_t weight[LIST];
-    } list;
-  };
+struct List {
+  uint64_t entry[LIST];        // ~key, index: rises in the order of the tokens
+  uint64_t weight[LIST];
+};
+struct Bins {
+  uint64_t weight[kBins];
+  uint32_t count[kBins];
+};
+struct SharedBase {
   uint64_t part[kWaves];
   uint64_t found[4];
-  uint64_t strip[kStrips];
+  uint64_t strip[kStrips];     // also a scratch value of each thread
+  uint32_t rank[kThreads];
   uint32_t count, lowest, highest, slot;
   int last;
+};
+static_assert(kStrips == kThreads, "a strip a thread");
+struct SharedFirst : SharedBase {
+  List<kShort> list;
+  float lanes[kThreads];
+  uint32_t kept;
+};
+struct SharedWeigh : SharedBase {
+  Bins bin;
+};
+struct SharedCut : SharedBase {
+  union {
+    Bins bin;
+    List<kList> list;
+  };
+  uint64_t few[kFew], few_weight[kFew];
 };
 
 template <typename SH>
@@ -280,8 +304,6 @@ __device__ __forceinline__ void sort_entries(uint64_t* e, int n) {
 
 // A row in the workspace.
 struct State {
-  uint32_t listed;            // entries of the list
-  int arrived[2];             // workgroups, in launches 2 and 3
   int mode;                   // what launch 3 does
   int32_t above, upto, at_k;  // bins: sums up to `above`, listed above .. upto and at_k (-1: none)
   uint32_t before_k;          // tokens in bins before at_k
@@ -289,67 +311,64 @@ struct State {
   uint64_t weight_above, total;
 };
 enum { kDone = 0, kCut = 1, kNarrow = 2 };
-struct Space {
+struct alignas(256) Space {
+  uint32_t listed;                       // entries of the list
+  int arrived[3];                        // workgroups, in each launch; zero between calls, as listed
+  int over;                              // the first launch's list did not hold
   State state;
-  float top[kStrips];
+  float top[kStrips];                    // of a wave
   uint32_t first[kStrips];               // index of the first largest (greedy rows)
-  float reach[kStrips * kReach];
   uint64_t sum[kStrips];
-  uint64_t entry[kList];
+  uint64_t entry[kLong];
   uint64_t weight[kBins];
   uint32_t count[kBins];
 };
+static_assert(offsetof(Space, over) == KVX_SAMPLE_COUNTER_BYTES && sizeof(Space) % 256 == 0, "what a caller clears");
 
 template <typename T>
 __device__ __forceinline__ void put(T* to, T v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename T>
 __device__ __forceinline__ T get(const T* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// True in the workgroup that comes last of `count`; what all have put is there then.
+// True in the workgroup that comes last of `count` at a counter, which is zero again then; what all
+// have put is there.
 template <typename SH>
 __device__ __forceinline__ bool come_last(int* counter, int count, SH& s) {
-  if (count == 1) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    return true;
-  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0)
+  if (count == 1) return true;
+  if (threadIdx.x == 0) {
     s.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+    if (s.last) put(counter, 0);
+  }
   __syncthreads();
   return s.last != 0;
 }
 
-
-template <int DT, int LIST>
+template <int DT, typename SH, int LIST>
 struct Sampler {
   const Row<DT> row;
-  SharedOf<LIST>& s;
+  SH& s;
   Setting set;
   static constexpr int N = Logits<DT>::N;
 
   __device__ __forceinline__ uint64_t weight(float x) const { return weight_of(x, set.top, set.by); }
 
-  // Entries of the tokens that `take` accepts among y, to places that `reserve` gives out
-  // (called by one lane with their number) below `most`.
-  template <typename F, typename R>
-  __device__ __forceinline__ void append(const float* y, int32_t first, uint64_t* to, uint32_t most, F take, R reserve) const {
-    bool some = false;
+  // Entries of the tokens that `take` accepts among y, to places of a list in LDS (below `most`)
+  // that its counter gives out, to a lane at a time.
+  template <typename F>
+  __device__ __forceinline__ void append(const float* y, int32_t first, uint64_t* to, uint32_t* count, uint32_t most, F take) const {
+    uint32_t mine = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) some |= take(y[e]);
-    if (!__any(some)) return;
+    for (int e = 0; e < N; ++e) mine += take(y[e]) ? 1 : 0;
+    if (mine == 0) return;
+    uint32_t at = atomicAdd(count, mine);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const bool mine = take(y[e]);
-      const uint64_t who = __ballot(mine);
-      if (who == 0) continue;
-      uint32_t at = 0;
-      const int lane = threadIdx.x & 63, one = __builtin_ctzll(who);
-      if (lane == one) at = reserve((uint32_t)__popcll(who));
-      at = (uint32_t)__shfl((int)at, one, 64) + (uint32_t)__popcll(who & ((1ull << lane) - 1));
-      if (mine && at < most) put(to + at, (uint64_t)~key_of(y[e]) << 32 | (uint32_t)(first + e));
-    }
+    for (int e = 0; e < N; ++e)
+      if (take(y[e])) {
+        if (at < most) to[at] = (uint64_t)~key_of(y[e]) << 32 | (uint32_t)(first + e);
+        ++at;
+      }
   }
   // The row's tokens that `take` accepts, as entries; their number.
   template <typename F>
@@ -358,7 +377,7 @@ struct Sampler {
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
     row.template all<true, 2>([&](const float* y, int32_t first) {
-      append(y, first, s.list.entry, LIST, take, [&](uint32_t n) { return atomicAdd(&s.count, n); });
+      append(y, first, s.list.entry, &s.count, LIST, take);
     });
     __syncthreads();
     return (int)s.count;
@@ -399,6 +418,125 @@ struct Sampler {
     __syncthreads();
     return s.found[0];
   }
+  // For i < n <= kFew, in thread i (all threads call): the number of entries j < n that are less than
+  // entry i, in order of their tokens (BY_INDEX: of their indexes), and the sum of their weights,
+  // formed by several threads where n is small.
+  struct Counted {
+    uint32_t number;
+    uint64_t sum;
+  };
+  template <bool BY_INDEX>
+  __device__ __forceinline__ Counted counted(int n, const uint64_t* entry, const uint64_t* weights) {
+    const int each = n <= 64 ? 64 : n <= 128 ? 128 : 256;      // threads of a share
+    const int i = threadIdx.x & (each - 1), share = threadIdx.x / each, shares = kThreads / each;
+    const uint64_t mine = entry[i < n ? i : 0];
+    Counted c = {0, 0};
+#pragma unroll 8
+    for (int j = share; j < n; j += shares) {
+      const uint64_t e = entry[j], w = weights[j];
+      const bool less = BY_INDEX ? (uint32_t)e < (uint32_t)mine : e < mine;
+      c.number += less ? 1u : 0u;
+      c.sum += less ? w : 0;
+    }
+    if (shares == 1) return c;
+    s.strip[threadIdx.x] = c.sum;
+    s.rank[threadIdx.x] = c.number;
+    __syncthreads();
+    if (share == 0)
+      for (int x = 1; x < shares; ++x) {
+        c.sum += s.strip[x * each + i];
+        c.number += s.rank[x * each + i];
+      }
+    __syncthreads();
+    return c;
+  }
+
+  // The entry among the first n of the list, in bins lo .. hi, behind which there are `target`
+  // entries, itself included (or their weights reach it), and the sum of these weights.
+  struct Picked {
+    uint64_t entry, sum;
+  };
+  __device__ __forceinline__ Picked pick(int n, int lo, int hi, bool by_count, uint64_t target) {
+    // 256 bins over the range, in LDS that sums of strips use otherwise
+    const float scale = (float)kThreads / (float)(hi - lo + 1);
+    auto sub = [&](float x) {
+      const float y = x == set.top ? 0.0f : (set.top - x) * set.bins;
+      const int i = (int)((y - (float)lo) * scale);
+      return i < 0 ? 0 : i < kThreads ? i : kThreads - 1;
+    };
+    auto logit = [&](uint64_t e) { return of_key(~(uint32_t)(e >> 32)); };
+    auto inside = [&](float x) {
+      const int i = bin_of(x);
+      return i >= lo && i <= hi;
+    };
+    __syncthreads();
+    s.strip[threadIdx.x] = 0;
+    s.rank[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const float x = logit(s.list.entry[i]);
+      if (!inside(x)) continue;
+      atomicAdd(&s.rank[sub(x)], 1u);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&s.strip[sub(x)]), (unsigned long long)s.list.weight[i]);
+    }
+    __syncthreads();
+    const uint64_t c = s.rank[threadIdx.x], w = s.strip[threadIdx.x];
+    const uint64_t c1 = block_scan(c, s), w1 = block_scan(w, s);
+    const uint64_t a = by_count ? c1 : w1, z = by_count ? c : w;
+    __syncthreads();
+    if (a - z < target && target <= a) {
+      s.found[0] = c1 - c;
+      s.found[1] = w1 - w;
+      s.found[2] = c;
+      s.slot = threadIdx.x;
+    }
+    __syncthreads();
+    const uint64_t before_c = s.found[0], before_w = s.found[1], own = s.found[2];
+    const int bin = (int)s.slot;
+    __syncthreads();
+    if (own <= kFew) {
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t e = s.list.entry[i];
+        const float x = logit(e);
+        if (inside(x) && sub(x) == bin) s.few[atomicAdd(&s.count, 1u)] = e;
+      }
+      __syncthreads();
+      const int m = (int)own;
+      if ((int)threadIdx.x < m) s.few_weight[threadIdx.x] = weight(logit(s.few[threadIdx.x]));
+      __syncthreads();
+      const Counted before = counted<false>(m, s.few, s.few_weight);
+      if ((int)threadIdx.x < m) {
+        const uint64_t mine = s.few_weight[threadIdx.x], sum = before_w + before.sum;
+        const bool it = by_count ? before_c + before.number + 1 == target : sum < target && target <= sum + mine;
+        if (it) {
+          s.found[0] = s.few[threadIdx.x];
+          s.found[1] = sum + mine;
+        }
+      }
+    } else {       // many equal ones: all in order
+      uint64_t sums[kMine];
+      order(n, sums);
+      uint64_t ahead = 0;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int at = threadIdx.x * kMine + i;
+        ahead += at < n && bin_of(logit(s.list.entry[at])) < lo;
+      }
+      const int first = (int)block_sum(ahead, s);
+      const uint64_t base = first > 0 ? sum_at(sums, first - 1) : 0;
+      const int at = by_count ? first + (int)target - 1 : reach(n, sums, base + target);
+      const uint64_t sum = sum_at(sums, at) - base;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        s.found[0] = s.list.entry[at];
+        s.found[1] = sum;
+      }
+    }
+    __syncthreads();
+    return Picked{s.found[0], s.found[1]};
+  }
+
   __device__ __forceinline__ static uint64_t up_to(double p, uint64_t total) {     // what top-p's sum has to reach
     const double t = ceil(p * (double)total);
     return t < 1.0 ? 1 : t < (double)total ? (uint64_t)t : total;
@@ -448,16 +586,47 @@ struct Sampler {
     }
   }
 
+  // Cuts and draw from a list of n <= kFew entries in any order, which holds the first k tokens.
+  __device__ __forceinline__ void finish_few(const SampleArgs& a, int b, int n) {
+    const int i = threadIdx.x;
+    const bool mine = i < n;
+    const uint64_t e = mine ? s.list.entry[i] : 0;
+    const float x = mine ? of_key(~(uint32_t)(e >> 32)) : -INFINITY;
+    const uint64_t w = mine ? weight(x) : 0;
+    if (mine) s.list.weight[i] = w;
+    __syncthreads();
+    // (barriers inside: called by all threads, whatever they hold)
+    const Counted better = counted<false>(n, s.list.entry, s.list.weight);
+    bool keep = mine && better.number < (uint32_t)set.k;
+    if (set.p <= 1.0) {
+      const uint64_t t = up_to(set.p, block_sum(keep ? w : 0, s));
+      keep = keep && better.sum < t;
+    }
+    keep = keep && w >= set.least;
+    const uint64_t total = block_sum(keep ? w : 0, s);
+    if (mine) s.list.weight[i] = keep ? w : 0;
+    __syncthreads();
+    const uint64_t t = behind(set.u, total);
+    const uint64_t before = counted<true>(n, s.list.entry, s.list.weight).sum;
+    if (keep && before <= t && t < before + w) put_token(a, b, (int32_t)(uint32_t)e, x, total);
+  }
+
   // The place in lo .. hi - 1 at which the sum of f over it, in order of the vocabulary, first
   // exceeds t (less than all of it).
   template <typename F>
   __device__ __forceinline__ int32_t locate(int32_t lo, int32_t hi, uint64_t t, F f) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    while (hi - lo > kThreads) {
+    while (hi - lo > kThreads * kFinal) {
       const int32_t per = ((hi - lo + kWaves - 1) / kWaves + 63) / 64 * 64;
       uint64_t sum = 0;
       const int32_t a = lo + wave * per, z = a + per < hi ? a + per : hi;
-      for (int32_t i = a + lane; i < z; i += 64) sum += f(row.at(i), i);
+      for (int32_t i = a + lane; i < z; i += 64 * kFinal) {
+        float y[kFinal];
+#pragma unroll
+        for (int j = 0; j < kFinal; ++j) y[j] = row.at(i + 64 * j < z ? i + 64 * j : a);
+#pragma unroll
+        for (int j = 0; j < kFinal; ++j) sum += i + 64 * j < z ? f(y[j], i + 64 * j) : 0;
+      }
       sum = wave_sum(sum);
       __syncthreads();
       if (lane == 0) s.part[wave] = sum;
@@ -468,9 +637,22 @@ struct Sampler {
       hi = lo + per < hi ? lo + per : hi;
       __syncthreads();
     }
-    const int32_t i = lo + (int32_t)threadIdx.x;
-    const uint64_t v = i < hi ? f(row.at(i), i) : 0, sum = block_scan(v, s);
-    if (v > 0 && sum - v <= t && t < sum) s.slot = (uint32_t)i;
+    const int32_t i = lo + (int32_t)threadIdx.x * kFinal;
+    float y[kFinal];
+    uint64_t v[kFinal], mine = 0;
+#pragma unroll
+    for (int j = 0; j < kFinal; ++j) y[j] = row.at(i + j < hi ? i + j : lo);
+#pragma unroll
+    for (int j = 0; j < kFinal; ++j) {
+      v[j] = i + j < hi ? f(y[j], i + j) : 0;
+      mine += v[j];
+    }
+    uint64_t sum = block_scan(mine, s) - mine;
+#pragma unroll
+    for (int j = 0; j < kFinal; ++j) {
+      if (sum <= t && t < sum + v[j]) s.slot = (uint32_t)(i + j);
+      sum += v[j];
+    }
     __syncthreads();
     return (int32_t)s.slot;
   }
@@ -718,382 +900,569 @@ __device__ __forceinline__ Setting setting(const SampleArgs& a, int b, float top
 __device__ __forceinline__ float temperature_of(const SampleArgs& a, int b) {
   return a.temperature == nullptr ? 1.0f : a.temperature[b];
 }
-// Which way a row goes through launch 2.
+// Which way a row goes: through the first launch alone, or the first two or three.
 enum { kPlain, kByList, kByBins };
-__device__ __forceinline__ int way_of(const Setting& set, int strips) {
+__device__ __forceinline__ int way_of(const Setting& set, int chunks) {
   if (set.k == 0) return set.p > 1.0 ? kPlain : kByBins;
-  return set.k <= (1 << (kReach - 1)) * strips ? kByList : kByBins;
+  return set.k <= kThreads / 2 && (int64_t)set.k * chunks <= kLong * 3 / 4 ? kByList : kByBins;
 }
 
 template <int DT>
-__device__ __forceinline__ Row<DT> row_of(const SampleArgs& a, int b) {
-  return Row<DT>(static_cast<const typename Logits<DT>::T*>(a.logits) + b * a.stride, a.V);
+__device__ __forceinline__ Row<DT> row_of(const SampleArgs& a, int b, int per) {
+  return Row<DT>(static_cast<const typename Logits<DT>::T*>(a.logits) + b * a.stride, a.V, per);
 }
 
+// How a row is shared out.
+struct Shape {
+  int32_t chunks;      // workgroups
+  int32_t subs;        // strips of a wave, one behind the other
+  int32_t per;         // vectors of a strip
+};
+
 template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_top_kernel(SampleArgs a, Space* spaces, int chunks) {
-  constexpr int N = Logits<DT>::N;
-  const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
-  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
-  const Row<DT> row = row_of<DT>(a, b);
+__global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space* spaces, Shape shape) {
+  using LG = Logits<DT>;
+  constexpr int N = LG::N;
+  using Z = Sampler<DT, SharedFirst, kShort>;
+  __shared__ SharedFirst s;
+  const int chunks = shape.chunks, b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = chunk * kWaves + wave, waves = chunks * kWaves;
+  const Row<DT> row = row_of<DT>(a, b, shape.subs * shape.per);      // strips: the waves' parts
   Space& space = spaces[b];
+  const typename Row<DT>::Strip part = row.strip(n, waves);
+
+  // the first logits of every lane, in registers
+  const u32x4_t* from = reinterpret_cast<const u32x4_t*>(row.x + row.head);
+  u32x4_t q[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (part.v0 + lane + 64 * i < part.v1) q[i] = from[part.v0 + lane + 64 * i];
+  int32_t loose = n == 0 || n == waves - 1 ? (lane < 2 * N ? row.loose(lane) : -1) : -1;
+  if (loose >= 0 && !(loose < row.head ? n == 0 : n == waves - 1)) loose = -1;
+  const float single = loose >= 0 ? row.at(loose) : -INFINITY;
   const float temperature = temperature_of(a, b);
-  if (chunk == 0 && threadIdx.x == 0) {
-    space.state.listed = 0;
-    space.state.arrived[0] = space.state.arrived[1] = 0;
-    space.state.mode = kDone;
+  const bool greedy = !(temperature > 0.0f);
+  const Setting first_set = setting(a, b, 0.0f, temperature);
+  const int way = greedy ? kByList : way_of(first_set, chunks);
+  // f(N logits, index of the first) for the held ones and those outside whole vectors; for vectors
+  // i0 .. i1 - 1 of every lane
+  auto held = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int32_t v = part.v0 + lane + 64 * i;
+      float y[N];
+      LG::get(q[i], y);
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e] = v < part.v1 ? clean(y[e]) : -INFINITY;
+      f(y, row.head + v * N);
+    }
+    if (n == 0 || n == waves - 1) {
+      float y[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e] = -INFINITY;
+      y[0] = single;
+      f(y, loose);
+    }
+  };
+  auto stream = [&](int i0, int i1, auto f) {
+    const int32_t v0 = part.v0 + 64 * i0, v1 = part.v0 + 64 * i1 < part.v1 ? part.v0 + 64 * i1 : part.v1;
+    if (v0 < v1) row.template vectors<false, 4>(v0, v1, lane, 64, f);
+  };
+  const int vectors = shape.subs * shape.per / 64;      // of a lane
+
+  float most = -INFINITY;
+  auto largest_of = [&](const float* y, int32_t) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = fmaxf(most, y[e]);
+  };
+  if (way != kByList) {
+    held(largest_of);
+    stream(kHeld, vectors, largest_of);
+#pragma unroll
+    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i, 64));
+    if (lane == 0) space.top[n] = most;
+    if (way == kByBins && chunks > 1)
+      for (int i = chunk * kThreads + (int)threadIdx.x; i < kBins; i += chunks * kThreads) {
+        space.weight[i] = 0;
+        space.count[i] = 0;
+      }
+    return;
   }
-  if (!(temperature > 0.0f)) {
-    float most = -INFINITY;
+  if (greedy) {
     uint32_t first = ~0u;
-    row.template of_strip<false, 4>(n, strips, [&](const float* y, int32_t at) {
+    auto best = [&](const float* y, int32_t at) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (y[e] > most || (y[e] == most && (uint32_t)(at + e) < first)) {
           most = y[e];
           first = (uint32_t)(at + e);
         }
-    });
+    };
+    auto over_wave = [&] {
 #pragma unroll
-    for (int i = 32; i; i >>= 1) {
-      const float m = __shfl_xor(most, i, 64);
-      const uint32_t f = (uint32_t)__shfl_xor((int)first, i, 64);
+      for (int i = 32; i; i >>= 1) {
+        const float m = __shfl_xor(most, i, 64);
+        const uint32_t f = (uint32_t)__shfl_xor((int)first, i, 64);
+        if (m > most || (m == most && f < first)) {
+          most = m;
+          first = f;
+        }
+      }
+    };
+    held(best);
+    stream(kHeld, vectors, best);
+    over_wave();
+    if (lane == 0) {
+      put(&space.top[n], most);
+      put(&space.first[n], first);
+    }
+    if (!come_last(&space.arrived[0], chunks, s) || threadIdx.x >= 64) return;
+    most = -INFINITY;
+    first = ~0u;
+    for (int i = lane; i < waves; i += 64) {
+      const float m = get(&space.top[i]);
+      const uint32_t f = get(&space.first[i]);
       if (m > most || (m == most && f < first)) {
         most = m;
         first = f;
       }
     }
+    over_wave();
     if (lane == 0) {
-      space.top[n] = most;
-      space.first[n] = first;
-    }
-    return;
-  }
-  const Setting set = setting(a, b, 0.0f, temperature);
-  const int way = way_of(set, strips);
-  if (way == kByBins && chunks > 1)
-    for (int i = chunk * kThreads + (int)threadIdx.x; i < kBins; i += chunks * kThreads) {
-      space.weight[i] = 0;
-      space.count[i] = 0;
-    }
-  float most = -INFINITY;
-  row.template of_strip<false, 4>(n, strips, [&](const float* y, int32_t) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) most = fmaxf(most, y[e]);
-  });
-  if (way == kByList) {      // the lanes' maxima in falling order
-#pragma unroll
-    for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-      for (int j = size >> 1; j; j >>= 1) {
-        const float o = __shfl_xor(most, j, 64);
-        const bool larger = ((lane & j) == 0) == ((lane & size) == 0);
-        most = larger ? fmaxf(most, o) : fminf(most, o);
-      }
-#pragma unroll
-    for (int r = 0; r < kReach; ++r)
-      if (lane == (1 << r) - 1) space.reach[n * kReach + r] = most;
-  } else {
-#pragma unroll
-    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i, 64));
-  }
-  if (lane == 0) space.top[n] = most;
-}
-
-// A logit that at least k of the row reach, and hardly more: the largest number, to 11 bits, that
-// the maxima of enough lanes do.  By one wave.
-__device__ __forceinline__ float bound_of(const Space& space, int strips, int k) {
-  constexpr int M = kStrips / 64;
-  const int lane = threadIdx.x & 63;
-  float v[M][kReach];
-#pragma unroll
-  for (int i = 0; i < M; ++i)
-#pragma unroll
-    for (int r = 0; r < kReach; ++r) v[i][r] = lane + 64 * i < strips ? space.reach[(lane + 64 * i) * kReach + r] : -INFINITY;
-  uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);    // enough reach lo
-  auto enough = [&](uint32_t key) {
-    const float x = of_key(key);
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      if (64 * i >= strips) break;
-#pragma unroll
-      for (int r = 0; r < kReach; ++r) count += __popcll(__ballot(v[i][r] >= x)) * (r == 0 ? 1 : 1 << (r - 1));
-    }
-    return count >= k;
-  };
-#pragma unroll 1
-  for (int step = 0; step < 20; ++step) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (enough(mid)) lo = mid;
-    else hi = mid;
-  }
-  return of_key(lo);
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a, Space* spaces, int chunks) {
-  constexpr int N = Logits<DT>::N;
-  using SH = SharedOf<kShort>;
-  using Z = Sampler<DT, kShort>;
-  __shared__ SH s;
-  // the rows that were read last first: what of them is still in the caches
-  const int at = blockIdx.x / chunks, b = a.B - 1 - at, chunk = blockIdx.x - at * chunks;
-  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
-  Space& space = spaces[b];
-  const float temperature = temperature_of(a, b);
-  float top = -INFINITY;
-  for (int i = lane; i < strips; i += 64) top = fmaxf(top, space.top[i]);
-#pragma unroll
-  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
-  const bool none = top == -INFINITY;
-  if (none || !(temperature > 0.0f)) {      // nothing is allowed, or the best token is asked for
-    if (chunk != 0 || threadIdx.x >= 64) return;
-    uint32_t first = ~0u;
-    for (int i = lane; !none && i < strips; i += 64)
-      if (space.top[i] == top && space.first[i] < first) first = space.first[i];
-#pragma unroll
-    for (int i = 32; i; i >>= 1) {
-      const uint32_t f = (uint32_t)__shfl_xor((int)first, i, 64);
-      first = f < first ? f : first;
-    }
-    if (lane == 0) {
+      const bool none = most == -INFINITY;
       a.tokens[b] = none ? -1 : (int32_t)first;
       if (a.logprob != nullptr) a.logprob[b] = none ? -INFINITY : 0.0f;
     }
     return;
   }
-  Z z{row_of<DT>(a, b), s, setting(a, b, top, temperature)};
-  const Setting& set = z.set;
-  const int way = way_of(set, strips);
 
-  if (way == kPlain) {
-    auto weight = [&](float x, int32_t) -> uint64_t {
+  // A logit that k of the workgroup's reach: the largest number, to 16 bits, that k of its lanes'
+  // maxima so far do.
+  auto bound_now = [&] {
+    constexpr int M = kThreads / 64;
+    __syncthreads();
+    s.lanes[threadIdx.x] = most;
+    __syncthreads();
+    float v[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) v[i] = s.lanes[lane + 64 * i];
+    uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);    // k reach lo
+#pragma unroll 1
+    for (int step = 0; step < 16; ++step) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      const float x = of_key(mid);
+      int reach = 0;
+#pragma unroll
+      for (int i = 0; i < M; ++i) reach += __popcll(__ballot(v[i] >= x));
+      if (reach >= first_set.k) lo = mid;
+      else hi = mid;
+    }
+    return of_key(lo);
+  };
+  Z z{row, s, first_set};
+  held(largest_of);
+  if (threadIdx.x == 0) s.count = s.kept = 0;
+  float bound = bound_now();
+  auto list = [&](const float* y, int32_t first) {
+    z.append(y, first, s.list.entry, &s.count, kShort, [&](float x) { return x >= bound && x != -INFINITY; });
+  };
+  held(list);
+  for (int i = kHeld; i < vectors; i *= 4) {
+    stream(i, 4 * i < vectors ? 4 * i : vectors, [&](const float* y, int32_t first) {
+      largest_of(y, first);
+      list(y, first);
+    });
+    bound = bound_now();
+  }
+  float top = most;       // of the wave, for the launches behind
+#pragma unroll
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
+  if (lane == 0) space.top[n] = top;
+  __syncthreads();
+  uint32_t listed = s.count;
+  bool over = listed > kShort;
+
+  constexpr int M = kLong / kThreads;
+  auto logit = [](uint64_t e) { return of_key(~(uint32_t)(e >> 32)); };
+  uint64_t e[M];       // ~0: none
+  // f(e[i]) for those that n entries come to
+  auto every = [&](uint32_t n, auto f) {
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      if ((uint32_t)(i * kThreads) < n) f(e[i], threadIdx.x + i * kThreads);
+  };
+  if (over) listed = 0;
+  every(listed, [&](uint64_t& v, uint32_t j) { v = j < listed ? s.list.entry[j] : ~0ull; });
+  if (chunks > 1) {       // what reaches the last bound, to all workgroups' list
+    uint32_t kept = 0;
+    every(listed, [&](uint64_t& v, uint32_t) {
+      if (v != ~0ull && logit(v) < bound) v = ~0ull;
+      kept += v != ~0ull;
+    });
+    const uint32_t upto = (uint32_t)block_scan(kept, s);
+    if (threadIdx.x == kThreads - 1)
+      s.slot = __hip_atomic_fetch_add(&space.listed, over ? kLong + 1u : upto, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    uint32_t at = s.slot + upto - kept;
+    every(listed, [&](uint64_t& v, uint32_t) {
+      if (v == ~0ull) return;
+      if (at < kLong) put(&space.entry[at], v);
+      ++at;
+    });
+    if (!come_last(&space.arrived[0], chunks, s)) return;
+    listed = get(&space.listed);
+    over = listed > kLong;
+    every(over ? 0 : listed, [&](uint64_t& v, uint32_t j) { v = j < listed ? get(&space.entry[j]) : ~0ull; });
+  }
+  // their largest and least logits
+  uint32_t hi = 0, lo = ~0u;
+  every(over ? 0 : listed, [&](uint64_t& v, uint32_t) {
+    const uint32_t k = ~(uint32_t)(v >> 32);
+    if (v == ~0ull) return;
+    hi = k > hi ? k : hi;
+    lo = k < lo ? k : lo;
+  });
+#pragma unroll
+  for (int i = 32; i; i >>= 1) {
+    const uint32_t x = (uint32_t)__shfl_xor((int)hi, i, 64), y = (uint32_t)__shfl_xor((int)lo, i, 64);
+    hi = x > hi ? x : hi;
+    lo = y < lo ? y : lo;
+  }
+  __syncthreads();       // all have read `listed`
+  if (threadIdx.x == 0 && chunks > 1) put(&space.listed, 0u);
+  if (lane == 0) s.part[wave] = (uint64_t)hi << 32 | lo;
+  s.rank[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    hi = (uint32_t)(s.part[w] >> 32) > hi ? (uint32_t)(s.part[w] >> 32) : hi;
+    lo = (uint32_t)s.part[w] < lo ? (uint32_t)s.part[w] : lo;
+  }
+  if (listed == 0 && !over) {      // nothing is allowed
+    if (threadIdx.x == 0) {
+      space.over = 0;
+      a.tokens[b] = -1;
+      if (a.logprob != nullptr) a.logprob[b] = -INFINITY;
+    }
+    return;
+  }
+  if (!over) {
+    // first in the list: all, or those in the bins, of 256 between the two, that hold the first k
+    z.set.top = of_key(hi);
+    const float scale = (float)kThreads / (z.set.top - of_key(lo));
+    auto bin = [&](float x) {      // infinite logits: all in the first
+      const float y = (z.set.top - x) * scale;
+      return y > 0.0f ? y < (float)kThreads ? (int)y : kThreads - 1 : 0;
+    };
+    int limit = kThreads;
+    if (listed > kThreads / 4 && listed > (uint32_t)z.set.k) {
+      every(listed, [&](uint64_t& v, uint32_t) {
+        if (v != ~0ull) atomicAdd(&s.rank[bin(logit(v))], 1u);
+      });
+      __syncthreads();
+      const uint32_t c = s.rank[threadIdx.x], upto = (uint32_t)block_scan(c, s), k = (uint32_t)z.set.k;
+      if (threadIdx.x == 0) s.slot = kThreads;
+      __syncthreads();
+      if (upto >= k && upto - c < k) s.slot = threadIdx.x;
+      __syncthreads();
+      limit = (int)s.slot;
+    }
+    uint32_t mine = 0;
+    every(listed, [&](uint64_t& v, uint32_t) {
+      if (v != ~0ull && bin(logit(v)) > limit) v = ~0ull;
+      mine += v != ~0ull;
+    });
+    uint32_t at = mine > 0 ? atomicAdd(&s.kept, mine) : 0;
+    every(listed, [&](uint64_t& v, uint32_t) {
+      if (v == ~0ull) return;
+      if (at < kShort) s.list.entry[at] = v;
+      ++at;
+    });
+    __syncthreads();
+    over = s.kept > kShort;
+  }
+  if (threadIdx.x == 0) space.over = over;
+  if (over) {       // by bins
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      space.weight[i] = 0;
+      space.count[i] = 0;
+    }
+    return;
+  }
+  const int rest = (int)s.kept;
+  if (rest <= kFew) {
+    z.finish_few(a, b, rest);
+    return;
+  }
+  uint64_t upto[Z::kMine];
+  z.order(rest, upto);
+  int keep = z.set.k < rest ? z.set.k : rest;
+  if (z.set.p <= 1.0) {
+    const int reached = z.reach(rest, upto, z.up_to(z.set.p, z.sum_at(upto, keep - 1))) + 1;
+    keep = reached < keep ? reached : keep;
+  }
+  uint64_t strong = 0;      // entries that min-p lets through come first
+#pragma unroll
+  for (int i = 0; i < Z::kMine; ++i) {
+    const int j = threadIdx.x * Z::kMine + i;
+    strong += j < rest && s.list.weight[j] >= z.set.least;
+  }
+  const int allowed = (int)block_sum(strong, s);
+  keep = allowed < keep ? allowed : keep;
+  z.draw_list(a, b, keep, z.sum_at(upto, keep - 1), z.set.u);
+}
+
+// What a row still needs after the first launch.
+struct Task {
+  int way;            // kByList: nothing
+  float temperature;
+};
+__device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space& space, int chunks) {
+  Task t;
+  t.temperature = temperature_of(a, b);
+  t.way = !(t.temperature > 0.0f) ? kByList : way_of(setting(a, b, 0.0f, t.temperature), chunks);
+  if (t.way == kByList && t.temperature > 0.0f && space.over != 0) t.way = kByBins;
+  return t;
+}
+__device__ __forceinline__ float top_of(const Space& space, int waves) {
+  const int lane = threadIdx.x & 63;
+  float top = -INFINITY;
+  for (int i = lane; i < waves; i += 64) top = fmaxf(top, space.top[i]);
+#pragma unroll
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
+  return top;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Space* spaces, Shape shape) {
+  constexpr int N = Logits<DT>::N;
+  using Z = Sampler<DT, SharedWeigh, 0>;
+  __shared__ SharedWeigh s;
+  const int chunks = shape.chunks, waves = chunks * kWaves, strips = waves * shape.subs;
+  const int lane = threadIdx.x & 63;
+  for (int item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
+    // the rows that were read last first: what of them is still in the caches
+    const int at = item / chunks, b = a.B - 1 - at, chunk = item - at * chunks;
+    const int n0 = (chunk * kWaves + (threadIdx.x >> 6)) * shape.subs;      // the wave's first strip
+    Space& space = spaces[b];
+    const Task task = task_of(a, b, space, chunks);
+    if (task.way == kByList) continue;
+    const float top = top_of(space, waves);
+    if (top == -INFINITY) {
+      if (chunk == 0 && threadIdx.x == 0) {
+        space.state.mode = kDone;
+        a.tokens[b] = -1;
+        if (a.logprob != nullptr) a.logprob[b] = -INFINITY;
+      }
+      continue;
+    }
+    __syncthreads();       // the last row's LDS is free
+    Z z{row_of<DT>(a, b, shape.per), s, setting(a, b, top, task.temperature)};
+    const Setting& set = z.set;
+    if (task.way == kPlain) {
+      auto weight = [&](float x, int32_t) -> uint64_t {
+        const uint64_t w = z.weight(x);
+        return w >= set.least ? w : 0;
+      };
+      for (int n = n0; n < n0 + shape.subs; ++n) {
+        uint64_t sum = 0;
+        z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t i) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : weight(y[e], i);
+        });
+        sum = wave_sum(sum);
+        if (lane == 0) put(&space.sum[n], sum);
+      }
+      if (!come_last(&space.arrived[1], chunks, s)) continue;
+      if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
+      __syncthreads();
+      z.draw_strips(a, b, strips, set.u, weight);
+      continue;
+    }
+
+    // a histogram of the strips of this workgroup, then of all
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      s.bin.weight[i] = 0;
+      s.bin.count[i] = 0;
+    }
+    __syncthreads();
+    for (int n = n0; n < n0 + shape.subs; ++n)
+      z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int i = y[e] == -INFINITY ? kBins : z.bin_of(y[e]);
+          if (i >= kBins) continue;
+          atomicAdd(&s.bin.count[i], 1u);
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin.weight[i]), (unsigned long long)z.weight(y[e]));
+        }
+      });
+    __syncthreads();
+    if (chunks > 1) {
+      for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        if (s.bin.count[i] == 0) continue;
+        __hip_atomic_fetch_add(&space.count[i], s.bin.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_fetch_add(&space.weight[i], s.bin.weight[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      if (!come_last(&space.arrived[1], chunks, s)) continue;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        s.bin.weight[i] = get(&space.weight[i]);
+        s.bin.count[i] = get(&space.count[i]);
+      }
+      __syncthreads();
+    }
+    z.plan(space.state);
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Space* spaces, Shape shape) {
+  using Z = Sampler<DT, SharedCut, kList>;
+  constexpr int N = Logits<DT>::N;
+  __shared__ SharedCut s;
+  const int chunks = shape.chunks, waves = chunks * kWaves, strips = waves * shape.subs;
+  const int lane = threadIdx.x & 63;
+  for (int item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
+    const int b = item / chunks, chunk = item - b * chunks;
+    const int n0 = (chunk * kWaves + (threadIdx.x >> 6)) * shape.subs;      // the wave's first strip
+    Space& space = spaces[b];
+    const Task task = task_of(a, b, space, chunks);
+    if (task.way != kByBins) continue;
+    const State st = space.state;
+    if (st.mode == kDone || (st.mode == kNarrow && chunk != 0)) continue;
+    __syncthreads();       // the last row's LDS is free
+    Z z{row_of<DT>(a, b, shape.per), s, setting(a, b, top_of(space, waves), task.temperature)};
+    const Setting& set = z.set;
+    typename Z::Cut cut = {-INFINITY, 0, 0, true};
+    auto kept = [&](float x, int32_t i) -> uint64_t {
+      if (!(x > cut.x || (x == cut.x && (cut.all || i <= cut.index)))) return 0;
       const uint64_t w = z.weight(x);
       return w >= set.least ? w : 0;
     };
     uint64_t sum = 0;
-    z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t i) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : weight(y[e], i);
-    });
-    sum = wave_sum(sum);
-    if (lane == 0) put(&space.sum[n], sum);
-    if (!come_last(&space.state.arrived[0], chunks, s)) return;
-    if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
-    __syncthreads();
-    z.draw_strips(a, b, strips, set.u, weight);
-    return;
-  }
 
-  if (way == kByList) {
-    if (threadIdx.x < 64) {
-      const float x = bound_of(space, strips, set.k);
-      if (lane == 0) s.found[0] = __float_as_uint(x);
-    }
-    __syncthreads();
-    const float bound = __uint_as_float((uint32_t)s.found[0]);
-    z.row.template of_strip<true, 4>(n, strips, [&](const float* y, int32_t first) {
-      z.append(y, first, space.entry, kShort, [&](float x) { return x >= bound && x != -INFINITY; },
-               [&](uint32_t m) {
-                 return __hip_atomic_fetch_add(&space.state.listed, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-               });
-    });
-    if (!come_last(&space.state.arrived[0], chunks, s)) return;
-    const int listed = (int)get(&space.state.listed);
-    if (listed > kShort) {
-      if (threadIdx.x == 0) space.state.mode = kNarrow;
-      return;
-    }
-    for (int i = threadIdx.x; i < listed; i += kThreads) s.list.entry[i] = get(&space.entry[i]);
-    __syncthreads();
-    uint64_t upto[Z::kMine];
-    z.order(listed, upto);
-    int keep = set.k < listed ? set.k : listed;
-    if (set.p <= 1.0) {
-      const int reached = z.reach(listed, upto, z.up_to(set.p, z.sum_at(upto, keep - 1))) + 1;
-      keep = reached < keep ? reached : keep;
-    }
-    uint64_t strong = 0;      // entries that min-p lets through come first
+    if (st.mode == kNarrow) {
+      for (int stage = set.k > 0 ? 0 : 1; stage < (set.p <= 1.0 ? 2 : 1); ++stage) {      // top-k, top-p
+        uint64_t target = (uint64_t)set.k;
+        if (stage == 1) {
+          uint64_t total = cut.weight;
+          if (cut.all) {
+            sum = 0;
+            z.row.template all<true, 1>([&](const float* y, int32_t) {
 #pragma unroll
-    for (int i = 0; i < Z::kMine; ++i) {
-      const int j = threadIdx.x * Z::kMine + i;
-      strong += j < listed && s.list.weight[j] >= set.least;
-    }
-    const int allowed = (int)block_sum(strong, s);
-    keep = allowed < keep ? allowed : keep;
-    z.draw_list(a, b, keep, z.sum_at(upto, keep - 1), set.u);
-    return;
-  }
-
-  // a histogram of the strips of this workgroup, then of all
-  for (int i = threadIdx.x; i < kBins; i += kThreads) {
-    s.bin.weight[i] = 0;
-    s.bin.count[i] = 0;
-  }
-  __syncthreads();
-  z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int i = y[e] == -INFINITY ? kBins : z.bin_of(y[e]);
-      if (i >= kBins) continue;
-      atomicAdd(&s.bin.count[i], 1u);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin.weight[i]), (unsigned long long)z.weight(y[e]));
-    }
-  });
-  __syncthreads();
-  if (chunks > 1) {
-    for (int i = threadIdx.x; i < kBins; i += kThreads) {
-      if (s.bin.count[i] == 0) continue;
-      __hip_atomic_fetch_add(&space.count[i], s.bin.count[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_fetch_add(&space.weight[i], s.bin.weight[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    if (!come_last(&space.state.arrived[0], chunks, s)) return;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) {
-      s.bin.weight[i] = get(&space.weight[i]);
-      s.bin.count[i] = get(&space.count[i]);
-    }
-    __syncthreads();
-  }
-  z.plan(space.state);
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Space* spaces, int chunks) {
-  using SH = SharedOf<kList>;
-  using Z = Sampler<DT, kList>;
-  constexpr int N = Logits<DT>::N;
-  __shared__ SH s;
-  const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
-  Space& space = spaces[b];
-  const int mode = space.state.mode;
-  if (mode == kDone || (mode == kNarrow && chunk != 0)) return;
-  const int lane = threadIdx.x & 63, n = chunk * kWaves + (threadIdx.x >> 6), strips = chunks * kWaves;
-  float top = -INFINITY;
-  for (int i = lane; i < strips; i += 64) top = fmaxf(top, space.top[i]);
-#pragma unroll
-  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
-  Z z{row_of<DT>(a, b), s, setting(a, b, top, temperature_of(a, b))};
-  const Setting& set = z.set;
-  typename Z::Cut cut = {-INFINITY, 0, 0, true};
-  auto kept = [&](float x, int32_t i) -> uint64_t {
-    if (!(x > cut.x || (x == cut.x && (cut.all || i <= cut.index)))) return 0;
-    const uint64_t w = z.weight(x);
-    return w >= set.least ? w : 0;
-  };
-  uint64_t sum = 0;
-
-  if (mode == kNarrow) {
-    for (int stage = set.k > 0 ? 0 : 1; stage < (set.p <= 1.0 ? 2 : 1); ++stage) {      // top-k, top-p
-      uint64_t target = (uint64_t)set.k;
-      if (stage == 1) {
-        uint64_t total = cut.weight;
-        if (cut.all) {
-          sum = 0;
-          z.row.template all<true, 1>([&](const float* y, int32_t) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : z.weight(y[e]);
-          });
-          total = block_sum(sum, s);
+              for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : z.weight(y[e]);
+            });
+            total = block_sum(sum, s);
+          }
+          target = z.up_to(set.p, total);
         }
-        target = z.up_to(set.p, total);
+        cut = z.find_cut(stage == 0, target);
       }
-      cut = z.find_cut(stage == 0, target);
-    }
-    for (int m = threadIdx.x >> 6; m < strips; m += kWaves) {
-      sum = 0;
-      z.row.template of_strip<true, 1>(m, strips, [&](const float* y, int32_t first) {
+      __syncthreads();
+      for (int m = threadIdx.x >> 6; m < strips; m += kWaves) {
+        sum = 0;
+        z.row.template of_strip<true, 1>(m, strips, [&](const float* y, int32_t first) {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (y[e] != -INFINITY) sum += kept(y[e], first + e);
+          for (int e = 0; e < N; ++e)
+            if (y[e] != -INFINITY) sum += kept(y[e], first + e);
+        });
+        sum = wave_sum(sum);
+        if (lane == 0) s.strip[m] = sum;
+      }
+      __syncthreads();
+      z.draw_strips(a, b, strips, set.u, kept);
+      continue;
+    }
+
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    for (int n = n0; n < n0 + shape.subs; ++n) {
+      sum = 0;
+      z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t first) {
+        bool some = false;
+#pragma unroll
+        for (int e = 0; e < N; ++e) some |= y[e] != -INFINITY && z.bin_of(y[e]) < st.above;
+        if (__any(some)) {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (y[e] != -INFINITY && z.bin_of(y[e]) < st.above) sum += kept(y[e], first + e);
+        }
+        z.append(y, first, s.list.entry, &s.count, kList, [&](float x) {
+          const int i = z.bin_of(x);
+          return x != -INFINITY && i < kBins && ((i >= st.above && i <= st.upto) || i == st.at_k);
+        });
       });
       sum = wave_sum(sum);
-      if (lane == 0) s.strip[m] = sum;
+      if (lane == 0) put(&space.sum[n], sum);
     }
     __syncthreads();
-    z.draw_strips(a, b, strips, set.u, kept);
-    return;
-  }
-
-  const State st = space.state;
-  z.row.template of_strip<true, 1>(n, strips, [&](const float* y, int32_t first) {
-    bool some = false;
+    const uint32_t mine = s.count;       // no more than the plan has counted, which fits
+    if (threadIdx.x == 0)
+      s.slot = mine == 0 ? 0 : __hip_atomic_fetch_add(&space.listed, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < mine; i += kThreads) put(&space.entry[s.slot + i], s.list.entry[i]);
+    if (!come_last(&space.arrived[2], chunks, s)) continue;
+    const int listed = (int)get(&space.listed);
+    {
+      uint64_t e[kList / kThreads];
 #pragma unroll
-    for (int e = 0; e < N; ++e) some |= y[e] != -INFINITY && z.bin_of(y[e]) < st.above;
-    if (__any(some)) {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (y[e] != -INFINITY && z.bin_of(y[e]) < st.above) sum += kept(y[e], first + e);
-    }
-    z.append(y, first, space.entry, kList,
-             [&](float x) {
-               const int i = z.bin_of(x);
-               return x != -INFINITY && i < kBins && ((i >= st.above && i <= st.upto) || i == st.at_k);
-             },
-             [&](uint32_t m) {
-               return __hip_atomic_fetch_add(&space.state.listed, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-             });
-  });
-  sum = wave_sum(sum);
-  if (lane == 0) put(&space.sum[n], sum);
-  if (!come_last(&space.state.arrived[1], chunks, s)) return;
-  const int listed = (int)get(&space.state.listed);
-  for (int i = threadIdx.x; i < listed; i += kThreads) s.list.entry[i] = get(&space.entry[i]);
-  if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
-  __syncthreads();
-  if (listed > 0) {
-    uint64_t upto[Z::kMine];
-    z.order(listed, upto);
-    int keep = listed;
-    uint64_t total = st.total;
-    if (st.at_k >= 0) {       // tokens of bin at_k come last
-      uint64_t before = 0;
-#pragma unroll
-      for (int i = 0; i < Z::kMine; ++i) {
-        const int j = threadIdx.x * Z::kMine + i;
-        before += j < listed && z.bin_of(of_key(~(uint32_t)(s.list.entry[j] >> 32))) < st.at_k;
+      for (int i = 0; i < kList / kThreads; ++i)
+        e[i] = (int)threadIdx.x + i * kThreads < listed ? get(&space.entry[threadIdx.x + i * kThreads]) : 0;
+      for (int i = 0; i < kList / kThreads; ++i) {
+        const int at = threadIdx.x + i * kThreads;
+        if (at < listed) s.list.entry[at] = e[i];
       }
-      const int ahead = (int)block_sum(before, s);
-      keep = ahead + (int)((uint32_t)set.k - st.before_k);
-      const uint64_t whole = z.sum_at(upto, keep - 1);
-      total = st.weight_k + whole - (ahead > 0 ? z.sum_at(upto, ahead - 1) : 0);
+      __syncthreads();
+      for (int i = threadIdx.x; i < listed; i += kThreads)
+        s.list.weight[i] = z.weight(of_key(~(uint32_t)(s.list.entry[i] >> 32)));
     }
-    if (set.p <= 1.0) {
-      const uint64_t t = z.up_to(set.p, total);
-      const int reached = z.reach(listed, upto, t > st.weight_above ? t - st.weight_above : 1) + 1;
-      keep = reached < keep ? reached : keep;
+    __syncthreads();       // all have read `listed`
+    if (threadIdx.x == 0) put(&space.listed, 0u);
+    uint64_t last = ~0ull;
+    if (listed > 0) {
+      uint64_t total = st.total;
+      if (st.at_k >= 0) {
+        const typename Z::Picked k = z.pick(listed, st.at_k, st.at_k, true, (uint64_t)((uint32_t)set.k - st.before_k));
+        total = st.weight_k + k.sum;
+        last = k.entry;
+      }
+      if (set.p <= 1.0) {
+        const uint64_t t = z.up_to(set.p, total);
+        last = z.pick(listed, st.above, st.upto, false, t > st.weight_above ? t - st.weight_above : 1).entry;
+      }
+      cut = {of_key(~(uint32_t)(last >> 32)), (int32_t)(uint32_t)last, 0, false};
     }
-    const uint64_t e = s.list.entry[keep - 1];
-    cut = {of_key(~(uint32_t)(e >> 32)), (int32_t)(uint32_t)e, 0, false};
-    for (int i = threadIdx.x; i < keep; i += kThreads) {
-      const uint64_t w = s.list.weight[i];
-      if (w >= set.least)
-        atomicAdd(reinterpret_cast<unsigned long long*>(&s.strip[z.row.strip_of((int32_t)(uint32_t)s.list.entry[i], strips)]),
+    if ((int)threadIdx.x < strips) s.strip[threadIdx.x] = get(&space.sum[threadIdx.x]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < listed; i += kThreads) {
+      const uint64_t e = s.list.entry[i], w = s.list.weight[i];
+      if (e <= last && w >= set.least)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.strip[z.row.strip_of((int32_t)(uint32_t)e, strips)]),
                   (unsigned long long)w);
     }
     __syncthreads();
+    z.draw_strips(a, b, strips, set.u, kept);
   }
-  z.draw_strips(a, b, strips, set.u, kept);
 }
 
-// Workgroups of a row: as many as fill the chip, of two vectors a lane at least.
-constexpr int kFill = 2048;
-template <int DT>
-int chunks_of(int B, int V) {
-  const int most = (V / Logits<DT>::N + 2 * kThreads - 1) / (2 * kThreads);
-  int n = kFill / B;
-  n = n < most ? n : most;
-  return n < 1 ? 1 : n < kStrips / kWaves ? n : kStrips / kWaves;
-}
-
+// Workgroups of a row: as many as fill the chip, of kHeld vectors a lane at least.
+constexpr int kFill = 1024;
 template <int DT>
 hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
+  const int vecs = a.V / Logits<DT>::N, part = kHeld * kThreads, most = (vecs + part - 1) / part;
+  Shape shape;
+  shape.chunks = kFill / a.B < most ? kFill / a.B : most;
+  shape.chunks = shape.chunks < 1 ? 1 : shape.chunks < kStrips / kWaves ? shape.chunks : kStrips / kWaves;
+  const int waves = shape.chunks * kWaves, of_wave = (vecs + waves - 1) / waves;
+  shape.subs = 1;
+  while (2 * shape.subs * waves <= kStrips && of_wave >= 2 * shape.subs * 64 * kHeld) shape.subs *= 2;
+  shape.per = ((of_wave + shape.subs - 1) / shape.subs + 63) / 64 * 64;
+  shape.per = shape.per > 0 ? shape.per : 64;
   Space* spaces = static_cast<Space*>(ws);
-  const int chunks = chunks_of<DT>(a.B, a.V);
-  const dim3 grid((unsigned)(a.B * chunks)), block(kThreads);
-  hipLaunchKernelGGL((sample_top_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
-  hipLaunchKernelGGL((sample_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
-  hipLaunchKernelGGL((sample_cut_kernel<DT>), grid, block, 0, stream, a, spaces, chunks);
+  const dim3 grid((unsigned)(a.B * shape.chunks)), some((unsigned)(a.B * shape.chunks < kFill ? a.B * shape.chunks : kFill)),
+      block(kThreads);
+  hipLaunchKernelGGL((sample_kernel<DT>), grid, block, 0, stream, a, spaces, shape);
+  hipLaunchKernelGGL((sample_weigh_kernel<DT>), some, block, 0, stream, a, spaces, shape);
+  hipLaunchKernelGGL((sample_cut_kernel<DT>), some, block, 0, stream, a, spaces, shape);
   return hipGetLastError();
 }
 

@@ -41,6 +41,7 @@ FLAG_KEYS_STRIPPED = 4
 FLAG_PLANES_READY = 8
 SCRATCH_MAX_BYTES = 256 << 20   # KVX_SCRATCH_MAX_BYTES of include/kvx.h
 ATTEND_COUNTER_BYTES = 16384    # KVX_ATTEND_COUNTER_BYTES
+SAMPLE_COUNTER_BYTES = 16       # KVX_SAMPLE_COUNTER_BYTES, of every row
 
 STATUS = {
     0: "KVX_OK", 1: "KVX_ERR_NULL", 2: "KVX_ERR_SHAPE", 3: "KVX_ERR_INDEX",
@@ -806,11 +807,16 @@ def norm_rope(q, k, q_weight, k_weight, rope, positions, eps=1e-6, out=None, str
 
 
 def sample_workspace(logits, stream=None):
-    """A workspace for sample_tokens calls of these logits' shape, to be kept between them."""
+    """A workspace for sample_tokens calls of these logits' shape, to be kept between them
+    (its counters cleared, as the first use needs)."""
     if logits.dim() != 2:
         raise ValueError("logits must be [B, V]")
     need = int(load().kvx_sample_workspace_bytes(_dtype_code(logits), *logits.shape))
-    return _scratch(need, logits.device, stream)
+    with torch.cuda.stream(_torch_stream(stream, logits.device)):
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=logits.device)
+        if need:
+            workspace.view(logits.shape[0], -1)[:, :SAMPLE_COUNTER_BYTES].zero_()
+        return workspace
 
 
 def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,

@@ -172,12 +172,15 @@ def test_repeats_streams_and_graphs(gpu_kvx):
     t, p, m, k = f(t), f(p), f(m), torch.tensor(k, dtype=torch.int32, device=DEV)
     x, u = _logits(B, V, "bf16", 13), torch.rand(B, device=DEV)
     ws = gpu_kvx.sample_workspace(x)
-    ws.fill_(255)
+    ws.view(B, -1)[:, gpu_kvx.SAMPLE_COUNTER_BYTES:].fill_(255)
     want = gpu_kvx.sample_tokens(x, u, t, k, p, m, with_logprob=True, workspace=ws)
     for _ in range(5):
         got = gpu_kvx.sample_tokens(x, u, t, k, p, m, with_logprob=True, workspace=ws)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     torch.cuda.synchronize()
+    assert (ws.view(B, -1)[:, :gpu_kvx.SAMPLE_COUNTER_BYTES] == 0).all()
+    few = gpu_kvx.sample_tokens(x[:3, :500], u[:3], t[:3], k[:3], p[:3], m[:3], workspace=ws)      # other sizes in it
+    assert torch.equal(few, gpu_kvx.sample_tokens(x[:3, :500].contiguous(), u[:3], t[:3], k[:3], p[:3], m[:3]))
     s = torch.cuda.Stream()
     got = gpu_kvx.sample_tokens(x, u, t, k, p, m, with_logprob=True, stream=s)
     s.synchronize()
