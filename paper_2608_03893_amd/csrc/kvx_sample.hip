@@ -37,7 +37,7 @@ constexpr int kFew = 256;                  // most tokens that are ranked by cou
 constexpr int kBins = 2048;
 constexpr int kStrips = 256;               // most strips of a row, and waves
 constexpr int kHeld = 4;                   // vectors of a lane that the first bound is from
-constexpr int kFinal = 4;                  // logits of a thread in the last step of a draw
+constexpr int kFinal = 8;                  // logits of a thread in the last step of a draw
 constexpr int kFraction = 43;              // bits of a weight behind the point
 constexpr double kOne = 8796093022208.0;   // 2^43: the best token's weight
 constexpr float kRange = 30.5f;            // 44 ln 2: what a weight of 2^-44 is below the best, over T
@@ -69,6 +69,7 @@ struct Logits<1> {
   }
 };
 
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ float clean(float x) { return x == x ? x : -INFINITY; }   // NaN: not allowed
 
 // Rising with x, equal for the two zeros.
@@ -78,10 +79,12 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// 2^43 times exp((x - top) / T), to the nearest whole number; by = log2(e) / T.
+// 2^43 times exp((x - top) / T), to the nearest whole number; by = log2(e) / T.  Without branches,
+// so that the chains of several logits run side by side.
 __device__ __forceinline__ uint64_t weight_of(float x, float top, double by) {
-  const double y = x == top ? 0.0 : ((double)x - (double)top) * by;
-  if (!(y > -45.0)) return 0;
+  const double z = x == top ? 0.0 : ((double)x - (double)top) * by;
+  const bool some = z > -45.0;      // (not where z is NaN)
+  const double y = some ? z : 0.0;
   const double n = rint(y), t = (y - n) * 0.69314718055994530942;
   double p = 1.0 / 39916800.0;      // the exponential's series to t^11: 6e-15
   p = __builtin_fma(p, t, 1.0 / 3628800.0);
@@ -97,7 +100,7 @@ __device__ __forceinline__ uint64_t weight_of(float x, float top, double by) {
   p = __builtin_fma(p, t, 1.0);
   // the sum with 2^52 has the rounded number in its low bits
   const double r = ldexp(p, (int)n + kFraction) + 4503599627370496.0;
-  return __builtin_bit_cast(uint64_t, r) & 0xfffffffffffffull;
+  return some ? __builtin_bit_cast(uint64_t, r) & 0xfffffffffffffull : 0;
 }
 
 __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
@@ -457,6 +460,22 @@ struct Sampler {
     uint64_t entry, sum;
   };
   __device__ __forceinline__ Picked pick(int n, int lo, int hi, bool by_count, uint64_t target) {
+    if (n <= kFew) {       // counted among all, less what comes before the range
+      const int i = threadIdx.x;
+      const uint64_t e = i < n ? s.list.entry[i] : 0;
+      const int bin = i < n ? bin_of(of_key(~(uint32_t)(e >> 32))) : kBins;
+      const uint64_t mine = i < n ? s.list.weight[i] : 0;
+      const Counted before = counted<false>(n, s.list.entry, s.list.weight);
+      const uint64_t ahead = block_sum(bin < lo ? (by_count ? 1 : mine) : 0, s);
+      const uint64_t at = (by_count ? (uint64_t)before.number : before.sum) - ahead;
+      if (bin >= lo && bin <= hi && at < target && target <= at + (by_count ? 1 : mine)) {
+        s.found[0] = e;
+        s.found[1] = before.sum + mine;
+      }
+      const uint64_t skipped = by_count ? block_sum(bin < lo ? mine : 0, s) : ahead;
+      __syncthreads();
+      return Picked{s.found[0], s.found[1] - skipped};
+    }
     // 256 bins over the range, in LDS that sums of strips use otherwise
     const float scale = (float)kThreads / (float)(hi - lo + 1);
     auto sub = [&](float x) {
@@ -743,7 +762,7 @@ struct Sampler {
   };
   __device__ __forceinline__ int bin_of(float x) const {
     const float y = x == set.top ? 0.0f : (set.top - x) * set.bins;    // rises as x falls
-    return y < (float)kBins ? (int)y : kBins;
+    return y < (float)kBins && x != -INFINITY ? (int)y : kBins;
   }
   __device__ __forceinline__ bool in(const Range& r, float x) const {
     if (r.bin >= 0) return bin_of(x) == r.bin;
@@ -966,7 +985,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   };
   auto stream = [&](int i0, int i1, auto f) {
     const int32_t v0 = part.v0 + 64 * i0, v1 = part.v0 + 64 * i1 < part.v1 ? part.v0 + 64 * i1 : part.v1;
-    if (v0 < v1) row.template vectors<false, 4>(v0, v1, lane, 64, f);
+    if (v0 < v1) row.template vectors<false, 8>(v0, v1, lane, 64, f);
   };
   const int vectors = shape.subs * shape.per / 64;      // of a lane
 
@@ -1079,7 +1098,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
   if (lane == 0) space.top[n] = top;
   __syncthreads();
-  uint32_t listed = s.count;
+  uint32_t listed = uniform(s.count);
   bool over = listed > kShort;
 
   constexpr int M = kLong / kThreads;
@@ -1110,7 +1129,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       ++at;
     });
     if (!come_last(&space.arrived[0], chunks, s)) return;
-    listed = get(&space.listed);
+    listed = uniform(get(&space.listed));
     over = listed > kLong;
     every(over ? 0 : listed, [&](uint64_t& v, uint32_t j) { v = j < listed ? get(&space.entry[j]) : ~0ull; });
   }
@@ -1212,25 +1231,26 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   z.draw_list(a, b, keep, z.sum_at(upto, keep - 1), z.set.u);
 }
 
-// What a row still needs after the first launch.
+// What a row still needs after the first launch; all that says so is loaded at once.
 struct Task {
   int way;            // kByList: nothing
-  float temperature;
+  Setting set;
 };
 __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space& space, int chunks) {
-  Task t;
-  t.temperature = temperature_of(a, b);
-  t.way = !(t.temperature > 0.0f) ? kByList : way_of(setting(a, b, 0.0f, t.temperature), chunks);
-  if (t.way == kByList && t.temperature > 0.0f && space.over != 0) t.way = kByBins;
-  return t;
-}
-__device__ __forceinline__ float top_of(const Space& space, int waves) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, waves = chunks * kWaves;
+  const float temperature = temperature_of(a, b);
+  const int over = space.over;
   float top = -INFINITY;
-  for (int i = lane; i < waves; i += 64) top = fmaxf(top, space.top[i]);
+#pragma unroll
+  for (int i = 0; i < kStrips / 64; ++i) top = fmaxf(top, lane + 64 * i < waves ? space.top[lane + 64 * i] : -INFINITY);
+  Task t;
+  t.set = setting(a, b, 0.0f, temperature);
+  t.way = !(temperature > 0.0f) ? kByList : way_of(t.set, chunks);
+  if (t.way == kByList && temperature > 0.0f && over != 0) t.way = kByBins;
 #pragma unroll
   for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
-  return top;
+  t.set.top = top;
+  return t;
 }
 
 template <int DT>
@@ -1247,8 +1267,7 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
     Space& space = spaces[b];
     const Task task = task_of(a, b, space, chunks);
     if (task.way == kByList) continue;
-    const float top = top_of(space, waves);
-    if (top == -INFINITY) {
+    if (task.set.top == -INFINITY) {
       if (chunk == 0 && threadIdx.x == 0) {
         space.state.mode = kDone;
         a.tokens[b] = -1;
@@ -1257,7 +1276,7 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
       continue;
     }
     __syncthreads();       // the last row's LDS is free
-    Z z{row_of<DT>(a, b, shape.per), s, setting(a, b, top, task.temperature)};
+    Z z{row_of<DT>(a, b, shape.per), s, task.set};
     const Setting& set = z.set;
     if (task.way == kPlain) {
       auto weight = [&](float x, int32_t) -> uint64_t {
@@ -1266,9 +1285,9 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
       };
       for (int n = n0; n < n0 + shape.subs; ++n) {
         uint64_t sum = 0;
-        z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t i) {
+        z.row.template of_strip<true, 4>(n, strips, [&](const float* y, int32_t i) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) sum += y[e] == -INFINITY ? 0 : weight(y[e], i);
+          for (int e = 0; e < N; ++e) sum += weight(y[e], i);
         });
         sum = wave_sum(sum);
         if (lane == 0) put(&space.sum[n], sum);
@@ -1287,13 +1306,16 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
     }
     __syncthreads();
     for (int n = n0; n < n0 + shape.subs; ++n)
-      z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t) {
+      z.row.template of_strip<true, 4>(n, strips, [&](const float* y, int32_t) {
+        uint64_t w[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = z.weight(y[e]);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const int i = y[e] == -INFINITY ? kBins : z.bin_of(y[e]);
+          const int i = z.bin_of(y[e]);
           if (i >= kBins) continue;
           atomicAdd(&s.bin.count[i], 1u);
-          atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin.weight[i]), (unsigned long long)z.weight(y[e]));
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.bin.weight[i]), (unsigned long long)w[e]);
         }
       });
     __syncthreads();
@@ -1325,18 +1347,18 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
     const int b = item / chunks, chunk = item - b * chunks;
     const int n0 = (chunk * kWaves + (threadIdx.x >> 6)) * shape.subs;      // the wave's first strip
     Space& space = spaces[b];
+    const State st = space.state;
     const Task task = task_of(a, b, space, chunks);
     if (task.way != kByBins) continue;
-    const State st = space.state;
     if (st.mode == kDone || (st.mode == kNarrow && chunk != 0)) continue;
     __syncthreads();       // the last row's LDS is free
-    Z z{row_of<DT>(a, b, shape.per), s, setting(a, b, top_of(space, waves), task.temperature)};
+    Z z{row_of<DT>(a, b, shape.per), s, task.set};
     const Setting& set = z.set;
     typename Z::Cut cut = {-INFINITY, 0, 0, true};
     auto kept = [&](float x, int32_t i) -> uint64_t {
-      if (!(x > cut.x || (x == cut.x && (cut.all || i <= cut.index)))) return 0;
       const uint64_t w = z.weight(x);
-      return w >= set.least ? w : 0;
+      const bool in = (x > cut.x) | ((x == cut.x) & (cut.all | (i <= cut.index)));
+      return (in & (w >= set.least)) ? w : 0;
     };
     uint64_t sum = 0;
 
@@ -1377,18 +1399,20 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
     __syncthreads();
     for (int n = n0; n < n0 + shape.subs; ++n) {
       sum = 0;
-      z.row.template of_strip<true, 2>(n, strips, [&](const float* y, int32_t first) {
+      z.row.template of_strip<true, 4>(n, strips, [&](const float* y, int32_t first) {
         bool some = false;
 #pragma unroll
-        for (int e = 0; e < N; ++e) some |= y[e] != -INFINITY && z.bin_of(y[e]) < st.above;
+        for (int e = 0; e < N; ++e) some |= z.bin_of(y[e]) < st.above;
         if (__any(some)) {
 #pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (y[e] != -INFINITY && z.bin_of(y[e]) < st.above) sum += kept(y[e], first + e);
+          for (int e = 0; e < N; ++e) {
+            const uint64_t w = kept(y[e], first + e);
+            sum += z.bin_of(y[e]) < st.above ? w : 0;
+          }
         }
         z.append(y, first, s.list.entry, &s.count, kList, [&](float x) {
           const int i = z.bin_of(x);
-          return x != -INFINITY && i < kBins && ((i >= st.above && i <= st.upto) || i == st.at_k);
+          return i < kBins && ((i >= st.above && i <= st.upto) || i == st.at_k);
         });
       });
       sum = wave_sum(sum);
