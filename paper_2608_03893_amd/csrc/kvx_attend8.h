@@ -199,6 +199,12 @@ __device__ __forceinline__ int find_request(const int64_t* pre, int B, int64_t x
   return b;
 }
 
+// Where a row's sums are that have yet to be joined: in the partial sums of workgroups g0 .. g1,
+// row `row` of their slots.
+__device__ __forceinline__ uint64_t parts_of(int g0, int g1, int row) {
+  return (uint64_t)(uint32_t)(g1 - g0 + 1) << 32 | (uint32_t)g0 << 16 | (uint32_t)row;
+}
+
 // True in the workgroup that comes last of `count` at a counter, which is zero again then.
 // What its threads wrote with put2 before is out; `last` is a word of LDS.  Relaxed
 // operations at agent scope: the stores went past this XCD's L2 and have been waited for.

@@ -429,7 +429,27 @@ __device__ __forceinline__ void attend8_rows(const A& a, float* partial, int* co
     const int64_t g0 = unit0 / per, g1 = (unit0 + weight - 1) / per;
     bool done = g0 == g1;
     asm volatile("" : "+v"(ln));
-    if (!done) {
+    if constexpr (A::kJoinLater) {
+      if (!done && row0 < r.rows) {
+        const int mine_at = (int)(me - g0);
+        float* to = partial + (int64_t)(2 * me + (mine_at == 0 ? 1 : 0)) * ROWS * (D + 2);
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+          const int at_row = wave * 16 * NB + 16 * x + (ln & 15), row = blk * ROWS + at_row;
+          if (row >= r.rows) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < C; c += 4)
+              *reinterpret_cast<f32x4_t*>(to + at_row * D + (4 * (ln >> 4) + i) * C + c) =
+                  (f32x4_t){o[x][c][i], o[x][c + 1][i], o[x][c + 2][i], o[x][c + 3][i]};
+          if (ln >= 16) continue;
+          *reinterpret_cast<float2*>(to + ROWS * D + 2 * at_row) = make_float2(m[x], l[x]);
+          if (mine_at == 0)
+            a.parts[(int64_t)(r.row0 + row / a.G) * a.H * a.G + h * a.G + row % a.G] = parts_of((int)g0, (int)g1, at_row);
+        }
+      }
+    } else if (!done) {
       const int parts = (int)(g1 - g0) + 1, mine_at = (int)(me - g0);
       auto slot = [&](int i) { return 2 * ((int)g0 + i) + (i == 0 ? 1 : 0); };
       auto put = [&](int i) {

@@ -217,7 +217,7 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
         ksc = a.scales[(int64_t)h * a.N + page] * a.scale_log2;
         vsc = a.scales[(int64_t)(a.H + h) * a.N + page];
       }
-      auto load = [&](Stage<D>& s, int q) {
+      auto load = [&](Stage<D>& s, int q, bool keys, bool values) {
         const int key = q * kQuant + wave * kStep;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -226,8 +226,10 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
           const int64_t off = (((int64_t)p << a.log2p) + ((key + 16 * t) & P1)) * D;
           const uint8_t* kp = kc + off;
           const uint8_t* vp = vc + off;
+          if (keys)
 #pragma unroll
-          for (int u = 0; u < U; ++u) s.k[t][u] = *reinterpret_cast<const uint4*>(kp + k_lane + 64 * u);
+            for (int u = 0; u < U; ++u) s.k[t][u] = *reinterpret_cast<const uint4*>(kp + k_lane + 64 * u);
+          if (!values) continue;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if (D == 128) {
@@ -240,7 +242,8 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
           }
         }
       };
-      auto compute = [&](Stage<D>& s, int q) {
+      // then(): once the keys are in the scores
+      auto compute = [&](Stage<D>& s, int q, auto then) {
         const int key = q * kQuant + wave * kStep;
         float x[NB][8];
 #pragma unroll
@@ -265,6 +268,7 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][4 * t + e] = acc[i][e] * sc;
         }
+        then();
         const int p0 = __builtin_amdgcn_readlane(page, 2 * (q - qa));
         const int p1 = __builtin_amdgcn_readlane(page, 2 * (q - qa) + 1);
         float v0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vsc), 2 * (q - qa)));
@@ -388,10 +392,22 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
       const int64_t room = (int64_t)lim_hi - wave * kStep;
       int qe = room < 0 ? qa : (int)(room / kQuant) + 1;
       qe = qe < qb ? qe : qb;
-      for (int q = qa; q < qe; ++q) {
+      if constexpr (A::template kAhead<NB>) {
+        // the next step's keys on the way behind the scores, in the registers of this one's
         Stage<D> s;
-        load(s, q);
-        compute(s, q);
+        if (qa < qe) load(s, qa, true, false);
+        for (int q = qa; q < qe; ++q) {
+          load(s, q, false, true);
+          compute(s, q, [&] {
+            if (q + 1 < qe) load(s, q + 1, true, false);
+          });
+        }
+      } else {
+        for (int q = qa; q < qe; ++q) {
+          Stage<D> s;
+          load(s, q, true, true);
+          compute(s, q, [] {});
+        }
       }
     }
 
@@ -441,7 +457,22 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
     // units have one
     const int g0 = share_of(unit0 + kStart), g1 = share_of(unit0 + kStart + quanta - 1);
     bool done = g0 == g1 || quanta + kStart <= small;
-    if (!done) {
+    if constexpr (A::kJoinLater) {
+      if (!done) {
+        const int mine_at = uniform(me - g0);
+        float* to = partial + (int64_t)(2 * me + (mine_at == 0 ? 1 : 0)) * SLOT;
+#pragma unroll
+        for (int x = 0; x < IT; ++x) {
+          const int at_row = jr + x * STRIDE, out_row = blk * kRows + at_row;
+          if (at_row >= valid) break;
+          *reinterpret_cast<f32x4_t*>(to + at_row * D + jc) = sum[x];
+          if (jc != 0) continue;
+          *reinterpret_cast<float2*>(to + kRows * D + 2 * at_row) = make_float2(top[x], den[x]);
+          if (mine_at == 0)
+            a.parts[(int64_t)(r.row0 + out_row / a.G) * a.H * a.G + h * a.G + out_row % a.G] = parts_of(g0, g1, at_row);
+        }
+      }
+    } else if (!done) {
       const int parts = uniform(g1 - g0) + 1, mine_at = uniform(me - g0);
       auto slot = [&](int i) { return 2 * (g0 + i) + (i == 0 ? 1 : 0); };
       // Partial sums pass between workgroups on different XCDs, each with its own L2: they

@@ -29,7 +29,9 @@ struct Rows {
 }  // namespace
 
 hipError_t launch_prefix_own(const PrefixArgs& args, int dtype, int d, void* ws, hipStream_t stream) {
-  const OwnPart a{args};
+  OwnPart a{args};
+  // two units a CU and more: small workgroups, whatever the tables hold
+  if ((int64_t)a.B * a.H >= 512 && a.keys > 1024) a.keys = 1024;
   return with_kernel<Split, Rows>(a, dtype, d, [&](auto k) { return k.launch(a, ws, stream); });
 }
 

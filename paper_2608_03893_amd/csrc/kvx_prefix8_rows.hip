@@ -12,9 +12,7 @@ __global__ void __launch_bounds__(kThreads, 2) prefix8_rows_kernel(A a, float* p
 }
 
 template <typename A>
-hipError_t launch(const A& a, int d, void* ws, hipStream_t stream) {
-  int* counters = static_cast<int*>(ws);
-  float* partial = reinterpret_cast<float*>(counters + kCounters);
+hipError_t launch(const A& a, int d, float* partial, int* counters, hipStream_t stream) {
   if (d == 64)
     hipLaunchKernelGGL((prefix8_rows_kernel<64, kNb, A>), dim3(kGrid), dim3(kThreads), 0, stream, a, partial, counters);
   else
@@ -24,11 +22,12 @@ hipError_t launch(const A& a, int d, void* ws, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream) {
-  return launch(CommonPart{a}, d, ws, stream);
+hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, hipStream_t stream) {
+  return launch(CommonPart{a}, d, const_cast<float*>(a.partial), nullptr, stream);
 }
 hipError_t launch_prefix_own_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream) {
-  return launch(OwnPart{a}, d, ws, stream);
+  int* counters = static_cast<int*>(ws);
+  return launch(OwnPart{a}, d, reinterpret_cast<float*>(counters + kCounters), counters, stream);
 }
 
 }  // namespace kvx

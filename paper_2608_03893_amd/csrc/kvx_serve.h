@@ -37,6 +37,9 @@ hipError_t launch_store(const StoreArgs& a, int dtype, int d, hipStream_t stream
 
 struct AttendArgs {
   static constexpr bool kCausal = true;
+  template <int NB>
+  static constexpr bool kAhead = false;
+  static constexpr bool kJoinLater = false;
   const void* q;
   int64_t q_stride[2];      // elements: row, query head
   const uint8_t* codes;     // [2, H, N << log2p, d]
@@ -64,11 +67,17 @@ struct PrefixArgs : AttendArgs {
   const int32_t* shares;    // [prefixes + 1] requests of each prefix
   float* sums;              // [T, H * G, d] the common part's weighted values
   float* stats;             // [T, H * G, 2] reference and sum of its exponentials
-  int32_t prefixes, requests;
+  uint64_t* parts;          // [T, H * G] 0: there, else in which partial sums of workgroups (parts_of)
+  const float* partial;     // these, slots of slot_rows rows: values, then statistics
+  int32_t prefixes, requests, slot_rows, groups;
 };
-hipError_t launch_prefix_common(const PrefixArgs& a, int dtype, int d, void* ws, hipStream_t stream);
+// Rows of a slot of partial sums in the common part's kernel, and bytes of all of them.
+int prefix_slot_rows(const AttendArgs& a, int dtype, int d);
+int prefix_groups(int slot_rows);      // most workgroups, two slots each
+size_t prefix_partial_bytes(int S, int G, int T, int d, int dtype);
+hipError_t launch_prefix_common(const PrefixArgs& a, int dtype, int d, hipStream_t stream);
 hipError_t launch_prefix_own(const PrefixArgs& a, int dtype, int d, void* ws, hipStream_t stream);
-hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream);
+hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, hipStream_t stream);
 hipError_t launch_prefix_own_rows(const PrefixArgs& a, int d, void* ws, hipStream_t stream);
 
 struct NormRopeArgs {

@@ -392,18 +392,21 @@ static kvx_status check_prefix(const kvx_prefix_dims* p) {
   return KVX_OK;
 }
 
-// The workspace: counters and partial sums of either part, the common part's sums and statistics.
+// The workspace: counters and partial sums of the own part (or of both as one), then the common
+// part's: partial sums of its workgroups, a row's sums, statistics and where they are.
 struct PrefixSpace {
-  uint64_t sums, stats, bytes;
+  uint64_t partial, sums, stats, parts, bytes;
 };
 static PrefixSpace prefix_space(const kvx_attend_dims& m, int32_t S, int dt) {
-  const uint64_t own = kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt);
-  const uint64_t common = S > 0 ? kvx::attend_ws_bytes(S, m.G, m.T, m.d, dt) : 0;
   const uint64_t rows = S > 0 ? (uint64_t)m.T * m.H * m.G : 0;
+  const uint64_t partial = S > 0 ? kvx::prefix_partial_bytes(S, m.G, m.T, m.d, dt) : 0;
+  auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
   PrefixSpace s;
-  s.sums = ((own > common ? own : common) + 255) / 256 * 256;
-  s.stats = s.sums + (rows * m.d * 4 + 255) / 256 * 256;
-  s.bytes = s.stats + rows * 8;
+  s.partial = up(kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt));
+  s.sums = s.partial + up(partial);
+  s.stats = s.sums + up(rows * m.d * 4);
+  s.parts = s.stats + up(rows * 8);
+  s.bytes = s.parts + rows * 8;
   return s;
 }
 
@@ -468,9 +471,12 @@ kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims
   if (S == 0) {
     e = kvx::launch_attend(a, dt, m.d, workspace, on);
   } else {
+    char* ws = static_cast<char*>(workspace);
     a.shares = prefix_cu;
-    a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.sums);
-    a.stats = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.stats);
+    a.partial = reinterpret_cast<const float*>(ws + space.partial);
+    a.sums = reinterpret_cast<float*>(ws + space.sums);
+    a.stats = reinterpret_cast<float*>(ws + space.stats);
+    a.parts = reinterpret_cast<uint64_t*>(ws + space.parts);
     a.prefixes = S;
     a.requests = m.B;
     kvx::PrefixArgs c = a;
@@ -480,7 +486,9 @@ kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims
     c.M = prefix->max_pages;
     c.keys = (int64_t)c.M << log2p;
     if (prefix->longest > 0 && prefix->longest < c.keys) c.keys = prefix->longest;
-    e = kvx::launch_prefix_common(c, dt, m.d, workspace, on);
+    a.slot_rows = kvx::prefix_slot_rows(c, dt, m.d);
+    a.groups = kvx::prefix_groups(a.slot_rows);
+    e = kvx::launch_prefix_common(c, dt, m.d, on);
     if (e == hipSuccess) e = kvx::launch_prefix_own(a, dt, m.d, workspace, on);
   }
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "prefix attention launch: %s", hipGetErrorString(e));
