@@ -613,6 +613,14 @@ kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims
                               const int32_t* cu, float scale, void* out, float* lse, void* workspace,
                               size_t workspace_bytes, void* stream);
 
+/* Names of the kernels that kvx_attend_prefix8 would launch for these sizes and type,
+ * as a trace shows them: that over the prefixes and that over own keys, the same
+ * one where both go in one launch (a third then joins their sums); *common is NULL
+ * without prefixes, both for calls that launch nothing.  For profiling and tests;
+ * static strings. */
+kvx_status kvx_prefix_kernel_names(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, const kvx_pool* pool,
+                                   kvx_dtype dtype, const char** common, const char** own);
+
 /* RMS norm and position rotation of a step's query and key heads, as the target
  * model's layers do between their projections and the cache (kvx_store_cache8)
  * or the attention.  For row t, head h and x = q[t, h] (k[t, h] alike):

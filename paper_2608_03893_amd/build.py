@@ -23,7 +23,7 @@ SOURCES = ["kvx_api.hip", "kvx_kernels.hip", "kvx_map_bf16.hip", "kvx_map_sweep.
            "kvx_map_ks2.hip", "kvx_map_ks2_raw.hip", "kvx_xhead.hip", "kvx_noalloc.hip",
            "kvx_fit.hip", "kvx_mlp.hip", "kvx_serve.hip", "kvx_pages.hip", "kvx_store8.hip",
            "kvx_attend8.hip", "kvx_attend8_rows.hip", "kvx_normrope.hip", "kvx_sample.hip",
-           "kvx_prefix8_common.hip", "kvx_prefix8_own.hip", "kvx_prefix8_rows.hip"]
+           "kvx_prefix8_common.hip", "kvx_prefix8_own.hip", "kvx_prefix8_rows.hip", "kvx_prefix8_both.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

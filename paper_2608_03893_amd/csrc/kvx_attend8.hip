@@ -7,7 +7,8 @@ namespace {
 
 template <int DT, int D, int W, int NB>
 __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) attend8_split_kernel(AttendArgs a, float* partial, int* counters) {
-  attend8_split<DT, D, W, NB>(a, partial, counters);
+  __shared__ SplitLds<D, W, NB> lds;
+  attend8_split<DT, D, W, NB>(a, partial, counters, lds, Group{(int)blockIdx.x, (int)gridDim.x});
 }
 
 }  // namespace
@@ -42,18 +43,11 @@ struct Rows {
 }  // namespace
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, int d, void* ws, hipStream_t stream) {
-  return with_kernel<Split, Rows>(a, dtype, d, [&](auto k) { return k.launch(a, ws, stream); });
+  return with_kernel<Split, Rows>(a, dtype, d, by_rows(a, dtype, d), [&](auto k) { return k.launch(a, ws, stream); });
 }
 
 const char* attend_kernel_name(const AttendArgs& a, int dtype, int d) {
-  return with_kernel<Split, Rows>(a, dtype, d, [](auto k) -> const char* {
-    struct Name {
-      char text[48];
-      Name() { decltype(k)::name(text, sizeof(text)); }
-    };
-    static const Name name;
-    return name.text;
-  });
+  return with_kernel<Split, Rows>(a, dtype, d, by_rows(a, dtype, d), [](auto k) { return name_of(k); });
 }
 
 }  // namespace kvx

@@ -69,9 +69,28 @@ struct Stage {
   uint32_t v[8][V];         // key (lane >> 4) * 4 + (j & 3) of tile j >> 2, bytes (lane & 15) * 4 V ..
 };
 
+template <int D, int W, int NB>
+struct SplitLds {
+  int64_t part[W];
+  __attribute__((aligned(16))) float jo[W][16 * NB * (D + 4)];
+  float jm[W][16 * NB], jl[W][16 * NB];
+  int last;
+};
+
+// The workgroups of a call, or of a part of one.
+struct Group {
+  int block, grid;
+};
+
+// Request b's weight.
+template <int W, int NB, typename A>
+__device__ __forceinline__ int64_t weight_of(const A& a, const Request& r) {
+  return (int64_t)blocks_of<16 * NB>(r) * (quanta_of(r, W * kStep) + kStart) * a.H;
+}
+
 // W waves: 4, and kOcc workgroups a CU; or kLarge, and one.
 template <int DT, int D, int W, int NB, typename A>
-__device__ __forceinline__ void attend8_split(const A& a, float* partial, int* counters) {
+__device__ __forceinline__ void attend8_split(const A& a, float* partial, int* counters, SplitLds<D, W, NB>& lds, Group group) {
   constexpr int kFly = kFlying<D, NB>;
   constexpr int kWaves = W, kThreads = 64 * W, kQuant = W * kStep, kRows = 16 * NB;
   constexpr int U = D / 64, TERMS = DT == 0 ? 1 : 3, PT = kTerms<DT>;    // terms of queries, probabilities
@@ -80,10 +99,10 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
   constexpr int RS = D + 4;                                        // row stride in LDS
   constexpr int SLOT = kRows * (D + 2);                            // floats of a partial sum
   extern __shared__ int64_t pre[];                                 // [B] quanta of requests 0 .. b
-  __shared__ int64_t part[kWaves];
-  __shared__ __attribute__((aligned(16))) float jo[kWaves][kRows * RS];
-  __shared__ float jm[kWaves][kRows], jl[kWaves][kRows];
-  __shared__ int last;
+  auto& part = lds.part;
+  auto& jo = lds.jo;
+  auto &jm = lds.jm, &jl = lds.jl;
+  int& last = lds.last;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n = lane & 15, g4 = lane >> 4;
 
@@ -97,7 +116,7 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
   if (lanes) {
     const Request r = request(a, lane < a.B ? lane : a.B - 1);
     len_lane = r.len;
-    const int64_t w = lane < a.B ? (int64_t)blocks_of<kRows>(r) * (quanta_of(r, kQuant) + kStart) * a.H : 0;
+    const int64_t w = lane < a.B ? weight_of<W, NB>(a, r) : 0;
     pre_lane = w < UINT32_MAX ? (uint32_t)w : UINT32_MAX;
 #pragma unroll
     for (int n = 1; n < 64; n <<= 1) {
@@ -123,7 +142,7 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
            : lanes ? (int64_t)(uint32_t)__builtin_amdgcn_readlane(pre_lane, b - 1) : uniform(pre[b - 1]);
   };
   auto length = [&](int b) { return __builtin_amdgcn_readlane(len_lane, b); };
-  const int grid = gridDim.x;
+  const int grid = group.grid;
   const int64_t share_q = uniform(divide(total + grid - 1, grid));
   const int64_t per = share_q > kLeast<W> ? share_q : kLeast<W>;
   const int small = per + kSplit < kSmall ? (int)per + kSplit : kSmall;
@@ -138,7 +157,7 @@ __device__ __forceinline__ void attend8_split(const A& a, float* partial, int* c
     const int64_t in_unit = in_request - divide(in_request, w) * w;
     return 2 * in_unit < w ? x - in_unit : x - in_unit + w;
   };
-  const int me = xcd_order(blockIdx.x, grid);
+  const int me = xcd_order(group.block, grid);
   int64_t at = uniform(share_end(me * per));
   const int64_t end = uniform(share_end((me + 1) * per));
   if (at >= end) return;
@@ -668,17 +687,33 @@ bool large_workgroups(const AttendArgs& a) {
   return (double)units * keys >= least && (units < 512 || (rows <= 32 * B && LARGE >= 12 && keys > 1024));
 }
 
-// Workgroups: no more than there can be quanta; dynamic LDS.
-template <int DT, int D, int W, int NB>
-unsigned split_grid(const AttendArgs& a) {
-  constexpr int kFill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
+// Workgroups that there can be quanta for; a grid: no more than that or than fill the chip; dynamic
+// LDS.
+template <int W, int NB>
+double split_want(const AttendArgs& a) {
   const double units = ((double)a.T * a.G / (16 * NB) + a.B) * a.H, quant = W * kStep;
-  const double want = units * (a.keys / quant + 1 + kStart) / kLeast<W> + 1;
+  return units * (a.keys / quant + 1 + kStart) / kLeast<W> + 1;
+}
+template <int DT, int D, int W, int NB>
+unsigned split_grid(double want) {
+  constexpr int kFill = W > 4 ? 256 : 256 * kOcc<DT, D, NB>;
   return ((want < kFill ? (unsigned)want : kFill) + kXcds - 1) / kXcds * kXcds;
 }
+template <int DT, int D, int W, int NB>
+unsigned split_grid(const AttendArgs& a) { return split_grid<DT, D, W, NB>(split_want<W, NB>(a)); }
 inline size_t split_lds(const AttendArgs& a) { return (size_t)a.B * (sizeof(int64_t) + sizeof(int32_t)); }
 
 // f of the kernel for these sizes.
+// A kernel's name, as a trace shows it; a static string.
+template <typename K>
+const char* name_of(K) {
+  struct Name {
+    char text[64];
+    Name() { K::name(text, sizeof(text)); }
+  };
+  static const Name name;
+  return name.text;
+}
 // Split, Rows: the kernels of the caller.
 template <template <int, int, int, int> class Split, int DT, int D, int NB, typename F>
 auto with_split(const AttendArgs& a, F f) {
@@ -686,8 +721,8 @@ auto with_split(const AttendArgs& a, F f) {
   return large_workgroups<NB, LARGE>(a) ? f(Split<DT, D, LARGE, NB>()) : f(Split<DT, D, 4, NB>());
 }
 template <template <int, int, int, int> class Split, template <int> class Rows, typename F>
-auto with_kernel(const AttendArgs& a, int dtype, int d, F f) {
-  if (by_rows(a, dtype, d)) return d == 64 ? f(Rows<64>()) : f(Rows<128>());
+auto with_kernel(const AttendArgs& a, int dtype, int d, bool rows, F f) {
+  if (rows) return d == 64 ? f(Rows<64>()) : f(Rows<128>());
   if (two_tiles(a, dtype)) return d == 64 ? with_split<Split, 0, 64, 2>(a, f) : with_split<Split, 0, 128, 2>(a, f);
   if (dtype == 0) return d == 64 ? with_split<Split, 0, 64, 1>(a, f) : with_split<Split, 0, 128, 1>(a, f);
   return d == 64 ? with_split<Split, 1, 64, 1>(a, f) : with_split<Split, 1, 128, 1>(a, f);

@@ -15,11 +15,15 @@ namespace {
 struct CommonPart : PrefixArgs {      // a.B, a.tables, a.lens, a.M: the prefixes'
   static constexpr bool kCausal = false;
   template <int NB>
-  static constexpr bool kAhead = true;
+  static constexpr bool kAhead = NB == 2;      // where a step has work to hide loads behind
   static constexpr bool kJoinLater = true;
 };
-struct OwnPart : PrefixArgs {
+struct OwnPart : PrefixArgs {        // joins its sums and the common part's
   static constexpr bool kCausal = true;
+};
+struct OwnLater : PrefixArgs {       // leaves its sums to a kernel that joins both parts'
+  static constexpr bool kCausal = true;
+  static constexpr bool kJoinLater = true;
 };
 
 __device__ __forceinline__ int clamp_to(int v, int most) { return v < 0 ? 0 : v < most ? v : most; }
@@ -38,7 +42,7 @@ __device__ __forceinline__ Request request(const CommonPart& a, int s, int len) 
 __device__ __forceinline__ Request request(const CommonPart& a, int s) { return request(a, s, a.lens[s]); }
 __device__ __forceinline__ int last_key(const CommonPart&, const Request& r, int) { return r.len - 1; }
 
-struct FinishCommon {
+struct FinishLater {
   template <int DT, int D>
   __device__ __forceinline__ void row(const PrefixArgs& a, int64_t to, int jc, float top, float den, f32x4_t sum) const {
     *reinterpret_cast<f32x4_t*>(a.sums + to * D + jc) = sum;
@@ -59,15 +63,15 @@ struct FinishCommon {
     a.parts[to] = 0;
   }
 };
-__device__ __forceinline__ FinishCommon finisher(const CommonPart&, int) { return FinishCommon(); }
+__device__ __forceinline__ FinishLater finisher(const CommonPart&, int) { return FinishLater(); }
+__device__ __forceinline__ FinishLater finisher(const OwnLater&, int) { return FinishLater(); }
 
 struct FinishOwn {
   int joined;        // the request has a prefix
-  // f(values of the row, its statistics) for each of the common part's sums of row `to`, several on
-  // the way at a time; at: where a thread's values stand.
-  template <int D, int N, typename F>
-  __device__ __forceinline__ void common(const PrefixArgs& a, int64_t to, const int (&at)[N], F f) const {
-    const uint64_t parts = a.parts[to];
+  // f(values of the row, its statistics) for each of a part's sums of row `to`, which are where
+  // `parts` says, FLY of them on the way at a time; at: where a thread's values stand.
+  template <int D, int FLY, int N, typename F>
+  __device__ __forceinline__ static void each_sum(const PrefixArgs& a, int64_t to, uint64_t parts, const int (&at)[N], F f) {
     const int count = (int)(parts >> 32 & 0x7fffffff), g0 = (int)(parts >> 16 & 0xffff), row = (int)(parts & 0xffff);
     if (count == 0) {
       f32x4_t v[N];
@@ -77,8 +81,7 @@ struct FinishOwn {
       return;
     }
     // (rows that no prefix has, of starts that do not rise, hold anything)
-    if (count > a.groups - g0 || row >= a.slot_rows) return;
-    constexpr int FLY = N == 1 ? 8 : 1;
+    if (count > kPrefixGroups - g0 || row >= a.slot_rows) return;
     const int64_t slot = (int64_t)a.slot_rows * (D + 2);
     for (int i0 = 0; i0 < count; i0 += FLY) {
       f32x4_t v[FLY][N];
@@ -111,7 +114,7 @@ struct FinishOwn {
   __device__ __forceinline__ void row(const PrefixArgs& a, int64_t to, int jc, float top, float den, f32x4_t sum) const {
     if (joined) {
       const int at[1] = {jc};
-      common<D>(a, to, at, [&](const f32x4_t (&v)[1], float2 ml) {
+      each_sum<D, 8>(a, to, a.parts[to], at, [&](const f32x4_t (&v)[1], float2 ml) {
         const Both x = both(top, den, ml);
         sum = x.own * sum + x.other * v[0];
       });
@@ -125,7 +128,7 @@ struct FinishOwn {
       int at[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) at[n] = (4 * g4 + n / (C / 4)) * C + n % (C / 4) * 4;
-      common<D>(a, to, at, [&](const f32x4_t (&v)[N], float2 ml) {
+      each_sum<D, 1>(a, to, a.parts[to], at, [&](const f32x4_t (&v)[N], float2 ml) {
         const Both x = both(m, l, ml);
 #pragma unroll
         for (int n = 0; n < N; ++n)

@@ -61,20 +61,28 @@ size_t attend_ws_bytes(int B, int G, int T, int d, int dtype);
 hipError_t launch_attend_rows(const AttendArgs& a, int d, void* ws, hipStream_t stream);
 size_t attend_rows_ws_bytes(int d);
 
-// Attention over prefixes that requests share (kvx_prefix8_*.hip), in two launches: the common
+// Attention over prefixes that requests share (kvx_prefix8_*.hip), in two parts: the common
 // part's B, tables, lens, M and keys are the prefixes', the own part's the requests'.
+constexpr int64_t kPrefixRows = 65536;      // most rows (T * H * G) of both parts in one launch
 struct PrefixArgs : AttendArgs {
   const int32_t* shares;    // [prefixes + 1] requests of each prefix
-  float* sums;              // [T, H * G, d] the common part's weighted values
+  float* sums;              // [T, H * G, d] the part's weighted values
   float* stats;             // [T, H * G, 2] reference and sum of its exponentials
   uint64_t* parts;          // [T, H * G] 0: there, else in which partial sums of workgroups (parts_of)
   const float* partial;     // these, slots of slot_rows rows: values, then statistics
-  int32_t prefixes, requests, slot_rows, groups;
+  int32_t prefixes, requests, slot_rows;
 };
-// Rows of a slot of partial sums in the common part's kernel, and bytes of all of them.
+constexpr int kPrefixGroups = 1024;         // most workgroups of a part, two slots each
+hipError_t launch_prefix(const PrefixArgs& common, const PrefixArgs& own, int dtype, int d, void* ws, hipStream_t stream);
+// The kernels of the two parts, as a trace shows them (the same where both go in one launch).
+void prefix_kernel_names(const PrefixArgs& c, const PrefixArgs& o, int dtype, int d, const char** common, const char** own);
+const char* prefix_common_kernel_name(const AttendArgs& a, int dtype, int d);
+const char* prefix_own_kernel_name(const AttendArgs& a, int dtype, int d);
+bool prefix_by_rows(const AttendArgs& a, int dtype, int d);      // the common part's kernel
+// Rows of a slot of partial sums in the common part's kernel, and bytes of all slots.
 int prefix_slot_rows(const AttendArgs& a, int dtype, int d);
-int prefix_groups(int slot_rows);      // most workgroups, two slots each
 size_t prefix_partial_bytes(int S, int G, int T, int d, int dtype);
+// The parts in launches of their own; the own one reads the common one's sums.
 hipError_t launch_prefix_common(const PrefixArgs& a, int dtype, int d, hipStream_t stream);
 hipError_t launch_prefix_own(const PrefixArgs& a, int dtype, int d, void* ws, hipStream_t stream);
 hipError_t launch_prefix_common_rows(const PrefixArgs& a, int d, hipStream_t stream);

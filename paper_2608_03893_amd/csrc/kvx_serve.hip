@@ -392,27 +392,70 @@ static kvx_status check_prefix(const kvx_prefix_dims* p) {
   return KVX_OK;
 }
 
-// The workspace: counters and partial sums of the own part (or of both as one), then the common
-// part's: partial sums of its workgroups, a row's sums, statistics and where they are.
+// The workspace: counters and partial sums of the own part on its own, then for each part the
+// partial sums of its workgroups, a row's sums, statistics and where they are (of the own one where
+// both may go in one launch).
 struct PrefixSpace {
-  uint64_t partial, sums, stats, parts, bytes;
+  struct Part {
+    uint64_t partial, sums, stats, parts;
+  } part[2];
+  uint64_t bytes;
 };
 static PrefixSpace prefix_space(const kvx_attend_dims& m, int32_t S, int dt) {
-  const uint64_t rows = S > 0 ? (uint64_t)m.T * m.H * m.G : 0;
-  const uint64_t partial = S > 0 ? kvx::prefix_partial_bytes(S, m.G, m.T, m.d, dt) : 0;
-  auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
   PrefixSpace s;
-  s.partial = up(kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt));
-  s.sums = s.partial + up(partial);
-  s.stats = s.sums + up(rows * m.d * 4);
-  s.parts = s.stats + up(rows * 8);
-  s.bytes = s.parts + rows * 8;
+  std::memset(&s, 0, sizeof(s));
+  s.bytes = kvx::attend_ws_bytes(m.B, m.G, m.T, m.d, dt);
+  const uint64_t rows = (uint64_t)m.T * m.H * m.G;
+  auto take = [&](uint64_t n) {
+    const uint64_t at = (s.bytes + 255) / 256 * 256;
+    s.bytes = at + n;
+    return at;
+  };
+  for (int i = 0; S > 0 && i < (rows <= (uint64_t)kvx::kPrefixRows ? 2 : 1); ++i) {
+    s.part[i].partial = take(i == 0 ? kvx::prefix_partial_bytes(S, m.G, m.T, m.d, dt)
+                                    : (uint64_t)2 * kvx::kPrefixGroups * 16 * (m.d + 2) * 4);
+    s.part[i].sums = take(rows * m.d * 4);
+    s.part[i].stats = take(rows * 8);
+    s.part[i].parts = take(rows * 8);
+  }
   return s;
 }
 
 size_t kvx_prefix_workspace_bytes(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, kvx_dtype dtype) {
   if (check_attend(dims, dtype) != KVX_OK || check_prefix(prefix) != KVX_OK || dims->B == 0 || dims->T == 0) return 0;
   return prefix_space(*dims, prefix->S, dtype == KVX_BF16 ? 0 : 1).bytes;
+}
+
+// The common part's sizes.
+static void common_sizes(kvx::PrefixArgs& c, const kvx_prefix_dims& p, int log2p) {
+  c.B = p.S;
+  c.M = p.max_pages;
+  c.keys = (int64_t)c.M << log2p;
+  if (p.longest > 0 && p.longest < c.keys) c.keys = p.longest;
+}
+
+kvx_status kvx_prefix_kernel_names(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, const kvx_pool* pool,
+                                   kvx_dtype dtype, const char** common, const char** own) {
+  if (common == nullptr || own == nullptr) return set_error(KVX_ERR_NULL, "common or own is NULL");
+  *common = *own = nullptr;
+  int log2p;
+  kvx_status st = check_pool(pool, true, &log2p);
+  if (st != KVX_OK) return st;
+  if ((st = check_attend(dims, dtype)) != KVX_OK) return st;
+  if ((st = check_prefix(prefix)) != KVX_OK) return st;
+  if (dims->B == 0 || dims->T == 0) return ok();
+  kvx::PrefixArgs o;
+  std::memset(&o, 0, sizeof(o));
+  static_cast<kvx::AttendArgs&>(o) = attend_sizes(*dims, *pool, log2p);
+  const int dt = dtype == KVX_BF16 ? 0 : 1;
+  if (prefix->S == 0) {
+    *own = kvx::attend_kernel_name(o, dt, dims->d);
+    return ok();
+  }
+  kvx::PrefixArgs c = o;
+  common_sizes(c, *prefix, log2p);
+  kvx::prefix_kernel_names(c, o, dt, dims->d, common, own);
+  return ok();
 }
 
 kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims* prefix, const kvx_pool* pool,
@@ -471,25 +514,22 @@ kvx_status kvx_attend_prefix8(const kvx_attend_dims* dims, const kvx_prefix_dims
   if (S == 0) {
     e = kvx::launch_attend(a, dt, m.d, workspace, on);
   } else {
-    char* ws = static_cast<char*>(workspace);
     a.shares = prefix_cu;
-    a.partial = reinterpret_cast<const float*>(ws + space.partial);
-    a.sums = reinterpret_cast<float*>(ws + space.sums);
-    a.stats = reinterpret_cast<float*>(ws + space.stats);
-    a.parts = reinterpret_cast<uint64_t*>(ws + space.parts);
     a.prefixes = S;
     a.requests = m.B;
-    kvx::PrefixArgs c = a;
-    c.B = S;
+    kvx::PrefixArgs part[2] = {a, a};
+    for (int i = 0; i < 2; ++i) {
+      char* ws = static_cast<char*>(workspace);
+      part[i].partial = reinterpret_cast<const float*>(ws + space.part[i].partial);
+      part[i].sums = reinterpret_cast<float*>(ws + space.part[i].sums);
+      part[i].stats = reinterpret_cast<float*>(ws + space.part[i].stats);
+      part[i].parts = reinterpret_cast<uint64_t*>(ws + space.part[i].parts);
+    }
+    kvx::PrefixArgs& c = part[0];
+    common_sizes(c, *prefix, log2p);
     c.tables = prefix_tables;
     c.lens = prefix_lens;
-    c.M = prefix->max_pages;
-    c.keys = (int64_t)c.M << log2p;
-    if (prefix->longest > 0 && prefix->longest < c.keys) c.keys = prefix->longest;
-    a.slot_rows = kvx::prefix_slot_rows(c, dt, m.d);
-    a.groups = kvx::prefix_groups(a.slot_rows);
-    e = kvx::launch_prefix_common(c, dt, m.d, on);
-    if (e == hipSuccess) e = kvx::launch_prefix_own(a, dt, m.d, workspace, on);
+    e = kvx::launch_prefix(c, part[1], dt, m.d, workspace, on);
   }
   if (e != hipSuccess) return set_error(KVX_ERR_HIP, "prefix attention launch: %s", hipGetErrorString(e));
   return ok();

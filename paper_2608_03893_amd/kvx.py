@@ -32,7 +32,7 @@ __all__ = ["KvxError", "KvxNotBuilt", "load", "lib_path", "Dims", "Rope",
            "select_topk", "Mlp", "mlp_workspace_bytes", "mlp_map_cache", "mlp_map_layer",
            "Pool", "AttendDims", "PagePlan", "plan_pages", "store_cache8",
            "attend_workspace_bytes", "attend_workspace", "attend_kernel_name", "attend_cache8",
-           "PrefixDims", "prefix_workspace_bytes", "prefix_workspace", "attend_prefix8", "norm_rope", "sample_workspace", "sample_tokens"]
+           "PrefixDims", "prefix_workspace_bytes", "prefix_kernel_names", "prefix_workspace", "attend_prefix8", "norm_rope", "sample_workspace", "sample_tokens"]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 FLAG_TABLES_READY = 1
@@ -197,6 +197,9 @@ def load():
     L.kvx_prefix_workspace_bytes.restype = SZ
     L.kvx_attend_prefix8.argtypes = [AP, XDP, PP, I32, P, P, P, P, P, P, P, P, P, P, F32, P, P, P, SZ, P]
     L.kvx_attend_prefix8.restype = I32
+    CP = ctypes.POINTER(ctypes.c_char_p)
+    L.kvx_prefix_kernel_names.argtypes = [AP, XDP, PP, I32, CP, CP]
+    L.kvx_prefix_kernel_names.restype = I32
     L.kvx_sample_workspace_bytes.argtypes = [I32, I32, I32]
     L.kvx_sample_workspace_bytes.restype = SZ
     L.kvx_sample_tokens.argtypes = [I32, I32, I32, P, I64, P, P, P, P, P, P, P, P, SZ, P]
@@ -753,6 +756,17 @@ def prefix_workspace_bytes(dims: AttendDims, prefix: PrefixDims, dtype: str = "b
     if dtype not in ("bf16", "f32"):
         raise ValueError("dtype must be 'bf16' or 'f32'")
     return int(load().kvx_prefix_workspace_bytes(ctypes.byref(dims), ctypes.byref(prefix), 0 if dtype == "bf16" else 1))
+
+
+def prefix_kernel_names(dims: AttendDims, prefix: PrefixDims, pool: Pool, dtype: str = "bf16"):
+    """Kernels that the library would launch for these sizes, over the prefixes (None without) and
+    over own keys, as a trace shows them; the same one where both go in one launch."""
+    if dtype not in ("bf16", "f32"):
+        raise ValueError("dtype must be 'bf16' or 'f32'")
+    common, own = ctypes.c_char_p(), ctypes.c_char_p()
+    _check(load().kvx_prefix_kernel_names(ctypes.byref(dims), ctypes.byref(prefix), ctypes.byref(pool),
+                                          0 if dtype == "bf16" else 1, ctypes.byref(common), ctypes.byref(own)))
+    return tuple(None if n.value is None else n.value.decode() for n in (common, own))
 
 
 def prefix_workspace(q, pool, prefix_tables, block_tables, stream=None):

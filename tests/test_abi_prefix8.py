@@ -87,3 +87,20 @@ def test_empty_calls_launch_nothing(L):
         none = dict.fromkeys(("q", "codes", "scales", "ptables", "plens", "pcu", "tables", "lens", "cu", "out", "lse", "ws"))
         assert Prefix(dims=kvx.AttendDims(*dims), **none).run(L) == 0
         assert kvx.prefix_workspace_bytes(kvx.AttendDims(*dims), kvx.PrefixDims(1, 1, 0)) == 0
+
+
+def test_kernel_names():
+    dims, pool = (lambda B, T, d=128, G=8: kvx.AttendDims(B, 8, G, T, d, 0)), (lambda M: kvx.Pool(1000, 16, M))
+    names = kvx.prefix_kernel_names
+    assert names(dims(4, 4), kvx.PrefixDims(1, 100, 0), pool(5)) == ("prefix8_split_kernel<0, 128, 4, 1>",) * 2
+    assert names(dims(4, 4), kvx.PrefixDims(0, 100, 0), pool(5))[0] is None
+    assert names(dims(4, 4), kvx.PrefixDims(0, 100, 0), pool(5))[1] == kvx.attend_kernel_name(dims(4, 4), pool(5))
+    common, own = names(dims(64, 64), kvx.PrefixDims(1, 512, 0), pool(70))
+    assert common == "prefix8_common_split_kernel<0, 128, 8, 2>" and own == "prefix8_own_split_kernel<0, 128, 4, 1>"
+    common, own = names(dims(8, 2048), kvx.PrefixDims(1, 512, 0), pool(70))
+    assert common == "prefix8_common_rows_kernel<128, 2>" and own.startswith("prefix8_own_")
+    assert names(dims(0, 0), kvx.PrefixDims(1, 512, 0), pool(70)) == (None, None)
+    for bad in ((dims(4, 4, d=96), kvx.PrefixDims(1, 9, 0), pool(5)), (dims(4, 4), kvx.PrefixDims(-1, 9, 0), pool(5)),
+                (dims(4, 4), kvx.PrefixDims(1, 9, 0), pool(0))):
+        with pytest.raises(kvx.KvxError):
+            names(*bad)

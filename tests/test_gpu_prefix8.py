@@ -110,13 +110,29 @@ def test_prefixes_match_the_definition(gpu_kvx, dtype, d, P):
         _check(gpu_kvx, c, f"{dtype} d={d} P={P} {step} H={H} G={G}")
 
 
-def _name(kvx, c, part):
+def _names(kvx, c):
     T, heads, d = c["q"].shape
-    H = c["codes"].shape[1]
-    B, M = (c["ptables"] if part == "common" else c["tables"]).shape
-    return kvx.attend_kernel_name(kvx.AttendDims(B, H, heads // H, T, d, 0),
-                                  kvx.Pool(c["scales"].shape[2], c["codes"].shape[2] // c["scales"].shape[2], M),
-                                  "bf16" if c["q"].dtype == torch.bfloat16 else "f32")
+    H, (S_, Mp), (B, M) = c["codes"].shape[1], c["ptables"].shape, c["tables"].shape
+    return kvx.prefix_kernel_names(kvx.AttendDims(B, H, heads // H, T, d, 0), kvx.PrefixDims(S_, Mp, 0),
+                                   kvx.Pool(c["scales"].shape[2], c["codes"].shape[2] // c["scales"].shape[2], M),
+                                   "bf16" if c["q"].dtype == torch.bfloat16 else "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_both_parts_in_one_launch(gpu_kvx, dtype, d):
+    """Units over several workgroups in both parts, more than 64 of either, rows of nobody's prefix."""
+    rng = np.random.default_rng(d + len(dtype))
+    name = f"prefix8_split_kernel<{0 if dtype == 'bf16' else 1}, {d}, 4, 1>"
+    for c in (_case(rng, [1500, 40], [3, 1], [700, 3, 90, 1], [1, 2, 1, 1], 2, 4, d, 16, dtype),
+              _case(rng, [1], [1], [1], [1], 1, 1, d, 128, dtype),
+              _case(rng, [0, 700], [1, 1], [1100, 5, 7, 0, 64], [1, 1, 3, 2, 1], 2, 7, d, 32, dtype, first=1),
+              _case(rng, [10] * 70, [1] * 70, [3] * 72, [1, 0] * 36, 1, 1, d, 16, dtype, first=1)):
+        assert _names(gpu_kvx, c) == (name, name)
+        _check(gpu_kvx, c, name)
+
+
+WIDE = 9000        # entries of a table that keep the parts from one launch
 
 
 @pytest.mark.parametrize("part", ["common", "own"])
@@ -130,8 +146,9 @@ def test_every_kernel(gpu_kvx, kernel, part):
         lens = [int(x) for x in rng.integers(0, M * 16 + 1, B)]
         lens[-1] = M * 16
         count = [B // 2, 0, B - B // 2 - 1]
-        c = _case(rng, [37, 16, 200], count, lens, news, H, G, d, 16, dtype, M=M, first=1)
+        c = _case(rng, [37, 16, 200], count, lens, news, H, G, d, 16, dtype, Mp=WIDE, M=M, first=1)
     else:                   # as many prefixes, the rows of each spread over one to three requests
+        pages = 200 * M if size == "by rows" else M       # the work that it takes
         pre = [int(x) for x in rng.integers(0, M * 16 + 1, B)]
         pre[-1] = M * 16
         count, mine = [], []
@@ -140,8 +157,8 @@ def test_every_kernel(gpu_kvx, kernel, part):
             parts = np.diff([0] + cuts + [n]).tolist()
             count.append(len(parts))
             mine += parts
-        c = _case(rng, pre, count, [n + int(rng.integers(0, 9)) for n in mine], mine, H, G, d, 16, dtype, Mp=M)
-    assert _name(gpu_kvx, c, part) == kernel
+        c = _case(rng, pre, count, [n + int(rng.integers(0, 9)) for n in mine], mine, H, G, d, 16, dtype, Mp=pages, M=WIDE)
+    assert _names(gpu_kvx, c)[part == "own"] == kernel.replace("attend8", f"prefix8_{part}")
     _check(gpu_kvx, c, f"{part} {kernel}")
 
 
