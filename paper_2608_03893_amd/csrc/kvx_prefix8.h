@@ -81,7 +81,7 @@ struct FinishOwn {
       return;
     }
     // (rows that no prefix has, of starts that do not rise, hold anything)
-    if (count > kPrefixGroups - g0 || row >= a.slot_rows) return;
+    if (count > prefix_groups(a.slot_rows) - g0 || row >= a.slot_rows) return;
     const int64_t slot = (int64_t)a.slot_rows * (D + 2);
     for (int i0 = 0; i0 < count; i0 += FLY) {
       f32x4_t v[FLY][N];

@@ -56,10 +56,12 @@ int prefix_slot_rows(const AttendArgs& a, int dtype, int d) {
   return with_kernel<Split, Rows>(a, dtype, d, prefix_by_rows(a, dtype, d), [&](auto k) { return decltype(k)::kSlotRows; });
 }
 
-// Two slots for the first and the last unit of each workgroup: four a CU with blocks of 16 rows,
-// three with 32, one with 256, and room for as many slots as a row may name.
+// Slots for the first and the last unit of each workgroup.
 size_t prefix_partial_bytes(int S, int G, int T, int d, int dtype) {      // whichever kernel it will be
-  return (size_t)2 * kPrefixGroups * (may_go_by_rows(S, G, T, dtype) ? 256 : 32) * (d + 2) * sizeof(float);
+  size_t rows = 0;
+  for (int n : {16, 32, may_go_by_rows(S, G, T, dtype) ? 256 : 32})
+    rows = rows > (size_t)prefix_groups(n) * n ? rows : (size_t)prefix_groups(n) * n;
+  return 2 * rows * (d + 2) * sizeof(float);
 }
 
 }  // namespace kvx

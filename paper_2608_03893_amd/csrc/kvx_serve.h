@@ -72,7 +72,8 @@ struct PrefixArgs : AttendArgs {
   const float* partial;     // these, slots of slot_rows rows: values, then statistics
   int32_t prefixes, requests, slot_rows;
 };
-constexpr int kPrefixGroups = 1024;         // most workgroups of a part, two slots each
+// Most workgroups of a part whose slots have so many rows, two slots each.
+constexpr int prefix_groups(int slot_rows) { return slot_rows == 16 ? 1024 : slot_rows == 32 ? 768 : 256; }
 hipError_t launch_prefix(const PrefixArgs& common, const PrefixArgs& own, int dtype, int d, void* ws, hipStream_t stream);
 // The kernels of the two parts, as a trace shows them (the same where both go in one launch).
 void prefix_kernel_names(const PrefixArgs& c, const PrefixArgs& o, int dtype, int d, const char** common, const char** own);

@@ -413,7 +413,7 @@ static PrefixSpace prefix_space(const kvx_attend_dims& m, int32_t S, int dt) {
   };
   for (int i = 0; S > 0 && i < (rows <= (uint64_t)kvx::kPrefixRows ? 2 : 1); ++i) {
     s.part[i].partial = take(i == 0 ? kvx::prefix_partial_bytes(S, m.G, m.T, m.d, dt)
-                                    : (uint64_t)2 * kvx::kPrefixGroups * 16 * (m.d + 2) * 4);
+                                    : (uint64_t)2 * kvx::prefix_groups(16) * 16 * (m.d + 2) * 4);
     s.part[i].sums = take(rows * m.d * 4);
     s.part[i].stats = take(rows * 8);
     s.part[i].parts = take(rows * 8);
