@@ -14,9 +14,11 @@
 // through up to three launches; in each the workgroup that comes last at a row's counter goes on
 // with what all have found.
 //   1  The largest logits; the answer for greedy rows.  For a small top-k also the answer: a
-//      workgroup takes a list of the logits from a bound on that k of its own reach, which the
-//      maxima of its lanes say, anew whenever four times as much has been seen (so that a list
-//      holds few times k); last, the lists' tokens above the row's own such bound, the cut, the draw.
+//      workgroup lists the logits from a bound on that m of its own reach, which the maxima of its
+//      lanes say, anew whenever four times as much has been seen (so that a list holds few times
+//      m).  m is k where it has the whole row; else its share of k and what chance may add, and the
+//      workgroup that comes last looks whether k of all are above the highest bound: then nothing
+//      that was not listed is among them.  The lists' tokens above it, the cut, the draw.
 //   2  Rows without top-k and top-p: the strips' sums of weights; last: the draw.  Others: a
 //      histogram of counts and weights over the weights' range; last: the bins that the cuts lie in.
 //   3  Rows of the last kind: the strips' sums of weights above these bins, the tokens in them as
@@ -32,7 +34,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kList = 2048;                // most tokens of a list in LDS
 constexpr int kShort = 2048;               // and in the first launch
-constexpr int kLong = 6144;                // and of all workgroups of a row together
+constexpr int kLong = 3072;                // and of all workgroups of a row together
 constexpr int kFew = 256;                  // most tokens that are ranked by counting
 constexpr int kBins = 2048;
 constexpr int kStrips = 256;               // most strips of a row, and waves
@@ -245,7 +247,7 @@ struct SharedBase {
   uint32_t count, lowest, highest, slot;
   int last;
 };
-static_assert(kStrips == kThreads, "a strip a thread");
+static_assert(kStrips == kThreads && kStrips / kWaves <= 64, "a strip a thread, a chunk a lane");
 struct SharedFirst : SharedBase {
   List<kShort> list;
   float lanes[kThreads];
@@ -320,6 +322,7 @@ struct alignas(256) Space {
   int over;                              // the first launch's list did not hold
   State state;
   float top[kStrips];                    // of a wave
+  float bound[kStrips / kWaves];         // of a workgroup's list
   uint32_t first[kStrips];               // index of the first largest (greedy rows)
   uint64_t sum[kStrips];
   uint64_t entry[kLong];
@@ -919,11 +922,17 @@ __device__ __forceinline__ Setting setting(const SampleArgs& a, int b, float top
 __device__ __forceinline__ float temperature_of(const SampleArgs& a, int b) {
   return a.temperature == nullptr ? 1.0f : a.temperature[b];
 }
+// Logits of its own that a workgroup's list goes down to: of k spread over the chunks it holds more
+// once in 10^5 rows or less (its share plus nine; the row goes by bins then).
+__device__ __forceinline__ int listed_of(int k, int chunks) {
+  const int m = chunks > 1 ? (2 * k + chunks - 1) / chunks + 9 : k;
+  return m < k ? m : k;
+}
 // Which way a row goes: through the first launch alone, or the first two or three.
 enum { kPlain, kByList, kByBins };
 __device__ __forceinline__ int way_of(const Setting& set, int chunks) {
   if (set.k == 0) return set.p > 1.0 ? kPlain : kByBins;
-  return set.k <= kThreads / 2 && (int64_t)set.k * chunks <= kLong * 3 / 4 ? kByList : kByBins;
+  return set.k <= kThreads / 2 && listed_of(set.k, chunks) * chunks <= kLong * 3 / 4 ? kByList : kByBins;
 }
 
 template <int DT>
@@ -946,16 +955,19 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   __shared__ SharedFirst s;
   const int chunks = shape.chunks, b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = chunk * kWaves + wave, waves = chunks * kWaves;
-  const Row<DT> row = row_of<DT>(a, b, shape.subs * shape.per);      // strips: the waves' parts
+  const Row<DT> row = row_of<DT>(a, b, 64);
   Space& space = spaces[b];
-  const typename Row<DT>::Strip part = row.strip(n, waves);
 
-  // the first logits of every lane, in registers
+  // Vectors are dealt out to the waves sixteen at a time, so that neighbouring tokens, which are
+  // often likely together, go to different workgroups.  The first ones of every lane stay in
+  // registers.
   const u32x4_t* from = reinterpret_cast<const u32x4_t*>(row.x + row.head);
+  const int vectors = (row.vecs + 64 * waves - 1) / (64 * waves);      // of a lane
+  auto vector = [&](int i) { return ((i * 4 + (lane >> 4)) * waves + n) * 16 + (lane & 15); };
   u32x4_t q[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
-    if (part.v0 + lane + 64 * i < part.v1) q[i] = from[part.v0 + lane + 64 * i];
+    if (vector(i) < row.vecs) q[i] = from[vector(i)];
   int32_t loose = n == 0 || n == waves - 1 ? (lane < 2 * N ? row.loose(lane) : -1) : -1;
   if (loose >= 0 && !(loose < row.head ? n == 0 : n == waves - 1)) loose = -1;
   const float single = loose >= 0 ? row.at(loose) : -INFINITY;
@@ -968,11 +980,11 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   auto held = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-      const int32_t v = part.v0 + lane + 64 * i;
+      const int32_t v = vector(i);
       float y[N];
       LG::get(q[i], y);
 #pragma unroll
-      for (int e = 0; e < N; ++e) y[e] = v < part.v1 ? clean(y[e]) : -INFINITY;
+      for (int e = 0; e < N; ++e) y[e] = v < row.vecs ? clean(y[e]) : -INFINITY;
       f(y, row.head + v * N);
     }
     if (n == 0 || n == waves - 1) {
@@ -984,10 +996,29 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
     }
   };
   auto stream = [&](int i0, int i1, auto f) {
-    const int32_t v0 = part.v0 + 64 * i0, v1 = part.v0 + 64 * i1 < part.v1 ? part.v0 + 64 * i1 : part.v1;
-    if (v0 < v1) row.template vectors<false, 8>(v0, v1, lane, 64, f);
+    if (i0 >= i1) return;
+    constexpr int FLIGHT = 8;
+    u32x4_t p[FLIGHT];
+    auto load = [&](int i) {
+      const int v = vector(i);
+      return from[i < i1 && v < row.vecs ? v : 0];
+    };
+#pragma unroll
+    for (int i = 0; i < FLIGHT; ++i) p[i] = load(i0 + i);
+    for (int i = i0; i < i1; i += FLIGHT) {
+#pragma unroll
+      for (int j = 0; j < FLIGHT; ++j) {
+        if (i + j >= i1) break;
+        const int v = vector(i + j);
+        float y[N];
+        LG::get(p[j], y);
+        p[j] = load(i + j + FLIGHT);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = v < row.vecs ? clean(y[e]) : -INFINITY;
+        f(y, row.head + v * N);
+      }
+    }
   };
-  const int vectors = shape.subs * shape.per / 64;      // of a lane
 
   float most = -INFINITY;
   auto largest_of = [&](const float* y, int32_t) {
@@ -1055,8 +1086,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
     return;
   }
 
-  // A logit that k of the workgroup's reach: the largest number, to 16 bits, that k of its lanes'
+  // A logit that m of the workgroup's reach: the largest number, to 16 bits, that m of its lanes'
   // maxima so far do.
+  const int m = listed_of(first_set.k, chunks);
   auto bound_now = [&] {
     constexpr int M = kThreads / 64;
     __syncthreads();
@@ -1065,7 +1097,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
     float v[M];
 #pragma unroll
     for (int i = 0; i < M; ++i) v[i] = s.lanes[lane + 64 * i];
-    uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);    // k reach lo
+    uint32_t lo = key_of(-INFINITY), hi = key_of(INFINITY);    // m reach lo
 #pragma unroll 1
     for (int step = 0; step < 16; ++step) {
       const uint32_t mid = lo + (hi - lo) / 2;
@@ -1073,7 +1105,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       int reach = 0;
 #pragma unroll
       for (int i = 0; i < M; ++i) reach += __popcll(__ballot(v[i] >= x));
-      if (reach >= first_set.k) lo = mid;
+      if (reach >= m) lo = mid;
       else hi = mid;
     }
     return of_key(lo);
@@ -1085,7 +1117,24 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   auto list = [&](const float* y, int32_t first) {
     z.append(y, first, s.list.entry, &s.count, kShort, [&](float x) { return x >= bound && x != -INFINITY; });
   };
-  held(list);
+  {       // the held ones at once
+    uint32_t mine = 0;
+    held([&](const float* y, int32_t) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) mine += ((y[e] >= bound) & (y[e] != -INFINITY)) ? 1 : 0;
+    });
+    if (mine > 0) {
+      uint32_t at = atomicAdd(&s.count, mine);
+      held([&](const float* y, int32_t first) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if ((y[e] >= bound) & (y[e] != -INFINITY)) {
+            if (at < kShort) s.list.entry[at] = (uint64_t)~key_of(y[e]) << 32 | (uint32_t)(first + e);
+            ++at;
+          }
+      });
+    }
+  }
   for (int i = kHeld; i < vectors; i *= 4) {
     stream(i, 4 * i < vectors ? 4 * i : vectors, [&](const float* y, int32_t first) {
       largest_of(y, first);
@@ -1112,26 +1161,39 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   };
   if (over) listed = 0;
   every(listed, [&](uint64_t& v, uint32_t j) { v = j < listed ? s.list.entry[j] : ~0ull; });
-  if (chunks > 1) {       // what reaches the last bound, to all workgroups' list
-    uint32_t kept = 0;
-    every(listed, [&](uint64_t& v, uint32_t) {
-      if (v != ~0ull && logit(v) < bound) v = ~0ull;
-      kept += v != ~0ull;
-    });
-    const uint32_t upto = (uint32_t)block_scan(kept, s);
-    if (threadIdx.x == kThreads - 1)
-      s.slot = __hip_atomic_fetch_add(&space.listed, over ? kLong + 1u : upto, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  float floor = -INFINITY;      // the highest bound of a list
+  if (chunks > 1) {       // to all workgroups' list, what reaches the last bound
+    uint32_t kept = 0, upto = 0;
+    if (vectors > kHeld) {
+      every(listed, [&](uint64_t& v, uint32_t) {
+        if (v != ~0ull && logit(v) < bound) v = ~0ull;
+        kept += v != ~0ull;
+      });
+      upto = (uint32_t)block_scan(kept, s);
+    }
+    if (threadIdx.x == kThreads - 1) {
+      const uint32_t all = over ? kLong + 1u : vectors > kHeld ? upto : listed;
+      s.slot = __hip_atomic_fetch_add(&space.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      put(&space.bound[chunk], bound);
+    }
     __syncthreads();
     uint32_t at = s.slot + upto - kept;
-    every(listed, [&](uint64_t& v, uint32_t) {
+    every(listed, [&](uint64_t& v, uint32_t j) {
       if (v == ~0ull) return;
-      if (at < kLong) put(&space.entry[at], v);
-      ++at;
+      const uint32_t to = vectors > kHeld ? at : at + j;
+      if (to < kLong) put(&space.entry[to], v);
+      if (vectors > kHeld) ++at;
     });
     if (!come_last(&space.arrived[0], chunks, s)) return;
     listed = uniform(get(&space.listed));
+    floor = lane < chunks ? get(&space.bound[lane]) : -INFINITY;
     over = listed > kLong;
     every(over ? 0 : listed, [&](uint64_t& v, uint32_t j) { v = j < listed ? get(&space.entry[j]) : ~0ull; });
+#pragma unroll
+    for (int i = 32; i; i >>= 1) floor = fmaxf(floor, __shfl_xor(floor, i, 64));
+    every(over ? 0 : listed, [&](uint64_t& v, uint32_t) {
+      if (v != ~0ull && logit(v) < floor) v = ~0ull;
+    });
   }
   // their largest and least logits
   uint32_t hi = 0, lo = ~0u;
@@ -1174,7 +1236,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       return y > 0.0f ? y < (float)kThreads ? (int)y : kThreads - 1 : 0;
     };
     int limit = kThreads;
-    if (listed > kThreads / 4 && listed > (uint32_t)z.set.k) {
+    if (chunks > 1 || (listed > kThreads / 4 && listed > (uint32_t)z.set.k)) {
       every(listed, [&](uint64_t& v, uint32_t) {
         if (v != ~0ull) atomicAdd(&s.rank[bin(logit(v))], 1u);
       });
@@ -1185,6 +1247,8 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       if (upto >= k && upto - c < k) s.slot = threadIdx.x;
       __syncthreads();
       limit = (int)s.slot;
+      // fewer than k above the highest bound: others may be among them that were not listed
+      over = limit == kThreads && floor != -INFINITY;
     }
     uint32_t mine = 0;
     every(listed, [&](uint64_t& v, uint32_t) {
@@ -1198,7 +1262,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       ++at;
     });
     __syncthreads();
-    over = s.kept > kShort;
+    over = over || s.kept > kShort;
   }
   if (threadIdx.x == 0) space.over = over;
   if (over) {       // by bins

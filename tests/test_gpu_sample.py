@@ -131,6 +131,24 @@ def test_ties(gpu_kvx, V, dtype):
     _check(gpu_kvx, few, [SETTINGS[i % len(SETTINGS)] for i in range(len(u))], g.random(len(u)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [64, 128, 300])
+def test_likely_tokens_side_by_side(gpu_kvx, width, dtype):
+    """The top-k lie in one run of the vocabulary, anywhere in it, so that one workgroup has them
+    all; or every so many tokens."""
+    V, settings = 50021, [(1.0, k, p, m) for k in (2, 20, 50, 64, 120, 128) for p, m in ((1.0, 0.0), (0.9, 0.0))]
+    g = np.random.default_rng(width)
+    for B in (1, 4, len(settings)):
+        x = torch.tensor(g.standard_normal((B, V)) * 0.5)
+        for b in range(B):
+            at = (0, V - width, g.integers(0, V - width))[b % 3]
+            some = (np.arange(at, at + width) if b % 4 < 3 else np.arange(width) * 128 % V)
+            x[b, some] += torch.tensor(6.0 + g.random(width))
+        x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).to(DEV)
+        for i in range(0, len(settings), B):
+            _check(gpu_kvx, x, (settings * 2)[i:i + B], g.random(B))
+
+
 def test_rows_apart(gpu_kvx):
     """Views: a stride that is not the row's length, rows that begin anywhere, shared rows."""
     for dtype in ("bf16", "f32"):
