@@ -105,18 +105,28 @@ __device__ __forceinline__ uint64_t weight_of(float x, float top, double by) {
   return some ? __builtin_bit_cast(uint64_t, r) & 0xfffffffffffffull : 0;
 }
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-  for (int n = 32; n; n >>= 1) v += (uint64_t)__shfl_xor((unsigned long long)v, n, 64);
+// v of the lane that CTRL names, 0 in lanes of rows that ROWS leaves out and where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t moved(uint64_t v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
+}
+// Sum over the lanes up to this one; all lanes call.
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
+  v += moved<0x111, 0xf>(v);      // 1, 2, 4, 8 lanes on within rows of 16
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);      // a row's last lane to the next row, the second row's to the upper half
+  v += moved<0x143, 0xc>(v);
   return v;
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {   // inclusive
-#pragma unroll
-  for (int n = 1; n < 64; n <<= 1) {
-    const uint64_t u = (uint64_t)__shfl_up((unsigned long long)v, n, 64);
-    if (lane >= n) v += u;
-  }
-  return v;
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+  v = wave_scan(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+  return (uint64_t)hi << 32 | lo;
 }
 
 // A row's settings, restrictions that cannot bind switched off.
@@ -245,6 +255,7 @@ struct SharedBase {
   uint64_t strip[kStrips];     // also a scratch value of each thread
   uint32_t rank[kThreads];
   uint32_t count, lowest, highest, slot;
+  float logit;                 // of the token in `slot`
   int last;
 };
 static_assert(kStrips == kThreads && kStrips / kWaves <= 64, "a strip a thread, a chunk a lane");
@@ -279,7 +290,7 @@ __device__ __forceinline__ uint64_t block_sum(uint64_t v, SH& s) {
 template <typename SH>
 __device__ __forceinline__ uint64_t block_scan(uint64_t v, SH& s) {
   const int wave = threadIdx.x >> 6;
-  v = wave_scan(v, threadIdx.x & 63);
+  v = wave_scan(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 63) s.part[wave] = v;
   __syncthreads();
@@ -672,7 +683,10 @@ struct Sampler {
     uint64_t sum = block_scan(mine, s) - mine;
 #pragma unroll
     for (int j = 0; j < kFinal; ++j) {
-      if (sum <= t && t < sum + v[j]) s.slot = (uint32_t)(i + j);
+      if (sum <= t && t < sum + v[j]) {
+        s.slot = (uint32_t)(i + j);
+        s.logit = y[j];
+      }
       sum += v[j];
     }
     __syncthreads();
@@ -694,51 +708,59 @@ struct Sampler {
     __syncthreads();
     const typename Row<DT>::Strip where = row.strip((int)s.slot, strips);
     const int32_t token = locate(where.lo, where.hi, s.found[1], f);
-    if (threadIdx.x == 0) put_token(a, b, token, row.at(token), total);
+    if (threadIdx.x == 0) put_token(a, b, token, s.logit, total);
   }
 
   // ---- the cut by histograms ----
 
   // What launch 3 has to look at, from the histogram of the row, which becomes sums up to each bin.
-  __device__ __forceinline__ int first_bin(bool by_count, uint64_t target) {
-    constexpr int M = kBins / kThreads;
-    uint64_t below = 0;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const int j = threadIdx.x * M + i;
-      below += (by_count ? (uint64_t)s.bin.count[j] : s.bin.weight[j]) < target;
-    }
-    return (int)block_sum(below, s);      // kBins: no bin reaches it
-  }
   __device__ __forceinline__ void plan(State& to) {
-    constexpr int M = kBins / kThreads;
-    uint64_t c = 0, w = 0;
+    constexpr int M = kBins / kThreads;      // neighbouring bins of a thread
+    uint64_t c[M], w[M], c0 = 0, w0 = 0;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      c += s.bin.count[threadIdx.x * M + i];
-      w += s.bin.weight[threadIdx.x * M + i];
+      c[i] = c0 += s.bin.count[threadIdx.x * M + i];
+      w[i] = w0 += s.bin.weight[threadIdx.x * M + i];
     }
-    uint64_t c0 = block_scan(c, s) - c, w0 = block_scan(w, s) - w;
+    c0 = wave_scan(c0) - c0;
+    w0 = wave_scan(w0) - w0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 63) {
+      s.part[wave] = w0 + w[M - 1];
+      s.strip[wave] = c0 + c[M - 1];
+    }
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) {
+      w0 += s.part[x];
+      c0 += s.strip[x];
+    }
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      c0 += s.bin.count[threadIdx.x * M + i];
-      w0 += s.bin.weight[threadIdx.x * M + i];
-      s.bin.count[threadIdx.x * M + i] = (uint32_t)c0;
-      s.bin.weight[threadIdx.x * M + i] = w0;
+      c[i] += c0;
+      w[i] += w0;
+      s.bin.count[threadIdx.x * M + i] = (uint32_t)c[i];
+      s.bin.weight[threadIdx.x * M + i] = w[i];
     }
+    // the first bin up to which the count (or the weight) reaches the target; kBins: there is none
+    auto first_bin = [&](const uint64_t* sums, uint64_t target) {
+      uint64_t below = 0;
+#pragma unroll
+      for (int i = 0; i < M; ++i) below += sums[i] < target;
+      return (int)block_sum(below, s);
+    };
     __syncthreads();
     auto count = [&](int i) { return i < 0 ? 0u : s.bin.count[i]; };
     auto weight_to = [&](int i) { return i < 0 ? (uint64_t)0 : s.bin.weight[i]; };
     const bool by_k = set.k > 0 && (uint32_t)set.k < count(kBins - 1), by_p = set.p <= 1.0;
     State st;
-    st.at_k = by_k ? first_bin(true, (uint64_t)set.k) : -1;
+    st.at_k = by_k ? first_bin(c, (uint64_t)set.k) : -1;
     st.before_k = by_k ? count(st.at_k - 1) : 0;
     st.weight_k = by_k ? weight_to(st.at_k - 1) : 0;
     st.total = weight_to(kBins - 1);
     if (by_p) {       // for the least and the largest weight that top-k may leave
       const uint64_t least = by_k ? st.weight_k : st.total, most = by_k ? weight_to(st.at_k) : st.total;
-      st.above = least > 0 ? first_bin(false, up_to(set.p, least)) : 0;
-      st.upto = first_bin(false, up_to(set.p, most));
+      st.above = least > 0 ? first_bin(w, up_to(set.p, least)) : 0;
+      st.upto = most == least ? st.above : first_bin(w, up_to(set.p, most));
     } else {
       st.above = by_k ? st.at_k : kBins;       // else nothing is cut
       st.upto = by_k ? st.at_k : -1;
@@ -1390,9 +1412,18 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
         __hip_atomic_fetch_add(&space.weight[i], s.bin.weight[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       if (!come_last(&space.arrived[1], chunks, s)) continue;
-      for (int i = threadIdx.x; i < kBins; i += kThreads) {
-        s.bin.weight[i] = get(&space.weight[i]);
-        s.bin.count[i] = get(&space.count[i]);
+      constexpr int M = kBins / kThreads;
+      uint64_t w[M];
+      uint32_t c[M];
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        w[i] = get(&space.weight[threadIdx.x + i * kThreads]);
+        c[i] = get(&space.count[threadIdx.x + i * kThreads]);
+      }
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        s.bin.weight[threadIdx.x + i * kThreads] = w[i];
+        s.bin.count[threadIdx.x + i * kThreads] = c[i];
       }
       __syncthreads();
     }
@@ -1550,7 +1581,8 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
       block(kThreads);
   hipLaunchKernelGGL((sample_kernel<DT>), grid, block, 0, stream, a, spaces, shape);
   hipLaunchKernelGGL((sample_weigh_kernel<DT>), some, block, 0, stream, a, spaces, shape);
-  hipLaunchKernelGGL((sample_cut_kernel<DT>), some, block, 0, stream, a, spaces, shape);
+  if (a.top_k != nullptr || a.top_p != nullptr)      // else every row is answered by now
+    hipLaunchKernelGGL((sample_cut_kernel<DT>), some, block, 0, stream, a, spaces, shape);
   return hipGetLastError();
 }
 
