@@ -81,28 +81,49 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// 2^43 times exp((x - top) / T), to the nearest whole number; by = log2(e) / T.  Without branches,
-// so that the chains of several logits run side by side.
-__device__ __forceinline__ uint64_t weight_of(float x, float top, double by) {
+// 2^(j / 64).
+constexpr int kPowers = 64;
+__constant__ double kPower[kPowers] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
+};
+// 2^43 times exp((x - top) / T), to the nearest whole number; by = log2(e) / T.  The exponent of 2
+// is a whole number of 64ths, whose power is in `power` (LDS), and a rest r of half a 64th at most,
+// for which a polynomial of degree 4 through four Chebyshev points and 1 at r = 0 is off by 4.9e-15
+// (a series over a whole unit, of degree 11, took twice the time: these chains, not the reads, bound
+// the second launch).  Without branches, so that the chains of several logits run side by side.
+__device__ __forceinline__ uint64_t weight_of(float x, float top, double by, const double* power) {
   const double z = x == top ? 0.0 : ((double)x - (double)top) * by;
   const bool some = z > -45.0;      // (not where z is NaN)
   const double y = some ? z : 0.0;
-  const double n = rint(y), t = (y - n) * 0.69314718055994530942;
-  double p = 1.0 / 39916800.0;      // the exponential's series to t^11: 6e-15
-  p = __builtin_fma(p, t, 1.0 / 3628800.0);
-  p = __builtin_fma(p, t, 1.0 / 362880.0);
-  p = __builtin_fma(p, t, 1.0 / 40320.0);
-  p = __builtin_fma(p, t, 1.0 / 5040.0);
-  p = __builtin_fma(p, t, 1.0 / 720.0);
-  p = __builtin_fma(p, t, 1.0 / 120.0);
-  p = __builtin_fma(p, t, 1.0 / 24.0);
-  p = __builtin_fma(p, t, 1.0 / 6.0);
-  p = __builtin_fma(p, t, 0.5);
-  p = __builtin_fma(p, t, 1.0);
-  p = __builtin_fma(p, t, 1.0);
+  constexpr double kWhole = 6755399441055744.0;      // 1.5 2^52: a sum with it has the rounded number in its low bits
+  const double sum = __builtin_fma(y, (double)kPowers, kWhole);
+  const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, sum);
+  const double r = __builtin_fma(y, (double)kPowers, kWhole - sum);
+  double p = 0x1.3b2acb2c36b23p-31;
+  p = __builtin_fma(p, r, 0x1.c6b0b9214b9aep-23);
+  p = __builtin_fma(p, r, 0x1.ebfbdff82bb76p-15);
+  p = __builtin_fma(p, r, 0x1.62e42fefa2417p-7);
+  p = __builtin_fma(p, r, 1.0);
+  const uint64_t whole = __builtin_bit_cast(uint64_t, power[n & (kPowers - 1)]);
+  const uint64_t shift = (uint64_t)(uint32_t)(((n >> 6) + kFraction) * (1 << 20)) << 32;      // exponents of normal numbers
   // the sum with 2^52 has the rounded number in its low bits
-  const double r = ldexp(p, (int)n + kFraction) + 4503599627370496.0;
-  return some ? __builtin_bit_cast(uint64_t, r) & 0xfffffffffffffull : 0;
+  const double w = __builtin_fma(p, __builtin_bit_cast(double, whole + shift), 4503599627370496.0);
+  return some ? __builtin_bit_cast(uint64_t, w) & 0xfffffffffffffull : 0;
 }
 
 // v of the lane that CTRL names, 0 in lanes of rows that ROWS leaves out and where there is none.
@@ -250,6 +271,7 @@ struct Bins {
   uint32_t count[kBins];
 };
 struct SharedBase {
+  double power[kPowers];       // a kernel copies them before its first barrier
   uint64_t part[kWaves];
   uint64_t found[4];
   uint64_t strip[kStrips];     // also a scratch value of each thread
@@ -275,6 +297,10 @@ struct SharedCut : SharedBase {
   uint64_t few[kFew], few_weight[kFew];
 };
 
+template <typename SH>
+__device__ __forceinline__ void put_powers(SH& s) {
+  if (threadIdx.x < kPowers) s.power[threadIdx.x] = kPower[threadIdx.x];
+}
 template <typename SH>
 __device__ __forceinline__ uint64_t block_sum(uint64_t v, SH& s) {
   v = wave_sum(v);
@@ -369,7 +395,7 @@ struct Sampler {
   Setting set;
   static constexpr int N = Logits<DT>::N;
 
-  __device__ __forceinline__ uint64_t weight(float x) const { return weight_of(x, set.top, set.by); }
+  __device__ __forceinline__ uint64_t weight(float x) const { return weight_of(x, set.top, set.by, s.power); }
 
   // Entries of the tokens that `take` accepts among y, to places of a list in LDS (below `most`)
   // that its counter gives out, to a lane at a time.
@@ -975,6 +1001,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   constexpr int N = LG::N;
   using Z = Sampler<DT, SharedFirst, kShort>;
   __shared__ SharedFirst s;
+  put_powers(s);
   const int chunks = shape.chunks, b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = chunk * kWaves + wave, waves = chunks * kWaves;
   const Row<DT> row = row_of<DT>(a, b, 64);
@@ -1344,6 +1371,7 @@ __global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Sp
   constexpr int N = Logits<DT>::N;
   using Z = Sampler<DT, SharedWeigh, 0>;
   __shared__ SharedWeigh s;
+  put_powers(s);
   const int chunks = shape.chunks, waves = chunks * kWaves, strips = waves * shape.subs;
   const int lane = threadIdx.x & 63;
   for (int item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
@@ -1436,6 +1464,7 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
   using Z = Sampler<DT, SharedCut, kList>;
   constexpr int N = Logits<DT>::N;
   __shared__ SharedCut s;
+  put_powers(s);
   const int chunks = shape.chunks, waves = chunks * kWaves, strips = waves * shape.subs;
   const int lane = threadIdx.x & 63;
   for (int item = blockIdx.x; item < a.B * chunks; item += gridDim.x) {
