@@ -175,13 +175,14 @@ struct Row {
   }
   __device__ __forceinline__ float at(int32_t i) const { return clean(LG::one(x[i])); }
   // f(logits, their number, index of the first) for every vector of v0 .. v1 - 1 that thread `me`
-  // of `n` has, from the last on where BACK: what was read last is still in the caches.  FLIGHT:
-  // loads of a thread on the way
+  // of `n` has, from the last on where BACK: what was read last is still in the caches.  FLIGHT
+  // loads of a thread are on the way while as many vectors go through f.  f is there once, in a
+  // loop: rows run through it a few times only, and fetching an unrolled one took as long as running it
   template <bool BACK, int FLIGHT, typename F>
   __device__ __forceinline__ void vectors(int v0, int v1, int me, int n, F f) const {
     const u32x4_t* from = reinterpret_cast<const u32x4_t*>(x + head);
     const int steps = (v1 - v0 + n - 1) / n;
-    u32x4_t q[FLIGHT];
+    u32x4_t q[FLIGHT], next[FLIGHT];
     auto vector = [&](int s) {      // -1: none
       const int v = v0 + (BACK ? steps - 1 - s : s) * n + me;
       return s < steps && v < v1 ? v : -1;
@@ -192,18 +193,25 @@ struct Row {
     };
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i) q[i] = load(i);
+#pragma unroll 1
     for (int s = 0; s < steps; s += FLIGHT) {
+      const int some = steps - s < FLIGHT ? steps - s : FLIGHT;
+      if (s + FLIGHT < steps)
 #pragma unroll
-      for (int i = 0; i < FLIGHT; ++i) {
-        if (s + i >= steps) break;
+        for (int i = 0; i < FLIGHT; ++i) next[i] = load(s + FLIGHT + i);
+#pragma unroll 1
+      for (int i = 0; i < some; ++i) {
         const int v = vector(s + i);
         float y[LG::N];
-        LG::get(q[i], y);
-        q[i] = load(s + i + FLIGHT);
+        LG::get(q[0], y);
+#pragma unroll
+        for (int j = 0; j + 1 < FLIGHT; ++j) q[j] = q[j + 1];
 #pragma unroll
         for (int e = 0; e < LG::N; ++e) y[e] = v < 0 ? -INFINITY : clean(y[e]);
         f(y, head + v * LG::N);
       }
+#pragma unroll
+      for (int i = 0; i < FLIGHT; ++i) q[i] = next[i];
     }
   }
   // Strip n of `strips`: its vectors, and its logits, those outside whole vectors with the first
@@ -1367,7 +1375,7 @@ __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space&
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_weigh_kernel(SampleArgs a, Space* spaces, Shape shape) {
+__global__ void __launch_bounds__(kThreads, 3) sample_weigh_kernel(SampleArgs a, Space* spaces, Shape shape) {
   constexpr int N = Logits<DT>::N;
   using Z = Sampler<DT, SharedWeigh, 0>;
   __shared__ SharedWeigh s;
@@ -1568,14 +1576,13 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
     uint64_t last = ~0ull;
     if (listed > 0) {
       uint64_t total = st.total;
-      if (st.at_k >= 0) {
-        const typename Z::Picked k = z.pick(listed, st.at_k, st.at_k, true, (uint64_t)((uint32_t)set.k - st.before_k));
-        total = st.weight_k + k.sum;
-        last = k.entry;
-      }
-      if (set.p <= 1.0) {
+#pragma unroll 1
+      for (int stage = st.at_k >= 0 ? 0 : 1; stage < (set.p <= 1.0 ? 2 : 1); ++stage) {      // top-k, top-p
         const uint64_t t = z.up_to(set.p, total);
-        last = z.pick(listed, st.above, st.upto, false, t > st.weight_above ? t - st.weight_above : 1).entry;
+        const uint64_t target = stage == 0 ? (uint32_t)set.k - st.before_k : t > st.weight_above ? t - st.weight_above : 1;
+        const typename Z::Picked to = z.pick(listed, stage == 0 ? st.at_k : st.above, stage == 0 ? st.at_k : st.upto, stage == 0, target);
+        if (stage == 0) total = st.weight_k + to.sum;
+        last = to.entry;
       }
       cut = {of_key(~(uint32_t)(last >> 32)), (int32_t)(uint32_t)last, 0, false};
     }
