@@ -69,11 +69,14 @@ __device__ __forceinline__ FinishLater finisher(const OwnLater&, int) { return F
 struct FinishOwn {
   int joined;        // the request has a prefix
   // f(values of the row, its statistics) for each of a part's sums of row `to`, which are where
-  // `parts` says, FLY of them on the way at a time; at: where a thread's values stand.
-  template <int D, int FLY, int N, typename F>
-  __device__ __forceinline__ static void each_sum(const PrefixArgs& a, int64_t to, uint64_t parts, const int (&at)[N], F f) {
+  // `parts` says, FLY of them on the way at a time; at: where a thread's values stand.  Of several
+  // threads that share them, thread `share` takes every SHARES-th one.
+  template <int D, int FLY, int SHARES = 1, int N, typename F>
+  __device__ __forceinline__ static void each_sum(const PrefixArgs& a, int64_t to, uint64_t parts, const int (&at)[N], F f,
+                                                  int share = 0) {
     const int count = (int)(parts >> 32 & 0x7fffffff), g0 = (int)(parts >> 16 & 0xffff), row = (int)(parts & 0xffff);
     if (count == 0) {
+      if (share != 0) return;
       f32x4_t v[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) v[n] = *reinterpret_cast<const f32x4_t*>(a.sums + to * D + at[n]);
@@ -83,12 +86,12 @@ struct FinishOwn {
     // (rows that no prefix has, of starts that do not rise, hold anything)
     if (count > prefix_groups(a.slot_rows) - g0 || row >= a.slot_rows) return;
     const int64_t slot = (int64_t)a.slot_rows * (D + 2);
-    for (int i0 = 0; i0 < count; i0 += FLY) {
+    for (int i0 = share; i0 < count; i0 += FLY * SHARES) {
       f32x4_t v[FLY][N];
       float2 ml[FLY];
 #pragma unroll
       for (int i = 0; i < FLY; ++i) {
-        const int p = i0 + i < count ? i0 + i : count - 1;
+        const int p = i0 + i * SHARES < count ? i0 + i * SHARES : count - 1;
         const float* from = a.partial + (2 * (g0 + p) + (p == 0 ? 1 : 0)) * slot;
 #pragma unroll
         for (int n = 0; n < N; ++n) v[i][n] = *reinterpret_cast<const f32x4_t*>(from + row * D + at[n]);
@@ -96,7 +99,7 @@ struct FinishOwn {
       }
 #pragma unroll
       for (int i = 0; i < FLY; ++i)
-        if (i0 + i < count) f(v[i], ml[i]);
+        if (i0 + i * SHARES < count) f(v[i], ml[i]);
     }
   }
   // Factors of the sums so far and of further ones, whose statistics are joined.

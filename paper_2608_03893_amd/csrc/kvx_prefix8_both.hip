@@ -24,25 +24,37 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) pr
     attend8_split<DT, D, W, 1>(o, const_cast<float*>(o.partial), nullptr, lds.o, Group{block - grid, (int)gridDim.x - grid});
 }
 
-// A row's sums of both parts, by D / 4 threads.
+// A row's sums of both parts, by kShares times D / 4 threads.
+constexpr int kShares = 4;
 template <int DT, int D>
 __global__ void __launch_bounds__(256) prefix8_join_kernel(PrefixArgs c, PrefixArgs o) {
-  constexpr int Q = D / 4;
-  const int64_t to = ((int64_t)blockIdx.x * 256 + threadIdx.x) / Q;
-  const int t = (int)(to / (o.H * o.G)), at[1] = {(int)threadIdx.x % Q * 4};
-  if (t >= o.T) return;
+  constexpr int Q = D / 4, ROWS = 256 / (kShares * Q);
+  __shared__ f32x4_t sums[256];
+  __shared__ float2 stats[256];
+  const int share = (int)threadIdx.x / (ROWS * Q), place = (int)threadIdx.x - share * ROWS * Q;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + place / Q, rows = (int64_t)o.T * o.H * o.G, to = row < rows ? row : rows - 1;
+  const int t = (int)(to / (o.H * o.G)), at[1] = {place % Q * 4};
   const uint64_t own = o.parts[to], common = c.parts[to];      // (anything, for rows of no request)
   auto start = [&](int b) { return clamp_to(o.cu[clamp_to(b, o.requests)], o.T); };
-  if (t < start(0) || t >= start(o.requests)) return;
-  const bool joined = t >= start(o.shares[0]) && t < start(o.shares[o.prefixes]);
+  const bool live = row < rows && t >= start(0) && t < start(o.requests);
+  const bool joined = live && t >= start(o.shares[0]) && t < start(o.shares[o.prefixes]);
   float top = -INFINITY, den = 0.0f;
   f32x4_t sum = {0, 0, 0, 0};
   auto add = [&](const f32x4_t (&v)[1], float2 ml) {
     const FinishOwn::Both x = FinishOwn::both(top, den, ml);
     sum = x.own * sum + x.other * v[0];
   };
-  FinishOwn::each_sum<D, 8>(o, to, own, at, add);
-  if (joined) FinishOwn::each_sum<D, 16>(c, to, common, at, add);
+  if (live) FinishOwn::each_sum<D, 8, kShares>(o, to, own, at, add, share);
+  if (joined) FinishOwn::each_sum<D, 16, kShares>(c, to, common, at, add, share);
+  sums[threadIdx.x] = sum;
+  stats[threadIdx.x] = make_float2(top, den);
+  __syncthreads();
+  if (share != 0 || !live) return;
+#pragma unroll
+  for (int x = 1; x < kShares; ++x) {
+    const f32x4_t v[1] = {sums[x * ROWS * Q + place]};
+    add(v, stats[x * ROWS * Q + place]);
+  }
   Finish().row<DT, D>(o, to, at[0], top, den, sum);
 }
 
@@ -60,7 +72,7 @@ struct Both {
     const size_t lds = split_lds(c) > split_lds(o) ? split_lds(c) : split_lds(o);
     hipLaunchKernelGGL((prefix8_split_kernel<DT, D, W, NB>), dim3(first + second), dim3(64 * W), lds, stream, common, own, (int)first);
     const int64_t rows = (int64_t)o.T * o.H * o.G;
-    hipLaunchKernelGGL((prefix8_join_kernel<DT, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream,
+    hipLaunchKernelGGL((prefix8_join_kernel<DT, D>), dim3((unsigned)((rows * (D / 4) * kShares + 255) / 256)), dim3(256), 0, stream,
                        static_cast<const PrefixArgs&>(common), static_cast<const PrefixArgs&>(own));
     return hipGetLastError();
   }
