@@ -6,11 +6,15 @@
 //
 // A lane holds E channels of a head's first half and the E that half-split planes pair with
 // them (16 bytes each), so that a plane's two channels meet in a lane in both layouts, and a
-// row's squares are summed over 4 to 16 neighbouring lanes.  A wave takes one token's heads,
-// 64 / lanes of them at a time: it forms the token's d / 2 sines and cosines once, one plane a
-// lane, and shares them through LDS that is its own, without a barrier.
+// row's squares are summed over 4 to 16 neighbouring lanes.  A wave takes 64 / lanes heads of a
+// token, with that token's d / 2 sines and cosines, one plane a lane, shared through LDS that is
+// its own, without a barrier.  They are formed again for every wave of a token while its heads are
+// on the way: a wave for several heads a token, with the next ones loaded ahead, was no faster (8192
+// tokens of 72 heads 59 us, 1024 of 72 9.5).
 //
-// Bound by memory: every element is read once and written once.
+// Bound by memory, every element read once and written once: 8192 tokens of 72 bf16 heads of 128
+// channels, 302 MB, XXXX.  A step of 16 tokens of 48 heads is bound by the launch and its host time:
+// XXXX.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
 
@@ -18,6 +22,7 @@ namespace kvx {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int64_t kMost = 1 << 23;      // workgroups of a launch, whose threads are counted in 32 bits
 
 // 16 bytes of a row as floats, and back.
 template <int DT>
@@ -58,31 +63,19 @@ __global__ void __launch_bounds__(64 * kWaves) norm_rope_kernel(NormRopeArgs a) 
   __shared__ __attribute__((aligned(16))) float2 turn[kWaves][HALF];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = lane / LANES, at = lane % LANES * E;       // head of the group, channel of the half
-  const int64_t task = (int64_t)blockIdx.x * kWaves + wave;
-  const int64_t token = task / a.chunks;
-  if (token >= a.T) return;
-  const int chunk = (int)(task - token * a.chunks);
-  const int heads = a.heads[0] + a.heads[1];
-  const int g0 = chunk * a.groups, all = (heads + HEADS - 1) / HEADS;
-  const int g1 = g0 + a.groups < all ? g0 + a.groups : all;
-
-  struct Row {
-    u32x4_t x[2];
-    int head;          // in its tensor
-    bool key, live;
-  };
-  auto load = [&](Row& r, int g) {
-    const int h = g * HEADS + sub;
-    r.live = g < g1 && h < heads;
-    r.key = r.live && h >= a.heads[0];
-    r.head = r.live ? (r.key ? h - a.heads[0] : h) : 0;
-    const T* from = static_cast<const T*>(r.key ? a.x[1] : a.x[0]) + token * a.stride[r.key][0] +
-                    r.head * a.stride[r.key][1] + at;
-    r.x[0] = *reinterpret_cast<const u32x4_t*>(from);
-    r.x[1] = *reinterpret_cast<const u32x4_t*>(from + HALF);
-  };
-  Row row;
-  load(row, g0);
+  const int heads = a.heads[0] + a.heads[1], all = (heads + HEADS - 1) / HEADS;
+  const int64_t tasks = (int64_t)a.T * all;
+  const int64_t task = a.first + (int64_t)blockIdx.x * kWaves + wave;
+  if (task >= tasks) return;
+  const int64_t token = tasks >> 32 == 0 ? (int64_t)((uint32_t)task / (uint32_t)all) : task / all;
+  const int h = (int)(task - token * all) * HEADS + sub;
+  const bool live = h < heads, key = live && h >= a.heads[0];
+  const int head = live ? (key ? h - a.heads[0] : h) : 0;       // in its tensor
+  const T* from = static_cast<const T*>(key ? a.x[1] : a.x[0]) + token * a.stride[key][0] + head * a.stride[key][1] + at;
+  const u32x4_t lower = *reinterpret_cast<const u32x4_t*>(from), upper = *reinterpret_cast<const u32x4_t*>(from + HALF);
+  const T* weight = static_cast<const T*>(key ? a.weight[1] : a.weight[0]);
+  const T* weights = weight != nullptr ? weight + at : from;      // (not used then)
+  const u32x4_t w_lower = *reinterpret_cast<const u32x4_t*>(weights), w_upper = *reinterpret_cast<const u32x4_t*>(weights + HALF);
 
   // sine and cosine of plane `lane`, of a fraction of a turn
   const double p = (double)a.positions[token];
@@ -102,71 +95,64 @@ __global__ void __launch_bounds__(64 * kWaves) norm_rope_kernel(NormRopeArgs a) 
     sn[e] = v.y;
   }
 
-  for (int g = g0; g < g1; ++g) {
-    Row next;
-    if (g + 1 < g1) load(next, g + 1);
-    float x[2 * E];
-    O::get(row.x[0], x);
-    O::get(row.x[1], x + E);
-    const void* weight = row.key ? a.weight[1] : a.weight[0];
-    if (weight != nullptr) {
-      float y[2 * E], sum = 0.0f;
-      O::get(*reinterpret_cast<const u32x4_t*>(static_cast<const T*>(weight) + at), y);
-      O::get(*reinterpret_cast<const u32x4_t*>(static_cast<const T*>(weight) + HALF + at), y + E);
+  float x[2 * E];
+  O::get(lower, x);
+  O::get(upper, x + E);
+  if (weight != nullptr) {
+    float y[2 * E], sum = 0.0f;
+    O::get(w_lower, y);
+    O::get(w_upper, y + E);
 #pragma unroll
-      for (int i = 0; i < 2 * E; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
+    for (int i = 0; i < 2 * E; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
 #pragma unroll
-      for (int n = 1; n < LANES; n <<= 1) sum += __shfl_xor(sum, n, 64);
-      const float v = __builtin_fmaf(sum, 1.0f / D, a.eps);
-      float by = __builtin_amdgcn_rsqf(v);
-      by *= __builtin_fmaf(-0.5f * v * by, by, 1.5f);        // a Newton step: the last bits
-      if (v > 0x1p-90f && v < 0x1p110f) {
+    for (int n = 1; n < LANES; n <<= 1) sum += __shfl_xor(sum, n, 64);
+    const float v = __builtin_fmaf(sum, 1.0f / D, a.eps);
+    float by = __builtin_amdgcn_rsqf(v);
+    by *= __builtin_fmaf(-0.5f * v * by, by, 1.5f);        // a Newton step: the last bits
+    if (v > 0x1p-90f && v < 0x1p110f) {
 #pragma unroll
-        for (int i = 0; i < 2 * E; ++i) x[i] *= by * y[i];
-      } else {      // squares that fp32 does not hold (all lanes of a head agree)
-        double wide = 0.0;
+      for (int i = 0; i < 2 * E; ++i) x[i] *= by * y[i];
+    } else {      // squares that fp32 does not hold (all lanes of a head agree)
+      double wide = 0.0;
 #pragma unroll
-        for (int i = 0; i < 2 * E; ++i) wide += (double)x[i] * (double)x[i];
+      for (int i = 0; i < 2 * E; ++i) wide += (double)x[i] * (double)x[i];
 #pragma unroll
-        for (int n = 1; n < LANES; n <<= 1) wide += __shfl_xor(wide, n, 64);
-        const double by64 = 1.0 / sqrt(wide / D + (double)a.eps);
+      for (int n = 1; n < LANES; n <<= 1) wide += __shfl_xor(wide, n, 64);
+      const double by64 = 1.0 / sqrt(wide / D + (double)a.eps);
 #pragma unroll
-        for (int i = 0; i < 2 * E; ++i) x[i] = (float)((double)x[i] * by64) * y[i];
-      }
+      for (int i = 0; i < 2 * E; ++i) x[i] = (float)((double)x[i] * by64) * y[i];
     }
+  }
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      // plane (i, j): channels that pair up
-      const int i = STYLE == 0 ? e : (e < E / 2 ? 2 * e : E + 2 * (e - E / 2)), j = STYLE == 0 ? E + e : i + 1;
-      const float u = x[i], v = x[j];
-      x[i] = __builtin_fmaf(u, cs[e], -v * sn[e]);
-      x[j] = __builtin_fmaf(v, cs[e], u * sn[e]);
-    }
-    if (row.live) {
-      T* to = static_cast<T*>(row.key ? a.out[1] : a.out[0]) + (token * a.heads[row.key] + row.head) * D + at;
-      *reinterpret_cast<u32x4_t*>(to) = O::put(x);
-      *reinterpret_cast<u32x4_t*>(to + HALF) = O::put(x + E);
-    }
-    row = next;
+  for (int e = 0; e < E; ++e) {
+    // plane (i, j): channels that pair up
+    const int i = STYLE == 0 ? e : (e < E / 2 ? 2 * e : E + 2 * (e - E / 2)), j = STYLE == 0 ? E + e : i + 1;
+    const float u = x[i], v = x[j];
+    x[i] = __builtin_fmaf(u, cs[e], -v * sn[e]);
+    x[j] = __builtin_fmaf(v, cs[e], u * sn[e]);
+  }
+  if (live) {
+    T* to = static_cast<T*>(key ? a.out[1] : a.out[0]) + (token * a.heads[key] + head) * D + at;
+    *reinterpret_cast<u32x4_t*>(to) = O::put(x);
+    *reinterpret_cast<u32x4_t*>(to + HALF) = O::put(x + E);
   }
 }
-
-// Heads of a token that a wave takes, in groups of 64 / lanes.
-constexpr int64_t kFill = 4096;
 
 template <int DT, int D>
 hipError_t launch(NormRopeArgs a, int style, hipStream_t stream) {
   constexpr int HEADS = 64 / (D / (2 * Oct<DT>::N));
-  const int all = (a.heads[0] + a.heads[1] + HEADS - 1) / HEADS;
-  const int64_t most = (int64_t)a.T * all / kFill;
-  a.groups = most < 1 ? 1 : most < all ? (int)most : all;
-  a.chunks = (all + a.groups - 1) / a.groups;
-  const int64_t blocks = ((int64_t)a.T * a.chunks + kWaves - 1) / kWaves;
-  if (style == 0)
-    hipLaunchKernelGGL((norm_rope_kernel<DT, D, 0>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
-  else
-    hipLaunchKernelGGL((norm_rope_kernel<DT, D, 1>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, stream, a);
-  return hipGetLastError();
+  const int64_t tasks = (int64_t)a.T * ((a.heads[0] + a.heads[1] + HEADS - 1) / HEADS);
+  for (a.first = 0; a.first < tasks; a.first += kMost * kWaves) {
+    const int64_t want = (tasks - a.first + kWaves - 1) / kWaves;
+    const dim3 grid((unsigned)(want < kMost ? want : kMost)), block(64 * kWaves);
+    if (style == 0)
+      hipLaunchKernelGGL((norm_rope_kernel<DT, D, 0>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((norm_rope_kernel<DT, D, 1>), grid, block, 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

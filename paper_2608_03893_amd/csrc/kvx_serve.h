@@ -96,9 +96,9 @@ struct NormRopeArgs {
   void* out[2];             // [T, heads, d]
   const int32_t* positions; // [T]
   InvFreq turns;            // of each plane a position, 1 / (2 pi) times its frequency
+  int64_t first;            // of a launch's waves
   float eps;
   int32_t T, heads[2];
-  int32_t groups, chunks;   // head groups of a wave, waves of a token
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, int dtype, int d, int style, hipStream_t stream);
 
