@@ -1003,7 +1003,7 @@ struct Shape {
   int32_t per;         // vectors of a strip
 };
 
-template <int DT>
+template <int DT, int HELD>
 __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space* spaces, Shape shape) {
   using LG = Logits<DT>;
   constexpr int N = LG::N;
@@ -1021,9 +1021,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   const u32x4_t* from = reinterpret_cast<const u32x4_t*>(row.x + row.head);
   const int vectors = (row.vecs + 64 * waves - 1) / (64 * waves);      // of a lane
   auto vector = [&](int i) { return ((i * 4 + (lane >> 4)) * waves + n) * 16 + (lane & 15); };
-  u32x4_t q[kHeld];
+  u32x4_t q[HELD];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
+  for (int i = 0; i < HELD; ++i)
     if (vector(i) < row.vecs) q[i] = from[vector(i)];
   int32_t loose = n == 0 || n == waves - 1 ? (lane < 2 * N ? row.loose(lane) : -1) : -1;
   if (loose >= 0 && !(loose < row.head ? n == 0 : n == waves - 1)) loose = -1;
@@ -1036,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   // i0 .. i1 - 1 of every lane
   auto held = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
       const int32_t v = vector(i);
       float y[N];
       LG::get(q[i], y);
@@ -1084,7 +1084,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   };
   if (way != kByList) {
     held(largest_of);
-    stream(kHeld, vectors, largest_of);
+    stream(HELD, vectors, largest_of);
 #pragma unroll
     for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i, 64));
     if (lane == 0) space.top[n] = most;
@@ -1117,7 +1117,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       }
     };
     held(best);
-    stream(kHeld, vectors, best);
+    stream(HELD, vectors, best);
     over_wave();
     if (lane == 0) {
       put(&space.top[n], most);
@@ -1192,7 +1192,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       });
     }
   }
-  for (int i = kHeld; i < vectors; i *= 4) {
+  for (int i = HELD; i < vectors; i *= 4) {
     stream(i, 4 * i < vectors ? 4 * i : vectors, [&](const float* y, int32_t first) {
       largest_of(y, first);
       list(y, first);
@@ -1221,7 +1221,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   float floor = -INFINITY;      // the highest bound of a list
   if (chunks > 1) {       // to all workgroups' list, what reaches the last bound
     uint32_t kept = 0, upto = 0;
-    if (vectors > kHeld) {
+    if (vectors > HELD) {
       every(listed, [&](uint64_t& v, uint32_t) {
         if (v != ~0ull && logit(v) < bound) v = ~0ull;
         kept += v != ~0ull;
@@ -1229,7 +1229,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
       upto = (uint32_t)block_scan(kept, s);
     }
     if (threadIdx.x == kThreads - 1) {
-      const uint32_t all = over ? kLong + 1u : vectors > kHeld ? upto : listed;
+      const uint32_t all = over ? kLong + 1u : vectors > HELD ? upto : listed;
       s.slot = __hip_atomic_fetch_add(&space.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       put(&space.bound[chunk], bound);
     }
@@ -1237,9 +1237,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
     uint32_t at = s.slot + upto - kept;
     every(listed, [&](uint64_t& v, uint32_t j) {
       if (v == ~0ull) return;
-      const uint32_t to = vectors > kHeld ? at : at + j;
+      const uint32_t to = vectors > HELD ? at : at + j;
       if (to < kLong) put(&space.entry[to], v);
-      if (vectors > kHeld) ++at;
+      if (vectors > HELD) ++at;
     });
     if (!come_last(&space.arrived[0], chunks, s)) return;
     listed = uniform(get(&space.listed));
@@ -1600,7 +1600,7 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
 }
 
 // Workgroups of a row: as many as fill the chip, of kHeld vectors a lane at least.
-constexpr int kFill = 1024;
+constexpr int kFill = 1024, kLongPart = 2 * kHeld;
 template <int DT>
 hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
   const int vecs = a.V / Logits<DT>::N, part = kHeld * kThreads, most = (vecs + part - 1) / part;
@@ -1615,7 +1615,10 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
   Space* spaces = static_cast<Space*>(ws);
   const dim3 grid((unsigned)(a.B * shape.chunks)), some((unsigned)(a.B * shape.chunks < kFill ? a.B * shape.chunks : kFill)),
       block(kThreads);
-  hipLaunchKernelGGL((sample_kernel<DT>), grid, block, 0, stream, a, spaces, shape);
+  if (vecs >= shape.chunks * kThreads * kLongPart)
+    hipLaunchKernelGGL((sample_kernel<DT, 2 * kHeld>), grid, block, 0, stream, a, spaces, shape);
+  else
+    hipLaunchKernelGGL((sample_kernel<DT, kHeld>), grid, block, 0, stream, a, spaces, shape);
   hipLaunchKernelGGL((sample_weigh_kernel<DT>), some, block, 0, stream, a, spaces, shape);
   if (a.top_k != nullptr || a.top_p != nullptr)      // else every row is answered by now
     hipLaunchKernelGGL((sample_cut_kernel<DT>), some, block, 0, stream, a, spaces, shape);
