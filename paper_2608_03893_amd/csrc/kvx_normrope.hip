@@ -10,11 +10,12 @@
 // token, with that token's d / 2 sines and cosines, one plane a lane, shared through LDS that is
 // its own, without a barrier.  They are formed again for every wave of a token while its heads are
 // on the way: a wave for several heads a token, with the next ones loaded ahead, was no faster (8192
-// tokens of 72 heads 59 us, 1024 of 72 9.5).
+// tokens of 72 heads 59 us, 1024 of 72 9.5; now 55.6 and 8.2), nor is a loop over the heads, which
+// keeps the sine's constants in registers that other waves could have (60 us).
 //
 // Bound by memory, every element read once and written once: 8192 tokens of 72 bf16 heads of 128
-// channels, 302 MB, XXXX.  A step of 16 tokens of 48 heads is bound by the launch and its host time:
-// XXXX.
+// channels, 302 MB, in 55.6 us, 5.4 TB/s.  A step of 16 tokens of 48 heads runs for 3.4 us, hardly
+// more than an empty kernel, and takes 7 us a call, the host's time.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
 

@@ -25,6 +25,15 @@
 //      a list; last: the cut, the draw.
 // Where a list would not fit (thousands of equal logits at a cut) the row goes the next way, and at
 // last one workgroup narrows the bins down over the whole row.
+//
+// A logit is read once by way of a list, two or three times else, the later ones from the caches.
+// Large batches by lists are bound by these reads: 512 rows of 131072 fp32 logits, 268 MB, with one
+// k and p take 81 us, 3.3 TB/s, 72 of them in the first launch.  All others are bound by chains of
+// steps that wait for each other, each a microsecond or less: what says how a row goes, its logits,
+// the counter, what all have found, sums over the workgroup, the cut, the draw.  One row of 131072
+// takes 20 us (14.5 + 3 + 2.4 in the launches), 64 bf16 rows of 128257 with settings of their own 61
+// (17 + 20.5 + 26), 16 fp32 rows of 150001 with flat distributions 42.5 (4.7 + 15.7 + 24).
+// A workgroup of 1024 threads for each row took 39, 465, 659 us, and 152 for the batch.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
 
@@ -984,7 +993,9 @@ __device__ __forceinline__ int listed_of(int k, int chunks) {
   const int m = chunks > 1 ? (2 * k + chunks - 1) / chunks + 9 : k;
   return m < k ? m : k;
 }
-// Which way a row goes: through the first launch alone, or the first two or three.
+// Which way a row goes: through the first launch alone, or the first two or three.  By a list where
+// the maxima of a workgroup's lanes can say a bound for k and the lists fit: with k = 50 one row of
+// 131072 takes 20.4 us by a list and 28.6 by bins, 512 rows 81 and 284.
 enum { kPlain, kByList, kByBins };
 __device__ __forceinline__ int way_of(const Setting& set, int chunks) {
   if (set.k == 0) return set.p > 1.0 ? kPlain : kByBins;
@@ -1599,8 +1610,12 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(SampleArgs a, Spac
   }
 }
 
-// Workgroups of a row: as many as fill the chip, of kHeld vectors a lane at least.
-constexpr int kFill = 1024, kLongPart = 2 * kHeld;
+// Workgroups of a row: as many as fill the chip, of kHeld vectors a lane at least.  With 512 of them
+// 64 rows of 128257 with settings of their own take 79 us instead of 63 (512 rows by lists 85 instead
+// of 81, 64 rows by lists 33 instead of 35), with 2048 the 512 rows take 102.  A list's first bound is
+// from twice as many vectors where a lane has them: 64 rows of 131072 by lists take 34.7 us instead of
+// 36.8; loaded for nothing where it has fewer they cost one row 1 us and the 64 rows with settings 3.
+constexpr int kFill = 1024;
 template <int DT>
 hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
   const int vecs = a.V / Logits<DT>::N, part = kHeld * kThreads, most = (vecs + part - 1) / part;
@@ -1615,7 +1630,7 @@ hipError_t launch(const SampleArgs& a, void* ws, hipStream_t stream) {
   Space* spaces = static_cast<Space*>(ws);
   const dim3 grid((unsigned)(a.B * shape.chunks)), some((unsigned)(a.B * shape.chunks < kFill ? a.B * shape.chunks : kFill)),
       block(kThreads);
-  if (vecs >= shape.chunks * kThreads * kLongPart)
+  if (vecs >= shape.chunks * kThreads * 2 * kHeld)
     hipLaunchKernelGGL((sample_kernel<DT, 2 * kHeld>), grid, block, 0, stream, a, spaces, shape);
   else
     hipLaunchKernelGGL((sample_kernel<DT, kHeld>), grid, block, 0, stream, a, spaces, shape);
