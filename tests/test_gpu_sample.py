@@ -76,6 +76,19 @@ def test_batches(gpu_kvx, B, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,V", [(300, 60011), (600, 20013), (1100, 8200)])
+def test_long_rows_of_large_batches(gpu_kvx, B, V, dtype):
+    """Workgroups with many logits a lane, three of them a row or one."""
+    g = np.random.default_rng(B)
+    few = [(1.0, 50, 0.9, 0.0), (0.7, 128, 1.0, 0.0), (1.5, 1, 1.0, 0.0), (1.0, 20, 1.0, 0.1), (0.0, 5, 1.0, 0.0),
+           (1.0, 0, 0.95, 0.0), (1.0, 0, 1.0, 0.0), (1.2, 129, 0.9, 0.0)]
+    x = _logits(B, V, dtype, B)
+    x[5::9] = -float("inf")
+    x[5::9, V // 3:V // 3 + 40] = 1.0
+    _check(gpu_kvx, x, [few[b % len(few)] for b in range(B)], g.random(B))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_masks(gpu_kvx, dtype):
     """Masked logits: -inf and NaN, rows that have one token or none, the least finite number,
     +inf."""
