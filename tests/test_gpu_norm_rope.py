@@ -118,6 +118,22 @@ def test_extreme_values(gpu_kvx, dtype):
     _check(gpu_kvx.norm_rope(q, k, qw, kw, rope, far)[0], q, qw, 1e-6, far, rope, dtype)
 
 
+def test_more_rows_than_a_launch_takes(gpu_kvx):
+    """2^25 waves a launch; elements whose offset passes 2^31."""
+    T, d = 2 ** 25 + 77, 64
+    x = torch.empty((T, 1, d), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    parts = [slice(0, 500), slice(2 ** 25 - 300, T)]
+    for part in parts:
+        x[part] = torch.randn(x[part].shape, generator=g, device=DEV).to(x.dtype)
+    w = torch.rand(d, generator=g, device=DEV).to(x.dtype)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV) % 131072
+    out = torch.zeros_like(x)
+    gpu_kvx.norm_rope(x, None, w, None, ROPES[0], pos, out=(out, None))
+    for part in parts:
+        _check(out[part], x[part], w, 1e-6, pos[part], ROPES[0], "bf16")
+
+
 def test_empty_streams_and_graphs(gpu_kvx):
     q, k, qw, kw, pos = _case(0, 4, 2, 128, "bf16", 1)
     a, b = gpu_kvx.norm_rope(q, k, qw, kw, ROPES[0], pos)
