@@ -1,5 +1,5 @@
 // Attention over the 8-bit pool, split over the keys: the kernel's body, for whole requests
-// (kvx_attend8.hip) and for the parts of requests that share prefixes (kvx_prefix8.hip).
+// (kvx_attend8.hip) and for the parts of requests that share prefixes (kvx_prefix8_common.hip, _own.hip, _both.hip).
 //
 // For a block of 16 query rows (tokens times the G heads of a KV head) and a tile of
 // 16 keys the scores are S^T = K Q^T on the matrix cores: a lane then holds one query
