@@ -12,15 +12,18 @@ __global__ void __launch_bounds__(64 * W, (W == 4 ? kOcc<DT, D, NB> : W / 4)) pr
   attend8_split<DT, D, W, NB>(a, partial, counters, lds, Group{(int)blockIdx.x, (int)gridDim.x});
 }
 
+// Large workgroups of 32 rows: 8 waves, which have the registers for a step's keys ahead, also
+// where three waves a SIMD would fit (d = 64; whole calls: 64 requests after 8000 common keys 41.4
+// with 12 waves, 38.5 with 8, 40 requests of four prefixes 33.3 and 28.4, 16 after 8000 22.8 and 23.3).
 template <int DT, int D, int W, int NB>
 struct Split {
-  static constexpr int kSlotRows = 16 * NB;
+  static constexpr int kSlotRows = 16 * NB, kWaves = NB == 2 && W > 8 ? 8 : W;
   static hipError_t launch(const CommonPart& a, hipStream_t stream) {
-    hipLaunchKernelGGL((prefix8_common_split_kernel<DT, D, W, NB>), dim3(split_grid<DT, D, W, NB>(a)), dim3(64 * W),
+    hipLaunchKernelGGL((prefix8_common_split_kernel<DT, D, kWaves, NB>), dim3(split_grid<DT, D, kWaves, NB>(a)), dim3(64 * kWaves),
                        split_lds(a), stream, a, const_cast<float*>(a.partial), nullptr);
     return hipGetLastError();
   }
-  static void name(char* to, size_t n) { std::snprintf(to, n, "prefix8_common_split_kernel<%d, %d, %d, %d>", DT, D, W, NB); }
+  static void name(char* to, size_t n) { std::snprintf(to, n, "prefix8_common_split_kernel<%d, %d, %d, %d>", DT, D, kWaves, NB); }
 };
 
 template <int D>

@@ -158,7 +158,10 @@ def test_every_kernel(gpu_kvx, kernel, part):
             count.append(len(parts))
             mine += parts
         c = _case(rng, pre, count, [n + int(rng.integers(0, 9)) for n in mine], mine, H, G, d, 16, dtype, Mp=pages, M=WIDE)
-    assert _names(gpu_kvx, c)[part == "own"] == kernel.replace("attend8", f"prefix8_{part}")
+    name = kernel.replace("attend8", f"prefix8_{part}")
+    if part == "common":
+        name = name.replace("12, 2>", "8, 2>")      # large workgroups of 32 rows have 8 waves there
+    assert _names(gpu_kvx, c)[part == "own"] == name
     _check(gpu_kvx, c, f"{part} {kernel}")
 
 
