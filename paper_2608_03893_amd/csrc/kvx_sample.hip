@@ -20,7 +20,8 @@
 //      workgroup that comes last looks whether k of all are above the highest bound: then nothing
 //      that was not listed is among them.  The lists' tokens above it, the cut, the draw.
 //   2  Rows without top-k and top-p: the strips' sums of weights; last: the draw.  Others: a
-//      histogram of counts and weights over the weights' range; last: the bins that the cuts lie in.
+//      histogram of counts and weights over the logits that have a weight; last: the bins that the
+//      cuts lie in.
 //   3  Rows of the last kind: the strips' sums of weights above these bins, the tokens in them as
 //      a list; last: the cut, the draw.
 // Where a list would not fit (thousands of equal logits at a cut) the row goes the next way, and at
@@ -163,7 +164,7 @@ __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
 struct Setting {
   float top;            // its largest logit
   double by;            // log2(e) / T
-  float bins;           // of the histogram, a unit of the logits
+  float bins;           // of the histogram, a unit of the logits (see task_of)
   uint64_t least;       // weight that min-p asks for
   int32_t k;            // 0: all
   double p;             // 2: all
@@ -375,7 +376,7 @@ struct alignas(256) Space {
   int arrived[3];                        // workgroups, in each launch; zero between calls, as listed
   int over;                              // the first launch's list did not hold
   State state;
-  float top[kStrips];                    // of a wave
+  float top[kStrips], low[kStrips];      // of a wave; low: of rows by bins, else -inf
   float bound[kStrips / kWaves];         // of a workgroup's list
   uint32_t first[kStrips];               // index of the first largest (greedy rows)
   uint64_t sum[kStrips];
@@ -1094,11 +1095,23 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
     for (int e = 0; e < N; ++e) most = fmaxf(most, y[e]);
   };
   if (way != kByList) {
-    held(largest_of);
-    stream(HELD, vectors, largest_of);
+    float least = INFINITY;
+    auto ends_of = [&](const float* y, int32_t at) {
+      largest_of(y, at);
 #pragma unroll
-    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i, 64));
-    if (lane == 0) space.top[n] = most;
+      for (int e = 0; e < N; ++e) least = fminf(least, y[e] == -INFINITY ? INFINITY : y[e]);
+    };
+    held(ends_of);
+    stream(HELD, vectors, ends_of);
+#pragma unroll
+    for (int i = 32; i; i >>= 1) {
+      most = fmaxf(most, __shfl_xor(most, i, 64));
+      least = fminf(least, __shfl_xor(least, i, 64));
+    }
+    if (lane == 0) {
+      space.top[n] = most;
+      space.low[n] = least;
+    }
     if (way == kByBins && chunks > 1)
       for (int i = chunk * kThreads + (int)threadIdx.x; i < kBins; i += chunks * kThreads) {
         space.weight[i] = 0;
@@ -1213,7 +1226,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   float top = most;       // of the wave, for the launches behind
 #pragma unroll
   for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
-  if (lane == 0) space.top[n] = top;
+  if (lane == 0) {
+    space.top[n] = top;
+    space.low[n] = -INFINITY;
+  }
   __syncthreads();
   uint32_t listed = uniform(s.count);
   bool over = listed > kShort;
@@ -1372,16 +1388,32 @@ __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space&
   const int lane = threadIdx.x & 63, waves = chunks * kWaves;
   const float temperature = temperature_of(a, b);
   const int over = space.over;
-  float top = -INFINITY;
+  float top = -INFINITY, low = INFINITY;
 #pragma unroll
-  for (int i = 0; i < kStrips / 64; ++i) top = fmaxf(top, lane + 64 * i < waves ? space.top[lane + 64 * i] : -INFINITY);
+  for (int i = 0; i < kStrips / 64; ++i) {
+    const bool some = lane + 64 * i < waves;
+    top = fmaxf(top, some ? space.top[lane + 64 * i] : -INFINITY);
+    low = fminf(low, some ? space.low[lane + 64 * i] : INFINITY);
+  }
   Task t;
   t.set = setting(a, b, 0.0f, temperature);
   t.way = !(temperature > 0.0f) ? kByList : way_of(t.set, chunks);
   if (t.way == kByList && temperature > 0.0f && over != 0) t.way = kByBins;
 #pragma unroll
-  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
+  for (int i = 32; i; i >>= 1) {
+    top = fmaxf(top, __shfl_xor(top, i, 64));
+    low = fminf(low, __shfl_xor(low, i, 64));
+  }
   t.set.top = top;
+  // The bins cover the logits that have a weight, or only those that there are, where the densest
+  // bin would not fit a list well: of a normal distribution over 9 deviations it holds 0.4 9 / kBins
+  // of the tokens (16 rows of 131072, top-p, T = 100: 41 us; over the weights' range, in whose first
+  // bins all tokens are then, 677; but 64 rows of 128257 at ordinary temperatures take 63 with that
+  // and 65 with more bins in use).  The lowest logit's is the last; not for differences whose
+  // inverse fp32 does not hold.
+  const float spread = top - low, range = kRange * temperature;
+  constexpr float kDense = kList / 2 * (kBins / 3.6f);
+  if (spread < range && (float)a.V * range > spread * kDense && spread > 1e-30f) t.set.bins = (float)(kBins - 1) / spread;
   return t;
 }
 

@@ -145,6 +145,27 @@ def test_ties(gpu_kvx, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3000, 40009, 140001])
+def test_spreads(gpu_kvx, V, dtype):
+    """High temperatures, logits that differ by much less than a temperature or by next to nothing,
+    a few far below all others, most masked: wherever the cut lies in how many tokens."""
+    temperatures, cuts = (5.0, 30.0, 1e3, 1e30, float("inf")), ((0, 0.9), (0, 0.3), (V // 2, 1.0), (V // 3, 0.6), (200, 1.0))
+    settings = [(t, k, p, 0.0) for t in temperatures for k, p in cuts]
+    g = np.random.default_rng(V)
+    for kind in range(5):
+        x = torch.tensor(g.standard_normal((len(settings), V)) * (2.5, 1e-3, 1e-36, 2.5, 2.5)[kind])
+        if kind == 1:
+            x += 1.0
+        elif kind == 3:
+            x[:, ::1000] = -3e4
+        elif kind == 4:
+            x[torch.rand(x.shape, generator=torch.Generator().manual_seed(V)) < 0.8] = -float("inf")
+            x[1::4, 17] = torch.finfo(torch.bfloat16).min
+        x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).to(DEV)
+        _check(gpu_kvx, x, settings, g.random(len(settings)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("width", [64, 128, 300])
 def test_likely_tokens_side_by_side(gpu_kvx, width, dtype):
     """The top-k lie in one run of the vocabulary, anywhere in it, so that one workgroup has them
