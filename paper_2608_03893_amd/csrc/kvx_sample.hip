@@ -29,11 +29,11 @@
 //
 // A logit is read once by way of a list, two or three times else, the later ones from the caches.
 // Large batches by lists are bound by these reads: 512 rows of 131072 fp32 logits, 268 MB, with one
-// k and p take 81 us, 3.3 TB/s, 72 of them in the first launch.  All others are bound by chains of
+// k and p take 82 us, 3.3 TB/s, 72 of them in the first launch.  All others are bound by chains of
 // steps that wait for each other, each a microsecond or less: what says how a row goes, its logits,
 // the counter, what all have found, sums over the workgroup, the cut, the draw.  One row of 131072
-// takes 20 us (14.5 + 3 + 2.4 in the launches), 64 bf16 rows of 128257 with settings of their own 61
-// (17 + 20.5 + 26), 16 fp32 rows of 150001 with flat distributions 42.5 (4.7 + 15.7 + 24).
+// takes 20 us (14.5 + 3 + 2.4 in the launches), 64 bf16 rows of 128257 with settings of their own 64
+// (16.6 + 20.7 + 27), 16 fp32 rows of 150001 with flat distributions 44 (4.8 + 16.2 + 24.4).
 // A workgroup of 1024 threads for each row took 39, 465, 659 us, and 152 for the batch.
 #include "kvx_bf16.h"
 #include "kvx_serve.h"
@@ -44,7 +44,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kList = 2048;                // most tokens of a list in LDS
 constexpr int kShort = 2048;               // and in the first launch
-constexpr int kLong = 3072;                // and of all workgroups of a row together
+constexpr int kLong = 2560;                // and of all workgroups of a row together
 constexpr int kFew = 256;                  // most tokens that are ranked by counting
 constexpr int kBins = 2048;
 constexpr int kStrips = 256;               // most strips of a row, and waves
@@ -995,12 +995,13 @@ __device__ __forceinline__ int listed_of(int k, int chunks) {
   return m < k ? m : k;
 }
 // Which way a row goes: through the first launch alone, or the first two or three.  By a list where
-// the maxima of a workgroup's lanes can say a bound for k and the lists fit: with k = 50 one row of
-// 131072 takes 20.4 us by a list and 28.6 by bins, 512 rows 81 and 284.
+// the maxima of a workgroup's lanes can say a bound for k (all lists' shares then come to 2 k + 10
+// chunks, a third of their room): with k = 50 one row of 131072 takes 20.4 us by a list and 28.6 by
+// bins, 512 rows 81 and 284.
 enum { kPlain, kByList, kByBins };
-__device__ __forceinline__ int way_of(const Setting& set, int chunks) {
+__device__ __forceinline__ int way_of(const Setting& set) {
   if (set.k == 0) return set.p > 1.0 ? kPlain : kByBins;
-  return set.k <= kThreads / 2 && listed_of(set.k, chunks) * chunks <= kLong * 3 / 4 ? kByList : kByBins;
+  return set.k <= kThreads / 2 ? kByList : kByBins;
 }
 
 template <int DT>
@@ -1043,7 +1044,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(SampleArgs a, Space
   const float temperature = temperature_of(a, b);
   const bool greedy = !(temperature > 0.0f);
   const Setting first_set = setting(a, b, 0.0f, temperature);
-  const int way = greedy ? kByList : way_of(first_set, chunks);
+  const int way = greedy ? kByList : way_of(first_set);
   // f(N logits, index of the first) for the held ones and those outside whole vectors; for vectors
   // i0 .. i1 - 1 of every lane
   auto held = [&](auto f) {
@@ -1397,7 +1398,7 @@ __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space&
   }
   Task t;
   t.set = setting(a, b, 0.0f, temperature);
-  t.way = !(temperature > 0.0f) ? kByList : way_of(t.set, chunks);
+  t.way = !(temperature > 0.0f) ? kByList : way_of(t.set);
   if (t.way == kByList && temperature > 0.0f && over != 0) t.way = kByBins;
 #pragma unroll
   for (int i = 32; i; i >>= 1) {
@@ -1412,7 +1413,7 @@ __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space&
   // and 65 with more bins in use).  The lowest logit's is the last; not for differences whose
   // inverse fp32 does not hold.
   const float spread = top - low, range = kRange * temperature;
-  constexpr float kDense = kList / 2 * (kBins / 3.6f);
+  constexpr float kDense = kList * 3 / 4 * (kBins / 3.6f);
   if (spread < range && (float)a.V * range > spread * kDense && spread > 1e-30f) t.set.bins = (float)(kBins - 1) / spread;
   return t;
 }
