@@ -164,7 +164,7 @@ __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
 struct Setting {
   float top;            // its largest logit
   double by;            // log2(e) / T
-  float bins;           // of the histogram, a unit of the logits (see task_of)
+  float bins;           // of the histogram, a unit of half the logits (see task_of)
   uint64_t least;       // weight that min-p asks for
   int32_t k;            // 0: all
   double p;             // 2: all
@@ -538,8 +538,7 @@ struct Sampler {
     // 256 bins over the range, in LDS that sums of strips use otherwise
     const float scale = (float)kThreads / (float)(hi - lo + 1);
     auto sub = [&](float x) {
-      const float y = x == set.top ? 0.0f : (set.top - x) * set.bins;
-      const int i = (int)((y - (float)lo) * scale);
+      const int i = (int)((place_of(x) - (float)lo) * scale);
       return i < 0 ? 0 : i < kThreads ? i : kThreads - 1;
     };
     auto logit = [&](uint64_t e) { return of_key(~(uint32_t)(e >> 32)); };
@@ -830,8 +829,14 @@ struct Sampler {
     int bin;               // -1: by keys
     uint32_t lo, hi;
   };
+  // Where a logit is in the histogram, in bins; rises as x falls.  From half the logits, whose
+  // difference fp32 always holds: at temperatures near the end of its range the whole one may pass
+  // that though the logit has a weight.
+  __device__ __forceinline__ float place_of(float x) const {
+    return x == set.top ? 0.0f : __builtin_fmaf(-0.5f, x, 0.5f * set.top) * set.bins;
+  }
   __device__ __forceinline__ int bin_of(float x) const {
-    const float y = x == set.top ? 0.0f : (set.top - x) * set.bins;    // rises as x falls
+    const float y = place_of(x);
     return y < (float)kBins && x != -INFINITY ? (int)y : kBins;
   }
   __device__ __forceinline__ bool in(const Range& r, float x) const {
@@ -975,7 +980,8 @@ __device__ __forceinline__ Setting setting(const SampleArgs& a, int b, float top
   Setting set;
   set.top = top;
   set.by = 1.4426950408889634 / (double)temperature;
-  set.bins = (float)kBins / kRange / temperature;
+  // (no more than fp32 holds: where temperatures come near zero the bins are coarser)
+  set.bins = fminf(2.0f * (float)kBins / kRange / temperature, 0x1p127f);
   const int32_t k = a.top_k == nullptr ? 0 : a.top_k[b];
   set.k = k > 0 && k < a.V ? k : 0;
   const float p = a.top_p == nullptr ? 1.0f : a.top_p[b];
@@ -1413,7 +1419,7 @@ __device__ __forceinline__ Task task_of(const SampleArgs& a, int b, const Space&
   // bins all tokens are then, 677; but 64 rows of 128257 at ordinary temperatures take 63 with that
   // and 65 with more bins in use).  The lowest logit's is the last; not for differences whose
   // inverse fp32 does not hold.
-  const float spread = top - low, range = kRange * temperature;
+  const float spread = 0.5f * top - 0.5f * low, range = 0.5f * kRange * temperature;      // of half the logits
   constexpr float kDense = kList * 3 / 4 * (kBins / 3.6f);
   if (spread < range && (float)a.V * range > spread * kDense && spread > 1e-30f) t.set.bins = (float)(kBins - 1) / spread;
   return t;
