@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(64 * kWaves) norm_rope_kernel(NormRopeArgs a) 
     by *= __builtin_fmaf(-0.5f * v * by, by, 1.5f);        // a Newton step: the last bits
     if (v > 0x1p-90f && v < 0x1p110f) {
 #pragma unroll
-      for (int i = 0; i < 2 * E; ++i) x[i] *= by * y[i];
+      for (int i = 0; i < 2 * E; ++i) x[i] = x[i] * by * y[i];      // (by times a weight may pass fp32's range)
     } else {      // squares that fp32 does not hold (all lanes of a head agree)
       double wide = 0.0;
 #pragma unroll
