@@ -599,7 +599,8 @@ const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* 
  *   prefix_tables   int32 [S, prefix->max_pages]; entries out of range: unseen keys
  *   prefix_lens     int32 [S], at most prefix->max_pages * page_size
  *   prefix_cu       int32 [S + 1], rising, at most B
- *   workspace       >= kvx_prefix_workspace_bytes, else as in kvx_attend_cache8
+ *   workspace       >= kvx_prefix_workspace_bytes (no less for more rows T), else as in
+ *                   kvx_attend_cache8
  * dims, pool: the requests' (pool->max_pages: entries of a row of block_tables).
  * S == 0 is kvx_attend_cache8.  The two parts of a row are joined in fp32. */
 typedef struct kvx_prefix_dims {

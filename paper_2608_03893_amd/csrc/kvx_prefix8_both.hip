@@ -64,6 +64,8 @@ __global__ void __launch_bounds__(256) prefix8_join_kernel(PrefixArgs c, PrefixA
 template <int DT, int D>
 struct Both {
   static constexpr int W = 4, NB = 1;
+  static_assert(2 * kPrefixRows * (1 + kStart) >= (int64_t)16 * NB * kLeast<W> * (256 * kOcc<DT, D, NB> - 2),
+                "calls that fit have room for both parts' sums");
   static bool fits(const PrefixArgs& c, const PrefixArgs& o) {
     return split_want<W, NB>(c) + split_want<W, NB>(o) <= 256 * kOcc<DT, D, NB>;
   }

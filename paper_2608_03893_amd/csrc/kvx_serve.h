@@ -63,7 +63,9 @@ size_t attend_rows_ws_bytes(int d);
 
 // Attention over prefixes that requests share (kvx_prefix8_*.hip), in two parts: the common
 // part's B, tables, lens, M and keys are the prefixes', the own part's the requests'.
-constexpr int64_t kPrefixRows = 65536;      // most rows (T * H * G) of both parts in one launch
+// Most rows (T * H * G) of both parts in one launch, which fit the chip: of 16 rows and three
+// quanta at least, two a workgroup.
+constexpr int64_t kPrefixRows = 16 * 1024 / 3;
 struct PrefixArgs : AttendArgs {
   const int32_t* shares;    // [prefixes + 1] requests of each prefix
   float* sums;              // [T, H * G, d] the part's weighted values

@@ -394,7 +394,8 @@ static kvx_status check_prefix(const kvx_prefix_dims* p) {
 
 // The workspace: counters and partial sums of the own part on its own, then for each part the
 // partial sums of its workgroups, a row's sums, statistics and where they are (of the own one where
-// both may go in one launch).
+// both may go in one launch; calls of more rows need no less than the largest of these, so that a
+// workspace for many rows is enough for fewer).
 struct PrefixSpace {
   struct Part {
     uint64_t partial, sums, stats, parts;
@@ -417,6 +418,13 @@ static PrefixSpace prefix_space(const kvx_attend_dims& m, int32_t S, int dt) {
     s.part[i].sums = take(rows * m.d * 4);
     s.part[i].stats = take(rows * 8);
     s.part[i].parts = take(rows * 8);
+  }
+  const int64_t most = kvx::kPrefixRows / ((int64_t)m.H * m.G);
+  if (S > 0 && m.T > most && most > 0) {
+    kvx_attend_dims fewer = m;
+    fewer.T = (int32_t)most;
+    const uint64_t n = prefix_space(fewer, S, dt).bytes;
+    if (n > s.bytes) s.bytes = n;
   }
   return s;
 }
