@@ -584,8 +584,9 @@ kvx_status kvx_attend_cache8(const kvx_attend_dims* dims, const kvx_pool* pool, 
  * static string, NULL for invalid arguments and for calls that launch nothing. */
 const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* pool, kvx_dtype dtype);
 
-/* Attention of requests that share prefixes, each prefix read and multiplied once for
- * all rows that see it (a common context handed over once, and many continuations).
+/* Attention of requests that share prefixes (a common context handed over once, and
+ * many continuations), a prefix's codes read and widened once for every 16, 32 or 256
+ * query rows that see it, whichever of its requests these belong to.
  * Prefix s has prefix_lens[s] tokens in the pages prefix_tables[s]; requests
  * prefix_cu[s] .. prefix_cu[s + 1] - 1 share it, and those before prefix_cu[0] and from
  * prefix_cu[S] on have none.  A request's keys are its prefix's, all of which every row
@@ -602,7 +603,16 @@ const char* kvx_attend_kernel_name(const kvx_attend_dims* dims, const kvx_pool* 
  *   workspace       >= kvx_prefix_workspace_bytes (no less for more rows T), else as in
  *                   kvx_attend_cache8
  * dims, pool: the requests' (pool->max_pages: entries of a row of block_tables).
- * S == 0 is kvx_attend_cache8.  The two parts of a row are joined in fp32. */
+ * S == 0 is kvx_attend_cache8.  The two parts of a row are joined in fp32.
+ * For several requests that share thousands of keys.  Where few do, or few keys,
+ * kvx_attend_cache8 with a prefix's whole pages in every request's table is faster: bf16,
+ * 8 heads of 8 queries of 128 channels, a new token and up to 64 own keys a request, us,
+ * that call / this one:
+ *   requests of a prefix     1           2           5           16          64
+ *   304 common keys          7.9 / 11.6  8.0 / 12.1  8.0 / 12.2  10.3 / 12.7  12.9 / 18.5
+ *   5008                    12.9 / 13.4 14.9 / 15.5 20.0 / 17.2  27.0 / 24.7  64 / 37
+ *   30000                   21.5 / 29.3 31.2 / 29.6 54.4 / 33.1   146 / 44    332 / 118
+ *   16 prefixes of 5008 keys with one request each 34.8 / 39.4 */
 typedef struct kvx_prefix_dims {
   int32_t S, max_pages, longest;
 } kvx_prefix_dims;
@@ -666,7 +676,7 @@ kvx_status kvx_norm_rope(kvx_dtype dtype, int32_t T, int32_t Hq, int32_t Hk, int
  *   tokens       int32 [B]
  *   logprob      fp32 [B] or NULL: ln of the probability with which the token was
  *                drawn, among the kept ones (0 where the temperature is 0)
- *   workspace    >= kvx_sample_workspace_bytes, 256-byte aligned.  A row has
+ *   workspace    >= kvx_sample_workspace_bytes (50688 a row), 256-byte aligned.  A row has
  *                kvx_sample_workspace_bytes(dtype, 1, V) bytes of it, the first
  *                KVX_SAMPLE_COUNTER_BYTES of which are zero before the first use
  *                (counters, which every call leaves at zero; the rest may hold

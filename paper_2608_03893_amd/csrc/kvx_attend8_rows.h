@@ -12,7 +12,7 @@
 // there, and else to the probabilities.
 //
 // Bound by the matrix cores, with the exponentials (16 cycles for 64) beside them:
-// 2048 new tokens of 64 heads over 10240 keys, d = 128, 820 us: 755 TFLOP/s, and 1130 with the
+// 2048 new tokens of 64 heads over 10240 keys, d = 128, 812 us: 762 TFLOP/s, and 1140 with the
 // products of the probabilities' second term, where a large product of the library reaches
 // 1230 (another card: 920 us).  With one term, to form a step's scores beside the exponentials of
 // the step before took 8% longer.

@@ -785,8 +785,11 @@ def prefix_workspace(q, pool, prefix_tables, block_tables, stream=None):
 
 def attend_prefix8(q, pool, scales, prefix_tables, prefix_lens, prefix_cu, block_tables, lens, cu, scale=None,
                    out=None, with_lse=False, workspace=None, stream=None, longest=0, longest_prefix=0):
-    """attend_cache8 for requests that share prefixes, each of which is read once for all of them
-    (enqueued on the stream); returns out [T, H*G, d], with_lse also lse [T, H*G].  For inference.
+    """attend_cache8 for requests that share prefixes, which are read once for every 16 to 256 query
+    rows, whichever requests these belong to (enqueued on the stream); returns out [T, H*G, d],
+    with_lse also lse [T, H*G].  For inference.  For several requests that share thousands of keys:
+    where few do, or few keys, attend_cache8 with the prefix's pages in every table is faster
+    (include/kvx.h has figures).
 
     Prefix s: prefix_lens[s] tokens in the pages prefix_tables[s] of the same pool, shared by
     requests prefix_cu[s] .. prefix_cu[s + 1] - 1 (int32 [S, pages], [S], [S + 1]).  block_tables,
